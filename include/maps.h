@@ -1,11 +1,13 @@
 /*
  * maps.h -- C ABI of the MAPS memory-aware predictive scheduler hot path,
- * implemented as integer-only CUDA kernels for GB300 (sm_103a).
+ * implemented as integer-only CUDA kernels for GB300 (sm_103a), and of the KV
+ * memory that its decoders run on: block tables, a cache held in 4 bits, and
+ * attention over that cache.
  *
- * The four calls follow the scheduler's problem statement (Sec. 3.3): decoders
- * d_k with KV-token capacity C_k and waiting-queue length Q_k; requests with a
- * prompt length, a predicted output length, and a calibrated upper bound on
- * it (Sec. 3.2).
+ * The four scheduling calls follow the scheduler's problem statement (Sec.
+ * 3.3): decoders d_k with KV-token capacity C_k and waiting-queue length Q_k;
+ * requests with a prompt length, a predicted output length, and a calibrated
+ * upper bound on it (Sec. 3.2).
  *
  * Conventions shared by every call
  * --------------------------------
@@ -62,6 +64,9 @@ extern "C" {
 #define MAPS_E_TIMEOUT (-4)   /* a bounded device wait expired */
 #define MAPS_E_CUDA (-5)      /* CUDA runtime error; see maps_last_cuda_error */
 #define MAPS_E_WORKSPACE (-6) /* workspace smaller than the size query asked */
+
+#define MAPS_BF16 0 /* element types of keys, values, queries and outputs */
+#define MAPS_F16 1
 
 #define MAPS_MODE_SNAPSHOT 0
 #define MAPS_MODE_SEQUENTIAL 1
@@ -442,6 +447,141 @@ int maps_rr_pressure(const maps_rr_cfg *cfg, int64_t n_real, const int64_t *arri
                      const int32_t *prompt, const int32_t *out_len, int64_t *admit_us,
                      int64_t *done_us, int64_t *stats, int64_t *t_sim, void *ws,
                      size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Block tables and slot maps.  The paper counts a decoder's capacity in blocks
+ * of S tokens (Sec. 3.3); this call hands the blocks out.  Given each request's
+ * tokens now and wanted, it returns the blocks of requests that shrink (one
+ * that has finished wants 0, one whose drafted tokens were rejected wants
+ * fewer), takes blocks for those that grow, and maps every new token to its
+ * place in the cache.
+ *
+ * With hb = ceil(held / S) and wb = ceil(want / S):
+ *   1. want < held: the blocks table[r][wb .. hb) go onto the free stack, r
+ *      ascending, then along the row.  N = n_free + blocks returned.
+ *   2. want >= held: r needs wb - hb blocks.  In `order`, with P the sum of
+ *      the needs up to and with r, r is granted iff it needs none or P <= N
+ *      (so a request that needs none always goes on, and nothing overtakes
+ *      the first that does not fit).  The granted needs, in order and along
+ *      each row, take the stack's blocks from its top: need number i gets
+ *      entry N - 1 - i.
+ *   3. the new tokens of r are the positions held .. want - 1, at the indices
+ *      slot_off_out[r] .. slot_off_out[r + 1] of the outputs, granted or not.
+ *
+ *   R, S                requests (>= 0) and block size (>= 1).
+ *   held, want          [R] int32 tokens, in [0, max_blocks * S].
+ *   order               [R] int32 permutation of the requests (such as
+ *                       maps_order_local's), or NULL for index order.
+ *   table               [R][max_blocks] int32, updated in place: row r's first
+ *                       hb entries are its blocks; the new ones follow.  The
+ *                       other entries are left as they are.
+ *   free_blocks, pool   [pool] int32 stack of free blocks, updated in place.
+ *   n_free              int32 scalar, device: entries on the stack.
+ *   n_free_out          int32 scalar: entries left.
+ *   got_out             [R] int32: want where granted or shrunk, else held.
+ *   slot_off_out        [R + 1] int64.
+ *   slots_out           [slots_cap] int64: block * S + position mod S for
+ *                       every new token, -1 where r was refused.
+ *   pos_out             [slots_cap] int32 positions, or NULL.
+ * A call repeated on the same held, want, n_free and stack gives the same
+ * result.  Lengths out of their domain, an order entry outside [0, R), more
+ * new tokens than slots_cap or more returned blocks than the stack has room
+ * for are MAPS_E_RANGE (via maps_check).
+ * ---------------------------------------------------------------------- */
+size_t maps_block_tables_workspace_size(int32_t R);
+int maps_block_tables(int32_t R, int32_t S, const int32_t *held, const int32_t *want,
+                      const int32_t *order, int32_t *table, int32_t max_blocks,
+                      int32_t *free_blocks, int32_t pool, const int32_t *n_free,
+                      int32_t *n_free_out, int32_t *got_out, int64_t *slot_off_out,
+                      int64_t *slots_out, int64_t slots_cap, int32_t *pos_out, void *ws,
+                      size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
+ * A KV cache held in 4 bits.  No counterpart in the paper, whose decoders keep
+ * 16 bits: with 4 a decoder of the same memory has 3.8 times (D = 128) the
+ * token capacity C_k that the scheduler works with.
+ *
+ * A row x is one token's key or value of one KV head, D channels.  With the
+ * arithmetic in 32 bits, rounding to nearest (even at ties) at each step,
+ *     zero  = bf16(min x),  scale = bf16((max x - min x) * (1/15)),
+ *     inv   = 1 / scale, or 0 where scale < 2^-126,
+ *     code  = min(max(round((x - zero) * inv), 0), 15),
+ * and the row is held as the values scale * code + zero.  A row that holds an
+ * infinity or NaN, or whose spread passes the 32-bit range, is held as NaN.
+ *
+ * The cache is [n_blocks][H] records of maps_kv4_record_bytes(S, D) bytes
+ * (0: sizes not supported), 16-byte aligned.  D is 64, 128 or 256; S a
+ * multiple of 16 up to 4,096.  A record holds S/16 groups of 16 tokens, each
+ *     8 D bytes   K codes, a row of D/2 bytes per token, channel 2i in the low
+ *                 half of byte i;
+ *     8 D bytes   V codes, in 16-bit units of 4 neighbouring channels of one
+ *                 token (the first in the low bits): with B = min(D/32, 4),
+ *                 A = D/32/B, channel = g (D/8) + 4 (a B + b) + r and token =
+ *                 8h + 2t + e, the unit (h, a, g, t, b, e) has index
+ *                 ((((h A + a) 8 + g) 4 + t) B + b) 2 + e;
+ *     128 bytes   16 x {K scale, K zero}, 16 x {V scale, V zero}, bfloat16.
+ * A slot s is place s mod S of block floor(s / S), as maps_block_tables gives.
+ *
+ *   dtype               MAPS_BF16 or MAPS_F16, of k and v.
+ *   T, H                tokens (>= 0) and KV heads (>= 1); T * H <= 2^30.
+ *   k, v                element (i, h, d) is at i * row + h * head + d, in
+ *                       elements.  Any strides; bases and strides that are
+ *                       multiples of 16 bytes are read with wide loads.
+ *   slots               [T] int64; a negative slot: the token is skipped by
+ *                       maps_kv4_append, and read as zeros.  Slots of one
+ *                       append differ.  A slot past the cache is MAPS_E_RANGE
+ *                       (via maps_check) and treated as negative.
+ *   ws                  maps_kv4_workspace_size() bytes.
+ * ---------------------------------------------------------------------- */
+size_t maps_kv4_record_bytes(int32_t S, int32_t D);
+size_t maps_kv4_workspace_size(void);
+int maps_kv4_append(int32_t dtype, int64_t T, int32_t H, int32_t D, int32_t S, const void *k,
+                    int64_t k_row, int64_t k_head, const void *v, int64_t v_row, int64_t v_head,
+                    const int64_t *slots, void *cache, int64_t n_blocks, void *ws,
+                    size_t ws_bytes, void *stream);
+int maps_kv4_read(int32_t dtype, int64_t T, int32_t H, int32_t D, int32_t S, const int64_t *slots,
+                  const void *cache, int64_t n_blocks, void *k_out, int64_t k_row, int64_t k_head,
+                  void *v_out, int64_t v_row, int64_t v_head, void *ws, size_t ws_bytes,
+                  void *stream);
+
+/* ------------------------------------------------------------------------
+ * Attention over the 4-bit cache, for a batch of requests with any number of
+ * new tokens each: one (decode), a few (drafted tokens to be verified) or many
+ * (a chunk of a prompt).  The new tokens' keys and values are in the cache
+ * already (maps_kv4_append), so they are attended to as they are held.
+ *
+ * Request b's queries are the rows qo_off[b] .. qo_off[b + 1] of q; with n =
+ * kv_len[b] and m its queries, query i is at position p = n - m + i.  It sees
+ * the keys j in [0, n), j <= p where causal, j > p - window where window > 0;
+ * at a position below 0 it sees none.  With query head x on KV head x / (Hq / Hkv),
+ *     w_j = sm_scale * (q . k_j),  out = sum_j exp(w_j) v_j / sum_j exp(w_j),
+ *     lse = log(sum_j exp(w_j)),
+ * in 32 bits but for the weights, which meet the values' codes as products of
+ * 16-bit numbers; out is rounded once.  A query that sees no key has out = 0
+ * and lse = -infinity.  What the cache holds at places that no query sees is
+ * not used, whatever it is.
+ *
+ *   dtype               MAPS_BF16 or MAPS_F16, of q and out.
+ *   B, T                requests (>= 0) and rows of q (T <= 2^30).
+ *   Hq, Hkv             query and KV heads, Hq a multiple of Hkv, Hq <= 65,535.
+ *   D, S, cache, n_blocks   as for maps_kv4_append.
+ *   q, out              element (i, x, d) is at i * row + x * head + d; rows
+ *                       that no request has are neither read nor written.
+ *   qo_off              [B + 1] int64, non-decreasing within [0, T].
+ *   kv_len              [B] int32 tokens in the cache, in [0, max_blocks * S].
+ *   table               [B][max_blocks] int32 block tables.
+ *   causal, window      0 or 1; 0 (no window) or the keys seen, >= 1.
+ *   lse                 [T][Hq] float output, natural logarithm, or NULL.
+ * A length or a used table entry out of its domain is MAPS_E_RANGE (via
+ * maps_check); nothing outside the cache is read.
+ * ---------------------------------------------------------------------- */
+size_t maps_kv4_attention_workspace_size(int32_t B, int64_t T, int32_t Hq, int32_t Hkv, int32_t D);
+int maps_kv4_attention(int32_t dtype, int32_t B, int64_t T, int32_t Hq, int32_t Hkv, int32_t D,
+                       int32_t S, const void *q, int64_t q_row, int64_t q_head,
+                       const int64_t *qo_off, const int32_t *kv_len, const int32_t *table,
+                       int64_t max_blocks, const void *cache, int64_t n_blocks, float sm_scale,
+                       int32_t causal, int32_t window, void *out, int64_t o_row, int64_t o_head,
+                       float *lse, void *ws, size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -21,6 +21,8 @@ MAPS_E_TIMEOUT = -4
 MAPS_E_CUDA = -5
 MAPS_E_WORKSPACE = -6
 
+BF16, F16 = 0, 1
+
 MODE_SNAPSHOT = 0
 MODE_SEQUENTIAL = 1
 MODE_ALG1_SNAPSHOT = 2
@@ -67,8 +69,8 @@ def _load():
             f"{LIB_PATH} is missing: build it with paper_2609_15359_gb300.build.build() "
             "(nvcc, sm_103a). There is no CPU fallback.")
     lib = ctypes.CDLL(LIB_PATH)
-    i32, i64, u32, sz, vp = (ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32,
-                             ctypes.c_size_t, ctypes.c_void_p)
+    i32, i64, u32, sz, vp, f32 = (ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32,
+                                  ctypes.c_size_t, ctypes.c_void_p, ctypes.c_float)
     sigs = {
         "maps_version": ([], ctypes.c_int),
         "maps_last_cuda_error": ([], ctypes.c_int),
@@ -94,6 +96,19 @@ def _load():
         "maps_stream_run": ([ctypes.POINTER(StreamCfg), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz,
                              vp],
                             ctypes.c_int),
+        "maps_block_tables_workspace_size": ([i32], sz),
+        "maps_block_tables": ([i32, i32, vp, vp, vp, vp, i32, vp, i32, vp, vp, vp, vp, vp, i64, vp,
+                               vp, sz, vp], ctypes.c_int),
+        "maps_kv4_record_bytes": ([i32, i32], sz),
+        "maps_kv4_workspace_size": ([], sz),
+        "maps_kv4_append": ([i32, i64, i32, i32, i32, vp, i64, i64, vp, i64, i64, vp, vp, i64, vp,
+                             sz, vp], ctypes.c_int),
+        "maps_kv4_read": ([i32, i64, i32, i32, i32, vp, vp, i64, vp, i64, i64, vp, i64, i64, vp,
+                           sz, vp], ctypes.c_int),
+        "maps_kv4_attention_workspace_size": ([i32, i64, i32, i32, i32], sz),
+        "maps_kv4_attention": ([i32, i32, i64, i32, i32, i32, i32, vp, i64, i64, vp, vp, vp, i64,
+                                vp, i64, f32, i32, i32, vp, i64, i64, vp, vp, sz, vp],
+                               ctypes.c_int),
     }
     for name, (args, res) in sigs.items():
         fn = getattr(lib, name)
@@ -110,7 +125,10 @@ EXPORTS = ("maps_version", "maps_last_cuda_error", "maps_check", "maps_set_dispa
            "maps_dispatch_workspace_size", "maps_dispatch",
            "maps_order_local_workspace_size", "maps_order_local", "maps_order_local_static",
            "maps_stream_workspace_size", "maps_stream_run",
-           "maps_rr_pressure_workspace_size", "maps_rr_pressure")
+           "maps_rr_pressure_workspace_size", "maps_rr_pressure",
+           "maps_block_tables_workspace_size", "maps_block_tables", "maps_kv4_record_bytes",
+           "maps_kv4_workspace_size", "maps_kv4_append", "maps_kv4_read",
+           "maps_kv4_attention_workspace_size", "maps_kv4_attention")
 
 
 def _stream(stream) -> ctypes.c_void_p:
@@ -283,3 +301,103 @@ def maps_rr_pressure(N: int, C: int, t_tok_us: int, theta_ppm: int, arrival_us, 
                                 _ptr(admit_out, torch.int64), _ptr(done_out, torch.int64),
                                 _ptr(stats_out, torch.int64), _ptr(t_sim_out, torch.int64),
                                 ws.ptr, ws.nbytes, _stream(stream))
+
+
+def maps_block_tables(S: int, held, want, table, free_blocks, n_free, n_free_out, got_out,
+                      slot_off_out, slots_out, pos_out=None, order=None,
+                      ws: Workspace | None = None, stream=None) -> int:
+    """Hands out the KV blocks: table [R][max_blocks] and free_blocks [pool]
+    int32 are updated in place; slots_out [cap] int64 holds the new tokens'."""
+    R = held.numel()
+    ws = ws or Workspace()
+    ws.ensure(lib.maps_block_tables_workspace_size(R))
+    return lib.maps_block_tables(R, S, _ptr(held, torch.int32), _ptr(want, torch.int32),
+                                 _ptr(order, torch.int32), _ptr(table, torch.int32),
+                                 table.shape[1], _ptr(free_blocks, torch.int32),
+                                 free_blocks.numel(), _ptr(n_free, torch.int32),
+                                 _ptr(n_free_out, torch.int32), _ptr(got_out, torch.int32),
+                                 _ptr(slot_off_out, torch.int64), _ptr(slots_out, torch.int64),
+                                 slots_out.numel(), _ptr(pos_out, torch.int32), ws.ptr, ws.nbytes,
+                                 _stream(stream))
+
+
+def _rows(t, dtype=None):
+    """(pointer, row stride, head stride) of a [rows, heads, channels] tensor
+    whose channels are contiguous; any strides otherwise."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError("expected a CUDA tensor")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"expected {dtype}, got {t.dtype}")
+    if t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] > 1):
+        raise TypeError("expected [rows, heads, channels] with contiguous channels")
+    return ctypes.c_void_p(t.data_ptr()), t.stride(0), t.stride(1)
+
+
+def _dtype(t) -> int:
+    try:
+        return {torch.bfloat16: BF16, torch.float16: F16}[t.dtype]
+    except KeyError:
+        raise TypeError(f"expected torch.bfloat16 or torch.float16, got {t.dtype}") from None
+
+
+def kv4_cache_shape(n_blocks: int, H: int, S: int, D: int) -> tuple[int, int, int]:
+    """Shape of a 4-bit cache (uint8): [blocks][KV heads][record bytes]."""
+    nbytes = lib.maps_kv4_record_bytes(S, D)
+    if nbytes == 0:
+        raise ValueError(f"no 4-bit cache for blocks of {S} tokens and {D} channels")
+    return n_blocks, H, nbytes
+
+
+def _kv4(cache, S: int, D: int, H: int):
+    if cache.dim() != 3 or tuple(cache.shape) != kv4_cache_shape(cache.shape[0], H, S, D):
+        raise ValueError(f"a cache of {H} heads, blocks of {S} and {D} channels does not have shape "
+                         f"{tuple(cache.shape)}")
+    return _ptr(cache, torch.uint8)
+
+
+def maps_kv4_append(k, v, slots, cache, S: int, ws: Workspace | None = None, stream=None) -> int:
+    """Writes k, v [T, H, D] (bf16 or fp16) to the slots [T] int64 of the cache."""
+    T, H, D = k.shape
+    if v.shape != k.shape or slots.numel() != T:
+        raise ValueError("k, v and slots differ in size")
+    ws = ws or Workspace()
+    ws.ensure(lib.maps_kv4_workspace_size())
+    return lib.maps_kv4_append(_dtype(k), T, H, D, S, *_rows(k), *_rows(v, k.dtype),
+                               _ptr(slots, torch.int64), _kv4(cache, S, D, H), cache.shape[0],
+                               ws.ptr, ws.nbytes, _stream(stream))
+
+
+def maps_kv4_read(slots, cache, S: int, k_out, v_out, ws: Workspace | None = None,
+                  stream=None) -> int:
+    """Reads the slots [T] of the cache back into k_out, v_out [T, H, D]."""
+    T, H, D = k_out.shape
+    if v_out.shape != k_out.shape or slots.numel() != T:
+        raise ValueError("k_out, v_out and slots differ in size")
+    ws = ws or Workspace()
+    ws.ensure(lib.maps_kv4_workspace_size())
+    return lib.maps_kv4_read(_dtype(k_out), T, H, D, S, _ptr(slots, torch.int64),
+                             _kv4(cache, S, D, H), cache.shape[0], *_rows(k_out),
+                             *_rows(v_out, k_out.dtype), ws.ptr, ws.nbytes, _stream(stream))
+
+
+def maps_kv4_attention(q, qo_off, kv_len, table, cache, S: int, sm_scale: float, out, lse_out=None,
+                       causal: bool = True, window: int = 0, ws: Workspace | None = None,
+                       stream=None) -> int:
+    """Attention of q [T, Hq, D] over the 4-bit cache: qo_off [B + 1] int64,
+    kv_len [B] int32, table [B][max_blocks] int32; out like q, lse_out [T][Hq]
+    float32 or None."""
+    T, Hq, D = q.shape
+    B, Hkv = kv_len.numel(), cache.shape[1]
+    if out.shape != q.shape or qo_off.numel() != B + 1 or table.shape[0] != B:
+        raise ValueError("q, out, qo_off, kv_len and table differ in size")
+    if lse_out is not None and tuple(lse_out.shape) != (T, Hq):
+        raise ValueError("lse_out is [T, Hq]")
+    ws = ws or Workspace()
+    ws.ensure(lib.maps_kv4_attention_workspace_size(B, T, Hq, Hkv, D))
+    return lib.maps_kv4_attention(_dtype(q), B, T, Hq, Hkv, D, S, *_rows(q),
+                                  _ptr(qo_off, torch.int64), _ptr(kv_len, torch.int32),
+                                  _ptr(table, torch.int32), table.shape[1],
+                                  _kv4(cache, S, D, Hkv), cache.shape[0], float(sm_scale),
+                                  int(bool(causal)), int(window), *_rows(out, q.dtype),
+                                  _ptr(lse_out, torch.float32), ws.ptr, ws.nbytes,
+                                  _stream(stream))
