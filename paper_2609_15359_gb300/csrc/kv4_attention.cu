@@ -42,6 +42,8 @@ struct AttnArgs {
   const uint8_t *cache;
   float scale;
   int32_t causal, window, wide;
+  int64_t block_bytes;  // of all heads
+  int32_t block_groups, block_shift;  // groups of a block, and their logarithm where they are a power of two, else -1
   void *out;
   float *lse;
   int64_t *prefix;     // [B + 1] units before each request, where a block does not sum it up
@@ -79,44 +81,33 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-  uint32_t y;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(y) : "f"(hi), "f"(lo));
+__device__ __forceinline__ float lg2(float x) {
+  float y;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ float lo_bf16(uint32_t x) { return __uint_as_float(x << 16); }
-__device__ __forceinline__ float hi_bf16(uint32_t x) { return __uint_as_float(x & 0xffff0000u); }
+__device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
+  uint32_t y;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(y) : "f"(hi), "f"(lo));
+  return y;
+}
 
-// Two keys' codes as 16-bit numbers, one shift and one bit operation for both.  bfloat16: 16 + code,
-// the code in the mantissa's upper bits (128 + code would cost one shift less in four, and eight
-// times the rounding error of a sum that the offset dominates).  half: code * 2^-24, the bare code
-// being a subnormal number, which the tensor core multiplies exactly.
-template <class T>
-struct Key;
-template <>
-struct Key<__nv_bfloat16> {
-  static constexpr float kOffset = 16.0f, kUnit = 1.0f;
-  static constexpr int kParts = 1;  // 16-bit numbers that a weight is the sum of
-  static __device__ __forceinline__ uint32_t two(uint32_t w, int r) {  // codes r and r + 4 of a word
-    return ((r == 0 ? w << 3 : w >> (4 * r - 3)) & 0x00780078u) | 0x41804180u;
-  }
-  static __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-  }
+// A word's eight codes as four pairs of half numbers, in five operations: a bare code is the
+// subnormal number code * 2^-24, four bits higher it is code * 2^-20, and the tensor core multiplies
+// both exactly.  The odd pairs' factor of 16 is taken off in the other operand (keys) or the sum (values).
+struct Codes {
+  uint32_t x[4];  // codes (r, r + 4)
 };
-template <>
-struct Key<__half> {
-  static constexpr float kOffset = 0.0f, kUnit = 16777216.0f;
-  static constexpr int kParts = 2;  // a half output shows the rounding of a weight to 8 bits
-  static __device__ __forceinline__ uint32_t two(uint32_t w, int r) { return (w >> (4 * r)) & 0x000f000fu; }
-  static __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-  }
-};
-// Two values' codes as 128 + code in bfloat16, whatever the queries' type: a weight times a scale needs the range.
-__device__ __forceinline__ uint32_t two_values(uint32_t w, int r) { return ((w >> (4 * r)) & 0x000f000fu) | 0x43004300u; }
+__device__ __forceinline__ Codes codes_of(uint32_t w) {
+  const uint32_t v = w >> 8;
+  return {{w & 0x000f000fu, w & 0x00f000f0u, v & 0x000f000fu, v & 0x00f000f0u}};
+}
+constexpr float kEven = 16777216.0f, kOdd = 1048576.0f;  // 2^24, 2^20
+
+__device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
 
 // ---------------------------------------------------------------------------- the work, in units
 template <int D, int NT>
@@ -230,6 +221,13 @@ struct Cursor {
   }
 };
 
+struct Yes { static constexpr bool value = true; };
+struct No { static constexpr bool value = false; };
+
+// Weights are held relative to the largest weight times value scale seen, so that what enters the
+// second product is at most 1; scales count as at least 2^-60 there, so that a weight itself stays finite.
+constexpr float kMinLog = -60.0f;
+
 // ---------------------------------------------------------------------------- the kernel
 template <class T, int D, int NT>
 __global__ void __launch_bounds__(kThreads, 1) attn_few_kernel(const AttnArgs a) {
@@ -266,6 +264,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_few_kernel(const AttnArgs a)
   const int64_t me = static_cast<int64_t>(blockIdx.x) * kWarps + warp;
   const int64_t u0 = start(me), u1 = start(me + 1);
   const int group = a.Hq / a.Hkv;
+  const float sl2 = a.scale * 1.4426950408889634f, k_sign = a.scale < 0.0f ? -1.0f : 1.0f, k_unit = k_sign * kEven;
 
   if (u0 < u1) {
     // The loads run ahead of the products by the ring's depth; lanes below kGroups move one group each.
@@ -273,24 +272,25 @@ __global__ void __launch_bounds__(kThreads, 1) attn_few_kernel(const AttnArgs a)
     ahead.seek<Sh::kTok, Sh::kRows>(a, prefix, u0);
     Cursor at = ahead;
     int64_t issued = u0;
-    int32_t block = -1;  // the next unit's block of this lane's group, fetched one step early
+    // the next unit's group of this lane: whether it holds tokens, its block (fetched one step early), its place there and head
+    bool mine = false;
+    int32_t block = -1, place = 0;
     auto fetch = [&]() {
-      block = -1;
       const int32_t tok = ahead.r.lo + ahead.tile * Sh::kTok + lane * kGroup;
-      if (issued < u1 && lane < Sh::kGroups && tok < ahead.r.n) block = a.table[ahead.b * a.max_blocks + tok / a.S];
+      mine = issued < u1 && lane < Sh::kGroups && tok < ahead.r.n;
+      const int32_t grp = tok / kGroup, page = a.block_shift >= 0 ? grp >> a.block_shift : grp / a.block_groups;
+      place = ahead.h * a.block_groups + grp - page * a.block_groups;
+      if (mine) block = a.table[ahead.b * a.max_blocks + page];
     };
     auto issue = [&](int stage) {
-      const int32_t tok = ahead.r.lo + ahead.tile * Sh::kTok + lane * kGroup;
-      const bool mine = issued < u1 && lane < Sh::kGroups && tok < ahead.r.n;
       const bool good = mine && block >= 0 && block < a.n_blocks;
       if (mine && !good) flag_error(a.status, MAPS_E_RANGE);
       const uint32_t n = __popc(__ballot_sync(0xffffffffu, good));
       if (lane == 0) bar_expect(bar32 + 8 * stage, n * kv4_group_bytes(D));
       __syncwarp();
-      if (good) {
-        const int64_t rec = (static_cast<int64_t>(block) * a.Hkv + ahead.h) * (a.S / kGroup) + tok % a.S / kGroup;
-        bulk_load(ring32 + stage * Sh::kBytes + lane * kv4_group_bytes(D), a.cache + rec * kv4_group_bytes(D), kv4_group_bytes(D), bar32 + 8 * stage);
-      }
+      if (good)
+        bulk_load(ring32 + stage * Sh::kBytes + lane * kv4_group_bytes(D), a.cache + (block * a.block_bytes + place * static_cast<int64_t>(kv4_group_bytes(D))),
+                  kv4_group_bytes(D), bar32 + 8 * stage);
       if (issued < u1) {
         ++issued;
         if (++ahead.tile == ahead.r.tiles && issued < u1) ahead.next_item<Sh::kTok, Sh::kRows>(a);
@@ -310,44 +310,55 @@ __global__ void __launch_bounds__(kThreads, 1) attn_few_kernel(const AttnArgs a)
       const int64_t q0 = a.off[at.b];
       const int rows = r.n_q * group;  // n_q * group <= T * Hq fits the checks of the host
       uint32_t qf[NT][kSteps][2];
-      float qs[NT][2];
+      float qs[NT][2], qu[NT][2];  // a row's sum, and what a score of it is to be multiplied by
       int32_t row_lo[NT][2], row_hi[NT][2];
       int32_t all_lo = 0, all_hi = 0x7fffffff;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         const int R = at.rt * Sh::kRows + nt * 8 + g;
-        float sum = 0.0f;
-        if (R < rows) {
-          const T *src = static_cast<const T *>(a.q) + (q0 + R / group) * a.q_row + (at.h * group + R % group) * a.q_head + t * (D / 4);
+        // A row is scaled by a power of two to fill half's range; only its smallest channels, below 2^-38 of the largest, lose bits.
+        float x[kSteps * 4], top = 0.0f;
+        const bool there = R < rows;
+        const T *src = static_cast<const T *>(a.q) + (there ? (q0 + R / group) * a.q_row + (at.h * group + R % group) * a.q_head + t * (D / 4) : 0);
 #pragma unroll
-          for (int i = 0; i < kWords; ++i) {
-            uint32_t x[4];
+        for (int i = 0; i < kWords; ++i) {
+          uint4 y = make_uint4(0, 0, 0, 0);
+          T *z = reinterpret_cast<T *>(&y);
+          if (there) {
             if (a.wide) {
-              *reinterpret_cast<uint4 *>(x) = *reinterpret_cast<const uint4 *>(src + 8 * i);
+              y = *reinterpret_cast<const uint4 *>(src + 8 * i);
             } else {
-              const uint16_t *p = reinterpret_cast<const uint16_t *>(src + 8 * i);
 #pragma unroll
-              for (int e = 0; e < 4; ++e) x[e] = p[2 * e] | static_cast<uint32_t>(p[2 * e + 1]) << 16;
+              for (int e = 0; e < 8; ++e) z[e] = src[8 * i + e];
             }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const T *y = reinterpret_cast<const T *>(&x[e]);
-              sum += Cvt<T>::to(y[0]) + Cvt<T>::to(y[1]);
-            }
-            qf[nt][2 * i][0] = __byte_perm(x[0], x[2], 0x5410);
-            qf[nt][2 * i][1] = __byte_perm(x[0], x[2], 0x7632);
-            qf[nt][2 * i + 1][0] = __byte_perm(x[1], x[3], 0x5410);
-            qf[nt][2 * i + 1][1] = __byte_perm(x[1], x[3], 0x7632);
           }
-        } else {
 #pragma unroll
-          for (int i = 0; i < kSteps; ++i) qf[nt][i][0] = qf[nt][i][1] = 0;
+          for (int e = 0; e < 8; ++e) {
+            x[8 * i + e] = Cvt<T>::to(z[e]);
+            top = fmaxf(top, fabsf(x[8 * i + e]));
+          }
+        }
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const int ef = min(max(static_cast<int>(__float_as_uint(top) >> 23), 20), 254);  // top is 2^(ef - 127) or a little more
+        const float up = __uint_as_float(static_cast<uint32_t>(268 - ef) << 23);             // makes it 2^14 or a little more
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[8 * i + e] *= up, sum += x[8 * i + e];
+          qf[nt][2 * i][0] = pack_half(x[8 * i], x[8 * i + 4]);
+          qf[nt][2 * i][1] = pack_half(x[8 * i + 1] * 0.0625f, x[8 * i + 5] * 0.0625f);
+          qf[nt][2 * i + 1][0] = pack_half(x[8 * i + 2], x[8 * i + 6]);
+          qf[nt][2 * i + 1][1] = pack_half(x[8 * i + 3] * 0.0625f, x[8 * i + 7] * 0.0625f);
         }
         sum += __shfl_xor_sync(0xffffffffu, sum, 1);
         sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+        const float unit = fmaxf(fabsf(sl2) * __uint_as_float(static_cast<uint32_t>(ef - 14) << 23), 1.17549435e-38f);
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           qs[nt][e] = __shfl_sync(0xffffffffu, sum, (2 * t + e) * 4);
+          qu[nt][e] = __shfl_sync(0xffffffffu, unit, (2 * t + e) * 4);
           const int Rc = at.rt * Sh::kRows + nt * 8 + 2 * t + e;
           row_lo[nt][e] = 0;
           row_hi[nt][e] = r.n;  // a column that is no row sees everything; nobody reads it
@@ -387,152 +398,144 @@ __global__ void __launch_bounds__(kThreads, 1) attn_few_kernel(const AttnArgs a)
         }
         const uint8_t *buf = ring + stage * Sh::kBytes;
         const int32_t tok0 = r.lo + at.tile * Sh::kTok;
-        const bool full = tok0 >= all_lo && tok0 + Sh::kTok <= all_hi;  // every row sees every token
-
-        // ---- scores: 16 tokens x 8 rows, depth D
-        float s[Sh::kGroups][NT][4];
+        auto unit_sums = [&](auto every) {
+          constexpr bool kEvery = decltype(every)::value;  // every row sees every token
+          // ---- scores, up to a row's factor: 16 tokens x 8 rows, depth D
+          float s[Sh::kGroups][NT][4];
+          float vs[Sh::kGroups][2];
+          float top[NT][2];  // of score + log2(value scale)
 #pragma unroll
-        for (int gr = 0; gr < Sh::kGroups; ++gr) {
-          const uint8_t *grp = buf + gr * kv4_group_bytes(D);
-          uint32_t k0[kWords], k1[kWords];
-          if (kWords == 2) {
-            *reinterpret_cast<uint2 *>(k0) = *reinterpret_cast<const uint2 *>(grp + g * (D / 2) + t * (D / 8));
-            *reinterpret_cast<uint2 *>(k1) = *reinterpret_cast<const uint2 *>(grp + (g + 8) * (D / 2) + t * (D / 8));
-          } else {
+          for (int nt = 0; nt < NT; ++nt) top[nt][0] = top[nt][1] = -INFINITY;
 #pragma unroll
-            for (int i = 0; i < kWords; i += 4) {
-              *reinterpret_cast<uint4 *>(k0 + i) = *reinterpret_cast<const uint4 *>(grp + g * (D / 2) + t * (D / 8) + 4 * i);
-              *reinterpret_cast<uint4 *>(k1 + i) = *reinterpret_cast<const uint4 *>(grp + (g + 8) * (D / 2) + t * (D / 8) + 4 * i);
+          for (int gr = 0; gr < Sh::kGroups; ++gr) {
+            const uint8_t *grp = buf + gr * kv4_group_bytes(D);
+            uint32_t k0[kWords], k1[kWords];
+            if (kWords == 2) {
+              *reinterpret_cast<uint2 *>(k0) = *reinterpret_cast<const uint2 *>(grp + g * (D / 2) + t * (D / 8));
+              *reinterpret_cast<uint2 *>(k1) = *reinterpret_cast<const uint2 *>(grp + (g + 8) * (D / 2) + t * (D / 8));
+            } else {
+#pragma unroll
+              for (int i = 0; i < kWords; i += 4) {
+                *reinterpret_cast<uint4 *>(k0 + i) = *reinterpret_cast<const uint4 *>(grp + g * (D / 2) + t * (D / 8) + 4 * i);
+                *reinterpret_cast<uint4 *>(k1 + i) = *reinterpret_cast<const uint4 *>(grp + (g + 8) * (D / 2) + t * (D / 8) + 4 * i);
+              }
             }
-          }
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[gr][nt][e] = 0.0f;
-#pragma unroll
-          for (int st = 0; st < kSteps; ++st) {
-            const int i = st / 2, rr = st % 2 * 2;
-            const uint32_t a0 = Key<T>::two(k0[i], rr), a1 = Key<T>::two(k1[i], rr), a2 = Key<T>::two(k0[i], rr + 1), a3 = Key<T>::two(k1[i], rr + 1);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) Key<T>::mma(s[gr][nt], a0, a1, a2, a3, qf[nt][st][0], qf[nt][st][1]);
-          }
-          const uint32_t *par = reinterpret_cast<const uint32_t *>(grp + 16 * D);
-          const float sl2 = a.scale * 1.4426950408889634f;
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            const float2 p = kv4_param(par[g + 8 * half]);
-            const float ks = p.x * (sl2 * Key<T>::kUnit), kz = fmaf(-Key<T>::kOffset, p.x, p.y) * sl2;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-              for (int e = 0; e < 2; ++e) s[gr][nt][2 * half + e] = fmaf(ks, s[gr][nt][2 * half + e], kz * qs[nt][e]);
-          }
-          if (!full) {
+              for (int e = 0; e < 4; ++e) s[gr][nt][e] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) {
+              const Codes x = codes_of(k0[i]), y = codes_of(k1[i]);
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) {
+                mma(s[gr][nt], x.x[0], y.x[0], x.x[1], y.x[1], qf[nt][2 * i][0], qf[nt][2 * i][1]);
+                mma(s[gr][nt], x.x[2], y.x[2], x.x[3], y.x[3], qf[nt][2 * i + 1][0], qf[nt][2 * i + 1][1]);
+              }
+            }
+            const uint32_t *par = reinterpret_cast<const uint32_t *>(grp + 16 * D);
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
+              const float2 p = kv4_param(par[g + 8 * half]);
+              vs[gr][half] = kv4_param(par[16 + g + 8 * half]).x;
+              const float ks = p.x * k_unit, kz = p.y * k_sign, ls = fmaxf(lg2(vs[gr][half]), kMinLog);
               const int32_t tok = tok0 + gr * kGroup + g + 8 * half;
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int e = 0; e < 2; ++e)
-                  if (tok < row_lo[nt][e] || tok >= row_hi[nt][e]) s[gr][nt][2 * half + e] = -INFINITY;
+                for (int e = 0; e < 2; ++e) {
+                  float &x = s[gr][nt][2 * half + e];
+                  x = fmaf(ks, x, kz * qs[nt][e]);
+                  if (!kEvery && (tok < row_lo[nt][e] || tok >= row_hi[nt][e])) x = -INFINITY;
+                  top[nt][e] = fmaxf(top[nt][e], fmaf(x, qu[nt][e], ls));
+                }
             }
           }
-        }
 
-        // ---- running maximum
-        float ref[NT][2];
-        bool grew = false;
-        float mn[NT][2];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            float x = fmaxf(s[0][nt][e], s[0][nt][2 + e]);
-#pragma unroll
-            for (int gr = 1; gr < Sh::kGroups; ++gr) x = fmaxf(x, fmaxf(s[gr][nt][e], s[gr][nt][2 + e]));
-            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
-            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
-            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-            mn[nt][e] = fmaxf(m[nt][e], x);
-            grew |= mn[nt][e] > m[nt][e];
-          }
-        if (__any_sync(0xffffffffu, grew)) {
+          // ---- running maximum
+          bool grew = false;
+          float ref[NT][2];
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const float c = mn[nt][e] == -INFINITY ? 1.0f : ex2(m[nt][e] - mn[nt][e]);
-              m[nt][e] = mn[nt][e];
-              l[nt][e] *= c;
-              w[nt][e] *= c;
-#pragma unroll
-              for (int j = 0; j < kSteps; ++j) o[nt][j][e] *= c, o[nt][j][2 + e] *= c;
+              float x = top[nt][e];
+              x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+              x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+              x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+              top[nt][e] = fmaxf(m[nt][e], x);
+              grew |= top[nt][e] > m[nt][e];
             }
-        }
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) ref[nt][e] = m[nt][e] == -INFINITY ? 0.0f : m[nt][e];
-
-        // ---- weights and sums over the values
-#pragma unroll
-        for (int gr = 0; gr < Sh::kGroups; ++gr) {
-          const uint8_t *grp = buf + gr * kv4_group_bytes(D);
-          const uint32_t *par = reinterpret_cast<const uint32_t *>(grp + 16 * D) + 16;
-          constexpr int kParts = Key<T>::kParts;
-          uint32_t pf[NT][kParts][2];
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            const float2 p = kv4_param(par[g + 8 * half]);
-            const int32_t tok = tok0 + gr * kGroup + g + 8 * half;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              float ps[2], pz[2];
-#pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                const float x = ex2(s[gr][nt][2 * half + e] - ref[nt][e]);
-                l[nt][e] += x;
-                ps[e] = x * p.x;
-                pz[e] = x * p.y;
-                // a token that the row does not see has weight 0, and whatever its scale is stays out
-                if (!full && (tok < row_lo[nt][e] || tok >= row_hi[nt][e])) ps[e] = pz[e] = 0.0f;
-              }
-              const uint32_t hi = pack_bf16(ps[0], ps[1]);
-              float r0 = lo_bf16(hi), r1 = hi_bf16(hi);
-              pf[nt][0][half] = transpose8(hi);
-              if (kParts == 2) {
-                const uint32_t lo = pack_bf16(ps[0] - r0, ps[1] - r1);
-                r0 += lo_bf16(lo);
-                r1 += hi_bf16(lo);
-                pf[nt][kParts - 1][half] = transpose8(lo);
-              }
-              w[nt][0] += fmaf(-128.0f, r0, pz[0]);
-              w[nt][1] += fmaf(-128.0f, r1, pz[1]);
-            }
-          }
-          uint32_t v0[kWords], v1[kWords];
-          const uint8_t *vb = grp + 8 * D;
-          if (kWords == 2) {
-            *reinterpret_cast<uint2 *>(v0) = *reinterpret_cast<const uint2 *>(vb + lane * 8);
-            *reinterpret_cast<uint2 *>(v1) = *reinterpret_cast<const uint2 *>(vb + 256 + lane * 8);
-          } else {
-#pragma unroll
-            for (int i = 0; i < kWords; i += 4) {
-              *reinterpret_cast<uint4 *>(v0 + i) = *reinterpret_cast<const uint4 *>(vb + i / 4 * 512 + lane * 16);
-              *reinterpret_cast<uint4 *>(v1 + i) = *reinterpret_cast<const uint4 *>(vb + (kWords + i) / 4 * 512 + lane * 16);
-            }
-          }
-#pragma unroll
-          for (int j = 0; j < kSteps; ++j) {
-            const int i = j / 2, rr = j % 2 * 2;
-            const uint32_t a0 = two_values(v0[i], rr), a1 = two_values(v0[i], rr + 1), a2 = two_values(v1[i], rr), a3 = two_values(v1[i], rr + 1);
+          if (__any_sync(0xffffffffu, grew)) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-              for (int q = 0; q < kParts; ++q) Key<__nv_bfloat16>::mma(o[nt][j], a0, a1, a2, a3, pf[nt][q][0], pf[nt][q][1]);
+              for (int e = 0; e < 2; ++e) {
+                const float c = top[nt][e] == -INFINITY ? 1.0f : ex2(m[nt][e] - top[nt][e]);
+                m[nt][e] = top[nt][e];
+                l[nt][e] *= c;
+                w[nt][e] *= c;
+#pragma unroll
+                for (int j = 0; j < kSteps; ++j) o[nt][j][e] *= c, o[nt][j][2 + e] *= c;
+              }
           }
-        }
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) ref[nt][e] = m[nt][e] == -INFINITY ? 0.0f : -m[nt][e];
+
+          // ---- weights and sums over the values
+#pragma unroll
+          for (int gr = 0; gr < Sh::kGroups; ++gr) {
+            const uint8_t *grp = buf + gr * kv4_group_bytes(D);
+            const uint32_t *par = reinterpret_cast<const uint32_t *>(grp + 16 * D) + 16;
+            uint32_t pf[NT][2];
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              const float vz = kv4_param(par[g + 8 * half]).y;
+              const int32_t tok = tok0 + gr * kGroup + g + 8 * half;
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) {
+                float ps[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                  const float x = ex2(fmaf(s[gr][nt][2 * half + e], qu[nt][e], ref[nt][e]));
+                  l[nt][e] += x;
+                  // a token that the row does not see has weight 0, and whatever its scale is stays out
+                  const bool out = !kEvery && (tok < row_lo[nt][e] || tok >= row_hi[nt][e]);
+                  ps[e] = out ? 0.0f : x * vs[gr][half];
+                  w[nt][e] = out ? w[nt][e] : fmaf(x, vz, w[nt][e]);
+                }
+                pf[nt][half] = transpose8(pack_half(ps[0], ps[1]));
+              }
+            }
+            uint32_t v0[kWords], v1[kWords];
+            const uint8_t *vb = grp + 8 * D;
+            if (kWords == 2) {
+              *reinterpret_cast<uint2 *>(v0) = *reinterpret_cast<const uint2 *>(vb + lane * 8);
+              *reinterpret_cast<uint2 *>(v1) = *reinterpret_cast<const uint2 *>(vb + 256 + lane * 8);
+            } else {
+#pragma unroll
+              for (int i = 0; i < kWords; i += 4) {
+                *reinterpret_cast<uint4 *>(v0 + i) = *reinterpret_cast<const uint4 *>(vb + i / 4 * 512 + lane * 16);
+                *reinterpret_cast<uint4 *>(v1 + i) = *reinterpret_cast<const uint4 *>(vb + (kWords + i) / 4 * 512 + lane * 16);
+              }
+            }
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) {
+              const Codes x = codes_of(v0[i]), y = codes_of(v1[i]);
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) {
+                mma(o[nt][2 * i], x.x[0], x.x[1], y.x[0], y.x[1], pf[nt][0], pf[nt][1]);
+                mma(o[nt][2 * i + 1], x.x[2], x.x[3], y.x[2], y.x[3], pf[nt][0], pf[nt][1]);
+              }
+            }
+          }
+        };
+        if (tok0 >= all_lo && tok0 + Sh::kTok <= all_hi)
+          unit_sums(Yes{});
+        else
+          unit_sums(No{});
         __syncwarp();  // the stage has been read
         issue(stage);
         if (++stage == Sh::kStages) stage = 0, parity ^= 1;
@@ -566,8 +569,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_few_kernel(const AttnArgs a)
             T y[kCh];
 #pragma unroll
             for (int j = 0; j < kSteps; ++j) {
-              y[2 * j] = Cvt<T>::from((o[nt][j][e] + add) * inv);
-              y[2 * j + 1] = Cvt<T>::from((o[nt][j][2 + e] + add) * inv);
+              y[2 * j] = Cvt<T>::from(fmaf(o[nt][j][e], kEven, add) * inv);
+              y[2 * j + 1] = Cvt<T>::from(fmaf(o[nt][j][2 + e], kOdd, add) * inv);
             }
             if (a.wide) {
 #pragma unroll
@@ -591,8 +594,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_few_kernel(const AttnArgs a)
             float *dst = part + R * D + g * kCh;
 #pragma unroll
             for (int j = 0; j < kSteps; ++j) {
-              dst[2 * j] = o[nt][j][e] + w[nt][e];
-              dst[2 * j + 1] = o[nt][j][2 + e] + w[nt][e];
+              dst[2 * j] = fmaf(o[nt][j][e], kEven, w[nt][e]);
+              dst[2 * j + 1] = fmaf(o[nt][j][2 + e], kOdd, w[nt][e]);
             }
             if (g == 0) {
               part[Sh::kRows * D + R] = m[nt][e];
@@ -620,14 +623,56 @@ __global__ void __launch_bounds__(kThreads, 1) attn_few_kernel(const AttnArgs a)
   auto part_of = [&](int slot) -> const float * {
     return slot % 2 == 0 ? first_parts + slot / 2 * Sh::kPart : reinterpret_cast<const float *>(ring_all + slot / 2 * Sh::kStages * Sh::kBytes);
   };
-  auto write_row = [&](int b, int h, int rt, int R, int d, float num, float mm, float ll) {
-    const Req r = request<Sh::kTok, Sh::kRows>(a, b);
+  auto write_row = [&](int b, int h, int rt, int R, int d, float4 num, float mm, float ll) {
     const int row = rt * Sh::kRows + R;
-    if (row >= r.n_q * group) return;
-    const int64_t i = a.off[b] + row / group;
+    const int64_t q0 = a.off[b];
+    if (row >= (a.off[b + 1] - q0) * group) return;
+    const int64_t i = q0 + row / group;
     const int hq = h * group + row % group;
-    static_cast<T *>(a.out)[i * a.o_row + hq * a.o_head + d] = Cvt<T>::from(ll == 0.0f ? 0.0f : num / ll);
+    const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
+    T *dst = static_cast<T *>(a.out) + i * a.o_row + hq * a.o_head + d;
+    T y[4] = {Cvt<T>::from(num.x * inv), Cvt<T>::from(num.y * inv), Cvt<T>::from(num.z * inv), Cvt<T>::from(num.w * inv)};
+    if (a.wide) {
+      *reinterpret_cast<uint2 *>(dst) = *reinterpret_cast<const uint2 *>(y);
+    } else {
+#pragma unroll
+      for (int c = 0; c < 4; ++c) dst[c] = y[c];
+    }
     if (d == 0 && a.lse) a.lse[i * a.Hq + hq] = ll == 0.0f ? -INFINITY : (mm + log2f(ll)) * 0.6931471805599453f;
+  };
+  // Sums the parts k0 <= k < k1 that `has` says count, each brought to their common maximum; four channels a thread.
+  auto join = [&](int k0, int k1, auto has, auto part, auto load, auto load_one, auto put) {
+    for (int x = 4 * tid; x < Sh::kRows * D; x += 4 * kThreads) {
+      const int R = x / D, d = x - R * D;
+      float4 num = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      float M = -INFINITY, den = 0.0f;
+      for (int k = k0; k < k1; k += 4) {  // four at a time: their loads do not wait for one another
+        float4 v[4];
+        float mk[4], lk[4], top = M;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          mk[j] = -INFINITY, lk[j] = 0.0f, v[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          if (k + j < k1 && has(k + j)) {
+            const float *p = part(k + j);
+            v[j] = load(p + x);
+            mk[j] = load_one(p + Sh::kRows * D + R);
+            lk[j] = load_one(p + Sh::kRows * D + Sh::kRows + R);
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) top = fmaxf(top, mk[j]);
+        const float c = top == -INFINITY ? 1.0f : ex2(M - top);
+        num.x *= c, num.y *= c, num.z *= c, num.w *= c, den *= c;
+        M = top;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float f = top == -INFINITY ? 0.0f : ex2(mk[j] - top);
+          num.x = fmaf(f, v[j].x, num.x), num.y = fmaf(f, v[j].y, num.y), num.z = fmaf(f, v[j].z, num.z), num.w = fmaf(f, v[j].w, num.w);
+          den = fmaf(f, lk[j], den);
+        }
+      }
+      put(R, d, num, M, den);
+    }
   };
   for (int s0 = 0; s0 < 2 * kWarps;) {
     const int64_t id = s_id[s0];
@@ -640,26 +685,16 @@ __global__ void __launch_bounds__(kThreads, 1) attn_few_kernel(const AttnArgs a)
     const int tiles = s_tiles[s0], b = s_b[s0], h = s_h[s0], rt = s_rt[s0];
     const bool whole = id >= c0 && id + tiles <= c1;
     float *mine = a.parts + (static_cast<int64_t>(blockIdx.x) * 2 + (id < c0 ? 0 : 1)) * Sh::kPart;
-    for (int x = tid; x < Sh::kRows * D; x += kThreads) {
-      const int R = x / D, d = x - R * D;
-      float M = -INFINITY;
-      for (int s = s0; s < s1; ++s)
-        if (s_id[s] == id) M = fmaxf(M, part_of(s)[Sh::kRows * D + R]);
-      float num = 0.0f, den = 0.0f;
-      for (int s = s0; s < s1; ++s) {
-        if (s_id[s] != id) continue;
-        const float *p = part_of(s);
-        const float f = M == -INFINITY ? 1.0f : ex2(p[Sh::kRows * D + R] - M);
-        num = fmaf(f, p[x], num);
-        den = fmaf(f, p[Sh::kRows * D + Sh::kRows + R], den);
-      }
-      if (whole) {
-        write_row(b, h, rt, R, d, num, M, den);
-      } else {
-        mine[x] = num;
-        if (d == 0) mine[Sh::kRows * D + R] = M, mine[Sh::kRows * D + Sh::kRows + R] = den;
-      }
-    }
+    join(
+        s0, s1, [&](int k) { return s_id[k] == id; }, [&](int k) { return part_of(k); }, [](const float *p) { return *reinterpret_cast<const float4 *>(p); }, [](const float *p) { return *p; },
+        [&](int R, int d, float4 num, float mm, float ll) {
+          if (whole) {
+            write_row(b, h, rt, R, d, num, mm, ll);
+          } else {
+            *reinterpret_cast<float4 *>(mine + R * D + d) = num;
+            if (d == 0) mine[Sh::kRows * D + R] = mm, mine[Sh::kRows * D + Sh::kRows + R] = ll;
+          }
+        });
     if (!whole) {
       // blocks that hold a unit of the item: the first by its first unit, the last by its last
       auto block_of = [&](int64_t u) -> int64_t {
@@ -676,18 +711,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_few_kernel(const AttnArgs a)
       if (s_last) {
         __threadfence();
         if (tid == 0) atomicSub(&a.arrived[f >> 2], static_cast<uint32_t>(e - f + 1) << shift);  // for the next call
-        for (int x = tid; x < Sh::kRows * D; x += kThreads) {
-          const int R = x / D, d = x - R * D;
-          float M = -INFINITY, num = 0.0f, den = 0.0f;
-          for (int64_t c = f; c <= e; ++c) M = fmaxf(M, __ldcg(a.parts + (c * 2 + (c == f)) * Sh::kPart + Sh::kRows * D + R));
-          for (int64_t c = f; c <= e; ++c) {
-            const float *p = a.parts + (c * 2 + (c == f)) * Sh::kPart;
-            const float k = M == -INFINITY ? 1.0f : ex2(__ldcg(p + Sh::kRows * D + R) - M);
-            num = fmaf(k, __ldcg(p + x), num);
-            den = fmaf(k, __ldcg(p + Sh::kRows * D + Sh::kRows + R), den);
-          }
-          write_row(b, h, rt, R, d, num, M, den);
-        }
+        join(
+            static_cast<int>(f), static_cast<int>(e) + 1, [](int) { return true; }, [&](int c) { return a.parts + (static_cast<int64_t>(c) * 2 + (c == f)) * Sh::kPart; },
+            [](const float *p) { return __ldcg(reinterpret_cast<const float4 *>(p)); }, [](const float *p) { return __ldcg(p); },
+            [&](int R, int d, float4 num, float mm, float ll) { write_row(b, h, rt, R, d, num, mm, ll); });
       }
     }
     s0 = s1;
@@ -759,8 +786,13 @@ int maps_kv4_attention(int32_t dtype, int32_t B, int64_t T, int32_t Hq, int32_t 
   uint32_t *arrived = reinterpret_cast<uint32_t *>(static_cast<char *>(ws) + kArrivedAt);
   float *parts = c.take<float>(static_cast<size_t>(grid_size()) * 2 * kMaxParts);
   int64_t *prefix = c.take<int64_t>(B > kMaxLocalB ? static_cast<size_t>(B) + 1 : 0);
+  const int32_t groups = S / kGroup;
+  int32_t shift = -1;
+  for (int32_t i = 0; i < 16; ++i)
+    if (groups == 1 << i) shift = i;
   const AttnArgs a = {B, Hq, Hkv, S, T, n_blocks, max_blocks, q, q_row, q_head, o_row, o_head, qo_off, kv_len, table,
-                      static_cast<const uint8_t *>(cache), sm_scale, causal, window, wide, out, lse, prefix, arrived, parts, status_word(ws)};
+                      static_cast<const uint8_t *>(cache), sm_scale, causal, window, wide,
+                      static_cast<int64_t>(Hkv) * groups * kv4_group_bytes(D), groups, shift, out, lse, prefix, arrived, parts, status_word(ws)};
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (dtype == MAPS_BF16) return launch_dim<__nv_bfloat16>(D, a, s);
   return launch_dim<__half>(D, a, s);
