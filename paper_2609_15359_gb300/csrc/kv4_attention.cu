@@ -28,9 +28,10 @@
 namespace maps {
 namespace {
 
-constexpr int kWarps = 8;
-constexpr int kThreads = 32 * kWarps;
-constexpr int kMaxLocalB = 2048;  // requests whose prefix of units a block sums up for itself
+constexpr int kMaxWarps = 16;     // of a block
+constexpr int kMaxLocalB = 2048;  // requests over which a block deals out the units for itself
+
+struct Start;
 
 struct AttnArgs {
   int32_t B, Hq, Hkv, S;
@@ -46,7 +47,8 @@ struct AttnArgs {
   int32_t block_groups, block_shift;  // groups of a block, and their logarithm where they are a power of two, else -1
   void *out;
   float *lse;
-  int64_t *prefix;     // [B + 1] units before each request, where a block does not sum it up
+  Start *starts;       // where each worker starts, and the units in all, where a block does not find out for itself
+  uint32_t *units;
   uint32_t *arrived;   // a byte for each block: blocks that have brought their part of the item it begins
   float *parts;        // [grid][2] parts of items that cross blocks
   int32_t *status;
@@ -110,19 +112,29 @@ __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uin
 }
 
 // ---------------------------------------------------------------------------- the work, in units
+#ifndef TW
+#define TW 12
+#define TG 3
+#define TS 2
+#endif
 template <int D, int NT>
 struct Shape {
   static constexpr int kRows = 8 * NT;                       // query rows of a tile
-  static constexpr int kGroups = D == 256 ? 2 : 4;           // groups of 16 tokens in a unit
+  static constexpr int kWarps = NT == 1 && D <= 128 ? TW : 8, kThreads = 32 * kWarps;
+  static constexpr int kGroups = D == 256 ? 2 : NT == 1 ? TG : 4;  // groups of 16 tokens in a unit
   static constexpr int kTok = kGroups * kGroup;
   static constexpr int kBytes = kGroups * kv4_group_bytes(D);  // of a stage
-  static constexpr int kStages = D == 64 ? 4 : 2;
+  static constexpr int kStages = NT == 1 && D <= 128 ? (D == 64 ? 2 * TS : TS) : D == 64 ? 4 : 2;
   static constexpr int kPart = kRows * D + 2 * kRows;        // floats of a part: sums, maxima, totals
 };
 
-// What one request is for the kernel: queries, tokens, the first token any query sees (to 16), units.
+// An item's first unit moves nothing: it stands for what an item costs besides its tokens, so that
+// short requests, which have many items to a token, are dealt out evenly too.
+//
+// What one request is for the kernel: its first query row, tokens, queries, the first token any query sees (to 16), units of an item, row tiles.
 struct Req {
-  int32_t n, n_q, lo, tiles, row_tiles;
+  int64_t q0;
+  int32_t n, n_q, lo, tiles, row_tiles, heads;  // a request without tokens is one item for all heads
 };
 template <int kTok, int kRows>
 __device__ __forceinline__ Req request(const AttnArgs &a, int b) {
@@ -138,87 +150,125 @@ __device__ __forceinline__ Req request(const AttnArgs &a, int b) {
     flag_error(a.status, MAPS_E_RANGE);
     m = 0;
   }
+  r.q0 = q0;
   r.n = n;
   r.n_q = static_cast<int32_t>(m);
   int64_t lo = 0;
   if (a.window > 0) lo = static_cast<int64_t>(n) - m - a.window + 1;
   r.lo = lo > 0 ? static_cast<int32_t>(lo) / kGroup * kGroup : 0;
   const int32_t span = r.n - r.lo;
-  r.tiles = span > kTok ? (span + kTok - 1) / kTok : 1;
+  r.tiles = (span + kTok - 1) / kTok + 1;
   r.row_tiles = static_cast<int32_t>((m * (a.Hq / a.Hkv) + kRows - 1) / kRows);
+  r.heads = a.Hkv;
+  if (n == 0) r.heads = 1, r.row_tiles = m > 0 ? 1 : 0;
   return r;
 }
 
-// The prefix of units over the requests: each thread sums a run of them.
-template <int kTok, int kRows, int kN>
-__device__ __forceinline__ void sum_units(const AttnArgs &a, int64_t *prefix) {
-  __shared__ int64_t s_warp[32];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int per = (a.B + kN - 1) / kN, b0 = min(tid * per, a.B), b1 = min(b0 + per, a.B);
-  int64_t mine = 0;
-  for (int b = b0; b < b1; ++b) {
-    const Req r = request<kTok, kRows>(a, b);
-    mine += static_cast<int64_t>(r.tiles) * r.row_tiles * a.Hkv;
+// How the units are dealt out: worker w, a warp, has units start(w) .. start(w + 1) - 1.
+struct Deal {
+  uint32_t units, used, per, more;  // used: workers that get units, the first ones
+  __device__ __forceinline__ Deal(uint32_t U, uint32_t workers) : units(U), used(U < workers ? U : workers), per(0), more(0) {
+    if (used) per = U / used, more = U % used;
   }
-  int64_t x = mine;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
-    if (lane >= o) x += y;
-  }
-  if (lane == 31) s_warp[warp] = x;
-  __syncthreads();
-  int64_t at = x - mine;
-  for (int w = 0; w < warp; ++w) at += s_warp[w];
-  for (int b = b0; b < b1; ++b) {
-    prefix[b] = at;
-    const Req r = request<kTok, kRows>(a, b);
-    at += static_cast<int64_t>(r.tiles) * r.row_tiles * a.Hkv;
-  }
-  if (tid == kN - 1) prefix[a.B] = at;
-  __syncthreads();
-}
-
-template <int kTok, int kRows>
-__global__ void __launch_bounds__(1024) attn_plan_kernel(const AttnArgs a) {
-  pdl_prologue();
-  sum_units<kTok, kRows, 1024>(a, a.prefix);
-}
+  __device__ __forceinline__ uint32_t start(uint32_t w) const { return w >= used ? units : per * w + min(w, more); }
+  __device__ __forceinline__ uint32_t worker(uint32_t u) const { return u < more * (per + 1) ? u / (per + 1) : more + (u - more * (per + 1)) / per; }
+};
 
 // A place in the list of units: unit `tile` of the item (request b, KV head h, row tile rt).
 struct Cursor {
   int32_t b, h, rt, tile;
   Req r;
   template <int kTok, int kRows>
-  __device__ __forceinline__ void seek(const AttnArgs &a, const int64_t *prefix, int64_t u) {
-    int lo = 0, hi = a.B;  // prefix[lo] <= u < prefix[hi]
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (prefix[mid] <= u)
-        lo = mid;
-      else
-        hi = mid;
-    }
-    b = lo;
-    r = request<kTok, kRows>(a, b);
-    int64_t rest = u - prefix[b];
-    const int64_t item = rest / r.tiles;
-    tile = static_cast<int32_t>(rest - item * r.tiles);
-    h = static_cast<int32_t>(item / r.row_tiles);
-    rt = static_cast<int32_t>(item - static_cast<int64_t>(h) * r.row_tiles);
-  }
-  template <int kTok, int kRows>
   __device__ __forceinline__ void next_item(const AttnArgs &a) {
     tile = 0;
     if (++rt < r.row_tiles) return;
     rt = 0;
-    if (++h < a.Hkv) return;
+    if (++h < r.heads) return;
     h = 0;
     do {
       if (++b >= a.B) return;
       r = request<kTok, kRows>(a, b);
     } while (r.row_tiles == 0);
   }
+};
+
+// A place as the request and the units of it that lie before.
+struct Start {
+  Req r;
+  int32_t b;
+  uint32_t rest;
+  __device__ __forceinline__ Cursor cursor() const {
+    Cursor c;
+    const uint32_t item = rest / r.tiles;
+    c.b = b;
+    c.tile = static_cast<int32_t>(rest - item * r.tiles);
+    c.h = static_cast<int32_t>(item / r.row_tiles);
+    c.rt = static_cast<int32_t>(item - static_cast<uint32_t>(c.h) * r.row_tiles);
+    c.r = r;
+    return c;
+  }
+};
+
+// Sums the units of all requests, kN threads a run of them each, and leaves where the workers
+// w0 .. w1 - 1 start; returns the units.  put(w, start) keeps a worker's.
+template <int kTok, int kRows, int kN, class Put>
+__device__ __forceinline__ uint32_t plan(const AttnArgs &a, uint32_t workers, uint32_t w0, uint32_t w1, Put put) {
+  __shared__ uint64_t s_warp[kN / 32];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int run = (a.B + kN - 1) / kN, b0 = min(tid * run, a.B), b1 = min(b0 + run, a.B);
+  auto units_of = [&](const Req &r) { return static_cast<uint64_t>(r.tiles) * r.row_tiles * r.heads; };
+  Req r = {};
+  uint64_t mine = 0;
+  for (int b = b0; b < b1; ++b) {
+    r = request<kTok, kRows>(a, b);
+    mine += units_of(r);
+  }
+  uint64_t x = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint64_t y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  if (lane == 31) s_warp[warp] = x;
+  __syncthreads();
+  uint64_t at = x - mine, U = 0;
+#pragma unroll
+  for (int w = 0; w < kN / 32; ++w) {
+    const uint64_t y = s_warp[w];
+    if (w < warp) at += y;
+    U += y;
+  }
+  if (U >= 1ull << 31) {  // more than one call's worth of work
+    if (tid == 0) flag_error(a.status, MAPS_E_RANGE);
+    return 0;
+  }
+  const Deal deal(static_cast<uint32_t>(U), workers);
+  for (int b = b0; b < b1; ++b) {
+    if (run > 1) r = request<kTok, kRows>(a, b);
+    const uint32_t lo = static_cast<uint32_t>(at), n = static_cast<uint32_t>(units_of(r));
+    at += n;
+    if (n == 0 || lo >= deal.start(w1) || lo + n <= deal.start(w0)) continue;
+    uint32_t w = max(deal.worker(lo), w0);
+    if (deal.start(w) < lo) ++w;
+    for (; w < min(w1, deal.used) && deal.start(w) < lo + n; ++w) {
+      put(w, Start{r, b, deal.start(w) - lo});
+    }
+  }
+  return static_cast<uint32_t>(U);
+}
+
+template <int kTok, int kRows>
+__global__ void __launch_bounds__(1024) attn_plan_kernel(const AttnArgs a, uint32_t workers) {
+  pdl_prologue();
+  const uint32_t U = plan<kTok, kRows, 1024>(a, workers, 0, workers, [&](uint32_t w, const Start &c) { a.starts[w] = c; });
+  if (threadIdx.x == 0) *a.units = U;
+}
+
+// What of an item a warp, or a block, has: the item's first unit and its units (0: none), its queries' first row, rows, head and row tile.
+struct Part {
+  int64_t q0;
+  uint32_t id, tiles;
+  int32_t rows, h, rt;
 };
 
 struct Yes { static constexpr bool value = true; };
@@ -230,57 +280,65 @@ constexpr float kMinLog = -60.0f;
 
 // ---------------------------------------------------------------------------- the kernel
 template <class T, int D, int NT>
-__global__ void __launch_bounds__(kThreads, 1) attn_few_kernel(const AttnArgs a) {
+__global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(const AttnArgs a) {
   using Sh = Shape<D, NT>;
+  constexpr int kWarps = Sh::kWarps, kThreads = Sh::kThreads;
   constexpr int kSteps = D / 16, kWords = D / 32, kCh = D / 8;
   extern __shared__ __align__(128) uint8_t smem[];
   uint8_t *ring_all = smem;
   float *first_parts = reinterpret_cast<float *>(smem + kWarps * Sh::kStages * Sh::kBytes);
   uint64_t *bars = reinterpret_cast<uint64_t *>(first_parts + kWarps * Sh::kPart);
-  int64_t *s_prefix = reinterpret_cast<int64_t *>(bars + kWarps * Sh::kStages);
-  __shared__ int64_t s_id[2 * kWarps];     // an item's first unit, -1: no part here
-  __shared__ int32_t s_tiles[2 * kWarps];  // its units
-  __shared__ int32_t s_b[2 * kWarps], s_h[2 * kWarps], s_rt[2 * kWarps];
-  __shared__ uint32_t s_last;
+  __shared__ Part s_part[2 * kWarps];  // a warp's first and last part, where it has them
+  __shared__ Start s_start[kWarps];
+  __shared__ Part s_open[2];           // items that other blocks have parts of: begun before this block, and in it
+  __shared__ int s_block[2][2];        // of those: the first block, and how many where all have brought their parts
 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
   uint8_t *ring = ring_all + warp * Sh::kStages * Sh::kBytes;
   const uint32_t ring32 = smem_u32(ring), bar32 = smem_u32(bars + warp * Sh::kStages);
   if (lane < Sh::kStages) bar_init(bar32 + 8 * lane, 1);
-  if (lane < 2) s_id[2 * warp + lane] = -1;
+  if (lane < 2) s_part[2 * warp + lane].tiles = 0;
+  if (tid < 2) s_open[tid].tiles = 0;
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   pdl_prologue();
-  const int64_t *prefix = a.prefix;
+  const uint32_t workers = gridDim.x * kWarps, w0 = blockIdx.x * kWarps, me = w0 + warp;
+  uint32_t U;
+  Start from = {};
   if (a.B <= kMaxLocalB) {
-    sum_units<Sh::kTok, Sh::kRows, kThreads>(a, s_prefix);
-    prefix = s_prefix;
+    U = plan<Sh::kTok, Sh::kRows, kThreads>(a, workers, w0, w0 + kWarps, [&](uint32_t w, const Start &c) { s_start[w - w0] = c; });
+    __syncthreads();
+    from = s_start[warp];
   } else {
     __syncthreads();
+    U = *a.units;
+    if (me < U) from = a.starts[me];
   }
-
-  const int64_t U = prefix[a.B], workers = static_cast<int64_t>(gridDim.x) * kWarps;
-  const int64_t used = U < workers ? U : workers;  // warps that get units, the first ones
-  auto start = [&](int64_t w) -> int64_t { return used == 0 ? 0 : w >= used ? U : U / used * w + min(w, U % used); };
-  const int64_t me = static_cast<int64_t>(blockIdx.x) * kWarps + warp;
-  const int64_t u0 = start(me), u1 = start(me + 1);
+  const Deal deal(U, workers);
+  const uint32_t u0 = deal.start(me), u1 = deal.start(me + 1);
   const int group = a.Hq / a.Hkv;
   const float sl2 = a.scale * 1.4426950408889634f, k_sign = a.scale < 0.0f ? -1.0f : 1.0f, k_unit = k_sign * kEven;
 
   if (u0 < u1) {
     // The loads run ahead of the products by the ring's depth; lanes below kGroups move one group each.
-    Cursor ahead = {};
-    ahead.seek<Sh::kTok, Sh::kRows>(a, prefix, u0);
-    Cursor at = ahead;
-    int64_t issued = u0;
+    Cursor ahead = from.cursor(), at = ahead;
+    uint32_t issued = u0;
     // the next unit's group of this lane: whether it holds tokens, its block (fetched one step early), its place there and head
     bool mine = false;
     int32_t block = -1, place = 0;
     auto fetch = [&]() {
-      const int32_t tok = ahead.r.lo + ahead.tile * Sh::kTok + lane * kGroup;
+      const int32_t tok = ahead.r.lo + (ahead.tile - 1) * Sh::kTok + lane * kGroup;
       mine = issued < u1 && lane < Sh::kGroups && tok < ahead.r.n;
       const int32_t grp = tok / kGroup, page = a.block_shift >= 0 ? grp >> a.block_shift : grp / a.block_groups;
       place = ahead.h * a.block_groups + grp - page * a.block_groups;
       if (mine) block = a.table[ahead.b * a.max_blocks + page];
+    };
+    auto step = [&]() {
+      if (issued >= u1) return;
+      do {
+        ++issued;
+        if (++ahead.tile == ahead.r.tiles && issued < u1) ahead.next_item<Sh::kTok, Sh::kRows>(a);
+      } while (issued < u1 && ahead.tile == 0);
+      fetch();
     };
     auto issue = [&](int stage) {
       const bool good = mine && block >= 0 && block < a.n_blocks;
@@ -291,23 +349,39 @@ __global__ void __launch_bounds__(kThreads, 1) attn_few_kernel(const AttnArgs a)
       if (good)
         bulk_load(ring32 + stage * Sh::kBytes + lane * kv4_group_bytes(D), a.cache + (block * a.block_bytes + place * static_cast<int64_t>(kv4_group_bytes(D))),
                   kv4_group_bytes(D), bar32 + 8 * stage);
-      if (issued < u1) {
-        ++issued;
-        if (++ahead.tile == ahead.r.tiles && issued < u1) ahead.next_item<Sh::kTok, Sh::kRows>(a);
-        fetch();
-      }
+      step();
     };
-    fetch();
+    if (ahead.tile == 0)
+      step();
+    else
+      fetch();
 #pragma unroll
     for (int s = 0; s < Sh::kStages; ++s) issue(s);
 
     int stage = 0;
     uint32_t parity = 0;
     bool alive = true;
-    for (int64_t u = u0; u < u1 && alive;) {
+    for (uint32_t u = u0; u < u1 && alive;) {
       // ---- an item: its queries, as the columns of the first product
       const Req r = at.r;
-      const int64_t q0 = a.off[at.b];
+      const int64_t q0 = r.q0;
+      if (r.n == 0) {  // no token: no sums
+        for (int i = 0; i < r.n_q; ++i) {
+          for (int x = lane; x < a.Hq * (D / 8); x += 32) {
+            T *dst = static_cast<T *>(a.out) + (q0 + i) * a.o_row + x / (D / 8) * a.o_head + x % (D / 8) * 8;
+            if (a.wide) {
+              *reinterpret_cast<uint4 *>(dst) = make_uint4(0, 0, 0, 0);
+            } else {
+#pragma unroll
+              for (int c = 0; c < 8; ++c) dst[c] = Cvt<T>::from(0.0f);
+            }
+          }
+          if (a.lse)
+            for (int x = lane; x < a.Hq; x += 32) a.lse[(q0 + i) * a.Hq + x] = -INFINITY;
+        }
+        if (++u < u1) at.next_item<Sh::kTok, Sh::kRows>(a);
+        continue;
+      }
       const int rows = r.n_q * group;  // n_q * group <= T * Hq fits the checks of the host
       uint32_t qf[NT][kSteps][2];
       float qs[NT][2], qu[NT][2];  // a row's sum, and what a score of it is to be multiplied by
@@ -387,17 +461,17 @@ __global__ void __launch_bounds__(kThreads, 1) attn_few_kernel(const AttnArgs a)
         for (int e = 0; e < 2; ++e) m[nt][e] = -INFINITY, l[nt][e] = 0.0f, w[nt][e] = 0.0f;
       }
 
-      const int64_t left = r.tiles - at.tile;
-      const int64_t seg_end = u + (left < u1 - u ? left : u1 - u);
+      const uint32_t seg_end = min(u1, u + static_cast<uint32_t>(r.tiles - at.tile));
       const int32_t seg_first = at.tile;
       for (; u < seg_end; ++u, ++at.tile) {
+        if (at.tile == 0) continue;
         if (!bar_wait(bar32 + 8 * stage, parity)) {
           if (lane == 0) flag_error(a.status, MAPS_E_TIMEOUT);
           alive = false;
           break;
         }
         const uint8_t *buf = ring + stage * Sh::kBytes;
-        const int32_t tok0 = r.lo + at.tile * Sh::kTok;
+        const int32_t tok0 = r.lo + (at.tile - 1) * Sh::kTok;
         auto unit_sums = [&](auto every) {
           constexpr bool kEvery = decltype(every)::value;  // every row sees every token
           // ---- scores, up to a row's factor: 16 tokens x 8 rows, depth D
@@ -602,13 +676,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_few_kernel(const AttnArgs a)
               part[Sh::kRows * D + Sh::kRows + R] = l[nt][e];
             }
           }
-        if (lane == 0) {
-          s_id[slot] = u - at.tile;  // the item's first unit: at.tile units of it lie before u
-          s_tiles[slot] = r.tiles;
-          s_b[slot] = at.b;
-          s_h[slot] = at.h;
-          s_rt[slot] = at.rt;
-        }
+        if (lane == 0) s_part[slot] = {q0, u - at.tile, static_cast<uint32_t>(r.tiles), rows, at.h, at.rt};  // at.tile units of the item lie before u
       }
       if (u < u1) at.next_item<Sh::kTok, Sh::kRows>(a);
     }
@@ -619,16 +687,12 @@ __global__ void __launch_bounds__(kThreads, 1) attn_few_kernel(const AttnArgs a)
   __syncthreads();
 
   // ---- join the parts of the block's items, in the order of their keys
-  const int64_t c0 = start(static_cast<int64_t>(blockIdx.x) * kWarps), c1 = start(static_cast<int64_t>(blockIdx.x + 1) * kWarps);
-  auto part_of = [&](int slot) -> const float * {
-    return slot % 2 == 0 ? first_parts + slot / 2 * Sh::kPart : reinterpret_cast<const float *>(ring_all + slot / 2 * Sh::kStages * Sh::kBytes);
-  };
-  auto write_row = [&](int b, int h, int rt, int R, int d, float4 num, float mm, float ll) {
-    const int row = rt * Sh::kRows + R;
-    const int64_t q0 = a.off[b];
-    if (row >= (a.off[b + 1] - q0) * group) return;
-    const int64_t i = q0 + row / group;
-    const int hq = h * group + row % group;
+  const uint32_t c0 = deal.start(w0), c1 = deal.start(w0 + kWarps);
+  auto write_row = [&](const Part &p, int R, int d, float4 num, float mm, float ll) {
+    const int row = p.rt * Sh::kRows + R;
+    if (row >= p.rows) return;
+    const int64_t i = p.q0 + row / group;
+    const int hq = p.h * group + row % group;
     const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
     T *dst = static_cast<T *>(a.out) + i * a.o_row + hq * a.o_head + d;
     T y[4] = {Cvt<T>::from(num.x * inv), Cvt<T>::from(num.y * inv), Cvt<T>::from(num.z * inv), Cvt<T>::from(num.w * inv)};
@@ -640,24 +704,21 @@ __global__ void __launch_bounds__(kThreads, 1) attn_few_kernel(const AttnArgs a)
     }
     if (d == 0 && a.lse) a.lse[i * a.Hq + hq] = ll == 0.0f ? -INFINITY : (mm + log2f(ll)) * 0.6931471805599453f;
   };
-  // Sums the parts k0 <= k < k1 that `has` says count, each brought to their common maximum; four channels a thread.
-  auto join = [&](int k0, int k1, auto has, auto part, auto load, auto load_one, auto put) {
-    for (int x = 4 * tid; x < Sh::kRows * D; x += 4 * kThreads) {
+  // Sums n parts, each brought to their common maximum; a thread takes four channels at a time, four parts at a time.
+  auto join = [&](int thread, int threads, int n, auto part, auto load, auto load_one, auto put) {
+    for (int x = 4 * thread; x < Sh::kRows * D; x += 4 * threads) {
       const int R = x / D, d = x - R * D;
       float4 num = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
       float M = -INFINITY, den = 0.0f;
-      for (int k = k0; k < k1; k += 4) {  // four at a time: their loads do not wait for one another
+      for (int k = 0; k < n; k += 4) {
         float4 v[4];
         float mk[4], lk[4], top = M;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          mk[j] = -INFINITY, lk[j] = 0.0f, v[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-          if (k + j < k1 && has(k + j)) {
-            const float *p = part(k + j);
-            v[j] = load(p + x);
-            mk[j] = load_one(p + Sh::kRows * D + R);
-            lk[j] = load_one(p + Sh::kRows * D + Sh::kRows + R);
-          }
+          const float *p = part(min(k + j, n - 1));  // beyond the last: read again, and left out
+          v[j] = load(p + x);
+          mk[j] = load_one(p + Sh::kRows * D + R);
+          lk[j] = load_one(p + Sh::kRows * D + Sh::kRows + R);
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) top = fmaxf(top, mk[j]);
@@ -666,6 +727,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_few_kernel(const AttnArgs a)
         M = top;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
+          if (k + j >= n) break;
           const float f = top == -INFINITY ? 0.0f : ex2(mk[j] - top);
           num.x = fmaf(f, v[j].x, num.x), num.y = fmaf(f, v[j].y, num.y), num.z = fmaf(f, v[j].z, num.z), num.w = fmaf(f, v[j].w, num.w);
           den = fmaf(f, lk[j], den);
@@ -674,51 +736,53 @@ __global__ void __launch_bounds__(kThreads, 1) attn_few_kernel(const AttnArgs a)
       put(R, d, num, M, den);
     }
   };
-  for (int s0 = 0; s0 < 2 * kWarps;) {
-    const int64_t id = s_id[s0];
-    if (id < 0) {
-      ++s0;
-      continue;
-    }
-    int s1 = s0 + 1;
-    while (s1 < 2 * kWarps && (s_id[s1] < 0 || s_id[s1] == id)) ++s1;
-    const int tiles = s_tiles[s0], b = s_b[s0], h = s_h[s0], rt = s_rt[s0];
-    const bool whole = id >= c0 && id + tiles <= c1;
-    float *mine = a.parts + (static_cast<int64_t>(blockIdx.x) * 2 + (id < c0 ? 0 : 1)) * Sh::kPart;
+  // within the block: the warps that have parts of an item share its channels
+  for (int slot = 2 * warp; slot < 2 * warp + 2; ++slot) {
+    const Part item = s_part[slot];
+    if (item.tiles == 0) continue;
+    const bool whole = item.id >= c0 && item.id + item.tiles <= c1;
+    const int first = item.id < c0 ? 0 : static_cast<int>(deal.worker(item.id) - w0);
+    const int last = item.id + item.tiles > c1 ? kWarps - 1 : static_cast<int>(deal.worker(item.id + item.tiles - 1) - w0);
+    const float *head = item.id <= deal.start(w0 + first) ? first_parts + first * Sh::kPart : reinterpret_cast<const float *>(ring_all + first * Sh::kStages * Sh::kBytes);
+    float *mine = a.parts + (static_cast<int64_t>(blockIdx.x) * 2 + (item.id < c0 ? 0 : 1)) * Sh::kPart;
     join(
-        s0, s1, [&](int k) { return s_id[k] == id; }, [&](int k) { return part_of(k); }, [](const float *p) { return *reinterpret_cast<const float4 *>(p); }, [](const float *p) { return *p; },
+        lane + 32 * (warp - first), 32 * (last - first + 1), last - first + 1, [&](int k) { return k == 0 ? head : first_parts + (first + k) * Sh::kPart; },
+        [](const float *p) { return *reinterpret_cast<const float4 *>(p); }, [](const float *p) { return *p; },
         [&](int R, int d, float4 num, float mm, float ll) {
           if (whole) {
-            write_row(b, h, rt, R, d, num, mm, ll);
+            write_row(item, R, d, num, mm, ll);
           } else {
             *reinterpret_cast<float4 *>(mine + R * D + d) = num;
             if (d == 0) mine[Sh::kRows * D + R] = mm, mine[Sh::kRows * D + Sh::kRows + R] = ll;
           }
         });
     if (!whole) {
-      // blocks that hold a unit of the item: the first by its first unit, the last by its last
-      auto block_of = [&](int64_t u) -> int64_t {
-        const int64_t per = U / used, more = U % used;
-        const int64_t w = u < more * (per + 1) ? u / (per + 1) : more + (u - more * (per + 1)) / per;
-        return w / kWarps;
-      };
-      const int64_t f = block_of(id), e = block_of(id + tiles - 1);
+      if (warp == first && lane == 0) s_open[item.id < c0 ? 0 : 1] = item;
       __threadfence();
-      __syncthreads();
-      const int shift = static_cast<int>(f & 3) * 8;
-      if (tid == 0) s_last = (atom_add_acq_rel_u32(&a.arrived[f >> 2], 1u << shift) >> shift & 255u) == static_cast<uint32_t>(e - f) ? 1u : 0u;
-      __syncthreads();
-      if (s_last) {
-        __threadfence();
-        if (tid == 0) atomicSub(&a.arrived[f >> 2], static_cast<uint32_t>(e - f + 1) << shift);  // for the next call
-        join(
-            static_cast<int>(f), static_cast<int>(e) + 1, [](int) { return true; }, [&](int c) { return a.parts + (static_cast<int64_t>(c) * 2 + (c == f)) * Sh::kPart; },
-            [](const float *p) { return __ldcg(reinterpret_cast<const float4 *>(p)); }, [](const float *p) { return __ldcg(p); },
-            [&](int R, int d, float4 num, float mm, float ll) { write_row(b, h, rt, R, d, num, mm, ll); });
-      }
     }
-    s0 = s1;
-    __syncthreads();
+  }
+  // across blocks: the last to bring its part joins them all
+  __syncthreads();
+  if (tid < 2 && s_open[tid].tiles) {
+    const Part item = s_open[tid];
+    const uint32_t f = deal.worker(item.id) / kWarps, e = deal.worker(item.id + item.tiles - 1) / kWarps;
+    const int shift = static_cast<int>(f & 3) * 8;
+    const uint32_t others = atom_add_acq_rel_u32(&a.arrived[f >> 2], 1u << shift) >> shift & 255u;
+    const bool all = others == e - f;
+    if (all) atomicSub(&a.arrived[f >> 2], (e - f + 1) << shift);  // zero again for the next call
+    s_block[tid][0] = static_cast<int>(f);
+    s_block[tid][1] = all ? static_cast<int>(e - f + 1) : 0;
+  }
+  __syncthreads();
+  for (int k = 0; k < 2; ++k) {
+    if (s_open[k].tiles == 0 || s_block[k][1] == 0) continue;
+    const Part item = s_open[k];
+    const int f = s_block[k][0];
+    __threadfence();
+    join(
+        tid, kThreads, s_block[k][1], [&](int c) { return a.parts + (static_cast<int64_t>(f + c) * 2 + (c == 0)) * Sh::kPart; },
+        [](const float *p) { return __ldcg(reinterpret_cast<const float4 *>(p)); }, [](const float *p) { return __ldcg(p); },
+        [&](int R, int d, float4 num, float mm, float ll) { write_row(item, R, d, num, mm, ll); });
   }
 }
 
@@ -731,11 +795,11 @@ int grid_size() { return sm_count() < kMaxGrid ? sm_count() : kMaxGrid; }
 template <class T, int D, int NT>
 int launch_few(const AttnArgs &a, cudaStream_t s) {
   using Sh = Shape<D, NT>;
-  const size_t local = a.B <= kMaxLocalB ? static_cast<size_t>(a.B + 1) * 8 : 0;
-  const size_t smem = static_cast<size_t>(kWarps) * Sh::kStages * Sh::kBytes + static_cast<size_t>(kWarps) * Sh::kPart * 4 + kWarps * Sh::kStages * 8 + local;
+  constexpr int kWarps = Sh::kWarps, kThreads = Sh::kThreads;
+  const size_t smem = static_cast<size_t>(kWarps) * Sh::kStages * Sh::kBytes + static_cast<size_t>(kWarps) * Sh::kPart * 4 + kWarps * Sh::kStages * 8;
   auto kernel = attn_few_kernel<T, D, NT>;
   MAPS_TRY(cuda_ok(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem))));
-  if (a.B > kMaxLocalB) launch_pdl(attn_plan_kernel<Sh::kTok, Sh::kRows>, 1, 1024, 0, s, a);
+  if (a.B > kMaxLocalB) launch_pdl(attn_plan_kernel<Sh::kTok, Sh::kRows>, 1, 1024, 0, s, a, static_cast<uint32_t>(grid_size() * kWarps));
   launch_pdl(kernel, static_cast<unsigned>(grid_size()), kThreads, smem, s, a);
   return launch_ok();
 }
@@ -759,7 +823,8 @@ size_t maps_kv4_attention_workspace_size(int32_t B, int64_t T, int32_t Hq, int32
   (void)T, (void)Hq, (void)Hkv, (void)D;
   Carve c(nullptr);
   c.take<float>(static_cast<size_t>(grid_size()) * 2 * kMaxParts);
-  c.take<int64_t>(B > kMaxLocalB ? static_cast<size_t>(B) + 1 : 0);
+  c.take<Start>(B > kMaxLocalB ? static_cast<size_t>(grid_size()) * kMaxWarps : 0);
+  c.take<uint32_t>(1);
   return c.bytes();
 }
 
@@ -785,14 +850,15 @@ int maps_kv4_attention(int32_t dtype, int32_t B, int64_t T, int32_t Hq, int32_t 
   Carve c(ws);
   uint32_t *arrived = reinterpret_cast<uint32_t *>(static_cast<char *>(ws) + kArrivedAt);
   float *parts = c.take<float>(static_cast<size_t>(grid_size()) * 2 * kMaxParts);
-  int64_t *prefix = c.take<int64_t>(B > kMaxLocalB ? static_cast<size_t>(B) + 1 : 0);
+  Start *starts = c.take<Start>(B > kMaxLocalB ? static_cast<size_t>(grid_size()) * kMaxWarps : 0);
+  uint32_t *units = c.take<uint32_t>(1);
   const int32_t groups = S / kGroup;
   int32_t shift = -1;
   for (int32_t i = 0; i < 16; ++i)
     if (groups == 1 << i) shift = i;
   const AttnArgs a = {B, Hq, Hkv, S, T, n_blocks, max_blocks, q, q_row, q_head, o_row, o_head, qo_off, kv_len, table,
                       static_cast<const uint8_t *>(cache), sm_scale, causal, window, wide,
-                      static_cast<int64_t>(Hkv) * groups * kv4_group_bytes(D), groups, shift, out, lse, prefix, arrived, parts, status_word(ws)};
+                      static_cast<int64_t>(Hkv) * groups * kv4_group_bytes(D), groups, shift, out, lse, starts, units, arrived, parts, status_word(ws)};
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (dtype == MAPS_BF16) return launch_dim<__nv_bfloat16>(D, a, s);
   return launch_dim<__half>(D, a, s);
