@@ -8,19 +8,48 @@
 //
 // Everything follows from three exclusive sums over the requests: blocks given
 // back and new tokens in index order, blocks needed in the scheduler's order.
-// They are taken by one block (bt_scan_kernel), which also puts the returned
-// blocks on the stack; then every new token finds its request by bisection of
-// the token offsets and its block from the stack (bt_fill_kernel).  A new
-// block's first token always is a new token, so that token writes the table.
+// bt_scan_kernel takes them, one block for up to 1,024 requests, else a cluster
+// of eight blocks; its time is the latency of two rounds of loads and sums.
+// Then the sums are expanded, one thread a token: a coarse index and a short
+// bisection of the token offsets give the request, a record of it the rest.  A
+// new block's first token always is a new token, so that token writes the
+// table.  With few tokens one kernel does it all, and takes a block that was
+// just returned from its old row, so that returning and taking need not wait
+// for one another; with many, which the writes bound, the returned blocks go
+// onto the stack first and a token costs one load of it.
+#include <cooperative_groups.h>
+
+#include <algorithm>
+
 #include "maps_internal.cuh"
 
 namespace maps {
 namespace {
 
+namespace cg = cooperative_groups;
+
 constexpr int kScanThreads = 1024;
+constexpr int kCluster = 8;
+constexpr int kFillThreads = 256;
+constexpr int kFewTokens = 65536;  // up to here: one kernel, a token a thread
+constexpr int kManyEach = 8;       // beyond: tokens of a thread
+constexpr int kCoarse = 2048;      // marks of a coarse index
+
+// What the tokens of a request need to know of it.
+struct alignas(32) Request {
+  int64_t begin;   // its first new token
+  int64_t before;  // blocks granted ahead of its first, -1 where it is refused
+  int32_t held, last;  // tokens held, and the block of the last of them (where it is not full)
+};
+// The sums over all, for the kernels that expand them.
+struct alignas(32) Totals {
+  int64_t returned, tokens, stack;  // stack: entries once the returned blocks are on it
+  int32_t free, token_shift, returned_shift;
+};
 
 struct BTArgs {
   int32_t R, S, max_blocks, pool;
+  int32_t s_shift;  // log2 S where S is a power of two, else -1
   const int32_t *held, *want, *order;
   int32_t *table, *free_blocks;
   const int32_t *n_free;
@@ -29,10 +58,16 @@ struct BTArgs {
   int64_t *slots;
   int64_t slots_cap;
   int32_t *pos;
-  int64_t *before;  // [R] blocks granted ahead of each request's first, -1 where it is refused
-  int64_t *top;     // stack height after the returned blocks
+  Totals *totals;
+  Request *requests;  // [R]
+  int64_t *back;      // [R + 1] blocks given back ahead of each request's
+  int32_t *coarse;    // [2][kCoarse + 2] the requests of every 2^shift-th new token and returned block
   int32_t *status;
 };
+
+__device__ __forceinline__ uint32_t block_of(const BTArgs &a, uint32_t position) {
+  return a.s_shift >= 0 ? position >> a.s_shift : position / static_cast<uint32_t>(a.S);
+}
 
 struct Need {
   int32_t held, want, hb, wb;
@@ -48,8 +83,8 @@ __device__ __forceinline__ Need need_of(const BTArgs &a, int r, bool report) {
     if (report) flag_error(a.status, MAPS_E_RANGE);
     n.held = n.want = 0;
   }
-  n.hb = static_cast<int32_t>((static_cast<uint32_t>(n.held) + a.S - 1u) / static_cast<uint32_t>(a.S));
-  n.wb = static_cast<int32_t>((static_cast<uint32_t>(n.want) + a.S - 1u) / static_cast<uint32_t>(a.S));
+  n.hb = static_cast<int32_t>(block_of(a, static_cast<uint32_t>(n.held) + a.S - 1u));
+  n.wb = static_cast<int32_t>(block_of(a, static_cast<uint32_t>(n.want) + a.S - 1u));
   return n;
 }
 
@@ -83,106 +118,296 @@ __device__ __forceinline__ void block_scan2(int64_t &x, int64_t &y, int64_t &tx,
   __syncthreads();
 }
 
+// Sums of x and y ahead of this block over the cluster, and over all of it.
+template <int kBlocks>
+__device__ __forceinline__ void cluster_sums(int64_t x, int64_t y, int64_t &bx, int64_t &by, int64_t &tx, int64_t &ty) {
+  bx = by = 0;
+  tx = x;
+  ty = y;
+  if (kBlocks == 1) return;
+  __shared__ int64_t s_sum[2], s_all[4];
+  cg::cluster_group cl = cg::this_cluster();
+  if (threadIdx.x == 0) s_sum[0] = x, s_sum[1] = y;
+  cl.sync();
+  if (threadIdx.x < 32) {
+    const int k = threadIdx.x;
+    int64_t ux = 0, uy = 0;
+    if (k < kBlocks) {
+      const int64_t *p = cl.map_shared_rank(s_sum, k);
+      ux = p[0], uy = p[1];
+    }
+    const bool ahead = k < static_cast<int>(cl.block_rank());
+    int64_t v[4] = {ahead ? ux : 0, ahead ? uy : 0, ux, uy};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+      for (int o = 4; o > 0; o >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+      if (k == 0) s_all[i] = v[i];
+    }
+  }
+  cl.sync();  // nobody goes on to write its sums, or leaves, while they are being read
+  bx = s_all[0], by = s_all[1], tx = s_all[2], ty = s_all[3];
+}
+
+// The coarse index over sums: mark c is the request that element c << shift belongs to, so an
+// element's request lies between two neighbouring marks.
+__device__ __forceinline__ int mark_shift(int64_t total) {
+  const int bits = 64 - __clzll(total > kCoarse ? (total - 1) / kCoarse : 0);
+  return bits;
+}
+__device__ __forceinline__ void set_marks(int32_t *marks, int r, int64_t begin, int64_t n, int shift) {
+  for (int64_t c = (begin + (int64_t(1) << shift) - 1) >> shift; c << shift < begin + n; ++c) marks[c] = r;
+}
+__device__ __forceinline__ void end_marks(int32_t *marks, int R, int64_t total, int shift) { marks[(total + (int64_t(1) << shift) - 1) >> shift] = R - 1; }
+
+template <int kBlocks>
 __global__ void __launch_bounds__(kScanThreads) bt_scan_kernel(const BTArgs a) {
   pdl_prologue();
+  const int tid = threadIdx.x;
+  // the block's tiles of 1,024 requests; where it has more than one, a first pass sums them up
+  const int tiles = (a.R + kScanThreads - 1) / kScanThreads, each = (tiles + kBlocks - 1) / kBlocks;
+  const int r0 = static_cast<int>(min(static_cast<int64_t>(blockIdx.x) * each * kScanThreads, static_cast<int64_t>(a.R)));
+  const int r1 = static_cast<int>(min(r0 + static_cast<int64_t>(each) * kScanThreads, static_cast<int64_t>(a.R)));
+  const bool twice = kBlocks > 1 && each > 1;
+  const int ordered = a.order && r0 + tid < r1 ? a.order[r0 + tid] : r0 + tid;  // needed later, fetched now
   int32_t nf = *a.n_free;
   if (nf < 0 || nf > a.pool) {
-    if (threadIdx.x == 0) flag_error(a.status, MAPS_E_RANGE);
+    if (tid == 0) flag_error(a.status, MAPS_E_RANGE);
     nf = 0;
   }
-  // index order: blocks given back (written to the stack as their place is known) and new tokens
-  int64_t back = 0, toks = 0;
-  for (int base = 0; base < a.R; base += kScanThreads) {
-    const int r = base + threadIdx.x;
-    Need n = {0, 0, 0, 0};
-    if (r < a.R) n = need_of(a, r, true);
-    const int64_t mine = n.hb > n.wb ? n.hb - n.wb : 0;
-    int64_t x = mine, y = n.want > n.held ? n.want - n.held : 0, tx, ty;
-    block_scan2(x, y, tx, ty);
-    if (r < a.R) {
-      a.off[r] = toks + y;
-      for (int64_t i = 0, at = nf + back + x; i < mine; ++i, ++at) {
-        if (at >= a.pool) {
-          flag_error(a.status, MAPS_E_RANGE);
-          break;
-        }
-        a.free_blocks[at] = a.table[static_cast<int64_t>(r) * a.max_blocks + n.wb + i];
-      }
+
+  // index order: blocks given back and new tokens
+  auto index_values = [&](int r, bool report, int64_t &x, int64_t &y, Need &n) {
+    x = y = 0;
+    n = {0, 0, 0, 0};
+    if (r >= r1) return;
+    n = need_of(a, r, report);
+    if (n.hb > n.wb) x = n.hb - n.wb;
+    if (n.want > n.held) y = n.want - n.held;
+  };
+  int64_t bx = 0, by = 0, back = 0, toks = 0, unused = 0;
+  Need n;
+  if (twice) {
+    int64_t sx = 0, sy = 0, tx, ty;
+    for (int r = r0 + tid; r < r1; r += kScanThreads) {
+      int64_t x, y;
+      index_values(r, false, x, y, n);
+      sx += x, sy += y;
     }
-    back += tx;
-    toks += ty;
+    block_scan2(sx, sy, tx, ty);
+    cluster_sums<kBlocks>(tx, ty, bx, by, back, toks);
+  }
+  for (int base = r0, k = 0; k < each; base += kScanThreads, ++k) {
+    const int r = base + tid;
+    int64_t x, y, tx, ty;
+    index_values(r, true, x, y, n);
+    int32_t last = -1;
+    if (y && n.hb > 0) last = a.table[static_cast<int64_t>(r) * a.max_blocks + n.hb - 1];
+    int64_t sx = x, sy = y;
+    block_scan2(sx, sy, tx, ty);
+    if (!twice) cluster_sums<kBlocks>(tx, ty, bx, by, back, toks);
+    sx += bx, sy += by;
+    if (r < r1) {
+      a.off[r] = sy, a.back[r] = sx;
+      Request &q = a.requests[r];
+      q.begin = sy, q.held = n.held, q.last = last;
+      set_marks(a.coarse, r, sy, y, mark_shift(toks));
+      set_marks(a.coarse + kCoarse + 2, r, sx, x, mark_shift(back));
+    }
+    bx += tx, by += ty;
   }
   const int64_t N = min(static_cast<int64_t>(nf) + back, static_cast<int64_t>(a.pool));
+
   // the scheduler's order: blocks needed, granted while the stack lasts
-  int64_t need = 0;
-  __shared__ unsigned long long s_granted;
-  if (threadIdx.x == 0) s_granted = 0;
-  __syncthreads();
-  for (int base = 0; base < a.R; base += kScanThreads) {
-    const int i = base + threadIdx.x;
-    int r = -1;
-    Need n = {0, 0, 0, 0};
-    if (i < a.R) {
-      r = a.order ? a.order[i] : i;
-      if (r < 0 || r >= a.R) {
-        flag_error(a.status, MAPS_E_RANGE);
-        r = -1;
-      } else {
-        n = need_of(a, r, false);
-      }
+  auto place = [&](int i, int &r, Need &n) -> int64_t {
+    r = -1;
+    n = {0, 0, 0, 0};
+    if (i >= r1) return 0;
+    r = i == r0 + tid ? ordered : a.order ? a.order[i] : i;
+    if (r < 0 || r >= a.R) {
+      flag_error(a.status, MAPS_E_RANGE);
+      r = -1;
+      return 0;
     }
-    const int64_t mine = n.wb > n.hb ? n.wb - n.hb : 0;
-    int64_t x = mine, y = 0, tx, ty;
-    block_scan2(x, y, tx, ty);
-    if (r >= 0) {
-      const bool ok = mine == 0 || need + x + mine <= N;
-      a.before[r] = ok ? need + x : -1;
-      a.got[r] = n.want < n.held || ok ? n.want : n.held;
-      if (ok && mine) atomicMax(&s_granted, static_cast<unsigned long long>(need + x + mine));
+    n = need_of(a, r, false);
+    return n.wb > n.hb ? n.wb - n.hb : 0;
+  };
+  int64_t ahead = 0, all = 0;
+  if (twice) {
+    int64_t sx = 0, sy = 0, tx, ty;
+    for (int i = r0 + tid; i < r1; i += kScanThreads) {
+      int r;
+      sx += place(i, r, n);
     }
-    need += tx;
+    block_scan2(sx, sy, tx, ty);
+    cluster_sums<kBlocks>(tx, 0, ahead, unused, all, unused);
   }
+  int64_t granted = 0;  // the needs up to the last one granted
+  for (int base = r0, k = 0; k < each; base += kScanThreads, ++k) {
+    int r;
+    const int64_t x = place(base + tid, r, n);
+    int64_t sx = x, sy = 0, tx, ty;
+    block_scan2(sx, sy, tx, ty);
+    if (!twice) cluster_sums<kBlocks>(tx, 0, ahead, unused, all, unused);
+    sx += ahead;
+    if (r >= 0) {
+      const bool ok = x == 0 || sx + x <= N;
+      a.requests[r].before = ok ? sx : -1;
+      a.got[r] = n.want < n.held || ok ? n.want : n.held;
+      if (ok && x) granted = sx + x;
+    }
+    ahead += tx;
+  }
+  // the stack left: what the last one granted leaves
+  __shared__ unsigned long long s_granted;
+  if (tid == 0) s_granted = 0;
   __syncthreads();
-  if (threadIdx.x == 0) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) granted = max(granted, static_cast<int64_t>(__shfl_xor_sync(0xffffffffu, granted, o)));
+  if ((tid & 31) == 0 && granted) atomicMax(&s_granted, static_cast<unsigned long long>(granted));
+  __syncthreads();
+  int64_t most = static_cast<int64_t>(s_granted);
+  if (kBlocks > 1) {
+    cg::cluster_group cl = cg::this_cluster();
+    cl.sync();
+    if (blockIdx.x == 0 && tid == 0)
+      for (int k = 1; k < kBlocks; ++k) most = max(most, static_cast<int64_t>(*cl.map_shared_rank(&s_granted, k)));
+    cl.sync();
+  }
+  if (blockIdx.x == 0 && tid == 0) {
     a.off[a.R] = toks;
-    *a.top = N;
-    *a.n_free_out = static_cast<int32_t>(N - static_cast<int64_t>(s_granted));
-    if (toks > a.slots_cap) flag_error(a.status, MAPS_E_RANGE);
+    a.back[a.R] = back;
+    *a.totals = {N - nf, min(toks, a.slots_cap), N, nf, mark_shift(toks), mark_shift(back)};
+    end_marks(a.coarse, a.R, toks, mark_shift(toks));
+    end_marks(a.coarse + kCoarse + 2, a.R, back, mark_shift(back));
+    *a.n_free_out = static_cast<int32_t>(N - most);
+    if (toks > a.slots_cap || nf + back > a.pool) flag_error(a.status, MAPS_E_RANGE);
   }
 }
 
-__global__ void __launch_bounds__(256) bt_fill_kernel(const BTArgs a) {
-  pdl_prologue();
-  const int64_t j = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
-  const int64_t total = a.off[a.R];
-  if (j >= total || j >= a.slots_cap) return;
-  int lo = 0, hi = a.R;  // off[lo] <= j < off[hi]
+// The request that element x belongs to: the last r with sums[r] <= x, for 0 <= x < sums[R].
+__device__ __forceinline__ int owner(const int64_t *__restrict__ sums, const int32_t *__restrict__ marks, int shift, int64_t x) {
+  int lo = marks[x >> shift], hi = marks[(x >> shift) + 1] + 1;
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
-    if (a.off[mid] <= j)
+    if (sums[mid] <= x)
       lo = mid;
     else
       hi = mid;
   }
-  const Need n = need_of(a, lo, false);
-  const int32_t p = n.held + static_cast<int32_t>(j - a.off[lo]);
-  const int32_t bi = p / a.S, within = p - bi * a.S;
-  const int64_t before = a.before[lo];
+  return lo;
+}
+
+// The block that entry k of the returned ones is: still in its old row, which nothing overwrites.
+__device__ __forceinline__ int32_t returned(const BTArgs &a, int64_t k, int shift) {
+  const int r = owner(a.back, a.coarse + kCoarse + 2, shift, k);
+  return a.table[static_cast<int64_t>(r) * a.max_blocks + need_of(a, r, false).wb + (k - a.back[r])];
+}
+
+// The returned blocks onto the stack, by `blocks` blocks of which this is number b.
+__device__ __forceinline__ void push(const BTArgs &a, const Totals &t, int b, int blocks) {
+  for (int64_t k = static_cast<int64_t>(b) * kFillThreads + threadIdx.x; k < t.returned; k += static_cast<int64_t>(blocks) * kFillThreads)
+    a.free_blocks[t.free + k] = returned(a, k, t.returned_shift);
+}
+
+__global__ void __launch_bounds__(kFillThreads) bt_push_kernel(const BTArgs a) {
+  pdl_prologue();
+  push(a, *a.totals, blockIdx.x, gridDim.x);
+}
+
+// Few tokens: one a thread, since each is a chain of loads; further blocks put the returned ones onto the stack.
+__global__ void __launch_bounds__(kFillThreads) bt_fill_kernel(const BTArgs a, int token_blocks) {
+  pdl_prologue();
+  const Totals t = *a.totals;
+  if (static_cast<int>(blockIdx.x) >= token_blocks) {
+    push(a, t, blockIdx.x - token_blocks, gridDim.x - token_blocks);
+    return;
+  }
+  const int64_t j = static_cast<int64_t>(blockIdx.x) * kFillThreads + threadIdx.x;
+  if (j >= t.tokens) return;
+  const int r = owner(a.off, a.coarse, t.token_shift, j);
+  const Request q = a.requests[r];
+  const uint32_t p = static_cast<uint32_t>(q.held) + static_cast<uint32_t>(j - q.begin);
+  const uint32_t hb = block_of(a, static_cast<uint32_t>(q.held) + a.S - 1u), bi = block_of(a, p), within = p - bi * static_cast<uint32_t>(a.S);
   int64_t slot = -1;
-  if (before >= 0) {
-    int32_t *row = a.table + static_cast<int64_t>(lo) * a.max_blocks;
-    int32_t block;
-    if (bi >= n.hb) {
-      const int64_t at = *a.top - 1 - (before + (bi - n.hb));
-      block = at >= 0 ? a.free_blocks[at] : -1;
-      if (within == 0) row[bi] = block;
-    } else {
-      block = row[bi];
+  if (q.before >= 0) {
+    int32_t block = q.last;
+    if (bi >= hb) {
+      const int64_t at = t.stack - 1 - (q.before + (bi - hb));
+      block = at < 0 ? -1 : at < t.free ? a.free_blocks[at] : returned(a, at - t.free, t.returned_shift);
+      if (within == 0) a.table[static_cast<int64_t>(r) * a.max_blocks + bi] = block;
     }
     slot = static_cast<int64_t>(block) * a.S + within;
   }
   a.slots[j] = slot;
-  if (a.pos) a.pos[j] = p;
+  if (a.pos) a.pos[j] = static_cast<int32_t>(p);
+}
+
+// Many tokens: a warp maps 256 consecutive ones, lane by lane so that writes are whole lines, and all
+// eight loads of a lane's blocks are under way at once.
+__global__ void __launch_bounds__(kFillThreads) bt_fill_many_kernel(const BTArgs a) {
+  pdl_prologue();
+  const Totals t = *a.totals;
+  const int64_t j0 = (static_cast<int64_t>(blockIdx.x) * (kFillThreads / 32) + threadIdx.x / 32) * (32 * kManyEach) + threadIdx.x % 32;
+  int32_t at[kManyEach], owner_of[kManyEach], block[kManyEach];  // at: the stack's entry, -1: the block is known
+  uint32_t pos[kManyEach];
+  int64_t end = 0;
+  int r = -1;
+  uint32_t hb = 0;
+  Request q = {0, -1, 0, -1};
+#pragma unroll
+  for (int i = 0; i < kManyEach; ++i) {
+    const int64_t j = j0 + 32 * i;
+    at[i] = -1;
+    block[i] = -1;
+    pos[i] = 0;
+    if (j < t.tokens) {
+      if (j >= end) {
+        r = owner(a.off, a.coarse, t.token_shift, j);
+        q = a.requests[r];
+        end = a.off[r + 1];
+        hb = block_of(a, static_cast<uint32_t>(q.held) + a.S - 1u);
+      }
+      pos[i] = static_cast<uint32_t>(q.held) + static_cast<uint32_t>(j - q.begin);
+      const uint32_t bi = block_of(a, pos[i]);
+      if (q.before >= 0) {
+        if (bi >= hb)
+          at[i] = static_cast<int32_t>(max(t.stack - 1 - (q.before + (bi - hb)), int64_t(-1)));
+        else
+          block[i] = q.last;
+      }
+    }
+    owner_of[i] = r;
+  }
+#pragma unroll
+  for (int i = 0; i < kManyEach; ++i)
+    if (at[i] >= 0) block[i] = a.free_blocks[at[i]];
+#pragma unroll
+  for (int i = 0; i < kManyEach; ++i) {
+    const int64_t j = j0 + 32 * i;
+    if (j >= t.tokens) return;
+    const uint32_t bi = block_of(a, pos[i]), within = pos[i] - bi * static_cast<uint32_t>(a.S);
+    if (at[i] >= 0 && within == 0) a.table[static_cast<int64_t>(owner_of[i]) * a.max_blocks + bi] = block[i];
+    a.slots[j] = block[i] >= 0 ? static_cast<int64_t>(block[i]) * a.S + within : -1;
+    if (a.pos) a.pos[j] = static_cast<int32_t>(pos[i]);
+  }
+}
+
+// A launch of one cluster, programmatically serialised as launch_pdl's.
+void launch_cluster(void (*kernel)(BTArgs), int blocks, int threads, cudaStream_t s, const BTArgs &a) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(blocks));
+  cfg.blockDim = dim3(static_cast<unsigned>(threads));
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = static_cast<unsigned>(blocks);
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  (void)cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
 }  // namespace
@@ -190,10 +415,18 @@ __global__ void __launch_bounds__(256) bt_fill_kernel(const BTArgs a) {
 
 extern "C" {
 
+static void carve(maps::Carve &c, maps::BTArgs &a) {
+  a.totals = c.take<maps::Totals>(1);
+  a.requests = c.take<maps::Request>(static_cast<size_t>(a.R));
+  a.back = c.take<int64_t>(static_cast<size_t>(a.R) + 1);
+  a.coarse = c.take<int32_t>(2 * (maps::kCoarse + 2));
+}
+
 size_t maps_block_tables_workspace_size(int32_t R) {
   maps::Carve c(nullptr);
-  c.take<int64_t>(1);
-  c.take<int64_t>(R > 0 ? static_cast<size_t>(R) : 0);
+  maps::BTArgs a = {};
+  a.R = R > 0 ? R : 0;
+  carve(c, a);
   return c.bytes();
 }
 
@@ -216,14 +449,29 @@ int maps_block_tables(int32_t R, int32_t S, const int32_t *held, const int32_t *
   MAPS_TRY(check_ws(ws, ws_bytes, maps_block_tables_workspace_size(R)));
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   Carve c(ws);
-  BTArgs a = {R, S, max_blocks, pool, held, want, order, table, free_blocks, n_free, n_free_out,
-              got_out, slot_off_out, slots_out, slots_cap, pos_out, nullptr, nullptr,
+  int32_t s_shift = -1;
+  for (int i = 0; i < 31; ++i)
+    if (S == 1 << i) s_shift = i;
+  BTArgs a = {R, S, max_blocks, pool, s_shift, held, want, order, table, free_blocks, n_free, n_free_out,
+              got_out, slot_off_out, slots_out, slots_cap, pos_out, nullptr, nullptr, nullptr, nullptr,
               status_word(ws)};
-  a.top = c.take<int64_t>(1);
-  a.before = c.take<int64_t>(static_cast<size_t>(R));
-  launch_pdl(bt_scan_kernel, 1, kScanThreads, 0, s, a);
-  if (R > 0 && slots_cap > 0)
-    launch_pdl(bt_fill_kernel, static_cast<unsigned>((slots_cap + 255) / 256), 256, 0, s, a);
+  carve(c, a);
+  if (R <= kScanThreads)
+    launch_pdl(bt_scan_kernel<1>, 1, kScanThreads, 0, s, a);
+  else
+    launch_cluster(bt_scan_kernel<kCluster>, kCluster, kScanThreads, s, a);
+  if (R > 0) {
+    const int64_t rows = (static_cast<int64_t>(R) * max_blocks + 4 * kFillThreads - 1) / (4 * kFillThreads);
+    const int64_t back = std::min(std::min((static_cast<int64_t>(pool) + 4 * kFillThreads - 1) / (4 * kFillThreads), rows), static_cast<int64_t>(4 * sm_count()));
+    if (slots_cap <= kFewTokens) {
+      const int64_t tokens = (slots_cap + kFillThreads - 1) / kFillThreads;
+      if (tokens + back > 0) launch_pdl(bt_fill_kernel, static_cast<unsigned>(tokens + back), kFillThreads, 0, s, a, static_cast<int>(tokens));
+    } else {
+      const int64_t per = kFillThreads * kManyEach;
+      if (back > 0) launch_pdl(bt_push_kernel, static_cast<unsigned>(back), kFillThreads, 0, s, a);
+      launch_pdl(bt_fill_many_kernel, static_cast<unsigned>((slots_cap + per - 1) / per), kFillThreads, 0, s, a);
+    }
+  }
   return launch_ok();
 }
 

@@ -9,6 +9,7 @@ loads the library and fails loudly when it is missing.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -131,21 +132,22 @@ EXPORTS = ("maps_version", "maps_last_cuda_error", "maps_check", "maps_set_dispa
            "maps_kv4_attention_workspace_size", "maps_kv4_attention")
 
 
-def _stream(stream) -> ctypes.c_void_p:
-    s = torch.cuda.current_stream() if stream is None else stream
-    return ctypes.c_void_p(s.cuda_stream)
+def _stream(stream) -> int:
+    if stream is None:  # the raw handle: a stream object costs more than the rest of a call
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return stream.cuda_stream
 
 
-def _ptr(t, dtype=None) -> ctypes.c_void_p:
+def _ptr(t, dtype=None) -> int | None:
     if t is None:
-        return ctypes.c_void_p(0)
+        return None
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError("expected a CUDA tensor")
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"expected {dtype}, got {t.dtype}")
     if not t.is_contiguous():
         raise TypeError("expected a contiguous tensor")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 class Workspace:
@@ -161,12 +163,18 @@ class Workspace:
         return self
 
     @property
-    def ptr(self) -> ctypes.c_void_p:
-        return ctypes.c_void_p(self.buf.data_ptr())
+    def ptr(self) -> int:
+        return self.buf.data_ptr()
 
     @property
     def nbytes(self) -> int:
         return self.buf.numel()
+
+
+@functools.lru_cache(maxsize=4096)
+def _need(query: str, *sizes: int) -> int:
+    """A workspace size query: it depends on the sizes alone."""
+    return getattr(lib, query)(*sizes)
 
 
 def maps_check(ws: Workspace, stream=None) -> int:
@@ -310,7 +318,7 @@ def maps_block_tables(S: int, held, want, table, free_blocks, n_free, n_free_out
     int32 are updated in place; slots_out [cap] int64 holds the new tokens'."""
     R = held.numel()
     ws = ws or Workspace()
-    ws.ensure(lib.maps_block_tables_workspace_size(R))
+    ws.ensure(_need("maps_block_tables_workspace_size", R))
     return lib.maps_block_tables(R, S, _ptr(held, torch.int32), _ptr(want, torch.int32),
                                  _ptr(order, torch.int32), _ptr(table, torch.int32),
                                  table.shape[1], _ptr(free_blocks, torch.int32),
@@ -328,28 +336,32 @@ def _rows(t, dtype=None):
         raise TypeError("expected a CUDA tensor")
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"expected {dtype}, got {t.dtype}")
-    if t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] > 1):
+    row, head, channel = t.stride()
+    if channel != 1:
         raise TypeError("expected [rows, heads, channels] with contiguous channels")
-    return ctypes.c_void_p(t.data_ptr()), t.stride(0), t.stride(1)
+    return t.data_ptr(), row, head
+
+
+_DTYPES = {torch.bfloat16: BF16, torch.float16: F16}
 
 
 def _dtype(t) -> int:
     try:
-        return {torch.bfloat16: BF16, torch.float16: F16}[t.dtype]
+        return _DTYPES[t.dtype]
     except KeyError:
         raise TypeError(f"expected torch.bfloat16 or torch.float16, got {t.dtype}") from None
 
 
 def kv4_cache_shape(n_blocks: int, H: int, S: int, D: int) -> tuple[int, int, int]:
     """Shape of a 4-bit cache (uint8): [blocks][KV heads][record bytes]."""
-    nbytes = lib.maps_kv4_record_bytes(S, D)
+    nbytes = _need("maps_kv4_record_bytes", S, D)
     if nbytes == 0:
         raise ValueError(f"no 4-bit cache for blocks of {S} tokens and {D} channels")
     return n_blocks, H, nbytes
 
 
 def _kv4(cache, S: int, D: int, H: int):
-    if cache.dim() != 3 or tuple(cache.shape) != kv4_cache_shape(cache.shape[0], H, S, D):
+    if cache.shape != kv4_cache_shape(cache.shape[0], H, S, D):
         raise ValueError(f"a cache of {H} heads, blocks of {S} and {D} channels does not have shape "
                          f"{tuple(cache.shape)}")
     return _ptr(cache, torch.uint8)
@@ -361,7 +373,7 @@ def maps_kv4_append(k, v, slots, cache, S: int, ws: Workspace | None = None, str
     if v.shape != k.shape or slots.numel() != T:
         raise ValueError("k, v and slots differ in size")
     ws = ws or Workspace()
-    ws.ensure(lib.maps_kv4_workspace_size())
+    ws.ensure(_need("maps_kv4_workspace_size"))
     return lib.maps_kv4_append(_dtype(k), T, H, D, S, *_rows(k), *_rows(v, k.dtype),
                                _ptr(slots, torch.int64), _kv4(cache, S, D, H), cache.shape[0],
                                ws.ptr, ws.nbytes, _stream(stream))
@@ -374,7 +386,7 @@ def maps_kv4_read(slots, cache, S: int, k_out, v_out, ws: Workspace | None = Non
     if v_out.shape != k_out.shape or slots.numel() != T:
         raise ValueError("k_out, v_out and slots differ in size")
     ws = ws or Workspace()
-    ws.ensure(lib.maps_kv4_workspace_size())
+    ws.ensure(_need("maps_kv4_workspace_size"))
     return lib.maps_kv4_read(_dtype(k_out), T, H, D, S, _ptr(slots, torch.int64),
                              _kv4(cache, S, D, H), cache.shape[0], *_rows(k_out),
                              *_rows(v_out, k_out.dtype), ws.ptr, ws.nbytes, _stream(stream))
@@ -393,7 +405,7 @@ def maps_kv4_attention(q, qo_off, kv_len, table, cache, S: int, sm_scale: float,
     if lse_out is not None and tuple(lse_out.shape) != (T, Hq):
         raise ValueError("lse_out is [T, Hq]")
     ws = ws or Workspace()
-    ws.ensure(lib.maps_kv4_attention_workspace_size(B, T, Hq, Hkv, D))
+    ws.ensure(_need("maps_kv4_attention_workspace_size", B, T, Hq, Hkv, D))
     return lib.maps_kv4_attention(_dtype(q), B, T, Hq, Hkv, D, S, *_rows(q),
                                   _ptr(qo_off, torch.int64), _ptr(kv_len, torch.int32),
                                   _ptr(table, torch.int32), table.shape[1],
