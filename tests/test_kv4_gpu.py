@@ -230,6 +230,49 @@ def test_append_consecutive_tokens(M):
         assert np.array_equal(one.cpu().numpy()[:, H - 1], ref[:, H - 1])
 
 
+@pytest.mark.parametrize("how", ["dense", "fused", "odd"])
+@pytest.mark.parametrize("T,H,D,S,name", [(20000, 2, 128, 16, "bf16"), (9001, 5, 64, 48, "fp16"), (5003, 8, 256, 32, "bf16"),
+                                          (40001, 1, 128, 64, "fp16")])
+def test_many_rows_equal_few(M, T, H, D, S, name, how):
+    """One call of many tokens writes and reads what calls of a few do: runs of every length and phase,
+    slots out of order, skipped and non-finite tokens."""
+    rng = np.random.default_rng(T)
+    dt = TYPES[name][0]
+    n = T // S + 40
+    slots = np.full(T, -1, np.int64)
+    free = rng.permutation(n)
+    i = used = 0
+    while i < T and used + 9 < n:  # a run over whole blocks, from any place in the first, then a gap
+        run = int(min(T - i, rng.choice([1, 3, 15, 16, 17, 33, 200, 1000])))
+        start = int(rng.integers(0, S)) if rng.random() < 0.5 else 0
+        need = -(-(start + run) // S)
+        if used + need > n:
+            break
+        p = np.arange(start, start + run)
+        slots[i:i + run] = free[used:used + need][p // S] * S + p % S
+        used += need
+        i += run + int(rng.integers(0, 3))
+    k, v = (torch.randn(T, H, D, device="cuda").to(dt) for _ in range(2))
+    k[rng.integers(0, T, 9)] = 0.5
+    v[rng.integers(0, T, 9), 0, 3] = float("nan")
+    k[rng.integers(0, T, 9), H - 1, D - 1] = float("inf")
+    k, v, at = laid_out(k, how), laid_out(v, how), dev(slots)
+    ws = M.Workspace()
+    shape = M.kv4_cache_shape(n, H, S, D)
+    one, parts = (torch.full(shape, 0xA5, dtype=torch.uint8, device="cuda") for _ in range(2))
+    assert M.maps_kv4_append(k, v, at, one, S, ws=ws) == 0
+    for a in range(0, T, 997):
+        assert M.maps_kv4_append(k[a:a + 997], v[a:a + 997], at[a:a + 997], parts, S, ws=ws) == 0
+    assert torch.equal(one, parts)
+    outs = [[laid_out(torch.full((T, H, D), 9.0, dtype=dt, device="cuda"), how) for _ in range(2)] for _ in range(2)]
+    assert M.maps_kv4_read(at, one, S, *outs[0], ws=ws) == 0
+    for a in range(0, T, 997):
+        assert M.maps_kv4_read(at[a:a + 997], one, S, outs[1][0][a:a + 997], outs[1][1][a:a + 997], ws=ws) == 0
+    assert M.maps_check(ws) == 0
+    for x, y in zip(*outs):
+        assert torch.equal(torch.nan_to_num(x, nan=123.0), torch.nan_to_num(y, nan=123.0))
+
+
 def test_append_reports_slots_past_the_cache(M):
     k = torch.randn(3, 1, 64, device="cuda").half()
     cache = torch.zeros(M.kv4_cache_shape(2, 1, 16, 64), dtype=torch.uint8, device="cuda")
