@@ -23,89 +23,19 @@
 // memory with bulk copies, two or more stages ahead; nothing is waited for across warps until the end. What
 // a run begins or ends inside of is joined afterwards: within the block through shared memory, across blocks
 // by the last block to arrive, in the order of the keys, so results do not depend on timing.
-#include "kv4.cuh"
+#include "kv4_attention.cuh"
 
 namespace maps {
 namespace {
 
-constexpr int kMaxWarps = 16;     // of a block
-constexpr int kMaxLocalB = 2048;  // requests over which a block deals out the units for itself
+constexpr int kMaxWarps = 16;  // of a block
+constexpr int kFewRows = 32;    // query rows of a request to a KV head, up to which this form serves it where the other may
 
-struct Start;
-
-struct AttnArgs {
-  int32_t B, Hq, Hkv, S;
-  int64_t T, n_blocks, max_blocks;
-  const void *q;
-  int64_t q_row, q_head, o_row, o_head;
-  const int64_t *off;
-  const int32_t *len, *table;
-  const uint8_t *cache;
-  float scale;
-  int32_t causal, window, wide;
-  int64_t block_bytes;  // of all heads
-  int32_t block_groups, block_shift;  // groups of a block, and their logarithm where they are a power of two, else -1
-  void *out;
-  float *lse;
-  Start *starts;       // where each worker starts, and the units in all, where a block does not find out for itself
-  uint32_t *units;
-  uint32_t *arrived;   // a byte for each block: blocks that have brought their part of the item it begins
-  float *parts;        // [grid][2] parts of items that cross blocks
-  int32_t *status;
-};
-
-// ---------------------------------------------------------------------------- small device helpers
-__device__ __forceinline__ uint32_t smem_u32(const void *p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
-__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t n) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(n) : "memory"); }
-__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-  return ok != 0;
-}
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {  // bounded
-  for (uint32_t i = 0; i < kSpinLimit; ++i)
-    if (bar_try(bar, parity)) return true;
-  return false;
-}
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
-}
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
   uint32_t y;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
-__device__ __forceinline__ float lg2(float x) {
-  float y;
-  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
-  uint32_t y;
-  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(y) : "f"(hi), "f"(lo));
-  return y;
-}
-
-// A word's eight codes as four pairs of half numbers, in five operations: a bare code is the
-// subnormal number code * 2^-24, four bits higher it is code * 2^-20, and the tensor core multiplies
-// both exactly.  The odd pairs' factor of 16 is taken off in the other operand (keys) or the sum (values).
-struct Codes {
-  uint32_t x[4];  // codes (r, r + 4)
-};
-__device__ __forceinline__ Codes codes_of(uint32_t w) {
-  const uint32_t v = w >> 8;
-  return {{w & 0x000f000fu, w & 0x00f000f0u, v & 0x000f000fu, v & 0x00f000f0u}};
-}
-constexpr float kEven = 16777216.0f, kOdd = 1048576.0f;  // 2^24, 2^20
-
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
@@ -161,18 +91,9 @@ __device__ __forceinline__ Req request(const AttnArgs &a, int b) {
   r.row_tiles = static_cast<int32_t>((m * (a.Hq / a.Hkv) + kRows - 1) / kRows);
   r.heads = a.Hkv;
   if (n == 0) r.heads = 1, r.row_tiles = m > 0 ? 1 : 0;
+  if (n > 0 && a.few_rows > 0 && m * (a.Hq / a.Hkv) > a.few_rows) r.row_tiles = 0;  // the other form's
   return r;
 }
-
-// How the units are dealt out: worker w, a warp, has units start(w) .. start(w + 1) - 1.
-struct Deal {
-  uint32_t units, used, per, more;  // used: workers that get units, the first ones
-  __device__ __forceinline__ Deal(uint32_t U, uint32_t workers) : units(U), used(U < workers ? U : workers), per(0), more(0) {
-    if (used) per = U / used, more = U % used;
-  }
-  __device__ __forceinline__ uint32_t start(uint32_t w) const { return w >= used ? units : per * w + min(w, more); }
-  __device__ __forceinline__ uint32_t worker(uint32_t u) const { return u < more * (per + 1) ? u / (per + 1) : more + (u - more * (per + 1)) / per; }
-};
 
 // A place in the list of units: unit `tile` of the item (request b, KV head h, row tile rt).
 struct Cursor {
@@ -260,16 +181,9 @@ __device__ __forceinline__ uint32_t plan(const AttnArgs &a, uint32_t workers, ui
 template <int kTok, int kRows>
 __global__ void __launch_bounds__(1024) attn_plan_kernel(const AttnArgs a, uint32_t workers) {
   pdl_prologue();
-  const uint32_t U = plan<kTok, kRows, 1024>(a, workers, 0, workers, [&](uint32_t w, const Start &c) { a.starts[w] = c; });
+  const uint32_t U = plan<kTok, kRows, 1024>(a, workers, 0, workers, [&](uint32_t w, const Start &c) { static_cast<Start *>(a.starts)[w] = c; });
   if (threadIdx.x == 0) *a.units = U;
 }
-
-// What of an item a warp, or a block, has: the item's first unit and its units (0: none), its queries' first row, rows, head and row tile.
-struct Part {
-  int64_t q0;
-  uint32_t id, tiles;
-  int32_t rows, h, rt;
-};
 
 struct Yes { static constexpr bool value = true; };
 struct No { static constexpr bool value = false; };
@@ -311,7 +225,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(con
   } else {
     __syncthreads();
     U = *a.units;
-    if (me < U) from = a.starts[me];
+    if (me < U) from = static_cast<const Start *>(a.starts)[me];
   }
   const Deal deal(U, workers);
   const uint32_t u0 = deal.start(me), u1 = deal.start(me + 1);
@@ -789,8 +703,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(con
 constexpr int kMaxParts = 16 * 128 + 32;  // floats of the largest part (two row tiles of 128 channels, or one of 256)
 // The counters of arrivals lie in the control block, behind the status word: calls that share a
 // workspace leave that zero, and so does this one.
-constexpr int kArrivedAt = 64, kMaxGrid = kCtrlBytes - kArrivedAt;
-int grid_size() { return sm_count() < kMaxGrid ? sm_count() : kMaxGrid; }
+constexpr int kArrivedAt = 64;
 
 template <class T, int D, int NT>
 int launch_few(const AttnArgs &a, cudaStream_t s) {
@@ -799,8 +712,8 @@ int launch_few(const AttnArgs &a, cudaStream_t s) {
   const size_t smem = static_cast<size_t>(kWarps) * Sh::kStages * Sh::kBytes + static_cast<size_t>(kWarps) * Sh::kPart * 4 + kWarps * Sh::kStages * 8;
   auto kernel = attn_few_kernel<T, D, NT>;
   MAPS_TRY(cuda_ok(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem))));
-  if (a.B > kMaxLocalB) launch_pdl(attn_plan_kernel<Sh::kTok, Sh::kRows>, 1, 1024, 0, s, a, static_cast<uint32_t>(grid_size() * kWarps));
-  launch_pdl(kernel, static_cast<unsigned>(grid_size()), kThreads, smem, s, a);
+  if (a.B > kMaxLocalB) launch_pdl(attn_plan_kernel<Sh::kTok, Sh::kRows>, 1, 1024, 0, s, a, static_cast<uint32_t>(attn_grid() * kWarps));
+  launch_pdl(kernel, static_cast<unsigned>(attn_grid()), kThreads, smem, s, a);
   return launch_ok();
 }
 
@@ -818,13 +731,20 @@ int launch_dim(int D, const AttnArgs &a, cudaStream_t s) {
 
 extern "C" {
 
-size_t maps_kv4_attention_workspace_size(int32_t B, int64_t T, int32_t Hq, int32_t Hkv, int32_t D) {
+static void carve(maps::Carve &c, maps::AttnArgs &a, int32_t B, int64_t T, int32_t Hq, int32_t Hkv, int32_t D) {
   using namespace maps;
-  (void)T, (void)Hq, (void)Hkv, (void)D;
-  Carve c(nullptr);
-  c.take<float>(static_cast<size_t>(grid_size()) * 2 * kMaxParts);
-  c.take<Start>(B > kMaxLocalB ? static_cast<size_t>(grid_size()) * kMaxWarps : 0);
-  c.take<uint32_t>(1);
+  a.parts = c.take<float>(static_cast<size_t>(attn_grid()) * 2 * kMaxParts);
+  a.starts = c.take<Start>(B > kMaxLocalB ? static_cast<size_t>(attn_grid()) * kMaxWarps : 0);
+  a.units = c.take<uint32_t>(1);
+  // requests with many queries there can only be where there are more rows than requests
+  a.few_rows = Hkv > 0 && attn_many_dim(D) && T > B && T * (Hq / Hkv) > kFewRows ? kFewRows : 0;
+  if (a.few_rows) attn_many_carve(c, a, B, D);
+}
+
+size_t maps_kv4_attention_workspace_size(int32_t B, int64_t T, int32_t Hq, int32_t Hkv, int32_t D) {
+  maps::Carve c(nullptr);
+  maps::AttnArgs a = {};
+  carve(c, a, B, T, Hq, Hkv, D);
   return c.bytes();
 }
 
@@ -847,21 +767,20 @@ int maps_kv4_attention(int32_t dtype, int32_t B, int64_t T, int32_t Hq, int32_t 
       !aligned(lse, 4) || !aligned(out, 2))
     return MAPS_E_INVALID;
   const bool wide = aligned(q, 16) && aligned(out, 16) && q_row % 8 == 0 && q_head % 8 == 0 && o_row % 8 == 0 && o_head % 8 == 0;
-  Carve c(ws);
-  uint32_t *arrived = reinterpret_cast<uint32_t *>(static_cast<char *>(ws) + kArrivedAt);
-  float *parts = c.take<float>(static_cast<size_t>(grid_size()) * 2 * kMaxParts);
-  Start *starts = c.take<Start>(B > kMaxLocalB ? static_cast<size_t>(grid_size()) * kMaxWarps : 0);
-  uint32_t *units = c.take<uint32_t>(1);
   const int32_t groups = S / kGroup;
   int32_t shift = -1;
   for (int32_t i = 0; i < 16; ++i)
     if (groups == 1 << i) shift = i;
-  const AttnArgs a = {B, Hq, Hkv, S, T, n_blocks, max_blocks, q, q_row, q_head, o_row, o_head, qo_off, kv_len, table,
-                      static_cast<const uint8_t *>(cache), sm_scale, causal, window, wide,
-                      static_cast<int64_t>(Hkv) * groups * kv4_group_bytes(D), groups, shift, out, lse, starts, units, arrived, parts, status_word(ws)};
+  AttnArgs a = {B, Hq, Hkv, S, T, n_blocks, max_blocks, q, q_row, q_head, o_row, o_head, qo_off, kv_len, table,
+                static_cast<const uint8_t *>(cache), sm_scale, causal, window, wide,
+                static_cast<int64_t>(Hkv) * groups * kv4_group_bytes(D), groups, shift, out, lse};
+  a.arrived = reinterpret_cast<uint32_t *>(static_cast<char *>(ws) + kArrivedAt);
+  a.status = status_word(ws);
+  Carve c(ws);
+  carve(c, a, B, T, Hq, Hkv, D);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (dtype == MAPS_BF16) return launch_dim<__nv_bfloat16>(D, a, s);
-  return launch_dim<__half>(D, a, s);
+  MAPS_TRY(dtype == MAPS_BF16 ? launch_dim<__nv_bfloat16>(D, a, s) : launch_dim<__half>(D, a, s));
+  return a.few_rows ? attn_many(dtype, D, a, s) : MAPS_OK;
 }
 
 }  // extern "C"
