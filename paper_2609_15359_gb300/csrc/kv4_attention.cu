@@ -185,9 +185,6 @@ __global__ void __launch_bounds__(1024) attn_plan_kernel(const AttnArgs a, uint3
   if (threadIdx.x == 0) *a.units = U;
 }
 
-struct Yes { static constexpr bool value = true; };
-struct No { static constexpr bool value = false; };
-
 // Weights are held relative to the largest weight times value scale seen, so that what enters the
 // second product is at most 1; scales count as at least 2^-60 there, so that a weight itself stays finite.
 constexpr float kMinLog = -60.0f;

@@ -52,13 +52,14 @@ __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t n) { asm volatil
 __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
+// Sleeps for up to 20 us where the phase is not over: polling costs the other warps issue slots.
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
   uint32_t ok;
-  asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(bar), "r"(parity), "r"(20000u) : "memory");
   return ok != 0;
 }
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {  // bounded
-  for (uint32_t i = 0; i < kSpinLimit; ++i)
+  for (uint32_t i = 0; i < (1u << 18); ++i)
     if (bar_try(bar, parity)) return true;
   return false;
 }
@@ -103,6 +104,9 @@ struct Deal {
   __device__ __forceinline__ uint32_t worker(uint32_t u) const { return u < more * (per + 1) ? u / (per + 1) : more + (u - more * (per + 1)) / per; }
 };
 
+
+struct Yes { static constexpr bool value = true; };
+struct No { static constexpr bool value = false; };
 
 // The form for many queries (kv4_attention_many.cu).
 bool attn_many_dim(int D);

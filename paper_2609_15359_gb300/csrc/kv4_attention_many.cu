@@ -7,9 +7,12 @@
 //
 //   warps 0-3, 4-7   softmax of a tile, a row a thread: S from tensor memory, running maximum and sum, P back;
 //                    they rescale O when the maximum has grown by more than 2^8, and write it out at the end
-//   warps 8-11       the cache's codes to operands in shared memory, two steps deep
+//   warps 8-11       the values' codes to operands in shared memory, one step deep
+//   warp 15          the same of the keys, two deep: a step's keys may be wanted a second time (below)
 //   warp 12          issues the products; the two tiles alternate, so that one's softmax runs beside the other's products
-//   warp 13          bulk copies of the cache's records, a ring of groups ahead
+//   warp 13          bulk copies of the cache's records, up to three steps ahead
+//   warp 14          walks the block's items and tells the others what each is; in their registers it would cost the
+//                    inner loops, which need little of it, a fifth of theirs
 //
 // Keys enter the first product as bare codes (subnormal halves, exact; the odd pairs' factor of 16 is taken
 // off in Q) and s, z come in with the row's sum of Q in 32 bits, as in the form for few queries: two packed
@@ -29,9 +32,9 @@ namespace maps {
 namespace {
 
 constexpr int kThreads = 512;
+constexpr int kItemUnits = 3;  // what an item costs besides its steps, in steps: its queries, its output, the pipeline's start
 constexpr int kRows = 256, kTok = 128, kStepGroups = kTok / kGroup;
-constexpr int kLaunchRegs = 128, kSoftmaxRegs = 184, kOperandRegs = 88, kOtherRegs = 56;  // of a thread, by warpgroup
-constexpr int kRing = 14;  // groups of the cache under way or waiting
+constexpr int kRing = 3;  // steps of the cache's records under way or waiting
 
 struct MReq {
   int64_t q0;
@@ -52,7 +55,7 @@ __device__ __forceinline__ MReq many_request(const AttnArgs &a, int b) {
   return r;
 }
 
-// The tokens lo .. hi - 1 that a row tile's queries see between them (lo to 16), and its units: one for itself, and its steps.
+// The tokens lo .. hi - 1 that a row tile's queries see between them (lo to 16), and its units: kItemUnits for itself, and its steps.
 __device__ __forceinline__ int span(const AttnArgs &a, const MReq &r, int rt, int32_t &lo, int32_t &hi) {
   const int group = a.Hq / a.Hkv;
   const int first = rt * kRows / group, last = min(r.n_q - 1, (rt * kRows + kRows - 1) / group);
@@ -60,7 +63,7 @@ __device__ __forceinline__ int span(const AttnArgs &a, const MReq &r, int rt, in
   hi = a.causal ? static_cast<int32_t>(max(int64_t(0), shift + last + 1)) : r.n;
   const int64_t from = a.window > 0 ? shift + first - a.window + 1 : 0;
   lo = from > 0 ? static_cast<int32_t>(min(from, static_cast<int64_t>(hi))) / kGroup * kGroup : 0;
-  return 1 + (hi > lo ? (hi - lo + kTok - 1) / kTok : 0);
+  return kItemUnits + (hi > lo ? (hi - lo + kTok - 1) / kTok : 0);
 }
 
 struct ManyStart {
@@ -69,41 +72,19 @@ struct ManyStart {
   uint32_t rest;
 };
 
-// A block's run of units, item by item.
-struct Walk {
-  MReq r;
-  int32_t b, h, rt, tile, tiles, lo, hi;
-  uint32_t u, u1;
-  __device__ __forceinline__ Walk(const AttnArgs &a, const ManyStart &s, uint32_t u0, uint32_t u1) : r(s.r), b(s.b), h(0), rt(0), tile(0), tiles(0), lo(0), hi(0), u(u0), u1(u1) {
-    if (u >= u1) return;
-    uint32_t all = 0;
-    for (int t = 0; t < r.row_tiles; ++t) all += span(a, r, t, lo, hi);
-    h = static_cast<int32_t>(s.rest / all);
-    uint32_t rest = s.rest - static_cast<uint32_t>(h) * all;
-    while (rest >= static_cast<uint32_t>(tiles = span(a, r, rt, lo, hi))) rest -= tiles, ++rt;
-    tile = static_cast<int32_t>(rest);
-  }
-  __device__ __forceinline__ bool more() const { return u < u1; }
-  __device__ __forceinline__ int end() const { return static_cast<int>(min(static_cast<uint32_t>(tiles), tile + (u1 - u))); }  // of this run's units of the item
-  __device__ __forceinline__ int first_step() const { return max(tile, 1) - 1; }
-  __device__ __forceinline__ int steps() const { return end() - max(tile, 1); }
-  __device__ __forceinline__ int rows(const AttnArgs &a) const { return r.n_q * (a.Hq / a.Hkv); }
-  __device__ __forceinline__ bool second(const AttnArgs &a) const { return rt * kRows + 128 < rows(a); }  // whether the second tile has rows
-  __device__ __forceinline__ void next(const AttnArgs &a) {
-    u += end() - tile;
-    if (u >= u1) return;
-    tile = 0;
-    if (++rt == r.row_tiles) {
-      rt = 0;
-      if (++h == a.Hkv) {
-        h = 0;
-        do r = many_request(a, ++b);
-        while (r.row_tiles == 0);
-      }
-    }
-    tiles = span(a, r, rt, lo, hi);
-  }
+// What the warps are told of an item, or of what a block has of it.
+struct Seg {
+  int64_t q0;
+  int32_t steps;         // -1: no further item
+  int32_t token, hi;     // the first step's first token, and the end of those that any of the rows see
+  int32_t n, n_q, rows;  // of the request; rows of all its tiles
+  int32_t b, h, rt;
+  int32_t second;        // whether the second tile has rows
+  int32_t whole;
+  uint32_t id, tiles;    // the item's first unit and its units
 };
+constexpr int kSegs = 4;  // under way or told ahead
+constexpr int kHearers = 15;
 
 template <int kN, class Put>
 __device__ __forceinline__ uint32_t many_plan(const AttnArgs &a, uint32_t blocks, uint32_t w0, uint32_t w1, Put put) {
@@ -164,35 +145,47 @@ __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::befor
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t A, uint64_t B, uint32_t idesc, uint32_t add) {
-  asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(A), "l"(B), "r"(idesc), "r"(add) : "memory");
+// Operands in shared memory are rows of 64 halves (128 bytes) in the 128-byte swizzle, 8 rows to 1,024 bytes:
+// the low word of a descriptor is the address, the high word the same for all.
+__device__ __forceinline__ uint32_t rows_desc(uint32_t addr) { return (addr >> 4 & 0x3fffu) | 1u << 16; }
+constexpr uint32_t kDescHigh = 64u | 1u << 14 | 2u << 29;
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t A, uint32_t B, uint32_t idesc, uint32_t add) {
+  asm volatile("{\n.reg .pred p;\n.reg .b64 a, b;\nsetp.ne.b32 p, %4, 0;\nmov.b64 a, {%1, %5};\nmov.b64 b, {%2, %5};\n"
+               "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n}" ::"r"(d), "r"(A), "r"(B), "r"(idesc), "r"(add), "r"(kDescHigh) : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t A, uint64_t B, uint32_t idesc, uint32_t add) {
-  asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(A), "l"(B), "r"(idesc), "r"(add) : "memory");
-}
-// Descriptor of rows of 64 halves (128 bytes) in the 128-byte swizzle: 8 rows to 1,024 bytes.
-__device__ __forceinline__ uint64_t rows_desc(uint32_t addr) {
-  return static_cast<uint64_t>((addr >> 4) & 0x3fffu) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t A, uint32_t B, uint32_t idesc, uint32_t add) {
+  asm volatile("{\n.reg .pred p;\n.reg .b64 b;\nsetp.ne.b32 p, %4, 0;\nmov.b64 b, {%2, %5};\n"
+               "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n}" ::"r"(d), "r"(A), "r"(B), "r"(idesc), "r"(add), "r"(kDescHigh) : "memory");
 }
 // Instruction: halves in, 32-bit sums, 128 rows, N columns, both operands along the depth.
 __host__ __device__ constexpr uint32_t idesc_of(int N) { return (1u << 4) | (static_cast<uint32_t>(N / 8) << 17) | (8u << 24); }
 
 #define MAPS_R8(x, i) "=r"(x[i]), "=r"(x[i + 1]), "=r"(x[i + 2]), "=r"(x[i + 3]), "=r"(x[i + 4]), "=r"(x[i + 5]), "=r"(x[i + 6]), "=r"(x[i + 7])
 #define MAPS_W8(x, i) "r"(x[i]), "r"(x[i + 1]), "r"(x[i + 2]), "r"(x[i + 3]), "r"(x[i + 4]), "r"(x[i + 5]), "r"(x[i + 6]), "r"(x[i + 7])
-#define MAPS_32 "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}"
-__device__ __forceinline__ void tm_load32(uint32_t addr, uint32_t *x) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 " MAPS_32 ", [%32];" : MAPS_R8(x, 0), MAPS_R8(x, 8), MAPS_R8(x, 16), MAPS_R8(x, 24) : "r"(addr) : "memory");
-}
-__device__ __forceinline__ void tm_store32(uint32_t addr, const uint32_t *x) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], " MAPS_32 ";" ::MAPS_W8(x, 0), MAPS_W8(x, 8), MAPS_W8(x, 16), MAPS_W8(x, 24), "r"(addr) : "memory");
-}
-__device__ __forceinline__ void tm_load16(uint32_t addr, uint32_t *x) {
+__device__ __forceinline__ void tm_load16(uint32_t addr, uint32_t *x) {  // a row a thread
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];" : MAPS_R8(x, 0), MAPS_R8(x, 8) : "r"(addr) : "memory");
 }
-__device__ __forceinline__ void tm_store16(uint32_t addr, const uint32_t *x) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::MAPS_W8(x, 0), MAPS_W8(x, 8), "r"(addr) : "memory");
+// 16 rows and 32 columns as the four-lanes-a-row fragments of a warp-level product: registers 4 i .. 4 i + 3 are columns
+// 8 i + 2 (lane % 4) and the next, of row lane / 4 and of row lane / 4 + 8.
+__device__ __forceinline__ void tm_load_frag(uint32_t addr, uint32_t *x) {
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];" : MAPS_R8(x, 0), MAPS_R8(x, 8) : "r"(addr) : "memory");
 }
-__device__ __forceinline__ void tm_wait_load() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tm_load_frag2(uint32_t addr, uint32_t *x) {  // 16 columns
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];" : MAPS_R8(x, 0) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tm_store_frag(uint32_t addr, const uint32_t *x) {
+  asm volatile("tcgen05.st.sync.aligned.16x256b.x4.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::MAPS_W8(x, 0), MAPS_W8(x, 8), "r"(addr) : "memory");
+}
+// The same of 16 columns as halves, two to a word: register 2 i is row lane / 4, register 2 i + 1 the row 8 on.
+__device__ __forceinline__ void tm_store_halves(uint32_t addr, const uint32_t *x) {
+  asm volatile("tcgen05.st.sync.aligned.16x128b.x2.b32 [%4], {%0,%1,%2,%3};" ::"r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(addr) : "memory");
+}
+// The loads' registers pass through the wait, so that nothing uses them ahead of it.
+#define MAPS_RW8(x, i) "+r"(x[i]), "+r"(x[i + 1]), "+r"(x[i + 2]), "+r"(x[i + 3]), "+r"(x[i + 4]), "+r"(x[i + 5]), "+r"(x[i + 6]), "+r"(x[i + 7])
+__device__ __forceinline__ void tm_wait16(uint32_t *x) { asm volatile("tcgen05.wait::ld.sync.aligned;" : MAPS_RW8(x, 0), MAPS_RW8(x, 8)::"memory"); }
+__device__ __forceinline__ void tm_wait32(uint32_t *x) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : MAPS_RW8(x, 0), MAPS_RW8(x, 8), MAPS_RW8(x, 16), MAPS_RW8(x, 24)::"memory");
+}
 __device__ __forceinline__ void tm_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 union F2 {
@@ -221,22 +214,44 @@ __device__ __forceinline__ uint64_t fma2(uint64_t x, uint64_t y, uint64_t w) {
   return z;
 }
 
+struct Zero { static constexpr int value = 0; };
+struct One { static constexpr int value = 1; };
+
 template <int D>
 struct Lay {  // shared memory, from a 1,024-byte boundary
   static constexpr int kTile = 128 * D * 2;          // Q of a tile, K or V of a step
-  static constexpr int kQ = 0, kK = 2 * kTile, kV = 4 * kTile, kRingAt = 6 * kTile;
-  static constexpr int kPar = kRingAt + kRing * kv4_group_bytes(D);  // [2][64] {scale, scale, zero, zero} of two keys
-  static constexpr int kNan = kPar + 2 * kTok * 8;   // [2][4] bits: values held as NaN
-  static constexpr int kExp = kNan + 32;             // [2] the step's exponent
-  static constexpr int kBars = kExp + 16;
-  static constexpr int kBytes = kBars + 8 * (2 * kRing + 12) + 16;
+  static constexpr int kStep = kStepGroups * kv4_group_bytes(D);  // records
+  static constexpr int kQ = 0, kK = 2 * kTile, kV = 4 * kTile, kRingAt = 5 * kTile;
+  static constexpr int kPar = kRingAt + kRing * kStep;  // [4][64] {scale, scale, zero, zero} of two keys
+  static constexpr int kRow = kPar + 4 * kTok * 8;   // [256] a row's sum, what a score is to be multiplied by, and the keys that it sees
+  static constexpr int kNan = kRow + kRows * 16;     // [4][4] bits: values held as NaN
+  static constexpr int kExp = kNan + 64;             // [4] the step's exponent
+  static constexpr int kAgain = kExp + 16;           // [2] a tile's scores are wanted again
+  static constexpr int kFail = kAgain + 8;           // a wait has run out
+  static constexpr int kBars = kFail + 8;
+  static constexpr int kSegAt = kBars + 8 * (2 * kRing + 14 + 2 * kSegs);
+  static constexpr int kBytes = kSegAt + kSegs * static_cast<int>(sizeof(Seg));
   static constexpr int kPart = kRows * D + 2 * kRows;  // floats of a part: sums, maxima, totals
 };
-static_assert(Lay<128>::kBytes + 1024 < 231 * 1024, "shared memory");
-static_assert(Lay<128>::kBars % 8 == 0 && Lay<64>::kBars % 8 == 0 && Lay<128>::kPar % 16 == 0 && Lay<64>::kPar % 16 == 0, "alignment");
+static_assert(Lay<128>::kBytes + 1024 + 512 <= 227 * 1024, "shared memory");
+template <int D>
+constexpr bool lay_aligned() {  // to what is read and written there at once
+  using L = Lay<D>;
+  return L::kK % 1024 == 0 && L::kV % 1024 == 0 && L::kRingAt % 16 == 0 && L::kStep % 16 == 0 && L::kPar % 16 == 0 && L::kRow % 16 == 0 && L::kNan % 16 == 0 &&
+         L::kExp % 4 == 0 && L::kAgain % 4 == 0 && L::kFail % 4 == 0 && L::kBars % 8 == 0 && L::kSegAt % alignof(Seg) == 0;
+}
+static_assert(lay_aligned<64>() && lay_aligned<128>(), "alignment");
 
 constexpr int kNoExp = -400;     // of a step without a value
-constexpr float kSlack = 8.0f;   // powers of two that a weight may exceed 1 by before the sums are rescaled
+constexpr float kSlack = 8.0f;   // powers of two that a weight may exceed 1 by before the sums are rescaled at the next step
+constexpr float kMost = 15.0f;   // and that it may at all, for half's range
+
+// Whether any of a tile's 128 threads says so; barrier `id` of the block.
+__device__ __forceinline__ bool tile_any(int id, bool x) {
+  uint32_t y;
+  asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 q, %1, 0;\nbarrier.cta.red.or.pred p, %2, 128, q;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(y) : "r"(static_cast<uint32_t>(x)), "r"(id) : "memory");
+  return y != 0;
+}
 
 template <class T, int D>
 __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a) {
@@ -247,23 +262,28 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
   uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   const uint32_t base = smem_u32(smem), bars = base + L::kBars;
   // barriers
-  auto ring_full = [&](int i) { return bars + 8 * i; };
-  auto ring_free = [&](int i) { return bars + 8 * (kRing + i); };
-  const uint32_t b0 = bars + 16 * kRing;
-  auto kv_full = [&](int i) { return b0 + 8 * i; };
-  auto kv_free = [&](int i) { return b0 + 16 + 8 * i; };
-  auto q_full = [&](int t) { return b0 + 32 + 8 * t; };
-  auto s_full = [&](int t) { return b0 + 48 + 8 * t; };
-  auto p_full = [&](int t) { return b0 + 64 + 8 * t; };
-  auto o_full = [&](int t) { return b0 + 80 + 8 * t; };
+  auto step_full = [&](int i) { return bars + 8 * i; };  // a step's records are in the ring, and have been read
+  auto step_free = [&](int i) { return bars + 8 * (kRing + i); };
+  const uint32_t b0 = bars + 16 * kRing, v_full = b0, v_free = b0 + 8;
+  auto k_full = [&](int i) { return b0 + 16 + 8 * i; };
+  auto k_free = [&](int i) { return b0 + 32 + 8 * i; };
+  auto q_full = [&](int t) { return b0 + 48 + 8 * t; };
+  auto s_full = [&](int t) { return b0 + 64 + 8 * t; };
+  auto p_full = [&](int t) { return b0 + 80 + 8 * t; };
+  auto o_full = [&](int t) { return b0 + 96 + 8 * t; };
+  auto seg_full = [&](int i) { return b0 + 112 + 8 * i; };
+  auto seg_free = [&](int i) { return b0 + 112 + 8 * kSegs + 8 * i; };
 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (tid == 0) {
-    for (int i = 0; i < kRing; ++i) bar_init(ring_full(i), 1), bar_init(ring_free(i), 4);
+    for (int i = 0; i < 3; ++i) reinterpret_cast<int *>(smem + L::kAgain)[i] = 0;
+    for (int i = 0; i < kRing; ++i) bar_init(step_full(i), kStepGroups), bar_init(step_free(i), 5);
+    bar_init(v_full, 4), bar_init(v_free, 1);
     for (int i = 0; i < 2; ++i) {
-      bar_init(kv_full(i), 4), bar_init(kv_free(i), 1);
-      bar_init(q_full(i), 4), bar_init(s_full(i), 1), bar_init(p_full(i), 4), bar_init(o_full(i), 1);
+      bar_init(k_full(i), 1), bar_init(k_free(i), 1);
+      bar_init(q_full(i), 4), bar_init(s_full(i), 2), bar_init(p_full(i), 4), bar_init(o_full(i), 1);
     }
+    for (int i = 0; i < kSegs; ++i) bar_init(seg_full(i), 1), bar_init(seg_free(i), kHearers);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 12) {
@@ -285,177 +305,313 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
   tc_after();
   const Deal deal(U, gridDim.x);
   const uint32_t u0 = deal.start(me), u1 = deal.start(me + 1);
-  const uint32_t tmem = s_tmem;
+  const uint32_t tmem = s_tmem;  // 0
   const int group = a.Hq / a.Hkv;
   const float sl2 = a.scale * 1.4426950408889634f, k_sign = a.scale < 0.0f ? -1.0f : 1.0f;
   if (tid == 0) a.many_open[me].tiles = 0;
 
+  // the next item: waits for it, and says whether there is one; then what it is, and that this warp is done with it
+  uint32_t n_seg = 0;
+  // where a step's records lie in the ring, and the parity of the round
+  int place = 0;
+  uint32_t round = 0;
+  auto ring_on = [&]() {
+    if (++place == kRing) place = 0, round ^= 1u;
+  };
+  auto hear = [&](bool &ok) {
+    ok = bar_wait(seg_full(n_seg % kSegs), n_seg / kSegs & 1);
+    return ok && reinterpret_cast<const Seg *>(smem + L::kSegAt)[n_seg % kSegs].steps >= 0;
+  };
+  auto told = [&]() -> const Seg & { return reinterpret_cast<const Seg *>(smem + L::kSegAt)[n_seg % kSegs]; };
+  auto done = [&]() { bar_arrive(seg_free(n_seg++ % kSegs)); };  // by one lane
+
   if (warp < 8) {
     // ======================================================================== softmax
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
     const int t = warp >> 2, row = tid & 127;
     const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;  // 32 lanes of tensor memory to a warp
     const uint32_t s_at = tmem + lanes + t * 128, o_at = tmem + lanes + 256 + t * 128;
     uint32_t c = 0, n_s = 0, n_o = 0;  // steps, scores and sums so far
-    bool ok = true;
-    for (Walk w(a, s_start, u0, u1); w.more() && ok; w.next(a)) {
-      const int steps = w.steps(), rows = w.rows(a);
-      if (t == 1 && !w.second(a)) {
+    bool ok = true, failed = false;
+    while (hear(ok)) {
+      const Seg &w = told();
+      const int steps = w.steps, tok_at = w.token;
+      if (t == 1 && !w.second) {
         c += steps;
+        __syncwarp();
+        if (lane == 0) bar_arrive(seg_free(n_seg % kSegs));
+        ++n_seg;
         continue;
       }
-      const int R = w.rt * kRows + t * 128 + row;
-      const bool there = R < rows;
-      const int64_t i = w.r.q0 + (there ? R / group : 0);
-      const int hq = w.h * group + (there ? R % group : 0);
-      float m = -INFINITY, l = 0.0f, unit = 1.0f, sum = 0.0f;
       int run = kNoExp;
-      int32_t row_lo = 0, row_hi = 0x7fffffff;  // a row that is none sees everything; nobody reads it
-      if (there) {
-        const int64_t pos = static_cast<int64_t>(w.r.n) - w.r.n_q + R / group;
-        row_hi = pos < 0 ? 0 : a.causal ? static_cast<int32_t>(pos) + 1 : w.r.n;
-        if (a.window > 0 && pos - a.window + 1 > 0) row_lo = static_cast<int32_t>(pos - a.window + 1);
+      float4 *row_of = reinterpret_cast<float4 *>(smem + L::kRow) + t * 128;
+      const int R = w.rt * kRows + t * 128 + row;
+      const bool there = R < w.rows;
+      {
+        int32_t lo = 0, hi = 0x7fffffff;  // a row that is none sees everything; nobody reads it
+        if (there) {
+          const int64_t pos = static_cast<int64_t>(w.n) - w.n_q + R / group;
+          hi = pos < 0 ? 0 : a.causal ? static_cast<int32_t>(pos) + 1 : w.n;
+          if (a.window > 0 && pos - a.window + 1 > 0) lo = static_cast<int32_t>(pos - a.window + 1);
+        }
+        reinterpret_cast<int2 *>(row_of + row)[1] = make_int2(lo, hi);
       }
       if (steps > 0) {
-        // ---- the row of Q, scaled by a power of two to fill half's range, to shared memory; 8 channels in the order of the codes
-        const T *src = static_cast<const T *>(a.q) + i * a.q_row + hq * a.q_head;
-        uint4 raw[D / 8];
-        float top = 0.0f;
+        // ---- the warp's 32 rows of Q, D/8 lanes to a row, each row scaled by a power of two to fill half's range; 8 channels
+        // in the order of the codes.  Small loops here and below: what is met once an item is not in the instruction cache.
+        constexpr int kLanes = D / 8, kAt = 32 / kLanes;
+        const int rows = w.rows, h0 = w.h * group;
+        const int64_t q0 = w.q0;
+        constexpr int kBatch = 8;  // loads under way at once
+#pragma unroll 1
+        for (int x0 = 0; x0 < kLanes; x0 += kBatch) {
+        uint4 raws[kBatch];
 #pragma unroll
-        for (int x = 0; x < D / 8; ++x) {
-          raw[x] = make_uint4(0, 0, 0, 0);
-          T *y = reinterpret_cast<T *>(&raw[x]);
-          if (there) {
+        for (int x = 0; x < kBatch; ++x) {
+          const int Rx = w.rt * kRows + t * 128 + (warp & 3) * 32 + (x0 + x) * kAt + lane / kLanes;
+          raws[x] = make_uint4(0, 0, 0, 0);
+          if (Rx < rows) {
+            const T *src = static_cast<const T *>(a.q) + (q0 + Rx / group) * a.q_row + (h0 + Rx % group) * a.q_head + 8 * (lane % kLanes);
             if (a.wide) {
-              raw[x] = *reinterpret_cast<const uint4 *>(src + 8 * x);
+              raws[x] = *reinterpret_cast<const uint4 *>(src);
             } else {
+              T *z = reinterpret_cast<T *>(&raws[x]);
 #pragma unroll
-              for (int e = 0; e < 8; ++e) y[e] = src[8 * x + e];
+              for (int e = 0; e < 8; ++e) z[e] = src[e];
             }
           }
-#pragma unroll
-          for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(Cvt<T>::to(y[e])));
         }
-        const int ef = min(max(static_cast<int>(__float_as_uint(top) >> 23), 20), 254);
-        const float up = __uint_as_float(static_cast<uint32_t>(268 - ef) << 23);
-        unit = fmaxf(fabsf(sl2) * __uint_as_float(static_cast<uint32_t>(ef - 14) << 23), 1.17549435e-38f);
 #pragma unroll
-        for (int x = 0; x < D / 8; ++x) {
-          const T *y = reinterpret_cast<const T *>(&raw[x]);
-          float q[8];
+        for (int x = 0; x < kBatch; ++x) {
+          const int r = (warp & 3) * 32 + (x0 + x) * kAt + lane / kLanes, at = lane % kLanes;
+          const T *y = reinterpret_cast<const T *>(&raws[x]);
+          float q[8], top = 0.0f, sum = 0.0f;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) q[e] = Cvt<T>::to(y[e]) * up, sum += q[e];
+          for (int e = 0; e < 8; ++e) q[e] = Cvt<T>::to(y[e]), top = fmaxf(top, fabsf(q[e]));
+#pragma unroll
+          for (int o = kLanes / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+          const int ef = min(max(static_cast<int>(__float_as_uint(top) >> 23), 20), 254);
+          const float up = __uint_as_float(static_cast<uint32_t>(268 - ef) << 23);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) q[e] *= up, sum += q[e];
+#pragma unroll
+          for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
           const uint4 z = make_uint4(pack_half(q[0], q[4]), pack_half(q[1] * 0.0625f, q[5] * 0.0625f), pack_half(q[2], q[6]),
                                      pack_half(q[3] * 0.0625f, q[7] * 0.0625f));
-          *reinterpret_cast<uint4 *>(smem + L::kQ + t * L::kTile + x / 8 * 16384 + row * 128 + ((x % 8 ^ (row & 7)) << 4)) = z;
+          *reinterpret_cast<uint4 *>(smem + L::kQ + t * L::kTile + at / 8 * 16384 + r * 128 + ((at % 8 ^ (r & 7)) << 4)) = z;
+          if (at == 0)
+            *reinterpret_cast<float2 *>(row_of + r) =
+                make_float2(sum, fmaxf(fabsf(sl2) * __uint_as_float(static_cast<uint32_t>(ef - 14) << 23), 1.17549435e-38f));
+        }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) bar_arrive(q_full(t));
       }
-      const uint64_t sum2 = two(sum, sum), unit2 = two(unit, unit);
-      int32_t all_lo = row_lo, all_hi = row_hi;
+      __syncwarp();
+      // From here on a thread has the columns of its place among four lanes, of four rows: a key's scale and zero are
+      // then read once for four rows, where a thread for each row would have every warp read them all.
+      float fsum[4], funit[4], fm[4], fl[4], top[4];
+      bool pending = false;  // a row's maximum has grown, and the sums are to follow before the next step's weights
+      int32_t flo[4], fhi[4];
+      int32_t all_lo = 0, all_hi = 0x7fffffff;
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) {
+      for (int e = 0; e < 4; ++e) {
+        const float4 x = row_of[(warp & 3) * 32 + 8 * e + (lane >> 2)];
+        fsum[e] = x.x;
+        funit[e] = x.y;
+        flo[e] = __float_as_int(x.z);
+        fhi[e] = __float_as_int(x.w);
+        fm[e] = top[e] = -INFINITY;
+        fl[e] = 0.0f;
+        all_lo = max(all_lo, flo[e]);
+        all_hi = min(all_hi, fhi[e]);
+      }
+#pragma unroll
+      for (int o = 4; o < 32; o <<= 1) {
         all_lo = max(all_lo, __shfl_xor_sync(0xffffffffu, all_lo, o));
         all_hi = min(all_hi, __shfl_xor_sync(0xffffffffu, all_hi, o));
       }
 
       for (int j = 0; j < steps; ++j, ++c) {
-        const int buf = c & 1;
-        ok = bar_wait(kv_full(buf), c >> 1 & 1) && bar_wait(s_full(t), n_s & 1);
-        if (!ok) break;
+        const int buf = c & 3;
+        ok = bar_wait(s_full(t), n_s & 1);
         ++n_s;
         tc_after();
-        uint64_t x[64];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) tm_load32(s_at + 32 * k, reinterpret_cast<uint32_t *>(x) + 32 * k);
-        tm_wait_load();
         const uint4 *par = reinterpret_cast<const uint4 *>(smem + L::kPar + buf * kTok * 8);
-        const int32_t tok0 = w.lo + (w.first_step() + j) * kTok;
-        float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        const int32_t tok0 = tok_at + j * kTok;
         const bool every = tok0 >= all_lo && tok0 + kTok <= all_hi;
-        const int c_lo = row_lo - tok0, c_hi = row_hi - tok0;
+        // S is taken in eighths of 16 keys.  x[4 h + 2 i + e]: columns 8 i .. of row 2 h + e; scores, up to the row's
+        // factor, in place of their products.
+        auto load = [&](uint64_t *x, int k) {
+          tm_load_frag2(s_at + 16 * k, reinterpret_cast<uint32_t *>(x));
+          tm_load_frag2(s_at + (16u << 16) + 16 * k, reinterpret_cast<uint32_t *>(x) + 8);
+        };
+        auto landed = [](uint64_t *x) { tm_wait16(reinterpret_cast<uint32_t *>(x)); };
+        auto scores = [&](auto all, uint64_t *x, int k) {  // all: every row sees every key
 #pragma unroll
-        for (int k = 0; k < 64; ++k) {
-          const uint4 p = par[k];
-          F2 s, z;
-          s.u[0] = p.x, s.u[1] = p.y, z.u[0] = p.z, z.u[1] = p.w;
-          F2 y;
-          y.v = fma2(s.v, x[k], mul2(z.v, sum2));
-          x[k] = y.v;
-        }
-        if (!every) {
+          for (int i = 0; i < 2; ++i) {
+            const uint4 p = par[8 * k + 4 * i + (lane & 3)];
+            F2 s, z;
+            s.u[0] = p.x, s.u[1] = p.y, z.u[0] = p.z, z.u[1] = p.w;
 #pragma unroll
-          for (int k = 0; k < 64; ++k) {
-            F2 y;
-            y.v = x[k];
-            if (2 * k < c_lo || 2 * k >= c_hi) y.f[0] = -INFINITY;
-            if (2 * k + 1 < c_lo || 2 * k + 1 >= c_hi) y.f[1] = -INFINITY;
-            x[k] = y.v;
+            for (int e = 0; e < 4; ++e) {
+              uint64_t &y = x[4 * (e >> 1) + 2 * i + (e & 1)];
+              y = fma2(s.v, y, mul2(z.v, two(fsum[e], fsum[e])));
+              if (!decltype(all)::value) {
+                const int tok = tok0 + 16 * k + 8 * i + 2 * (lane & 3);
+                F2 v;
+                v.v = y;
+                if (tok < flo[e] || tok >= fhi[e]) v.f[0] = -INFINITY;
+                if (tok + 1 < flo[e] || tok + 1 >= fhi[e]) v.f[1] = -INFINITY;
+                y = v.v;
+              }
+            }
           }
-        }
+        };
+        auto larger = [&](const uint64_t *x) {
 #pragma unroll
-        for (int k = 0; k < 64; ++k) {
-          F2 y;
-          y.v = x[k];
-          top[k & 3] = fmaxf(top[k & 3], fmaxf(y.f[0], y.f[1]));
-        }
-        const float mt = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * unit;
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              F2 y;
+              y.v = x[4 * (e >> 1) + 2 * i + (e & 1)];
+              asm("max.f32 %0, %0, %1, %2;" : "+f"(top[e]) : "f"(y.f[0]), "f"(y.f[1]));
+            }
+        };
+        auto join_top = [&]() {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], 1));
+            top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], 2)) * funit[e];
+          }
+        };
         const int E = reinterpret_cast<const int *>(smem + L::kExp)[buf];
-        if (j == 0) {
-          m = mt;
-          run = E;
-        } else if (__any_sync(0xffffffffu, mt > m + kSlack || (m == -INFINITY && mt > m)) || E > run) {
-          // ---- the sums to a new maximum or exponent: the product before has to be done
-          ok = bar_wait(o_full(t), (n_o - 1) & 1);
-          if (!ok) break;
+        // the sums so far to the maxima in top, where larger, and to exponent en: the product before has to be done
+        auto rescale = [&](int en) {
+          if (j > 0 && !bar_wait(o_full(t), (n_o - 1) & 1)) failed = true;
           tc_after();
-          const float mn = fmaxf(m, mt);
-          const int en = max(run, E);
-          const float down = mn == -INFINITY ? 1.0f : ex2(m - mn), f = down * ex2(static_cast<float>(run - en));
+          const float f_run = ex2(static_cast<float>(run - en));
+          float f[4];
 #pragma unroll
-          for (int k = 0; k < D; k += 16) {
-            uint32_t o[16];
-            tm_load16(o_at + k, o);
-            tm_wait_load();
-#pragma unroll
-            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-            tm_store16(o_at + k, o);
+          for (int e = 0; e < 4; ++e) {
+            const float mn = fmaxf(fm[e], top[e]), down = mn == -INFINITY ? 1.0f : ex2(fm[e] - mn);
+            f[e] = down * f_run;
+            fl[e] *= down;
+            fm[e] = mn;
           }
-          l *= down;
-          m = mn;
           run = en;
-        }
-        const float lag = static_cast<float>(max(E - run, -60));  // this step's values lie so many powers of two lower
-        const float ref = lag - (m == -INFINITY ? 0.0f : m);
-        const uint64_t ref2 = two(ref, ref);
-        uint64_t total[2] = {0, 0};
+#pragma unroll 1
+          for (int k = 0; k < 2 * D; k += 32) {
+            uint32_t o[16];
+            const int h = k >= D;
+            const uint32_t at = o_at + (h ? (16u << 16) + k - D : k);
+            tm_load_frag(at, o);
+            tm_wait16(o);
+            const float g0 = h ? f[2] : f[0], g1 = h ? f[3] : f[1];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          uint32_t p[32];
-#pragma unroll
-          for (int e = 0; e < 32; ++e) {
-            F2 y;
-            y.v = fma2(x[32 * k + e], unit2, ref2);
-            y.f[0] = ex2(y.f[0]);
-            y.f[1] = ex2(y.f[1]);
-            total[e & 1] = add2(total[e & 1], y.v);
-            p[e] = pack_half(y.f[0], y.f[1]);
+            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * (e >> 1 & 1 ? g1 : g0));
+            tm_store_frag(at, o);
           }
-          tm_store32(s_at + 32 * k, p);
-        }
-        F2 sums;
-        sums.v = add2(total[0], total[1]);
-        l = fmaf(sums.f[0] + sums.f[1], ex2(-lag), l);
-        // a value held as NaN is left out of the product, and makes a row that sees it NaN here
+        };
+        if (ok && j == 0) {
+          // the first step finds its maxima before its weights
+#pragma unroll 1
+          for (int k = 0; k < 8; ++k) {
+            uint64_t x[8];
+            load(x, k);
+            landed(x);
+            scores(No{}, x, k);
+            larger(x);
+          }
+          join_top();
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          uint32_t bad = reinterpret_cast<const uint32_t *>(smem + L::kNan)[4 * buf + k];
-          while (bad) {
-            const int col = 32 * k + __ffs(bad) - 1;
-            bad &= bad - 1;
-            if (col >= c_lo && col < c_hi) l = NAN;
+          for (int e = 0; e < 4; ++e) fm[e] = top[e];
+          run = E;
+        } else if (ok && (pending || E > run)) {
+          rescale(max(run, E));
+        }
+        // Weights against the maxima so far, in the place of the scores that have been read.  A weight may be up to
+        // 2^15 then; a row that has grown past that, and with it the whole tile, has its scores computed again.
+        const float lag = static_cast<float>(max(E - run, -60));  // this step's values lie so many powers of two lower
+        uint64_t total[4];
+        auto weigh = [&](auto all) {
+          float ref[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            ref[e] = lag - (fm[e] == -INFINITY ? 0.0f : fm[e]);
+            total[e] = 0;
+            top[e] = -INFINITY;
+          }
+          // a loop of one quarter: the warps of all kinds together have to fit the instruction cache
+#pragma unroll 1
+          for (int k = 0; k < 8; ++k) {
+            uint64_t z[8];
+            load(z, k);
+            landed(z);
+            scores(all, z, k);
+            larger(z);
+            uint32_t p[8];
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int at = 4 * (e >> 1) + 2 * i + (e & 1);
+                F2 v;
+                v.v = fma2(z[at], two(funit[e], funit[e]), two(ref[e], ref[e]));
+                v.f[0] = ex2(v.f[0]);
+                v.f[1] = ex2(v.f[1]);
+                total[e] = add2(total[e], v.v);
+                p[at] = pack_half(v.f[0], v.f[1]);
+              }
+            tm_store_halves(s_at + 8 * k, p);
+            tm_store_halves(s_at + (16u << 16) + 8 * k, p + 4);
+          }
+          join_top();
+        };
+        if (ok) {
+          if (every)
+            weigh(Yes{});
+          else
+            weigh(No{});
+        }
+        bool again = false;
+        pending = false;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          again |= top[e] > fm[e] + kMost || (fm[e] == -INFINITY && top[e] > fm[e]);
+          pending |= top[e] > fm[e] + kSlack;
+        }
+        pending = __any_sync(0xffffffffu, pending);
+        if (!ok || failed) *reinterpret_cast<volatile int *>(smem + L::kFail) = 1;
+        if (tile_any(1 + t, again || !ok || failed)) {  // every warp of the tile comes here once for every wait on s_full
+          ok = !*reinterpret_cast<volatile int *>(smem + L::kFail);
+          if (!ok) break;
+          rescale(run);
+          if (lane == 0 && (warp & 3) == 0) reinterpret_cast<volatile int *>(smem + L::kAgain)[t] = 1;
+          pending = false;
+          tc_before();
+          __syncwarp();
+          if (lane == 0) bar_arrive(p_full(t));
+          --j, --c;  // the same step
+          continue;
+        }
+        const float up = ex2(-lag);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          F2 y;
+          y.v = total[e];
+          fl[e] = fmaf(y.f[0] + y.f[1], up, fl[e]);
+        }
+        // a value held as NaN is left out of the product, and makes a row that sees it NaN here
+        const uint4 nans = reinterpret_cast<const uint4 *>(smem + L::kNan)[buf];
+        if (nans.x | nans.y | nans.z | nans.w) {
+#pragma unroll 1
+          for (int col = 0; col < kTok; ++col) {
+            const uint32_t word = col < 32 ? nans.x : col < 64 ? nans.y : col < 96 ? nans.z : nans.w;
+            if (!(word >> (col & 31) & 1u)) continue;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (tok0 + col >= flo[e] && tok0 + col < fhi[e]) fl[e] = NAN;
           }
         }
         tm_wait_store();
@@ -466,123 +622,294 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
       }
       if (!ok) break;
 
-      // ---- the item's rows, or this block's part of them
-      const bool whole = w.tile == 0 && w.end() == w.tiles;
-      const uint32_t id = w.u - w.tile;
+      // ---- the item's rows, or this block's part of them; a row a thread again
+      const int64_t i = w.q0 + (there ? R / group : 0);
+      const int hq = w.h * group + (there ? R % group : 0);
+      float m = -INFINITY, l = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        fl[e] += __shfl_xor_sync(0xffffffffu, fl[e], 1);
+        fl[e] += __shfl_xor_sync(0xffffffffu, fl[e], 2);
+        const float x = __shfl_sync(0xffffffffu, fm[e], (lane & 7) * 4), y = __shfl_sync(0xffffffffu, fl[e], (lane & 7) * 4);
+        if (lane >> 3 == e) m = x, l = y;
+      }
+      const bool whole = w.whole;
+      const uint32_t id = w.id;
       if (steps > 0) {
         ok = bar_wait(o_full(t), (n_o - 1) & 1);
         if (!ok) break;
         tc_after();
       }
-      if (whole) {
-        const float f = l == 0.0f ? 0.0f : ex2(static_cast<float>(run)) / l;
-        T *dst = static_cast<T *>(a.out) + i * a.o_row + hq * a.o_head;
+      const float f = whole ? (l == 0.0f ? 0.0f : ex2(static_cast<float>(run)) / l) : run == kNoExp ? 0.0f : ex2(static_cast<float>(run));
+      T *dst = static_cast<T *>(a.out) + i * a.o_row + hq * a.o_head;
+      const int at = t * 128 + row;
+      float *part = a.many_parts + (static_cast<int64_t>(me) * 2 + (id < u0 ? 0 : 1)) * L::kPart;
+#pragma unroll 1
+      for (int k = 0; k < D; k += 16) {
+        uint32_t o[16];
+        if (steps > 0) {
+          tm_load16(o_at + k, o);
+          tm_wait16(o);
+        } else {
 #pragma unroll
-        for (int k = 0; k < D; k += 32) {
-          uint32_t o[32];
-          if (steps > 0) {
-            tm_load32(o_at + k, o);
-            tm_wait_load();
+          for (int e = 0; e < 16; ++e) o[e] = 0;
+        }
+        float v[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e] = f == 0.0f ? 0.0f : __uint_as_float(o[e]) * f;
+        if (!whole) {
+#pragma unroll
+          for (int e = 0; e < 16; e += 4) *reinterpret_cast<float4 *>(part + at * D + k + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+        } else if (there) {
+          T y[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) y[e] = Cvt<T>::from(v[e]);
+          if (a.wide) {
+#pragma unroll
+            for (int e = 0; e < 16; e += 8) *reinterpret_cast<uint4 *>(dst + k + e) = *reinterpret_cast<const uint4 *>(y + e);
           } else {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = 0;
-          }
-          T y[32];
-#pragma unroll
-          for (int e = 0; e < 32; ++e) y[e] = Cvt<T>::from(l == 0.0f ? 0.0f : __uint_as_float(o[e]) * f);
-          if (there) {
-            if (a.wide) {
-#pragma unroll
-              for (int e = 0; e < 32; e += 8) *reinterpret_cast<uint4 *>(dst + k + e) = *reinterpret_cast<const uint4 *>(y + e);
-            } else {
-#pragma unroll
-              for (int e = 0; e < 32; ++e) dst[k + e] = y[e];
-            }
+            for (int e = 0; e < 16; ++e) dst[k + e] = y[e];
           }
         }
-        if (there && a.lse) a.lse[i * a.Hq + hq] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
-      } else {
-        float *part = a.many_parts + (static_cast<int64_t>(me) * 2 + (id < u0 ? 0 : 1)) * L::kPart;
-        const int at = t * 128 + row;
-        const float f = run == kNoExp ? 0.0f : ex2(static_cast<float>(run));
-#pragma unroll
-        for (int k = 0; k < D; k += 32) {
-          uint32_t o[32];
-          if (steps > 0) {
-            tm_load32(o_at + k, o);
-            tm_wait_load();
-          }
-#pragma unroll
-          for (int e = 0; e < 32; e += 4) {
-            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            if (steps > 0) v = make_float4(__uint_as_float(o[e]) * f, __uint_as_float(o[e + 1]) * f, __uint_as_float(o[e + 2]) * f, __uint_as_float(o[e + 3]) * f);
-            *reinterpret_cast<float4 *>(part + at * D + k + e) = v;
-          }
-        }
+      }
+      if (!whole) {
         part[kRows * D + at] = m;
         part[kRows * D + kRows + at] = l;
-        if (tid == 0 && id >= u0) a.many_open[me] = {w.r.q0, id, static_cast<uint32_t>(w.tiles), rows, w.h, w.rt};
+        if (tid == 0 && id >= u0) a.many_open[me] = {w.q0, id, w.tiles, w.rows, w.h, w.rt};
+      } else if (there && a.lse) {
+        a.lse[i * a.Hq + hq] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
       }
       tc_before();  // the sums have been read, before the next item's first product
+      __syncwarp();
+      if (lane == 0) bar_arrive(seg_free(n_seg % kSegs));
+      ++n_seg;
     }
     if (!ok && lane == 0) flag_error(a.status, MAPS_E_TIMEOUT);
   } else if (warp < 12) {
-    // ======================================================================== codes to operands
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOperandRegs));
+    // ======================================================================== values
     const int w4 = warp - 8;
     uint32_t c = 0;
     bool ok = true;
-    for (Walk w(a, s_start, u0, u1); w.more() && ok; w.next(a)) {
-      const int steps = w.steps();
+    while (hear(ok)) {
+      const int steps = told().steps, tok_at = told().token, hi = told().hi;
       for (int j = 0; j < steps; ++j, ++c) {
-        const int buf = c & 1;
-        ok = bar_wait(kv_free(buf), (c >> 1 & 1) ^ 1);
-        for (int g = 0; g < kStepGroups && ok; ++g) {
-          const uint32_t s = c * kStepGroups + g;
-          ok = bar_wait(ring_full(s % kRing), s / kRing & 1);
-        }
+        ok = bar_wait(step_full(place), round);
         if (!ok) break;
-        const int32_t tok0 = w.lo + (w.first_step() + j) * kTok;
-        auto record = [&](int g) -> const uint8_t * { return smem + L::kRingAt + ((c * kStepGroups + g) % kRing) * kv4_group_bytes(D); };
-        // ---- the step's largest value, and the values held as NaN: every warp finds them, 4 tokens a lane
+        const int32_t tok0 = tok_at + j * kTok;
+        auto record = [&](int g) -> const uint8_t * { return smem + L::kRingAt + place * L::kStep + g * kv4_group_bytes(D); };
+        // ---- the step's largest value, from 4 tokens a lane; every warp finds it
         const uint4 v4 = *reinterpret_cast<const uint4 *>(record(lane >> 2) + 16 * D + 64 + (lane & 3) * 16);
         const uint32_t vp[4] = {v4.x, v4.y, v4.z, v4.w};
         float big = 0.0f;
-        uint32_t bad = 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float2 p = kv4_param(vp[e]);
-          if (tok0 + 4 * lane + e >= w.hi) continue;
-          if (p.x != p.x || p.y != p.y)
-            bad |= 1u << e;
-          else
-            big = fmaxf(big, fmaxf(fabsf(p.y), fabsf(fmaf(15.0f, p.x, p.y))));
+          if (tok0 + 4 * lane + e >= hi) continue;
+          if (p.x == p.x && p.y == p.y) big = fmaxf(big, fmaxf(fabsf(p.y), fabsf(fmaf(15.0f, p.x, p.y))));
         }
-        bad <<= (lane & 7) * 4;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
-#pragma unroll
-        for (int o = 4; o > 0; o >>= 1) bad |= __shfl_xor_sync(0xffffffffu, bad, o);
         // v 2^-E is below 2^15
         const int E = big == 0.0f ? kNoExp : max(static_cast<int>(__float_as_uint(big) >> 23) - 141, -112);
         const float down = big == 0.0f ? 0.0f : __uint_as_float(static_cast<uint32_t>(127 - E) << 23);
-        if (w4 == 0) {
-          if ((lane & 7) == 0) reinterpret_cast<uint32_t *>(smem + L::kNan)[4 * buf + (lane >> 3)] = bad;
-          if (lane == 0) reinterpret_cast<int *>(smem + L::kExp)[buf] = E;
+        // scales and zeros of the lane's tokens, two side by side; those left out are zero
+        uint32_t vs[2], vz[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float2 p0 = kv4_param(vp[2 * e]), p1 = kv4_param(vp[2 * e + 1]);
+          const int32_t tok = tok0 + 4 * lane + 2 * e;
+          if (tok >= hi || p0.x != p0.x || p0.y != p0.y) p0 = make_float2(0.0f, 0.0f);
+          if (tok + 1 >= hi || p1.x != p1.x || p1.y != p1.y) p1 = make_float2(0.0f, 0.0f);
+          vs[e] = pack_half(p0.x * down, p1.x * down);
+          vz[e] = pack_half(p0.y * down, p1.y * down);
         }
-        // ---- keys' scales and zeros, two tokens side by side
-        {
-          const int g = w4 + 4 * (lane >> 4), tau = lane & 15, at = g * kGroup + tau;
-          float2 p = kv4_param(*reinterpret_cast<const uint32_t *>(record(g) + 16 * D + 4 * tau));
-          if (tok0 + at >= w.hi) p = make_float2(0.0f, 0.0f);
-          float *dst = reinterpret_cast<float *>(smem + L::kPar + buf * kTok * 8) + (at >> 1) * 4 + (at & 1);
-          dst[0] = p.x * (k_sign * kEven);
-          dst[2] = p.y * k_sign;
-        }
-        uint8_t *K = smem + L::kK + buf * L::kTile, *V = smem + L::kV + buf * L::kTile;
+        ok = bar_wait(v_free, (c & 1) ^ 1);
+        if (!ok) break;
+        uint8_t *V = smem + L::kV;
 #pragma unroll 1
         for (int g = w4; g < kStepGroups; g += 4) {
           const uint8_t *rec = record(g);
+          // ---- values: a lane has 4 channels of 8 tokens, which are 16 bytes of each channel's row
+#pragma unroll 1
+          for (int hh = 0; hh < (D == 128 ? 2 : 1); ++hh) {
+            const int h = D == 128 ? hh : lane >> 4;
+            const int cg = D == 128 ? lane >> 2 : (lane >> 1) & 7, b = D == 128 ? lane & 3 : lane & 1;
+            const int f = D == 128 ? (cg >> 1) & 3 : ((cg >> 2) + 2 * h) & 3;  // the order of the four loads, for their banks
+            uint32_t v[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) v[t] = *reinterpret_cast<const uint32_t *>(rec + 8 * D + (((h * 8 + cg) * 4 + (t ^ f)) * (D / 32) + b) * 4);
+            if (f & 1) {
+              uint32_t y = v[0];
+              v[0] = v[1], v[1] = y;
+              y = v[2], v[2] = v[3], v[3] = y;
+            }
+            if (f & 2) {
+              uint32_t y = v[0];
+              v[0] = v[2], v[2] = y;
+              y = v[1], v[1] = v[3], v[3] = y;
+            }
+            const int turn = D == 128 ? b >> 1 | (cg & 1) << 1 : cg & 3;  // the order of the lane's channels, so that eight lanes write to eight different banks
+            uint4 out[4];
+            const __half2 off = __float2half2_rn(1024.0f);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+              const uint32_t su = __shfl_sync(0xffffffffu, vs[t & 1], 4 * g + 2 * h + (t >> 1)), zu = __shfl_sync(0xffffffffu, vz[t & 1], 4 * g + 2 * h + (t >> 1));
+              const __half2 s = *reinterpret_cast<const __half2 *>(&su), z = *reinterpret_cast<const __half2 *>(&zu);
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                const uint32_t code = ((v[t] >> (4 * (r ^ turn))) & 0x000f000fu) | 0x64006400u;  // 1024 + code
+                const __half2 y = __hfma2(__hsub2(*reinterpret_cast<const __half2 *>(&code), off), s, z);
+                reinterpret_cast<uint32_t *>(&out[r])[t] = *reinterpret_cast<const uint32_t *>(&y);
+              }
+            }
+            const int t8 = 2 * g + h;  // 8 tokens of the step's 128
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int ch = cg * (D / 8) + 4 * b + (r ^ turn);
+              *reinterpret_cast<uint4 *>(V + t8 / 8 * (D * 128) + ch * 128 + ((t8 % 8 ^ (ch & 7)) << 4)) = out[r];
+            }
+          }
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) bar_arrive(step_free(place)), bar_arrive(v_full);
+        ring_on();
+      }
+      if (!ok) break;
+      __syncwarp();
+      if (lane == 0) bar_arrive(seg_free(n_seg % kSegs));
+      ++n_seg;
+    }
+    if (!ok && lane == 0) flag_error(a.status, MAPS_E_TIMEOUT);
+  } else {
+    if (warp == 12 && lane == 0) {
+      // ====================================================================== products
+      constexpr uint32_t kQK = idesc_of(kTok), kPV = idesc_of(D);
+      uint32_t c = 0, n_q[2] = {0, 0}, n_p[2] = {0, 0};
+      bool ok = true;
+      // Tensor memory is taken whole, so it starts at 0; with the tile and the buffer constants too, nothing of an
+      // instruction has to be brought to uniform registers while the tensor cores wait for it.
+      auto scores_of = [&](auto tile, auto buffer) {
+        constexpr int t = decltype(tile)::value, buf = decltype(buffer)::value;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          constexpr int kStep = 32 / 16, kBlock = 16384 / 16;  // of a descriptor's address
+          const uint32_t off = k / 4 * kBlock + k % 4 * kStep;
+          mma_ss(t * 128, rows_desc(base + L::kQ + t * L::kTile) + off, rows_desc(base + L::kK + buf * L::kTile) + off, kQK, k > 0);
+        }
+        tc_commit(s_full(t));
+        bar_arrive(s_full(t));  // passes on what this thread has seen of the step: the keys' scales and zeros
+      };
+      auto scores = [&](int t, int buf) {
+        if (t == 0)
+          buf ? scores_of(Zero{}, One{}) : scores_of(Zero{}, Zero{});
+        else
+          buf ? scores_of(One{}, One{}) : scores_of(One{}, Zero{});
+      };
+      auto sums_of = [&](auto tile, bool more) {
+        constexpr int t = decltype(tile)::value;
+#pragma unroll
+        for (int k = 0; k < kTok / 16; ++k)
+          mma_ts(256 + t * 128, t * 128 + 8 * k, rows_desc(base + L::kV) + (k / 4 * (D * 8) + k % 4 * 2), kPV, more || k > 0);
+        tc_commit(o_full(t));
+      };
+      auto sums = [&](int t, bool more) { t == 0 ? sums_of(Zero{}, more) : sums_of(One{}, more); };
+      while (hear(ok)) {
+        const int steps = told().steps, tiles = told().second ? 2 : 1;
+        done();
+        if (steps == 0) continue;
+        for (int t = 0; t < tiles && ok; ++t) ok = bar_wait(q_full(t), n_q[t]++ & 1);
+        ok = ok && bar_wait(k_full(c & 1), c >> 1 & 1);
+        if (!ok) break;
+        tc_after();
+        for (int t = 0; t < tiles; ++t) scores(t, c & 1);
+        for (int j = 0; j < steps && ok; ++j, ++c) {
+          const int buf = c & 1;
+          for (int t = 0; t < tiles; ++t) {
+            for (;;) {
+              ok = bar_wait(p_full(t), n_p[t]++ & 1);
+              if (!ok) break;
+              tc_after();
+              volatile int *again = reinterpret_cast<volatile int *>(smem + L::kAgain) + t;
+              if (!*again) break;
+              *again = 0;
+              scores(t, buf);
+            }
+            if (!ok) break;
+            if (t == tiles - 1) tc_commit(k_free(buf));  // nobody wants these scores again
+            ok = t > 0 || bar_wait(v_full, c & 1);
+            if (!ok) break;
+            tc_after();
+            sums(t, j > 0);
+            if (t == tiles - 1) tc_commit(v_free);
+            if (j + 1 < steps) {
+              if (t == 0) {
+                ok = bar_wait(k_full(buf ^ 1), (c + 1) >> 1 & 1);
+                if (!ok) break;
+                tc_after();
+              }
+              scores(t, buf ^ 1);
+            }
+          }
+        }
+      }
+      if (!ok) flag_error(a.status, MAPS_E_TIMEOUT);
+    } else if (warp == 13) {
+      // ====================================================================== loads: a group a lane
+      bool ok = true;
+      while (hear(ok)) {
+        const int steps = told().steps, tok_at = told().token, hi = told().hi, head_groups = told().h * a.block_groups;
+        const int32_t *table = a.table + told().b * a.max_blocks;
+        __syncwarp();
+        if (lane == 0) bar_arrive(seg_free(n_seg % kSegs));
+        ++n_seg;
+        for (int j = 0; j < steps && ok; ++j) {
+          if (lane < kStepGroups) {
+            const int32_t tok = tok_at + j * kTok + lane * kGroup;
+            bool load = tok < hi;
+            int64_t at = 0;
+            if (load) {
+              const int32_t grp = tok / kGroup, page = a.block_shift >= 0 ? grp >> a.block_shift : grp / a.block_groups;
+              const int32_t block = table[page];
+              if (block < 0 || block >= a.n_blocks) {
+                flag_error(a.status, MAPS_E_RANGE);
+                load = false;
+              }
+              at = block * a.block_bytes + (head_groups + grp - page * a.block_groups) * static_cast<int64_t>(kv4_group_bytes(D));
+            }
+            ok = bar_wait(step_free(place), round ^ 1u);
+            if (ok) {
+              bar_expect(step_full(place), load ? kv4_group_bytes(D) : 0);
+              if (load) bulk_load(base + L::kRingAt + place * L::kStep + lane * kv4_group_bytes(D), a.cache + at, kv4_group_bytes(D), step_full(place));
+            }
+          }
+          ok = __all_sync(0xffffffffu, ok);
+          ring_on();
+        }
+        if (!ok) break;
+      }
+      if (!ok) {
+        if (lane == 0) flag_error(a.status, MAPS_E_TIMEOUT);
+        // let what is under way land: a step's barrier is over once all of it has
+        for (int i = 0; i < kRing; ++i) (void)bar_wait(step_full(i), 0), (void)bar_wait(step_full(i), 1);
+      }
+    } else if (warp == 15) {
+      // ====================================================================== keys
+      uint32_t c = 0;
+      bool ok = true;
+      while (hear(ok)) {
+        const int steps = told().steps, tok_at = told().token, hi = told().hi;
+        for (int j = 0; j < steps; ++j, ++c) {
+          const int buf = c & 1;
+          ok = bar_wait(step_full(place), round) && bar_wait(k_free(buf), (c >> 1 & 1) ^ 1);
+          if (!ok) break;
+          const int32_t tok0 = tok_at + j * kTok;
+          auto record = [&](int g) -> const uint8_t * { return smem + L::kRingAt + place * L::kStep + g * kv4_group_bytes(D); };
+          uint8_t *K = smem + L::kK + buf * L::kTile;
+#pragma unroll 1
+          for (int g = 0; g < kStepGroups; ++g) {
+            const uint8_t *rec = record(g);
           // ---- keys: a token's row, 8 channels to 16 bytes
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
@@ -602,141 +929,100 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
               *reinterpret_cast<uint4 *>(K + chunk / 8 * 16384 + row * 128 + ((chunk % 8 ^ (row & 7)) << 4)) = make_uint4(z.x[0], z.x[1], z.x[2], z.x[3]);
             }
           }
-          // ---- values: a lane has 4 channels of 8 tokens, which are 16 bytes of each channel's row
+          }
+        // ---- the step's largest value, and the values held as NaN, from 4 tokens a lane
+        const uint4 v4 = *reinterpret_cast<const uint4 *>(record(lane >> 2) + 16 * D + 64 + (lane & 3) * 16);
+        const uint32_t vp[4] = {v4.x, v4.y, v4.z, v4.w};
+        float big = 0.0f;
+        uint32_t bad = 0;
 #pragma unroll
-          for (int hh = 0; hh < (D == 128 ? 2 : 1); ++hh) {
-            const int h = D == 128 ? hh : lane >> 4;
-            const int cg = D == 128 ? lane >> 2 : (lane >> 1) & 7, b = D == 128 ? lane & 3 : lane & 1;
-            const int f = D == 128 ? (cg >> 1) & 3 : ((cg >> 2) + 2 * h) & 3;  // the order of the four loads, for their banks
-            uint32_t v[4];
+        for (int e = 0; e < 4; ++e) {
+          const float2 p = kv4_param(vp[e]);
+          if (tok0 + 4 * lane + e >= hi) continue;
+          if (p.x != p.x || p.y != p.y)
+            bad |= 1u << e;
+          else
+            big = fmaxf(big, fmaxf(fabsf(p.y), fabsf(fmaf(15.0f, p.x, p.y))));
+        }
+        bad <<= (lane & 7) * 4;
 #pragma unroll
-            for (int t = 0; t < 4; ++t) v[t] = *reinterpret_cast<const uint32_t *>(rec + 8 * D + (((h * 8 + cg) * 4 + (t ^ f)) * (D / 32) + b) * 4);
-            if (f & 1) {
-              uint32_t y = v[0];
-              v[0] = v[1], v[1] = y;
-              y = v[2], v[2] = v[3], v[3] = y;
-            }
-            if (f & 2) {
-              uint32_t y = v[0];
-              v[0] = v[2], v[2] = y;
-              y = v[1], v[1] = v[3], v[3] = y;
-            }
-            const uint32_t *par = reinterpret_cast<const uint32_t *>(rec + 16 * D + 64) + 8 * h;
-            uint4 out[4];
-            const __half2 off = __float2half2_rn(1024.0f);
+        for (int o = 16; o > 0; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-              float2 p0 = kv4_param(par[2 * t]), p1 = kv4_param(par[2 * t + 1]);
-              const int32_t tok = tok0 + g * kGroup + 8 * h + 2 * t;
-              if (tok >= w.hi || p0.x != p0.x || p0.y != p0.y) p0 = make_float2(0.0f, 0.0f);
-              if (tok + 1 >= w.hi || p1.x != p1.x || p1.y != p1.y) p1 = make_float2(0.0f, 0.0f);
-              const __half2 s = __floats2half2_rn(p0.x * down, p1.x * down), z = __floats2half2_rn(p0.y * down, p1.y * down);
+        for (int o = 4; o > 0; o >>= 1) bad |= __shfl_xor_sync(0xffffffffu, bad, o);
+        // v 2^-E is below 2^15
+        const int E = big == 0.0f ? kNoExp : max(static_cast<int>(__float_as_uint(big) >> 23) - 141, -112);
+        if ((lane & 7) == 0) reinterpret_cast<uint32_t *>(smem + L::kNan)[4 * (c & 3) + (lane >> 3)] = bad;
+        if (lane == 0) reinterpret_cast<int *>(smem + L::kExp)[c & 3] = E;
+        // ---- keys' scales and zeros, two tokens side by side
+        {
+          const uint4 k4 = *reinterpret_cast<const uint4 *>(record(lane >> 2) + 16 * D + (lane & 3) * 16);
+          const uint32_t kp[4] = {k4.x, k4.y, k4.z, k4.w};
 #pragma unroll
-              for (int r = 0; r < 4; ++r) {
-                const uint32_t code = ((v[t] >> (4 * r)) & 0x000f000fu) | 0x64006400u;  // 1024 + code
-                const __half2 y = __hfma2(__hsub2(*reinterpret_cast<const __half2 *>(&code), off), s, z);
-                reinterpret_cast<uint32_t *>(&out[r])[t] = *reinterpret_cast<const uint32_t *>(&y);
-              }
-            }
-            const int t8 = 2 * g + h;  // 8 tokens of the step's 128
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const int ch = cg * (D / 8) + 4 * b + r;
-              *reinterpret_cast<uint4 *>(V + t8 / 8 * (D * 128) + ch * 128 + ((t8 % 8 ^ (ch & 7)) << 4)) = out[r];
-            }
+          for (int e = 0; e < 4; e += 2) {
+            float2 p0 = kv4_param(kp[e]), p1 = kv4_param(kp[e + 1]);
+            if (tok0 + 4 * lane + e >= hi) p0 = make_float2(0.0f, 0.0f);
+            if (tok0 + 4 * lane + e + 1 >= hi) p1 = make_float2(0.0f, 0.0f);
+            reinterpret_cast<float4 *>(smem + L::kPar + (c & 3) * kTok * 8)[2 * lane + e / 2] =
+                make_float4(p0.x * (k_sign * kEven), p1.x * (k_sign * kEven), p0.y * k_sign, p1.y * k_sign);
           }
         }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane < kStepGroups) bar_arrive(ring_free((c * kStepGroups + lane) % kRing));
-        if (lane == 0) bar_arrive(kv_full(buf));
-      }
-    }
-    if (!ok && lane == 0) flag_error(a.status, MAPS_E_TIMEOUT);
-  } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-    if (warp == 12 && lane == 0) {
-      // ====================================================================== products
-      constexpr uint32_t kQK = idesc_of(kTok), kPV = idesc_of(D);
-      uint32_t c = 0, n_q[2] = {0, 0}, n_p[2] = {0, 0};
-      bool ok = true;
-      auto scores = [&](int t, int buf) {
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-          const uint32_t off = k / 4 * 16384 + k % 4 * 32;
-          mma_ss(tmem + t * 128, rows_desc(base + L::kQ + t * L::kTile + off), rows_desc(base + L::kK + buf * L::kTile + off), kQK, k > 0);
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) bar_arrive(step_free(place)), bar_arrive(k_full(buf));
+          ring_on();
         }
-        tc_commit(s_full(t));
-      };
-      for (Walk w(a, s_start, u0, u1); w.more() && ok; w.next(a)) {
-        const int steps = w.steps(), tiles = w.second(a) ? 2 : 1;
-        if (steps == 0) continue;
-        for (int t = 0; t < tiles && ok; ++t) ok = bar_wait(q_full(t), n_q[t]++ & 1);
-        ok = ok && bar_wait(kv_full(c & 1), c >> 1 & 1);
         if (!ok) break;
-        tc_after();
-        for (int t = 0; t < tiles; ++t) scores(t, c & 1);
-        for (int j = 0; j < steps && ok; ++j, ++c) {
-          const int buf = c & 1;
-          for (int t = 0; t < tiles; ++t) {
-            ok = bar_wait(p_full(t), n_p[t]++ & 1);
-            if (!ok) break;
-            tc_after();
-#pragma unroll
-            for (int k = 0; k < kTok / 16; ++k)
-              mma_ts(tmem + 256 + t * 128, tmem + t * 128 + 8 * k, rows_desc(base + L::kV + buf * L::kTile + k / 4 * (D * 128) + k % 4 * 32), kPV, j > 0 || k > 0);
-            tc_commit(o_full(t));
-            if (t == tiles - 1) tc_commit(kv_free(buf));
-            if (j + 1 < steps) {
-              if (t == 0) {
-                ok = bar_wait(kv_full(buf ^ 1), (c + 1) >> 1 & 1);
-                if (!ok) break;
-                tc_after();
-              }
-              scores(t, buf ^ 1);
-            }
-          }
-        }
+        __syncwarp();
+        if (lane == 0) bar_arrive(seg_free(n_seg % kSegs));
+        ++n_seg;
       }
-      if (!ok) flag_error(a.status, MAPS_E_TIMEOUT);
-    } else if (warp == 13) {
-      // ====================================================================== loads: a group a lane
-      uint32_t c = 0;
+      if (!ok && lane == 0) flag_error(a.status, MAPS_E_TIMEOUT);
+    } else if (warp == 14 && lane == 0) {
+      // ====================================================================== the block's items
       bool ok = true;
-      for (Walk w(a, s_start, u0, u1); w.more() && ok; w.next(a)) {
-        const int steps = w.steps();
-        for (int j = 0; j < steps && ok; ++j, ++c) {
-          if (lane < kStepGroups) {
-            const uint32_t s = c * kStepGroups + lane;
-            const int32_t tok = w.lo + (w.first_step() + j) * kTok + lane * kGroup;
-            bool load = tok < w.hi;
-            int64_t at = 0;
-            if (load) {
-              const int32_t grp = tok / kGroup, page = a.block_shift >= 0 ? grp >> a.block_shift : grp / a.block_groups;
-              const int32_t block = a.table[w.b * a.max_blocks + page];
-              if (block < 0 || block >= a.n_blocks) {
-                flag_error(a.status, MAPS_E_RANGE);
-                load = false;
-              }
-              at = block * a.block_bytes + (w.h * a.block_groups + grp - page * a.block_groups) * static_cast<int64_t>(kv4_group_bytes(D));
-            }
-            ok = bar_wait(ring_free(s % kRing), (s / kRing & 1) ^ 1);
-            if (ok) {
-              bar_expect(ring_full(s % kRing), load ? kv4_group_bytes(D) : 0);
-              if (load) bulk_load(base + L::kRingAt + s % kRing * kv4_group_bytes(D), a.cache + at, kv4_group_bytes(D), ring_full(s % kRing));
+      auto tell = [&](const Seg &x) {
+        ok = bar_wait(seg_free(n_seg % kSegs), (n_seg / kSegs & 1) ^ 1);
+        if (!ok) return;
+        reinterpret_cast<Seg *>(smem + L::kSegAt)[n_seg % kSegs] = x;
+        bar_arrive(seg_full(n_seg++ % kSegs));
+      };
+      Seg x = {};
+      if (u0 < u1) {
+        MReq r = s_start.r;
+        int32_t lo, hi;
+        uint32_t all = 0, rest = s_start.rest;
+        for (int t = 0; t < r.row_tiles; ++t) all += span(a, r, t, lo, hi);
+        int b = s_start.b, h = static_cast<int>(rest / all), rt = 0, tiles;
+        rest -= static_cast<uint32_t>(h) * all;
+        while (rest >= static_cast<uint32_t>(tiles = span(a, r, rt, lo, hi))) rest -= tiles, ++rt;
+        int tile = static_cast<int>(rest);
+        for (uint32_t u = u0; ok;) {
+          const int end = static_cast<int>(min(static_cast<uint32_t>(tiles), tile + (u1 - u)));  // of the block's units of the item
+          x.q0 = r.q0, x.n = r.n, x.n_q = r.n_q, x.rows = r.n_q * group;
+          x.steps = max(end - max(tile, kItemUnits), 0);
+          x.token = lo + (max(tile, kItemUnits) - kItemUnits) * kTok, x.hi = hi;
+          x.b = b, x.h = h, x.rt = rt;
+          x.second = rt * kRows + 128 < x.rows;
+          x.whole = tile == 0 && end == tiles;
+          x.id = u - tile, x.tiles = tiles;
+          tell(x);
+          u += end - tile;
+          if (u >= u1) break;
+          tile = 0;
+          if (++rt == r.row_tiles) {
+            rt = 0;
+            if (++h == a.Hkv) {
+              h = 0;
+              do r = many_request(a, ++b);
+              while (r.row_tiles == 0);
             }
           }
-          ok = __all_sync(0xffffffffu, ok);
+          tiles = span(a, r, rt, lo, hi);
         }
       }
-      if (!ok) {
-        if (lane == 0) flag_error(a.status, MAPS_E_TIMEOUT);
-        // let what is under way land: each place of the ring was last filled in this step's round or the one before
-        for (int i = lane; i < kRing; i += 32) {
-          (void)bar_wait(ring_full(i), (c * kStepGroups + kStepGroups - 1) / kRing & 1);
-          (void)bar_wait(ring_full(i), ((c * kStepGroups + kStepGroups - 1) / kRing & 1) ^ 1);
-        }
-      }
+      x.steps = -1;
+      if (ok) tell(x);
+      if (!ok) flag_error(a.status, MAPS_E_TIMEOUT);
     }
     __syncwarp();
   }
@@ -795,11 +1081,6 @@ int launch(const AttnArgs &a, cudaStream_t s) {
   const unsigned grid = static_cast<unsigned>(attn_grid());
   const size_t smem = Lay<D>::kBytes + 1024;
   auto kernel = attn_many_kernel<T, D>;
-  // The register split below waits for ever where the block was launched with fewer than it adds up to.
-  static_assert((2 * kSoftmaxRegs + kOperandRegs + kOtherRegs) * 128 == kThreads * kLaunchRegs, "register split");
-  cudaFuncAttributes attr;
-  MAPS_TRY(cuda_ok(cudaFuncGetAttributes(&attr, kernel)));
-  if (attr.numRegs != kLaunchRegs) return cuda_ok(cudaErrorInvalidConfiguration);
   MAPS_TRY(cuda_ok(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem))));
   if (a.B > kMaxLocalB) launch_pdl(attn_many_plan_kernel, 1, 1024, 0, s, a, grid);
   launch_pdl(kernel, grid, kThreads, smem, s, a);
