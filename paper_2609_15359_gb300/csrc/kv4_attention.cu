@@ -42,19 +42,14 @@ __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uin
 }
 
 // ---------------------------------------------------------------------------- the work, in units
-#ifndef TW
-#define TW 12
-#define TG 3
-#define TS 2
-#endif
 template <int D, int NT>
 struct Shape {
   static constexpr int kRows = 8 * NT;                       // query rows of a tile
-  static constexpr int kWarps = NT == 1 && D <= 128 ? TW : 8, kThreads = 32 * kWarps;
-  static constexpr int kGroups = D == 256 ? 2 : NT == 1 ? TG : 4;  // groups of 16 tokens in a unit
+  static constexpr int kWarps = NT == 2 || D == 256 ? 8 : 12, kThreads = 32 * kWarps;
+  static constexpr int kGroups = D == 256 ? 2 : NT == 2 ? 4 : D == 64 ? 6 : 3;  // groups of 16 tokens in a unit
   static constexpr int kTok = kGroups * kGroup;
   static constexpr int kBytes = kGroups * kv4_group_bytes(D);  // of a stage
-  static constexpr int kStages = NT == 1 && D <= 128 ? (D == 64 ? 2 * TS : TS) : D == 64 ? 4 : 2;
+  static constexpr int kStages = D == 64 && NT == 2 ? 4 : 2;
   static constexpr int kPart = kRows * D + 2 * kRows;        // floats of a part: sums, maxima, totals
 };
 
@@ -184,6 +179,9 @@ __global__ void __launch_bounds__(1024) attn_plan_kernel(const AttnArgs a, uint3
   const uint32_t U = plan<kTok, kRows, 1024>(a, workers, 0, workers, [&](uint32_t w, const Start &c) { static_cast<Start *>(a.starts)[w] = c; });
   if (threadIdx.x == 0) *a.units = U;
 }
+
+template <int kN>
+struct Count { static constexpr int value = kN; };
 
 // Weights are held relative to the largest weight times value scale seen, so that what enters the
 // second product is at most 1; scales count as at least 2^-60 there, so that a weight itself stays finite.
@@ -615,29 +613,31 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(con
     }
     if (d == 0 && a.lse) a.lse[i * a.Hq + hq] = ll == 0.0f ? -INFINITY : (mm + log2f(ll)) * 0.6931471805599453f;
   };
-  // Sums n parts, each brought to their common maximum; a thread takes four channels at a time, four parts at a time.
-  auto join = [&](int thread, int threads, int n, auto part, auto load, auto load_one, auto put) {
+  // Sums n parts, each brought to their common maximum; a thread takes four channels at a time, and so many parts at a
+  // time that their loads hide one another.
+  auto join = [&](auto batch, int thread, int threads, int n, auto part, auto load, auto load_one, auto put) {
+    constexpr int kBatch = decltype(batch)::value;
     for (int x = 4 * thread; x < Sh::kRows * D; x += 4 * threads) {
       const int R = x / D, d = x - R * D;
       float4 num = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
       float M = -INFINITY, den = 0.0f;
-      for (int k = 0; k < n; k += 4) {
-        float4 v[4];
-        float mk[4], lk[4], top = M;
+      for (int k = 0; k < n; k += kBatch) {
+        float4 v[kBatch];
+        float mk[kBatch], lk[kBatch], top = M;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < kBatch; ++j) {
           const float *p = part(min(k + j, n - 1));  // beyond the last: read again, and left out
           v[j] = load(p + x);
           mk[j] = load_one(p + Sh::kRows * D + R);
           lk[j] = load_one(p + Sh::kRows * D + Sh::kRows + R);
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) top = fmaxf(top, mk[j]);
+        for (int j = 0; j < kBatch; ++j) top = fmaxf(top, mk[j]);
         const float c = top == -INFINITY ? 1.0f : ex2(M - top);
         num.x *= c, num.y *= c, num.z *= c, num.w *= c, den *= c;
         M = top;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < kBatch; ++j) {
           if (k + j >= n) break;
           const float f = top == -INFINITY ? 0.0f : ex2(mk[j] - top);
           num.x = fmaf(f, v[j].x, num.x), num.y = fmaf(f, v[j].y, num.y), num.z = fmaf(f, v[j].z, num.z), num.w = fmaf(f, v[j].w, num.w);
@@ -657,7 +657,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(con
     const float *head = item.id <= deal.start(w0 + first) ? first_parts + first * Sh::kPart : reinterpret_cast<const float *>(ring_all + first * Sh::kStages * Sh::kBytes);
     float *mine = a.parts + (static_cast<int64_t>(blockIdx.x) * 2 + (item.id < c0 ? 0 : 1)) * Sh::kPart;
     join(
-        lane + 32 * (warp - first), 32 * (last - first + 1), last - first + 1, [&](int k) { return k == 0 ? head : first_parts + (first + k) * Sh::kPart; },
+        Count<2>{}, lane + 32 * (warp - first), 32 * (last - first + 1), last - first + 1, [&](int k) { return k == 0 ? head : first_parts + (first + k) * Sh::kPart; },
         [](const float *p) { return *reinterpret_cast<const float4 *>(p); }, [](const float *p) { return *p; },
         [&](int R, int d, float4 num, float mm, float ll) {
           if (whole) {
@@ -691,7 +691,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(con
     const int f = s_block[k][0];
     __threadfence();
     join(
-        tid, kThreads, s_block[k][1], [&](int c) { return a.parts + (static_cast<int64_t>(f + c) * 2 + (c == 0)) * Sh::kPart; },
+        Count<8>{}, tid, kThreads, s_block[k][1], [&](int c) { return a.parts + (static_cast<int64_t>(f + c) * 2 + (c == 0)) * Sh::kPart; },
         [](const float *p) { return __ldcg(reinterpret_cast<const float4 *>(p)); }, [](const float *p) { return __ldcg(p); },
         [&](int R, int d, float4 num, float mm, float ll) { write_row(item, R, d, num, mm, ll); });
   }

@@ -275,6 +275,18 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
   auto seg_free = [&](int i) { return b0 + 112 + 8 * kSegs + 8 * i; };
 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  pdl_prologue();
+  uint32_t U;
+  const uint32_t me = blockIdx.x;
+  if (a.B <= kMaxLocalB) {
+    U = many_plan<kThreads>(a, gridDim.x, me, me + 1, [&](uint32_t, const ManyStart &s) { s_start = s; });
+    if (me == 0 && tid == 0) *a.many_units = U;  // for the kernel that joins
+  } else {
+    U = *a.many_units;
+    if (me < U && tid == 0) s_start = static_cast<const ManyStart *>(a.many_starts)[me];
+  }
+  if (tid == 0) a.many_open[me].tiles = 0;
+  if (U == 0) return;  // no request here has many queries
   if (tid == 0) {
     for (int i = 0; i < 3; ++i) reinterpret_cast<int *>(smem + L::kAgain)[i] = 0;
     for (int i = 0; i < kRing; ++i) bar_init(step_full(i), kStepGroups), bar_init(step_free(i), 5);
@@ -290,16 +302,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&s_tmem)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  pdl_prologue();
-  uint32_t U;
-  const uint32_t me = blockIdx.x;
-  if (a.B <= kMaxLocalB) {
-    U = many_plan<kThreads>(a, gridDim.x, me, me + 1, [&](uint32_t, const ManyStart &s) { s_start = s; });
-    if (me == 0 && tid == 0) *a.many_units = U;  // for the kernel that joins
-  } else {
-    U = *a.many_units;
-    if (me < U && tid == 0) s_start = static_cast<const ManyStart *>(a.many_starts)[me];
-  }
   tc_before();
   __syncthreads();
   tc_after();
@@ -308,7 +310,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
   const uint32_t tmem = s_tmem;  // 0
   const int group = a.Hq / a.Hkv;
   const float sl2 = a.scale * 1.4426950408889634f, k_sign = a.scale < 0.0f ? -1.0f : 1.0f;
-  if (tid == 0) a.many_open[me].tiles = 0;
 
   // the next item: waits for it, and says whether there is one; then what it is, and that this warp is done with it
   uint32_t n_seg = 0;
@@ -1035,10 +1036,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
 }
 
 // ---------------------------------------------------------------------------- the items that cross blocks
-constexpr int kJoinRows = 16;  // of a block
+constexpr int kJoinRows = 64;  // of a block
 
 template <class T, int D>
-__global__ void __launch_bounds__(256) attn_many_join_kernel(const AttnArgs a, uint32_t blocks) {
+__global__ void __launch_bounds__(512) attn_many_join_kernel(const AttnArgs a, uint32_t blocks) {
   pdl_prologue();
   constexpr int kPart = Lay<D>::kPart;
   const uint32_t f = blockIdx.x;
@@ -1047,7 +1048,7 @@ __global__ void __launch_bounds__(256) attn_many_join_kernel(const AttnArgs a, u
   const Deal deal(*a.many_units, blocks);
   const uint32_t e = deal.worker(item.id + item.tiles - 1);
   const int group = a.Hq / a.Hkv;
-  for (int x = 4 * threadIdx.x; x < kJoinRows * D; x += 4 * 256) {
+  for (int x = 4 * threadIdx.x; x < kJoinRows * D; x += 4 * 512) {
     const int at = blockIdx.y * kJoinRows + x / D, d = x % D, R = item.rt * kRows + at;
     if (R >= item.rows) continue;
     float M = -INFINITY, den = 0.0f;
@@ -1084,7 +1085,7 @@ int launch(const AttnArgs &a, cudaStream_t s) {
   MAPS_TRY(cuda_ok(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem))));
   if (a.B > kMaxLocalB) launch_pdl(attn_many_plan_kernel, 1, 1024, 0, s, a, grid);
   launch_pdl(kernel, grid, kThreads, smem, s, a);
-  launch_pdl(attn_many_join_kernel<T, D>, dim3(grid, kRows / kJoinRows), 256, 0, s, a, grid);
+  launch_pdl(attn_many_join_kernel<T, D>, dim3(grid, kRows / kJoinRows), 512, 0, s, a, grid);
   return launch_ok();
 }
 
