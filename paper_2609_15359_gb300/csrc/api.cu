@@ -1,5 +1,7 @@
 // api.cu -- library-wide entry points of the MAPS C ABI: version, last CUDA
 // error, and the sticky device status check.
+#include <atomic>
+
 #include "maps_internal.cuh"
 
 namespace maps {
@@ -9,9 +11,12 @@ static thread_local int g_last_cuda_error = 0;
 void set_last_cuda_error(cudaError_t e) { g_last_cuda_error = static_cast<int>(e); }
 
 int sm_count() {
+  static std::atomic<int> known[64];  // by device: asking costs as much as a launch's other host work
   int dev = 0, n = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return 1;
+  if (dev < 64 && (n = known[dev].load(std::memory_order_relaxed)) > 0) return n;
   if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 1;
+  if (dev < 64 && n > 0) known[dev].store(n, std::memory_order_relaxed);
   return n > 0 ? n : 1;
 }
 

@@ -707,8 +707,8 @@ int launch_few(const AttnArgs &a, cudaStream_t s) {
   using Sh = Shape<D, NT>;
   constexpr int kWarps = Sh::kWarps, kThreads = Sh::kThreads;
   const size_t smem = static_cast<size_t>(kWarps) * Sh::kStages * Sh::kBytes + static_cast<size_t>(kWarps) * Sh::kPart * 4 + kWarps * Sh::kStages * 8;
-  auto kernel = attn_few_kernel<T, D, NT>;
-  MAPS_TRY(cuda_ok(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem))));
+  constexpr auto kernel = attn_few_kernel<T, D, NT>;
+  MAPS_TRY(allow_smem<kernel>(smem));
   if (a.B > kMaxLocalB) launch_pdl(attn_plan_kernel<Sh::kTok, Sh::kRows>, 1, 1024, 0, s, a, static_cast<uint32_t>(attn_grid() * kWarps));
   launch_pdl(kernel, static_cast<unsigned>(attn_grid()), kThreads, smem, s, a);
   return launch_ok();

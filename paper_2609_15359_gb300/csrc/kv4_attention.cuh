@@ -2,11 +2,26 @@
 // how work is dealt out, and small device helpers.
 #pragma once
 
+#include <atomic>
+
 #include "kv4.cuh"
 
 namespace maps {
 
 constexpr int kMaxLocalB = 2048;  // requests over which a block deals out the units for itself
+// Lets a kernel have `bytes` of dynamic shared memory, once for each device.
+template <auto kKernel>
+int allow_smem(size_t bytes) {
+  static std::atomic<uint64_t> done;
+  int dev = 0;
+  MAPS_TRY(cuda_ok(cudaGetDevice(&dev)));
+  const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
+  if (done.load(std::memory_order_relaxed) & bit) return MAPS_OK;
+  MAPS_TRY(cuda_ok(cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes))));
+  done.fetch_or(bit, std::memory_order_relaxed);
+  return MAPS_OK;
+}
+
 constexpr int kMaxGrid = kCtrlBytes - 64;
 inline int attn_grid() { return sm_count() < kMaxGrid ? sm_count() : kMaxGrid; }
 

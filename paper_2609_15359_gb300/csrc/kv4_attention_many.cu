@@ -1081,8 +1081,8 @@ template <class T, int D>
 int launch(const AttnArgs &a, cudaStream_t s) {
   const unsigned grid = static_cast<unsigned>(attn_grid());
   const size_t smem = Lay<D>::kBytes + 1024;
-  auto kernel = attn_many_kernel<T, D>;
-  MAPS_TRY(cuda_ok(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem))));
+  constexpr auto kernel = attn_many_kernel<T, D>;
+  MAPS_TRY(allow_smem<kernel>(smem));
   if (a.B > kMaxLocalB) launch_pdl(attn_many_plan_kernel, 1, 1024, 0, s, a, grid);
   launch_pdl(kernel, grid, kThreads, smem, s, a);
   launch_pdl(attn_many_join_kernel<T, D>, dim3(grid, kRows / kJoinRows), 512, 0, s, a, grid);

@@ -143,7 +143,7 @@ def _ptr(t, dtype=None) -> int | None:
         return None
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError("expected a CUDA tensor")
-    if dtype is not None and t.dtype != dtype:
+    if dtype is not None and t.dtype is not dtype:
         raise TypeError(f"expected {dtype}, got {t.dtype}")
     if not t.is_contiguous():
         raise TypeError("expected a contiguous tensor")
@@ -155,20 +155,16 @@ class Workspace:
 
     def __init__(self, nbytes: int = 0, device=None):
         self.device = torch.device("cuda") if device is None else torch.device(device)
-        self.buf = torch.zeros(max(int(nbytes), 256), dtype=torch.uint8, device=self.device)
+        self._take(max(int(nbytes), 256))
+
+    def _take(self, nbytes: int) -> None:
+        self.buf = torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
+        self.ptr, self.nbytes = self.buf.data_ptr(), nbytes
 
     def ensure(self, nbytes: int) -> "Workspace":
-        if nbytes > self.buf.numel():
-            self.buf = torch.zeros(int(nbytes), dtype=torch.uint8, device=self.device)
+        if nbytes > self.nbytes:
+            self._take(int(nbytes))
         return self
-
-    @property
-    def ptr(self) -> int:
-        return self.buf.data_ptr()
-
-    @property
-    def nbytes(self) -> int:
-        return self.buf.numel()
 
 
 @functools.lru_cache(maxsize=4096)
