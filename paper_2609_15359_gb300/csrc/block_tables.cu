@@ -160,7 +160,53 @@ __device__ __forceinline__ void set_marks(int32_t *marks, int r, int64_t begin, 
 }
 __device__ __forceinline__ void end_marks(int32_t *marks, int R, int64_t total, int shift) { marks[(total + (int64_t(1) << shift) - 1) >> shift] = R - 1; }
 
-template <int kBlocks>
+// The request that element x belongs to: the last r with sums[r] <= x, for 0 <= x < sums[R].
+__device__ __forceinline__ int owner(const int64_t *sums, const int32_t *marks, int shift, int64_t x) {
+  int lo = marks[x >> shift], hi = marks[(x >> shift) + 1] + 1;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (sums[mid] <= x)
+      lo = mid;
+    else
+      hi = mid;
+  }
+  return lo;
+}
+
+// The block that entry k of the returned ones is: still in its old row, which nothing overwrites.
+__device__ __forceinline__ int32_t returned(const BTArgs &a, int64_t k, int shift) {
+  const int r = owner(a.back, a.coarse + kCoarse + 2, shift, k);
+  return a.table[static_cast<int64_t>(r) * a.max_blocks + need_of(a, r, false).wb + (k - a.back[r])];
+}
+
+// The returned blocks onto the stack, by `blocks` blocks of which this is number b.
+__device__ __forceinline__ void push(const BTArgs &a, const Totals &t, int b, int blocks) {
+  for (int64_t k = static_cast<int64_t>(b) * blockDim.x + threadIdx.x; k < t.returned; k += static_cast<int64_t>(blocks) * blockDim.x)
+    a.free_blocks[t.free + k] = returned(a, k, t.returned_shift);
+}
+
+// The slot of new token j, and its block into the table where it is the block's first.
+__device__ __forceinline__ void fill_token(const BTArgs &a, const Totals &t, int64_t j) {
+  if (j >= t.tokens) return;
+  const int r = owner(a.off, a.coarse, t.token_shift, j);
+  const Request q = a.requests[r];
+  const uint32_t p = static_cast<uint32_t>(q.held) + static_cast<uint32_t>(j - q.begin);
+  const uint32_t hb = block_of(a, static_cast<uint32_t>(q.held) + a.S - 1u), bi = block_of(a, p), within = p - bi * static_cast<uint32_t>(a.S);
+  int64_t slot = -1;
+  if (q.before >= 0) {
+    int32_t block = q.last;
+    if (bi >= hb) {
+      const int64_t at = t.stack - 1 - (q.before + (bi - hb));
+      block = at < 0 ? -1 : at < t.free ? a.free_blocks[at] : returned(a, at - t.free, t.returned_shift);
+      if (within == 0) a.table[static_cast<int64_t>(r) * a.max_blocks + bi] = block;
+    }
+    slot = static_cast<int64_t>(block) * a.S + within;
+  }
+  a.slots[j] = slot;
+  if (a.pos) a.pos[j] = static_cast<int32_t>(p);
+}
+
+template <int kBlocks, bool kAll>  // kAll: and expands the sums too
 __global__ void __launch_bounds__(kScanThreads) bt_scan_kernel(const BTArgs a) {
   pdl_prologue();
   const int tid = threadIdx.x;
@@ -283,31 +329,12 @@ __global__ void __launch_bounds__(kScanThreads) bt_scan_kernel(const BTArgs a) {
     *a.n_free_out = static_cast<int32_t>(N - most);
     if (toks > a.slots_cap || nf + back > a.pool) flag_error(a.status, MAPS_E_RANGE);
   }
-}
-
-// The request that element x belongs to: the last r with sums[r] <= x, for 0 <= x < sums[R].
-__device__ __forceinline__ int owner(const int64_t *__restrict__ sums, const int32_t *__restrict__ marks, int shift, int64_t x) {
-  int lo = marks[x >> shift], hi = marks[(x >> shift) + 1] + 1;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (sums[mid] <= x)
-      lo = mid;
-    else
-      hi = mid;
+  if (kAll) {
+    __syncthreads();  // the requests' records and the marks
+    const Totals t = *a.totals;
+    push(a, t, 0, 1);
+    for (int64_t j = tid; j < t.tokens; j += kScanThreads) fill_token(a, t, j);
   }
-  return lo;
-}
-
-// The block that entry k of the returned ones is: still in its old row, which nothing overwrites.
-__device__ __forceinline__ int32_t returned(const BTArgs &a, int64_t k, int shift) {
-  const int r = owner(a.back, a.coarse + kCoarse + 2, shift, k);
-  return a.table[static_cast<int64_t>(r) * a.max_blocks + need_of(a, r, false).wb + (k - a.back[r])];
-}
-
-// The returned blocks onto the stack, by `blocks` blocks of which this is number b.
-__device__ __forceinline__ void push(const BTArgs &a, const Totals &t, int b, int blocks) {
-  for (int64_t k = static_cast<int64_t>(b) * kFillThreads + threadIdx.x; k < t.returned; k += static_cast<int64_t>(blocks) * kFillThreads)
-    a.free_blocks[t.free + k] = returned(a, k, t.returned_shift);
 }
 
 __global__ void __launch_bounds__(kFillThreads) bt_push_kernel(const BTArgs a) {
@@ -319,28 +346,10 @@ __global__ void __launch_bounds__(kFillThreads) bt_push_kernel(const BTArgs a) {
 __global__ void __launch_bounds__(kFillThreads) bt_fill_kernel(const BTArgs a, int token_blocks) {
   pdl_prologue();
   const Totals t = *a.totals;
-  if (static_cast<int>(blockIdx.x) >= token_blocks) {
+  if (static_cast<int>(blockIdx.x) >= token_blocks)
     push(a, t, blockIdx.x - token_blocks, gridDim.x - token_blocks);
-    return;
-  }
-  const int64_t j = static_cast<int64_t>(blockIdx.x) * kFillThreads + threadIdx.x;
-  if (j >= t.tokens) return;
-  const int r = owner(a.off, a.coarse, t.token_shift, j);
-  const Request q = a.requests[r];
-  const uint32_t p = static_cast<uint32_t>(q.held) + static_cast<uint32_t>(j - q.begin);
-  const uint32_t hb = block_of(a, static_cast<uint32_t>(q.held) + a.S - 1u), bi = block_of(a, p), within = p - bi * static_cast<uint32_t>(a.S);
-  int64_t slot = -1;
-  if (q.before >= 0) {
-    int32_t block = q.last;
-    if (bi >= hb) {
-      const int64_t at = t.stack - 1 - (q.before + (bi - hb));
-      block = at < 0 ? -1 : at < t.free ? a.free_blocks[at] : returned(a, at - t.free, t.returned_shift);
-      if (within == 0) a.table[static_cast<int64_t>(r) * a.max_blocks + bi] = block;
-    }
-    slot = static_cast<int64_t>(block) * a.S + within;
-  }
-  a.slots[j] = slot;
-  if (a.pos) a.pos[j] = static_cast<int32_t>(p);
+  else
+    fill_token(a, t, static_cast<int64_t>(blockIdx.x) * kFillThreads + threadIdx.x);
 }
 
 // Many tokens: a warp maps 256 consecutive ones, lane by lane so that writes are whole lines, and all
@@ -456,11 +465,15 @@ int maps_block_tables(int32_t R, int32_t S, const int32_t *held, const int32_t *
               got_out, slot_off_out, slots_out, slots_cap, pos_out, nullptr, nullptr, nullptr, nullptr,
               status_word(ws)};
   carve(c, a);
-  if (R <= kScanThreads)
-    launch_pdl(bt_scan_kernel<1>, 1, kScanThreads, 0, s, a);
+  // a decode step's worth in one kernel: what one block has to expand besides costs less than a launch
+  const bool all = R <= kScanThreads && slots_cap <= 4 * kScanThreads && pool <= 16 * kScanThreads;
+  if (all)
+    launch_pdl(bt_scan_kernel<1, true>, 1, kScanThreads, 0, s, a);
+  else if (R <= kScanThreads)
+    launch_pdl(bt_scan_kernel<1, false>, 1, kScanThreads, 0, s, a);
   else
-    launch_cluster(bt_scan_kernel<kCluster>, kCluster, kScanThreads, s, a);
-  if (R > 0) {
+    launch_cluster(bt_scan_kernel<kCluster, false>, kCluster, kScanThreads, s, a);
+  if (R > 0 && !all) {
     const int64_t rows = (static_cast<int64_t>(R) * max_blocks + 4 * kFillThreads - 1) / (4 * kFillThreads);
     const int64_t back = std::min(std::min((static_cast<int64_t>(pool) + 4 * kFillThreads - 1) / (4 * kFillThreads), rows), static_cast<int64_t>(4 * sm_count()));
     if (slots_cap <= kFewTokens) {
