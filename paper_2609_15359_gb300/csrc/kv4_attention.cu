@@ -41,6 +41,31 @@ __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uin
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
+// Values for the second product.  Bare codes are all positive, so in sums over many tokens the products' sum and the sum
+// of the zeros are far larger than their difference: by 1,000 at 100,000 tokens, where a half output shows what 32-bit
+// sums then lose (6e-4 of the output's norm, 2e-4 its own rounding).  So for half the codes are taken about 8, at one
+// packed addition more for two; the zeros follow.
+template <class T>
+struct Value {
+  static constexpr float kEvenBy = kEven, kOddBy = kOdd, kCentre = 0.0f;
+  static __device__ __forceinline__ Codes of(uint32_t w) { return codes_of(w); }
+};
+template <>
+struct Value<__half> {
+  static constexpr float kEvenBy = 1.0f, kOddBy = 0.0625f, kCentre = 8.0f;
+  static __device__ __forceinline__ Codes of(uint32_t w) {
+    Codes c = codes_of(w);
+    const __half2 even = __float2half2_rn(-1032.0f), odd = __float2half2_rn(-1152.0f);  // 1024 + 8, 1024 + 16 * 8
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const uint32_t x = c.x[r] | 0x64006400u;
+      const __half2 y = __hadd2(*reinterpret_cast<const __half2 *>(&x), r % 2 ? odd : even);
+      c.x[r] = *reinterpret_cast<const uint32_t *>(&y);
+    }
+    return c;
+  }
+};
+
 // ---------------------------------------------------------------------------- the work, in units
 template <int D, int NT>
 struct Shape {
@@ -475,7 +500,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(con
             uint32_t pf[NT][2];
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-              const float vz = kv4_param(par[g + 8 * half]).y;
+              const float vz = fmaf(Value<T>::kCentre, vs[gr][half], kv4_param(par[g + 8 * half]).y);
               const int32_t tok = tok0 + gr * kGroup + g + 8 * half;
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt) {
@@ -506,7 +531,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(con
             }
 #pragma unroll
             for (int i = 0; i < kWords; ++i) {
-              const Codes x = codes_of(v0[i]), y = codes_of(v1[i]);
+              const Codes x = Value<T>::of(v0[i]), y = Value<T>::of(v1[i]);
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt) {
                 mma(o[nt][2 * i], x.x[0], x.x[1], y.x[0], y.x[1], pf[nt][0], pf[nt][1]);
@@ -552,8 +577,8 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(con
             T y[kCh];
 #pragma unroll
             for (int j = 0; j < kSteps; ++j) {
-              y[2 * j] = Cvt<T>::from(fmaf(o[nt][j][e], kEven, add) * inv);
-              y[2 * j + 1] = Cvt<T>::from(fmaf(o[nt][j][2 + e], kOdd, add) * inv);
+              y[2 * j] = Cvt<T>::from(fmaf(o[nt][j][e], Value<T>::kEvenBy, add) * inv);
+              y[2 * j + 1] = Cvt<T>::from(fmaf(o[nt][j][2 + e], Value<T>::kOddBy, add) * inv);
             }
             if (a.wide) {
 #pragma unroll
@@ -577,8 +602,8 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(con
             float *dst = part + R * D + g * kCh;
 #pragma unroll
             for (int j = 0; j < kSteps; ++j) {
-              dst[2 * j] = fmaf(o[nt][j][e], kEven, w[nt][e]);
-              dst[2 * j + 1] = fmaf(o[nt][j][2 + e], kOdd, w[nt][e]);
+              dst[2 * j] = fmaf(o[nt][j][e], Value<T>::kEvenBy, w[nt][e]);
+              dst[2 * j + 1] = fmaf(o[nt][j][2 + e], Value<T>::kOddBy, w[nt][e]);
             }
             if (g == 0) {
               part[Sh::kRows * D + R] = m[nt][e];
