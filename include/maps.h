@@ -1,8 +1,8 @@
 /*
  * maps.h -- C ABI of the MAPS memory-aware predictive scheduler hot path,
  * implemented as integer-only CUDA kernels for GB300 (sm_103a), and of the KV
- * memory that its decoders run on: block tables, a cache held in 4 bits, and
- * attention over that cache.
+ * memory that its decoders run on: block tables (integers too), a cache held in
+ * 4 bits, and attention over that cache.
  *
  * The four scheduling calls follow the scheduler's problem statement (Sec.
  * 3.3): decoders d_k with KV-token capacity C_k and waiting-queue length Q_k;
@@ -555,9 +555,11 @@ int maps_kv4_read(int32_t dtype, int64_t T, int32_t H, int32_t D, int32_t S, con
  * the keys j in [0, n), j <= p where causal, j > p - window where window > 0;
  * at a position below 0 it sees none.  With query head x on KV head x / (Hq / Hkv),
  *     w_j = sm_scale * (q . k_j),  out = sum_j exp(w_j) v_j / sum_j exp(w_j),
- *     lse = log(sum_j exp(w_j)),
- * in 32 bits but for the weights, which meet the values' codes as products of
- * 16-bit numbers; out is rounded once.  A query that sees no key has out = 0
+ *     lse = log(sum_j exp(w_j)).
+ * Scores, maxima, sums and lse are held in 32 bits; a weight is rounded to 11
+ * bits where it meets its value (with many queries a request, a value is too);
+ * out is rounded once more.  The order of the sums depends on the sizes alone, so
+ * a call repeated gives the same bits.  A query that sees no key has out = 0
  * and lse = -infinity.  What the cache holds at places that no query sees is
  * not used, whatever it is.
  *
@@ -572,6 +574,9 @@ int maps_kv4_read(int32_t dtype, int64_t T, int32_t H, int32_t D, int32_t S, con
  *   table               [B][max_blocks] int32 block tables.
  *   causal, window      0 or 1; 0 (no window) or the keys seen, >= 1.
  *   lse                 [T][Hq] float output, natural logarithm, or NULL.
+ *   ws                  about 5 MB, and 40 MB more where a request can have more
+ *                       than 32 query rows to a KV head (D = 64, 128).  After
+ *                       MAPS_E_TIMEOUT it is to be zero-filled anew.
  * A length or a used table entry out of its domain is MAPS_E_RANGE (via
  * maps_check); nothing outside the cache is read.
  * ---------------------------------------------------------------------- */

@@ -205,8 +205,11 @@ __global__ void __launch_bounds__(1024) attn_plan_kernel(const AttnArgs a, uint3
   if (threadIdx.x == 0) *a.units = U;
 }
 
-template <int kN>
-struct Count { static constexpr int value = kN; };
+// Parts joined so far, of four channels of a row.
+struct Sum {
+  float4 num;
+  float top, den;
+};
 
 // Weights are held relative to the largest weight times value scale seen, so that what enters the
 // second product is at most 1; scales count as at least 2^-60 there, so that a weight itself stays finite.
@@ -225,6 +228,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(con
   __shared__ Part s_part[2 * kWarps];  // a warp's first and last part, where it has them
   __shared__ Start s_start[kWarps];
   __shared__ Part s_open[2];           // items that other blocks have parts of: begun before this block, and in it
+  __shared__ uint64_t s_join;          // parts of those that have come to shared memory
   __shared__ int s_block[2][2];        // of those: the first block, and how many where all have brought their parts
 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
@@ -233,6 +237,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(con
   if (lane < Sh::kStages) bar_init(bar32 + 8 * lane, 1);
   if (lane < 2) s_part[2 * warp + lane].tiles = 0;
   if (tid < 2) s_open[tid].tiles = 0;
+  if (tid == 0) bar_init(smem_u32(&s_join), 1);
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   pdl_prologue();
   const uint32_t workers = gridDim.x * kWarps, w0 = blockIdx.x * kWarps, me = w0 + warp;
@@ -622,54 +627,47 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(con
 
   // ---- join the parts of the block's items, in the order of their keys
   const uint32_t c0 = deal.start(w0), c1 = deal.start(w0 + kWarps);
-  auto write_row = [&](const Part &p, int R, int d, float4 num, float mm, float ll) {
+  auto write_row = [&](const Part &p, int R, int d, const Sum &s) {
     const int row = p.rt * Sh::kRows + R;
     if (row >= p.rows) return;
     const int64_t i = p.q0 + row / group;
     const int hq = p.h * group + row % group;
-    const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
+    const float inv = s.den == 0.0f ? 0.0f : 1.0f / s.den;
     T *dst = static_cast<T *>(a.out) + i * a.o_row + hq * a.o_head + d;
-    T y[4] = {Cvt<T>::from(num.x * inv), Cvt<T>::from(num.y * inv), Cvt<T>::from(num.z * inv), Cvt<T>::from(num.w * inv)};
+    T y[4] = {Cvt<T>::from(s.num.x * inv), Cvt<T>::from(s.num.y * inv), Cvt<T>::from(s.num.z * inv), Cvt<T>::from(s.num.w * inv)};
     if (a.wide) {
       *reinterpret_cast<uint2 *>(dst) = *reinterpret_cast<const uint2 *>(y);
     } else {
 #pragma unroll
       for (int c = 0; c < 4; ++c) dst[c] = y[c];
     }
-    if (d == 0 && a.lse) a.lse[i * a.Hq + hq] = ll == 0.0f ? -INFINITY : (mm + log2f(ll)) * 0.6931471805599453f;
+    if (d == 0 && a.lse) a.lse[i * a.Hq + hq] = s.den == 0.0f ? -INFINITY : (s.top + log2f(s.den)) * 0.6931471805599453f;
   };
-  // Sums n parts, each brought to their common maximum; a thread takes four channels at a time, and so many parts at a
-  // time that their loads hide one another.
-  auto join = [&](auto batch, int thread, int threads, int n, auto part, auto load, auto load_one, auto put) {
-    constexpr int kBatch = decltype(batch)::value;
-    for (int x = 4 * thread; x < Sh::kRows * D; x += 4 * threads) {
-      const int R = x / D, d = x - R * D;
-      float4 num = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-      float M = -INFINITY, den = 0.0f;
-      for (int k = 0; k < n; k += kBatch) {
-        float4 v[kBatch];
-        float mk[kBatch], lk[kBatch], top = M;
+  // Sums the parts lo .. hi - 1, which lie in shared memory, into `s`, four channels from x on, brought to their common maximum.
+  auto add_parts = [&](Sum &s, int x, int lo, int hi, auto part) {
+    const int R = x / D;
+    for (int k = lo; k < hi; k += 2) {
+      float4 v[2];
+      float mk[2], lk[2], top = s.top;
 #pragma unroll
-        for (int j = 0; j < kBatch; ++j) {
-          const float *p = part(min(k + j, n - 1));  // beyond the last: read again, and left out
-          v[j] = load(p + x);
-          mk[j] = load_one(p + Sh::kRows * D + R);
-          lk[j] = load_one(p + Sh::kRows * D + Sh::kRows + R);
-        }
-#pragma unroll
-        for (int j = 0; j < kBatch; ++j) top = fmaxf(top, mk[j]);
-        const float c = top == -INFINITY ? 1.0f : ex2(M - top);
-        num.x *= c, num.y *= c, num.z *= c, num.w *= c, den *= c;
-        M = top;
-#pragma unroll
-        for (int j = 0; j < kBatch; ++j) {
-          if (k + j >= n) break;
-          const float f = top == -INFINITY ? 0.0f : ex2(mk[j] - top);
-          num.x = fmaf(f, v[j].x, num.x), num.y = fmaf(f, v[j].y, num.y), num.z = fmaf(f, v[j].z, num.z), num.w = fmaf(f, v[j].w, num.w);
-          den = fmaf(f, lk[j], den);
-        }
+      for (int j = 0; j < 2; ++j) {
+        const float *p = part(min(k + j, hi - 1));  // beyond the last: read again, and left out
+        v[j] = *reinterpret_cast<const float4 *>(p + x);
+        mk[j] = p[Sh::kRows * D + R];
+        lk[j] = p[Sh::kRows * D + Sh::kRows + R];
       }
-      put(R, d, num, M, den);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) top = fmaxf(top, mk[j]);
+      const float c = top == -INFINITY ? 1.0f : ex2(s.top - top);
+      s.num.x *= c, s.num.y *= c, s.num.z *= c, s.num.w *= c, s.den *= c;
+      s.top = top;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        if (k + j >= hi) break;
+        const float f = top == -INFINITY ? 0.0f : ex2(mk[j] - top);
+        s.num.x = fmaf(f, v[j].x, s.num.x), s.num.y = fmaf(f, v[j].y, s.num.y), s.num.z = fmaf(f, v[j].z, s.num.z), s.num.w = fmaf(f, v[j].w, s.num.w);
+        s.den = fmaf(f, lk[j], s.den);
+      }
     }
   };
   // within the block: the warps that have parts of an item share its channels
@@ -681,17 +679,17 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(con
     const int last = item.id + item.tiles > c1 ? kWarps - 1 : static_cast<int>(deal.worker(item.id + item.tiles - 1) - w0);
     const float *head = item.id <= deal.start(w0 + first) ? first_parts + first * Sh::kPart : reinterpret_cast<const float *>(ring_all + first * Sh::kStages * Sh::kBytes);
     float *mine = a.parts + (static_cast<int64_t>(blockIdx.x) * 2 + (item.id < c0 ? 0 : 1)) * Sh::kPart;
-    join(
-        Count<2>{}, lane + 32 * (warp - first), 32 * (last - first + 1), last - first + 1, [&](int k) { return k == 0 ? head : first_parts + (first + k) * Sh::kPart; },
-        [](const float *p) { return *reinterpret_cast<const float4 *>(p); }, [](const float *p) { return *p; },
-        [&](int R, int d, float4 num, float mm, float ll) {
-          if (whole) {
-            write_row(item, R, d, num, mm, ll);
-          } else {
-            *reinterpret_cast<float4 *>(mine + R * D + d) = num;
-            if (d == 0) mine[Sh::kRows * D + R] = mm, mine[Sh::kRows * D + Sh::kRows + R] = ll;
-          }
-        });
+    for (int x = 4 * (lane + 32 * (warp - first)); x < Sh::kRows * D; x += 4 * 32 * (last - first + 1)) {
+      Sum sum = {make_float4(0.0f, 0.0f, 0.0f, 0.0f), -INFINITY, 0.0f};
+      add_parts(sum, x, 0, last - first + 1, [&](int k) { return k == 0 ? head : first_parts + (first + k) * Sh::kPart; });
+      const int R = x / D, d = x - R * D;
+      if (whole) {
+        write_row(item, R, d, sum);
+      } else {
+        *reinterpret_cast<float4 *>(mine + R * D + d) = sum.num;
+        if (d == 0) mine[Sh::kRows * D + R] = sum.top, mine[Sh::kRows * D + Sh::kRows + R] = sum.den;
+      }
+    }
     if (!whole) {
       if (warp == first && lane == 0) s_open[item.id < c0 ? 0 : 1] = item;
       __threadfence();
@@ -710,15 +708,39 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(con
     s_block[tid][1] = all ? static_cast<int>(e - f + 1) : 0;
   }
   __syncthreads();
-  for (int k = 0; k < 2; ++k) {
-    if (s_open[k].tiles == 0 || s_block[k][1] == 0) continue;
-    const Part item = s_open[k];
-    const int f = s_block[k][0];
-    __threadfence();
-    join(
-        Count<8>{}, tid, kThreads, s_block[k][1], [&](int c) { return a.parts + (static_cast<int64_t>(f + c) * 2 + (c == 0)) * Sh::kPart; },
-        [](const float *p) { return __ldcg(reinterpret_cast<const float4 *>(p)); }, [](const float *p) { return __ldcg(p); },
-        [&](int R, int d, float4 num, float mm, float ll) { write_row(item, R, d, num, mm, ll); });
+  // Their parts come to shared memory, those of both items at once where they fit: a part then costs no round trip of its own.
+  const int n0 = s_open[0].tiles ? s_block[0][1] : 0, n = n0 + (s_open[1].tiles ? s_block[1][1] : 0);
+  if (n == 0) return;
+  __threadfence();
+  asm volatile("fence.proxy.async;" ::: "memory");  // what others wrote with plain stores, and this block in shared memory
+  __syncthreads();
+  constexpr int kRoom = Sh::kWarps * (Sh::kStages * Sh::kBytes / (Sh::kPart * 4) + 1), kTurns = (Sh::kRows * D / 4 + kThreads - 1) / kThreads;
+  static_assert(kRoom <= kThreads, "a thread loads a part at most");
+  const float *parts = reinterpret_cast<const float *>(smem);
+  const uint32_t joined = smem_u32(&s_join);
+  Sum sum[kTurns];
+  for (int p0 = 0; p0 < n; p0 += kRoom) {
+    const int p1 = min(n, p0 + kRoom);
+    if (tid == 0) bar_expect(joined, (p1 - p0) * Sh::kPart * 4);
+    if (tid < p1 - p0) {
+      const int k = p0 + tid >= n0 ? 1 : 0, c = p0 + tid - k * n0;
+      bulk_load(smem_u32(parts + tid * Sh::kPart), a.parts + (static_cast<int64_t>(s_block[k][0] + c) * 2 + (c == 0)) * Sh::kPart, Sh::kPart * 4, joined);
+    }
+    if (!bar_wait(joined, p0 / kRoom & 1) && tid == 0) flag_error(a.status, MAPS_E_TIMEOUT);
+    for (int k = 0; k < 2; ++k) {
+      const int lo = k ? n0 : 0, hi = k ? n : n0, from = max(lo, p0), to = min(hi, p1);
+      if (from >= to) continue;
+      const Part item = s_open[k];
+#pragma unroll
+      for (int i = 0; i < kTurns; ++i) {
+        const int x = 4 * (tid + i * kThreads);
+        if (x >= Sh::kRows * D) break;
+        if (from == lo) sum[i] = {make_float4(0.0f, 0.0f, 0.0f, 0.0f), -INFINITY, 0.0f};
+        add_parts(sum[i], x, from - p0, to - p0, [&](int c) { return parts + c * Sh::kPart; });
+        if (to == hi) write_row(item, x / D, x % D, sum[i]);
+      }
+    }
+    if (p1 < n) __syncthreads();  // the room is read before it is filled again
   }
 }
 

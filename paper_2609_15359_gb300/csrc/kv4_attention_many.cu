@@ -139,7 +139,6 @@ __global__ void __launch_bounds__(1024) attn_many_plan_kernel(const AttnArgs a, 
 }
 
 // ---------------------------------------------------------------------------- tensor memory, products, packed arithmetic
-__device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
