@@ -575,7 +575,7 @@ int maps_kv4_read(int32_t dtype, int64_t T, int32_t H, int32_t D, int32_t S, con
  *   causal, window      0 or 1; 0 (no window) or the keys seen, >= 1.
  *   lse                 [T][Hq] float output, natural logarithm, or NULL.
  *   ws                  about 5 MB, and 40 MB more where a request can have more
- *                       than 32 query rows to a KV head (D = 64, 128).  After
+ *                       than 96 query rows to a KV head (D = 64, 128).  After
  *                       MAPS_E_TIMEOUT it is to be zero-filled anew.
  * A length or a used table entry out of its domain is MAPS_E_RANGE (via
  * maps_check); nothing outside the cache is read.
