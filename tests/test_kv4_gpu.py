@@ -397,6 +397,21 @@ def test_one_long_request(M, Hq, H, D, name):
     check(M, np.random.default_rng(3), [20011, 3], [4, 2], Hq, H, D, 64, name, window=15000)
 
 
+@pytest.mark.parametrize("Hq,D,n,name", [(8, 128, 100003, "bf16"), (16, 128, 120001, "fp16"), (16, 256, 60001, "bf16"), (4, 64, 180007, "fp16")])
+def test_one_head_over_the_whole_device(M, Hq, D, n, name):
+    """One KV head's keys lie with every multiprocessor: more parts to join than shared memory takes at once."""
+    check(M, np.random.default_rng(11), [n], [1], Hq, 1, D, 64, name)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Hq,H", [(1, 1), (4, 2)])
+def test_rows_about_where_forms_and_tiles_end(M, Hq, H, D):
+    n_q = [96, 97, 127, 128, 129, 255, 256, 257, 385, 48, 49, 64, 65, 1, 0]
+    lens = [90, 97, 140, 128, 700, 100, 256, 300, 385, 48, 500, 64, 66, 1, 20]
+    check(M, np.random.default_rng(12), lens, n_q, Hq, H, D, 32, "bf16")
+    check(M, np.random.default_rng(13), lens, n_q, Hq, H, D, 16, "fp16", window=33)
+
+
 def test_many_short_requests(M):
     rng = np.random.default_rng(4)
     lens = rng.integers(0, 50, 2500).tolist()
