@@ -208,10 +208,16 @@ __global__ void __launch_bounds__(1024) attn_plan_kernel(const AttnArgs a, uint3
   if (threadIdx.x == 0) *a.units = U;
 }
 
-// Parts joined so far, of four channels of a row.
+// Parts joined so far, of kCh channels of a row.
+template <int kCh>
 struct Sum {
-  float4 num;
+  alignas(16) float num[kCh];
   float top, den;
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int c = 0; c < kCh; ++c) num[c] = 0.0f;
+    top = -INFINITY, den = 0.0f;
+  }
 };
 
 // Weights are held relative to the largest weight times value scale seen, so that what enters the
@@ -630,45 +636,56 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(con
 
   // ---- join the parts of the block's items, in the order of their keys
   const uint32_t c0 = deal.start(w0), c1 = deal.start(w0 + kWarps);
-  auto write_row = [&](const Part &p, int R, int d, const Sum &s) {
+  auto write_row = [&](const Part &p, int R, int d, const auto &s) {
+    constexpr int kN = sizeof(s.num) / 4;
     const int row = p.rt * Sh::kRows + R;
     if (row >= p.rows) return;
     const int64_t i = p.q0 + row / group;
     const int hq = p.h * group + row % group;
     const float inv = s.den == 0.0f ? 0.0f : 1.0f / s.den;
     T *dst = static_cast<T *>(a.out) + i * a.o_row + hq * a.o_head + d;
-    T y[4] = {Cvt<T>::from(s.num.x * inv), Cvt<T>::from(s.num.y * inv), Cvt<T>::from(s.num.z * inv), Cvt<T>::from(s.num.w * inv)};
+    alignas(16) T y[kN];
+#pragma unroll
+    for (int c = 0; c < kN; ++c) y[c] = Cvt<T>::from(s.num[c] * inv);
     if (a.wide) {
-      *reinterpret_cast<uint2 *>(dst) = *reinterpret_cast<const uint2 *>(y);
+      if (kN == 8)
+        *reinterpret_cast<uint4 *>(dst) = *reinterpret_cast<const uint4 *>(y);
+      else
+        *reinterpret_cast<uint2 *>(dst) = *reinterpret_cast<const uint2 *>(y);
     } else {
 #pragma unroll
-      for (int c = 0; c < 4; ++c) dst[c] = y[c];
+      for (int c = 0; c < kN; ++c) dst[c] = y[c];
     }
     if (d == 0 && a.lse) a.lse[i * a.Hq + hq] = s.den == 0.0f ? -INFINITY : (s.top + log2f(s.den)) * 0.6931471805599453f;
   };
   // Sums the parts lo .. hi - 1, which lie in shared memory, into `s`, four channels from x on, brought to their common maximum.
-  auto add_parts = [&](Sum &s, int x, int lo, int hi, auto part) {
+  auto add_parts = [&](auto &s, int x, int lo, int hi, auto part) {
+    constexpr int kN = sizeof(s.num) / 4;
     const int R = x / D;
     for (int k = lo; k < hi; k += 2) {
-      float4 v[2];
+      alignas(16) float v[2][kN];
       float mk[2], lk[2], top = s.top;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const float *p = part(min(k + j, hi - 1));  // beyond the last: read again, and left out
-        v[j] = *reinterpret_cast<const float4 *>(p + x);
+#pragma unroll
+        for (int c = 0; c < kN; c += 4) *reinterpret_cast<float4 *>(v[j] + c) = *reinterpret_cast<const float4 *>(p + x + c);
         mk[j] = p[Sh::kRows * D + R];
         lk[j] = p[Sh::kRows * D + Sh::kRows + R];
       }
 #pragma unroll
       for (int j = 0; j < 2; ++j) top = fmaxf(top, mk[j]);
       const float c = top == -INFINITY ? 1.0f : ex2(s.top - top);
-      s.num.x *= c, s.num.y *= c, s.num.z *= c, s.num.w *= c, s.den *= c;
+#pragma unroll
+      for (int d = 0; d < kN; ++d) s.num[d] *= c;
+      s.den *= c;
       s.top = top;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         if (k + j >= hi) break;
         const float f = top == -INFINITY ? 0.0f : ex2(mk[j] - top);
-        s.num.x = fmaf(f, v[j].x, s.num.x), s.num.y = fmaf(f, v[j].y, s.num.y), s.num.z = fmaf(f, v[j].z, s.num.z), s.num.w = fmaf(f, v[j].w, s.num.w);
+#pragma unroll
+        for (int d = 0; d < kN; ++d) s.num[d] = fmaf(f, v[j][d], s.num[d]);
         s.den = fmaf(f, lk[j], s.den);
       }
     }
@@ -682,14 +699,16 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(con
     const int last = item.id + item.tiles > c1 ? kWarps - 1 : static_cast<int>(deal.worker(item.id + item.tiles - 1) - w0);
     const float *head = item.id <= deal.start(w0 + first) ? first_parts + first * Sh::kPart : reinterpret_cast<const float *>(ring_all + first * Sh::kStages * Sh::kBytes);
     float *mine = a.parts + (static_cast<int64_t>(blockIdx.x) * 2 + (item.id < c0 ? 0 : 1)) * Sh::kPart;
-    for (int x = 4 * (lane + 32 * (warp - first)); x < Sh::kRows * D; x += 4 * 32 * (last - first + 1)) {
-      Sum sum = {make_float4(0.0f, 0.0f, 0.0f, 0.0f), -INFINITY, 0.0f};
+    for (int x = 8 * (lane + 32 * (warp - first)); x < Sh::kRows * D; x += 8 * 32 * (last - first + 1)) {
+      Sum<8> sum;
+      sum.clear();
       add_parts(sum, x, 0, last - first + 1, [&](int k) { return k == 0 ? head : first_parts + (first + k) * Sh::kPart; });
       const int R = x / D, d = x - R * D;
       if (whole) {
         write_row(item, R, d, sum);
       } else {
-        *reinterpret_cast<float4 *>(mine + R * D + d) = sum.num;
+#pragma unroll
+        for (int c = 0; c < 8; c += 4) *reinterpret_cast<float4 *>(mine + R * D + d + c) = *reinterpret_cast<const float4 *>(sum.num + c);
         if (d == 0) mine[Sh::kRows * D + R] = sum.top, mine[Sh::kRows * D + Sh::kRows + R] = sum.den;
       }
     }
@@ -721,7 +740,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(con
   static_assert(kRoom <= kThreads, "a thread loads a part at most");
   const float *parts = reinterpret_cast<const float *>(smem);
   const uint32_t joined = smem_u32(&s_join);
-  Sum sum[kTurns];
+  Sum<4> sum[kTurns];
   for (int p0 = 0; p0 < n; p0 += kRoom) {
     const int p1 = min(n, p0 + kRoom);
     if (tid == 0) bar_expect(joined, (p1 - p0) * Sh::kPart * 4);
@@ -738,7 +757,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(con
       for (int i = 0; i < kTurns; ++i) {
         const int x = 4 * (tid + i * kThreads);
         if (x >= Sh::kRows * D) break;
-        if (from == lo) sum[i] = {make_float4(0.0f, 0.0f, 0.0f, 0.0f), -INFINITY, 0.0f};
+        if (from == lo) sum[i].clear();
         add_parts(sum[i], x, from - p0, to - p0, [&](int c) { return parts + c * Sh::kPart; });
         if (to == hi) write_row(item, x / D, x % D, sum[i]);
       }
