@@ -208,6 +208,11 @@ __global__ void __launch_bounds__(1024) attn_plan_kernel(const AttnArgs a, uint3
   if (threadIdx.x == 0) *a.units = U;
 }
 
+// Where four channels from d on of row R lie in a part: rows are turned by 16 bytes for every second of them, or the lanes that
+// write a part, whose rows differ by two and whose channels by D/8, would meet in two banks.
+template <int D>
+__device__ __forceinline__ int in_part(int R, int d) { return R * D + ((d + 4 * (R >> 1)) & (D - 1)); }
+
 // Parts joined so far, of kCh channels of a row.
 template <int kCh>
 struct Sum {
@@ -613,12 +618,11 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(con
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             const int R = nt * 8 + 2 * t + e;
-            float *dst = part + R * D + g * kCh;
 #pragma unroll
-            for (int j = 0; j < kSteps; ++j) {
-              dst[2 * j] = fmaf(o[nt][j][e], Value<T>::kEvenBy, w[nt][e]);
-              dst[2 * j + 1] = fmaf(o[nt][j][2 + e], Value<T>::kOddBy, w[nt][e]);
-            }
+            for (int j = 0; j < kSteps; j += 2)
+              *reinterpret_cast<float4 *>(part + in_part<D>(R, g * kCh + 2 * j)) =
+                  make_float4(fmaf(o[nt][j][e], Value<T>::kEvenBy, w[nt][e]), fmaf(o[nt][j][2 + e], Value<T>::kOddBy, w[nt][e]),
+                              fmaf(o[nt][j + 1][e], Value<T>::kEvenBy, w[nt][e]), fmaf(o[nt][j + 1][2 + e], Value<T>::kOddBy, w[nt][e]));
             if (g == 0) {
               part[Sh::kRows * D + R] = m[nt][e];
               part[Sh::kRows * D + Sh::kRows + R] = l[nt][e];
@@ -661,7 +665,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(con
   // Sums the parts lo .. hi - 1, which lie in shared memory, into `s`, four channels from x on, brought to their common maximum.
   auto add_parts = [&](auto &s, int x, int lo, int hi, auto part) {
     constexpr int kN = sizeof(s.num) / 4;
-    const int R = x / D;
+    const int R = x / D, d = x - R * D;
     for (int k = lo; k < hi; k += 2) {
       alignas(16) float v[2][kN];
       float mk[2], lk[2], top = s.top;
@@ -669,7 +673,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(con
       for (int j = 0; j < 2; ++j) {
         const float *p = part(min(k + j, hi - 1));  // beyond the last: read again, and left out
 #pragma unroll
-        for (int c = 0; c < kN; c += 4) *reinterpret_cast<float4 *>(v[j] + c) = *reinterpret_cast<const float4 *>(p + x + c);
+        for (int c = 0; c < kN; c += 4) *reinterpret_cast<float4 *>(v[j] + c) = *reinterpret_cast<const float4 *>(p + in_part<D>(R, d + c));
         mk[j] = p[Sh::kRows * D + R];
         lk[j] = p[Sh::kRows * D + Sh::kRows + R];
       }
@@ -677,7 +681,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(con
       for (int j = 0; j < 2; ++j) top = fmaxf(top, mk[j]);
       const float c = top == -INFINITY ? 1.0f : ex2(s.top - top);
 #pragma unroll
-      for (int d = 0; d < kN; ++d) s.num[d] *= c;
+      for (int i = 0; i < kN; ++i) s.num[i] *= c;
       s.den *= c;
       s.top = top;
 #pragma unroll
@@ -685,7 +689,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(con
         if (k + j >= hi) break;
         const float f = top == -INFINITY ? 0.0f : ex2(mk[j] - top);
 #pragma unroll
-        for (int d = 0; d < kN; ++d) s.num[d] = fmaf(f, v[j][d], s.num[d]);
+        for (int i = 0; i < kN; ++i) s.num[i] = fmaf(f, v[j][i], s.num[i]);
         s.den = fmaf(f, lk[j], s.den);
       }
     }
@@ -708,7 +712,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(con
         write_row(item, R, d, sum);
       } else {
 #pragma unroll
-        for (int c = 0; c < 8; c += 4) *reinterpret_cast<float4 *>(mine + R * D + d + c) = *reinterpret_cast<const float4 *>(sum.num + c);
+        for (int c = 0; c < 8; c += 4) *reinterpret_cast<float4 *>(mine + in_part<D>(R, d + c)) = *reinterpret_cast<const float4 *>(sum.num + c);
         if (d == 0) mine[Sh::kRows * D + R] = sum.top, mine[Sh::kRows * D + Sh::kRows + R] = sum.den;
       }
     }
