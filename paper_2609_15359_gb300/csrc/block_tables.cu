@@ -17,6 +17,10 @@
 // just returned from its old row, so that returning and taking need not wait
 // for one another; with many, which the writes bound, the returned blocks go
 // onto the stack first and a token costs one load of it.
+//
+// Bound: a decode step (64 requests) by latency, 4.5 us for a launch and three rounds of dependent loads;
+// 4,096 requests with prompts up to 8,192 tokens, 32 MB mostly written, 26 us: 16 of them are sums and
+// launches, in the rest slots and positions are written at about 3 TB/s.
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -31,8 +35,10 @@ namespace cg = cooperative_groups;
 constexpr int kScanThreads = 1024;
 constexpr int kCluster = 8;
 constexpr int kFillThreads = 256;
-constexpr int kFewTokens = 65536;  // up to here: one kernel, a token a thread
-constexpr int kManyEach = 8;       // beyond: tokens of a thread
+// Up to here a token is a thread's, beyond a thread has eight: 2,048 requests with 131,072 new tokens take 11.4 us in the first
+// form and 14.7 in the second, with 1,048,576 of them 15.7 and 14.6.
+constexpr int kFewTokens = 1 << 19;
+constexpr int kManyEach = 8;
 constexpr int kCoarse = 2048;      // marks of a coarse index
 
 // What the tokens of a request need to know of it.
@@ -465,8 +471,10 @@ int maps_block_tables(int32_t R, int32_t S, const int32_t *held, const int32_t *
               got_out, slot_off_out, slots_out, slots_cap, pos_out, nullptr, nullptr, nullptr, nullptr,
               status_word(ws)};
   carve(c, a);
-  // a decode step's worth in one kernel: what one block has to expand besides costs less than a launch
-  const bool all = R <= kScanThreads && slots_cap <= 4 * kScanThreads && pool <= 16 * kScanThreads;
+  // A decode step's worth in one kernel: what one block has to expand besides costs less than a launch (64 requests, a token
+  // each: 3.9 us, 4.7 with two kernels; 256 with 8 tokens 5.4, 5.9; with 16 tokens 7.1, 6.3).  The sums are one block's up to
+  // its threads, then a cluster's of eight (1,024 requests: 7.8, 11.1 us; 2,048: 16.0, 15.6; 4,096: 24.2, 16.0).
+  const bool all = R <= kScanThreads && slots_cap <= 2 * kScanThreads && pool <= 16 * kScanThreads;
   if (all)
     launch_pdl(bt_scan_kernel<1, true>, 1, kScanThreads, 0, s, a);
   else if (R <= kScanThreads)

@@ -3,19 +3,24 @@
 // out_i = sum_j softmax_j(sm_scale q_i . k_j) v_j over the keys j that query i sees, with the
 // running maximum and sum of the softmax, so the cache is passed over once.
 //
+// Mathematics.  With k = s c + z (codes c), q . k = s (q . c) + z sum(q), and with weights p,
+// sum p v = sum (p s) c + sum p z: the matrix products run on bare codes, and scales and zeros cost
+// a few operations a token instead of D.  A code is a half number as it stands (codes_of), so eight
+// codes take five operations.  q is scaled by a power of two to fill half's range; p s is held
+// relative to the largest p s so far, so it is at most 1.
+//
 // Bound.  A key and value of D channels are D + 8 bytes and serve the few query rows (queries x
-// heads of one KV head) of one request, so the time is the cache's bytes; what has to keep up
-// is turning 4-bit codes into tensor-core operands.  Codes are therefore never scaled: with
-// k = s c + z, q . k = s (q . c) + z sum(q), and with weights p, sum p v = sum (p s) c + sum p z,
-// so the matrix products run on the codes themselves, at one shift and one bit operation for
-// two of them, with an offset that is taken off in 32 bits with the z term.  Scales then cost a
-// few operations a token instead of D.
+// heads of one KV head) of one request, so long calls are bound by the cache's bytes: 128 requests
+// of 64 to 8,192 tokens, 8 KV heads of 128 channels, 566 MB, take 116 us (4.9 TB/s, 0.72 of the
+// measured copy rate).  Within the passes it is 6.2 TB/s; the rest is a call's fixed part, about 11 us of
+// dependent steps: the plan (2), first queries and records (2), a first unit (4), the joins (3).  Short calls take little
+// else: one request of 2,048 tokens 12 us.
 //
 // Shape.  The products are transposed: 16 tokens (or 16 channels) are the 16 rows of an
-// m16n8k16 step and 8 query rows its columns, so up to 8 rows waste nothing, and K and V
-// are the register operand, straight from the cache's bytes by 16-byte loads from shared
-// memory.  P crosses from the first product's result to the second's operand by an 8 x 8
-// transpose between lanes.
+// m16n8k16 step and 8 query rows its columns, so up to 8 rows waste nothing (as the columns of a
+// tcgen05 product they would meet 128 rows and cross tensor memory twice), and K and V are the
+// register operand, straight from the cache's bytes by 16-byte loads from shared memory.  P
+// crosses from the first product's result to the second's operand by an 8 x 8 transpose between lanes.
 //
 // Split.  The call's work is cut into units of kTok tokens of one (request, KV head, tile of
 // query rows).  Every warp of the grid takes an equal run of consecutive units, whatever
@@ -73,8 +78,12 @@ struct Value<__half> {
 template <int D, int NT>
 struct Shape {
   static constexpr int kRows = 8 * NT;                       // query rows of a tile
+  // As many warps as their registers allow: a unit is a chain of dependent steps, hidden by other warps alone.
   static constexpr int kWarps = NT == 2 || D == 256 ? 8 : 12, kThreads = 32 * kWarps;
-  static constexpr int kGroups = D == 256 ? 2 : NT == 2 ? 4 : D == 64 ? 6 : 3;  // groups of 16 tokens in a unit
+  // Groups of 16 tokens in a unit: more of them share the row maxima and leave longer tails.  With 128 channels and 8 rows a
+  // decode step of 64 requests takes 46 us with two, 42 with three, 44 with four; with 16 rows, 64 requests of 1,000 and 4,096
+  // tokens take 38 and 106 us with two, 39 and 92 with three, 45 and 89 with four.
+  static constexpr int kGroups = D == 256 ? 2 : D == 64 && NT == 1 ? 6 : 3;
   static constexpr int kTok = kGroups * kGroup;
   static constexpr int kBytes = kGroups * kv4_group_bytes(D);  // of a stage
   static constexpr int kStages = D == 64 && NT == 2 ? 4 : 2;
@@ -789,7 +798,9 @@ int launch_few(const AttnArgs &a, cudaStream_t s) {
 
 template <class T>
 int launch_dim(int D, const AttnArgs &a, cudaStream_t s) {
-  // 8 rows to a tile where a request has at most 8 on average, else 16
+  // 8 rows to a tile where a request has at most 8 on average, else 16: for 16 rows two tiles of 8 pass over the cache twice
+  // (64 requests of 4,096 tokens, 128 channels: 112 us, 92 with one of 16; 1,000 tokens: 40, 39), for 8 a tile of 16 is half
+  // empty (65, 89).  256 channels of 16 rows do not fit a warp's registers.
   const bool one = a.T * (a.Hq / a.Hkv) <= static_cast<int64_t>(8) * a.B;
   if (D == 64) return one ? launch_few<T, 64, 1>(a, s) : launch_few<T, 64, 2>(a, s);
   if (D == 128) return one ? launch_few<T, 128, 1>(a, s) : launch_few<T, 128, 2>(a, s);

@@ -182,9 +182,6 @@ __device__ __forceinline__ void tm_store_halves(uint32_t addr, const uint32_t *x
 // The loads' registers pass through the wait, so that nothing uses them ahead of it.
 #define MAPS_RW8(x, i) "+r"(x[i]), "+r"(x[i + 1]), "+r"(x[i + 2]), "+r"(x[i + 3]), "+r"(x[i + 4]), "+r"(x[i + 5]), "+r"(x[i + 6]), "+r"(x[i + 7])
 __device__ __forceinline__ void tm_wait16(uint32_t *x) { asm volatile("tcgen05.wait::ld.sync.aligned;" : MAPS_RW8(x, 0), MAPS_RW8(x, 8)::"memory"); }
-__device__ __forceinline__ void tm_wait32(uint32_t *x) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;" : MAPS_RW8(x, 0), MAPS_RW8(x, 8), MAPS_RW8(x, 16), MAPS_RW8(x, 24)::"memory");
-}
 __device__ __forceinline__ void tm_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 union F2 {

@@ -4,14 +4,21 @@
 // levels: zero = bf16(min), scale = bf16((max - min) * (1/15)), code = round((x - zero) / scale)
 // with the reciprocal taken once per row, value = scale * code + zero.  scale * code has at
 // most 12 significant bits, so a value is rounded once.  D/8 lanes share a row, 8 channels
-// (16 bytes) each; extremes are joined by shuffles.  Both calls are bound by the bytes of
-// the 16-bit rows and the records.
+// (16 bytes) each; extremes are joined by shuffles.
+//
+// Bound: the bytes of the 16-bit rows and the records.  65,536 tokens of 8 heads and 128 channels, 340 MB a call,
+// take 84 us to append (4.1 TB/s, 0.60 of the measured copy rate; a row's minimum, maximum and
+// codes cost about as many issue slots) and 52 us to read (6.5 TB/s).  A decode step's rows take 2-5 us,
+// which is launch and latency.
 #include "kv4.cuh"
 
 namespace maps {
 namespace {
 
-constexpr int kManyWarps = 16;  // of a multiprocessor, from which on warps take 16 tokens each
+// Warps of a multiprocessor from which on a warp takes 16 tokens of a head: shared loads of slots and whole groups moved at
+// once, but fewer and longer threads.  8 heads of 128 channels, append / read, rows side by side and 16 to a warp:
+// 1,024 tokens (3 warps) 3.8 / 3.3 and 5.2 / 3.4 us; 4,096 (13) 9.7 / 7.9 and 9.4 / 4.7; 16,384 34.6 / 28.0 and 20.2 / 12.8.
+constexpr int kManyWarps = 8;
 
 struct KVArgs {
   int64_t T, n_blocks;
