@@ -21,8 +21,12 @@
 // Both would cost a score more work the other way round: a value's scale on the weights takes three operations
 // a score and eight warps' registers, on the values two for two of them.
 //
-// Bound.  128 x 128 scores cost the tensor cores 1,024 cycles at D = 128, and the softmax warps about as many
-// issue slots with packed arithmetic; shared memory is next, since each product reads its operands at full rate.
+// Bound.  A step's four products take the tensor cores about 2,200 cycles at D = 128, but each tile's chain of softmax
+// (4,100 cycles: scores, weights, the tile's vote, P) and products (2,700 from P to the next S, which replaces P) 6,900; the
+// tensor cores work 27 % of the time, and issue slots are 43 % taken.  Six chunks of 1,024 queries, 32 heads on 8, behind 1,500
+// to 9,000 tokens: 817 us, 530 TFLOP/s of 432 GFLOP (0.28 of the measured dense rate).  Shorter chains need the next S beside
+// P, for which tensor memory has no room at D = 128 but in halves; the one warp that makes the keys (5,000 cycles a step)
+// would be next.
 //
 // Split.  As in the other form, a call's steps are dealt out to the blocks in equal runs, whatever the
 // lengths; what a run begins or ends inside of is left as parts, which a second kernel joins.
