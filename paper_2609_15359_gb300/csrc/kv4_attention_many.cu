@@ -21,12 +21,12 @@
 // Both would cost a score more work the other way round: a value's scale on the weights takes three operations
 // a score and eight warps' registers, on the values two for two of them.
 //
-// Bound.  A step's four products take the tensor cores about 2,200 cycles at D = 128, but each tile's chain of softmax
-// (4,100 cycles: scores, weights, the tile's vote, P) and products (2,700 from P to the next S, which replaces P) 6,900; the
-// tensor cores work 27 % of the time, and issue slots are 43 % taken.  Six chunks of 1,024 queries, 32 heads on 8, behind 1,500
-// to 9,000 tokens: 817 us, 530 TFLOP/s of 432 GFLOP (0.28 of the measured dense rate).  Shorter chains need the next S beside
-// P, for which tensor memory has no room at D = 128 but in halves; the one warp that makes the keys (5,000 cycles a step)
-// would be next.
+// Bound.  A step's four products take the tensor cores about 2,200 cycles at D = 128 where nothing else runs, but a step
+// takes 6,800: each tile's chain of softmax (3,500 cycles: scores, weights, the tile's vote, P) and products (3,100 from P to the next
+// S, which replaces P), in which the products take two and a half times as long to issue as alone.  The tensor
+// cores work 28 % of the time, and issue slots are 43 % taken.  Six chunks of 1,024 queries, 32 heads on 8, behind 1,500
+// to 9,000 tokens: 782 us, 552 TFLOP/s of 432 GFLOP (0.29 of the measured dense rate).  S in halves of 64 keys, the first beside
+// P, so that the softmax need not wait for the sums, was 894 us: more and smaller products for the same thread.
 //
 // Split.  As in the other form, a call's steps are dealt out to the blocks in equal runs, whatever the
 // lengths; what a run begins or ends inside of is left as parts, which a second kernel joins.
@@ -214,8 +214,6 @@ __device__ __forceinline__ uint64_t fma2(uint64_t x, uint64_t y, uint64_t w) {
   return z;
 }
 
-struct Zero { static constexpr int value = 0; };
-struct One { static constexpr int value = 1; };
 
 template <int D>
 struct Lay {  // shared memory, from a 1,024-byte boundary
@@ -789,33 +787,26 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
       constexpr uint32_t kQK = idesc_of(kTok), kPV = idesc_of(D);
       uint32_t c = 0, n_q[2] = {0, 0}, n_p[2] = {0, 0};
       bool ok = true;
-      // Tensor memory is taken whole, so it starts at 0; with the tile and the buffer constants too, nothing of an
-      // instruction has to be brought to uniform registers while the tensor cores wait for it.
-      auto scores_of = [&](auto tile, auto buffer) {
-        constexpr int t = decltype(tile)::value, buf = decltype(buffer)::value;
-#pragma unroll
+      // Tensor memory is taken whole, so it starts at 0.  The loops are short ones for the instruction cache's sake, which they
+      // share with the softmax: straight-line code of its own for each tile and buffer 817 us (the chunks above), eight products
+      // in a row 806, four 796, two 782, one 801.
+      auto scores = [&](int t, int buf) {
+        const uint32_t q = rows_desc(base + L::kQ + t * L::kTile), k_at = rows_desc(base + L::kK + buf * L::kTile);
+#pragma unroll 2
         for (int k = 0; k < D / 16; ++k) {
           constexpr int kStep = 32 / 16, kBlock = 16384 / 16;  // of a descriptor's address
           const uint32_t off = k / 4 * kBlock + k % 4 * kStep;
-          mma_ss(t * 128, rows_desc(base + L::kQ + t * L::kTile) + off, rows_desc(base + L::kK + buf * L::kTile) + off, kQK, k > 0);
+          mma_ss(t * 128, q + off, k_at + off, kQK, k > 0);
         }
         tc_commit(s_full(t));
         bar_arrive(s_full(t));  // passes on what this thread has seen of the step: the keys' scales and zeros
       };
-      auto scores = [&](int t, int buf) {
-        if (t == 0)
-          buf ? scores_of(Zero{}, One{}) : scores_of(Zero{}, Zero{});
-        else
-          buf ? scores_of(One{}, One{}) : scores_of(One{}, Zero{});
-      };
-      auto sums_of = [&](auto tile, bool more) {
-        constexpr int t = decltype(tile)::value;
-#pragma unroll
+      auto sums = [&](int t, bool more) {
+#pragma unroll 2
         for (int k = 0; k < kTok / 16; ++k)
           mma_ts(256 + t * 128, t * 128 + 8 * k, rows_desc(base + L::kV) + (k / 4 * (D * 8) + k % 4 * 2), kPV, more || k > 0);
         tc_commit(o_full(t));
       };
-      auto sums = [&](int t, bool more) { t == 0 ? sums_of(Zero{}, more) : sums_of(One{}, more); };
       while (hear(ok)) {
         const int steps = told().steps, tiles = told().second ? 2 : 1;
         done();
