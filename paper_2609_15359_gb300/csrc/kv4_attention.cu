@@ -99,7 +99,7 @@ struct Req {
   int32_t n, n_q, lo, tiles, row_tiles, heads;  // a request without tokens is one item for all heads
 };
 template <int kTok, int kRows>
-__device__ __forceinline__ Req request(const AttnArgs &a, int b) {
+__device__ __forceinline__ Req request(const AttnArgs &a, int b, int32_t over) {
   Req r;
   const int64_t q0 = a.off[b], q1 = a.off[b + 1];
   int32_t n = a.len[b];
@@ -123,7 +123,7 @@ __device__ __forceinline__ Req request(const AttnArgs &a, int b) {
   r.row_tiles = static_cast<int32_t>((m * (a.Hq / a.Hkv) + kRows - 1) / kRows);
   r.heads = a.Hkv;
   if (n == 0) r.heads = 1, r.row_tiles = m > 0 ? 1 : 0;
-  if (n > 0 && a.few_rows > 0 && m * (a.Hq / a.Hkv) > a.few_rows) r.row_tiles = 0;  // the other form's
+  if (n > 0 && over > 0 && m * (a.Hq / a.Hkv) > over) r.row_tiles = 0;  // the other form's
   return r;
 }
 
@@ -132,7 +132,7 @@ struct Cursor {
   int32_t b, h, rt, tile;
   Req r;
   template <int kTok, int kRows>
-  __device__ __forceinline__ void next_item(const AttnArgs &a) {
+  __device__ __forceinline__ void next_item(const AttnArgs &a, int32_t over) {
     tile = 0;
     if (++rt < r.row_tiles) return;
     rt = 0;
@@ -140,7 +140,7 @@ struct Cursor {
     h = 0;
     do {
       if (++b >= a.B) return;
-      r = request<kTok, kRows>(a, b);
+      r = request<kTok, kRows>(a, b, over);
     } while (r.row_tiles == 0);
   }
 };
@@ -165,7 +165,7 @@ struct Start {
 // Sums the units of all requests, kN threads a run of them each, and leaves where the workers
 // w0 .. w1 - 1 start; returns the units.  put(w, start) keeps a worker's.
 template <int kTok, int kRows, int kN, class Put>
-__device__ __forceinline__ uint32_t plan(const AttnArgs &a, uint32_t workers, uint32_t w0, uint32_t w1, Put put) {
+__device__ __forceinline__ uint32_t plan(const AttnArgs &a, int32_t over, uint32_t workers, uint32_t w0, uint32_t w1, Put put) {
   __shared__ uint64_t s_warp[kN / 32];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int run = (a.B + kN - 1) / kN, b0 = min(tid * run, a.B), b1 = min(b0 + run, a.B);
@@ -173,7 +173,7 @@ __device__ __forceinline__ uint32_t plan(const AttnArgs &a, uint32_t workers, ui
   Req r = {};
   uint64_t mine = 0;
   for (int b = b0; b < b1; ++b) {
-    r = request<kTok, kRows>(a, b);
+    r = request<kTok, kRows>(a, b, over);
     mine += units_of(r);
   }
   uint64_t x = mine;
@@ -197,7 +197,7 @@ __device__ __forceinline__ uint32_t plan(const AttnArgs &a, uint32_t workers, ui
   }
   const Deal deal(static_cast<uint32_t>(U), workers);
   for (int b = b0; b < b1; ++b) {
-    if (run > 1) r = request<kTok, kRows>(a, b);
+    if (run > 1) r = request<kTok, kRows>(a, b, over);
     const uint32_t lo = static_cast<uint32_t>(at), n = static_cast<uint32_t>(units_of(r));
     at += n;
     if (n == 0 || lo >= deal.start(w1) || lo + n <= deal.start(w0)) continue;
@@ -213,8 +213,9 @@ __device__ __forceinline__ uint32_t plan(const AttnArgs &a, uint32_t workers, ui
 template <int kTok, int kRows>
 __global__ void __launch_bounds__(1024) attn_plan_kernel(const AttnArgs a, uint32_t workers) {
   pdl_prologue();
-  const uint32_t U = plan<kTok, kRows, 1024>(a, workers, 0, workers, [&](uint32_t w, const Start &c) { static_cast<Start *>(a.starts)[w] = c; });
-  if (threadIdx.x == 0) *a.units = U;
+  const int32_t over = many_over<1024>(a);
+  const uint32_t U = plan<kTok, kRows, 1024>(a, over, workers, 0, workers, [&](uint32_t w, const Start &c) { static_cast<Start *>(a.starts)[w] = c; });
+  if (threadIdx.x == 0) a.units[0] = U, a.units[1] = static_cast<uint32_t>(over);
 }
 
 // Where four channels from d on of row R lie in a part: rows are turned by 16 bytes for every second of them, or the lanes that
@@ -265,14 +266,17 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(con
   pdl_prologue();
   const uint32_t workers = gridDim.x * kWarps, w0 = blockIdx.x * kWarps, me = w0 + warp;
   uint32_t U;
+  int32_t over;  // rows from which a request is the other form's
   Start from = {};
   if (a.B <= kMaxLocalB) {
-    U = plan<Sh::kTok, Sh::kRows, kThreads>(a, workers, w0, w0 + kWarps, [&](uint32_t w, const Start &c) { s_start[w - w0] = c; });
+    over = many_over<kThreads>(a);
+    U = plan<Sh::kTok, Sh::kRows, kThreads>(a, over, workers, w0, w0 + kWarps, [&](uint32_t w, const Start &c) { s_start[w - w0] = c; });
     __syncthreads();
     from = s_start[warp];
   } else {
     __syncthreads();
-    U = *a.units;
+    U = a.units[0];
+    over = static_cast<int32_t>(a.units[1]);
     if (me < U) from = static_cast<const Start *>(a.starts)[me];
   }
   const Deal deal(U, workers);
@@ -298,7 +302,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(con
       if (issued >= u1) return;
       do {
         ++issued;
-        if (++ahead.tile == ahead.r.tiles && issued < u1) ahead.next_item<Sh::kTok, Sh::kRows>(a);
+        if (++ahead.tile == ahead.r.tiles && issued < u1) ahead.next_item<Sh::kTok, Sh::kRows>(a, over);
       } while (issued < u1 && ahead.tile == 0);
       fetch();
     };
@@ -341,7 +345,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(con
           if (a.lse)
             for (int x = lane; x < a.Hq; x += 32) a.lse[(q0 + i) * a.Hq + x] = -INFINITY;
         }
-        if (++u < u1) at.next_item<Sh::kTok, Sh::kRows>(a);
+        if (++u < u1) at.next_item<Sh::kTok, Sh::kRows>(a, over);
         continue;
       }
       const int rows = r.n_q * group;  // n_q * group <= T * Hq fits the checks of the host
@@ -639,7 +643,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(con
           }
         if (lane == 0) s_part[slot] = {q0, u - at.tile, static_cast<uint32_t>(r.tiles), rows, at.h, at.rt};  // at.tile units of the item lie before u
       }
-      if (u < u1) at.next_item<Sh::kTok, Sh::kRows>(a);
+      if (u < u1) at.next_item<Sh::kTok, Sh::kRows>(a, over);
     }
     if (!alive) {  // let what is under way land before the block ends
       for (int s = 0; s < Sh::kStages; ++s) (void)bar_wait(bar32 + 8 * s, s < stage ? parity ^ 1 : parity);
@@ -816,7 +820,7 @@ static void carve(maps::Carve &c, maps::AttnArgs &a, int32_t B, int64_t T, int32
   using namespace maps;
   a.parts = c.take<float>(static_cast<size_t>(attn_grid()) * 2 * kMaxParts);
   a.starts = c.take<Start>(B > kMaxLocalB ? static_cast<size_t>(attn_grid()) * kMaxWarps : 0);
-  a.units = c.take<uint32_t>(1);
+  a.units = c.take<uint32_t>(2);
   // requests with many queries there can only be where there are more rows than requests
   a.few_rows = Hkv > 0 && attn_many_dim(D) && T > B && T * (Hq / Hkv) > kFewRows ? kFewRows : 0;
   if (a.few_rows) attn_many_carve(c, a, B, D);

@@ -49,7 +49,7 @@ struct AttnArgs {
   uint32_t *arrived;   // a byte for each block: blocks that have brought their part of the item it begins
   float *parts;        // [grid][2] parts of items that cross blocks
   // the form for many queries
-  int32_t few_rows;       // a request with more query rows to a KV head goes there (0: none does)
+  int32_t few_rows;       // a request with more query rows to a KV head may go there (0: none does)
   void *many_starts;      // where each block starts, and the units in all
   uint32_t *many_units;
   float *many_parts;      // [grid][2]
@@ -122,6 +122,32 @@ struct Deal {
   __device__ __forceinline__ uint32_t start(uint32_t w) const { return w >= used ? units : per * w + min(w, more); }
   __device__ __forceinline__ uint32_t worker(uint32_t u) const { return u < more * (per + 1) ? u / (per + 1) : more + (u - more * (per + 1)) / per; }
 };
+
+// Query rows x keys x KV heads of all requests that may go to the form for many queries, up to which none does: its queries,
+// parts and joins cost 40 us and more whatever the lengths.  128 channels, one request of 256 rows and 4,096 tokens (8 million):
+// 36 us with few, 72 with many; four of 128 (17 million) 54, 57; 32 of 128 and 500 tokens (16 million) 75, 69; four of 256
+// (34 million) 89, 68.
+constexpr uint64_t kFewPairs = uint64_t(1) << 24;
+
+// The rows over which a request of this call goes to the form for many queries; 0: none does.  All kN threads call it.
+template <int kN>
+__device__ __forceinline__ int32_t many_over(const AttnArgs &a) {
+  if (a.few_rows == 0) return 0;
+  __shared__ unsigned long long s_pairs;
+  if (threadIdx.x == 0) s_pairs = 0;
+  __syncthreads();
+  const int64_t group = a.Hq / a.Hkv;
+  uint64_t pairs = 0;
+  for (int b = threadIdx.x; b < a.B; b += kN) {
+    const int64_t q0 = a.off[b], q1 = a.off[b + 1], rows = (q1 - q0) * group;
+    const int32_t n = a.len[b];
+    if (n < 0 || n > a.max_blocks * a.S || q0 < 0 || q1 < q0 || q1 > a.T || rows <= a.few_rows) continue;
+    pairs += min(static_cast<uint64_t>(rows) * static_cast<uint64_t>(n), uint64_t(1) << 32);
+  }
+  if (pairs) atomicAdd(&s_pairs, static_cast<unsigned long long>(pairs));
+  __syncthreads();
+  return s_pairs > kFewPairs / a.Hkv ? a.few_rows : 0;
+}
 
 struct Yes { static constexpr bool value = true; };
 struct No { static constexpr bool value = false; };

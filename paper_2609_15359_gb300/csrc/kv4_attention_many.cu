@@ -138,7 +138,7 @@ __device__ __forceinline__ uint32_t many_plan(const AttnArgs &a, uint32_t blocks
 
 __global__ void __launch_bounds__(1024) attn_many_plan_kernel(const AttnArgs a, uint32_t blocks) {
   pdl_prologue();
-  const uint32_t U = many_plan<1024>(a, blocks, 0, blocks, [&](uint32_t w, const ManyStart &s) { static_cast<ManyStart *>(a.many_starts)[w] = s; });
+  const uint32_t U = many_over<1024>(a) == 0 ? 0 : many_plan<1024>(a, blocks, 0, blocks, [&](uint32_t w, const ManyStart &s) { static_cast<ManyStart *>(a.many_starts)[w] = s; });
   if (threadIdx.x == 0) *a.many_units = U;
 }
 
@@ -277,7 +277,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
   uint32_t U;
   const uint32_t me = blockIdx.x;
   if (a.B <= kMaxLocalB) {
-    U = many_plan<kThreads>(a, gridDim.x, me, me + 1, [&](uint32_t, const ManyStart &s) { s_start = s; });
+    U = many_over<kThreads>(a) == 0 ? 0 : many_plan<kThreads>(a, gridDim.x, me, me + 1, [&](uint32_t, const ManyStart &s) { s_start = s; });
     if (me == 0 && tid == 0) *a.many_units = U;  // for the kernel that joins
   } else {
     U = *a.many_units;

@@ -487,6 +487,71 @@ def test_bad_tables_and_lengths_are_reported(M, n_q):
     assert status(table, [100, 100]) == 0
 
 
+def heavy(Hq):
+    """A request's tokens and queries that take a call past the work up to which one form serves all its requests."""
+    return 6100, 2800 // Hq + 1
+
+
+@pytest.mark.parametrize("name", ["bf16", "fp16"])
+@pytest.mark.parametrize("Hq,H,D,S,causal,window", [
+    (8, 2, 128, 16, True, 0), (4, 4, 128, 32, True, 0), (8, 1, 64, 16, True, 0), (3, 1, 128, 48, False, 0),
+    (4, 2, 64, 64, True, 200), (8, 1, 128, 16, True, 77), (5, 1, 64, 16, False, 300), (6, 3, 64, 16, True, 1)])
+def test_chunks_of_much_work(M, name, Hq, H, D, S, causal, window):
+    n, m = heavy(Hq)
+    lens = [513, 700, 128, n, 1100, 65, 0, 300, 0, 1, 2, 20, 64, 90, 257]
+    n_q = [513, 200, 128, m, 257, 65, 40, 1, 130, 99, 100, 97, 200, 0, 33]
+    check(M, np.random.default_rng(Hq * 11 + D), lens, n_q, Hq, H, D, S, name, causal=causal, window=window)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Hq,H", [(1, 1), (4, 2)])
+def test_rows_about_where_forms_end_in_much_work(M, Hq, H, D):
+    n, m = heavy(Hq)
+    n_q = [96, 97, 127, 128, 129, m, 255, 256, 257, 385, 48, 49, 64, 65, 1, 0]
+    lens = [90, 97, 140, 128, 700, n, 100, 256, 300, 385, 48, 500, 64, 66, 1, 20]
+    check(M, np.random.default_rng(14), lens, n_q, Hq, H, D, 32, "bf16", how="odd")
+    check(M, np.random.default_rng(15), lens, n_q, Hq, H, D, 16, "fp16", window=33)
+
+
+@pytest.mark.parametrize("gain,scale", [(30.0, None), (1.0, 0.0), (1.0, -0.1), (1e-4, 1.0), (200.0, 1.0)])
+def test_peaked_and_flat_weights_of_much_work(M, gain, scale):
+    n, m = heavy(4)
+    for name in ("bf16", "fp16"):
+        check(M, np.random.default_rng(16), [300, n, 260], [200, m, 256], 4, 2, 64, 16, name, gain=gain, scale=scale)
+
+
+def test_many_short_requests_beside_much_work(M):
+    rng = np.random.default_rng(17)
+    n, m = heavy(2)
+    lens = rng.integers(0, 40, 2300).tolist() + [n]
+    check(M, rng, lens, np.append(rng.integers(0, 3, 2300), m), 2, 1, 64, 16, "fp16")
+
+
+def test_nan_keys_in_much_work(M):
+    rng = np.random.default_rng(18)
+    T, n_q = 21500, 200
+    k = torch.randn(T, 1, 128, device="cuda").bfloat16()
+    v = torch.randn(T, 1, 128, device="cuda").bfloat16()
+    k[T - 2] = float("nan")
+    blocks = T // 16 + 1
+    cache = torch.zeros(M.kv4_cache_shape(blocks, 1, 16, 128), dtype=torch.uint8, device="cuda")
+    table = dev(rng.permutation(blocks)[None].astype(np.int32))
+    p = torch.arange(T, device="cuda")
+    ws = M.Workspace()
+    assert M.maps_kv4_append(k, v, table[0, p // 16].long() * 16 + p % 16, cache, 16, ws=ws) == 0
+    q = torch.randn(n_q, 4, 128, device="cuda").bfloat16()
+    out = torch.zeros_like(q)
+    args = (q, dev(np.array([0, n_q])), dev(np.array([T], np.int32)))
+    assert M.maps_kv4_attention(*args, table, cache, 16, 0.09, out, ws=ws) == 0
+    assert M.maps_check(ws) == 0
+    assert torch.isfinite(out[:-2]).all() and torch.isnan(out[-2:]).all()
+    for wrong in (-1, blocks, 2**31 - 1, -2**31):
+        t = table.clone()
+        t[0, 900] = wrong
+        assert M.maps_kv4_attention(*args, t, cache, 16, 0.09, out, ws=ws) == 0
+        assert M.maps_check(ws) == M.MAPS_E_RANGE
+
+
 def test_sweep(M):
     """Random shapes, types, lengths, windows and layouts."""
     rng = np.random.default_rng(12)
