@@ -588,6 +588,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
           rescale(run);
           if (lane == 0 && (warp & 3) == 0) reinterpret_cast<volatile int *>(smem + L::kAgain)[t] = 1;
           pending = false;
+          tm_wait_store();  // the weights have to be there before the next scores take their place
           tc_before();
           __syncwarp();
           if (lane == 0) bar_arrive(p_full(t));
