@@ -431,7 +431,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(con
       const int32_t seg_first = at.tile;
       for (; u < seg_end; ++u, ++at.tile) {
         if (at.tile == 0) continue;
-        if (!bar_wait(bar32 + 8 * stage, parity)) {
+        if (!warp_wait(bar32 + 8 * stage, parity)) {
           if (lane == 0) flag_error(a.status, MAPS_E_TIMEOUT);
           alive = false;
           break;

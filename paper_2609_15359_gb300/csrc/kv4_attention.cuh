@@ -77,11 +77,14 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
   asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(bar), "r"(parity), "r"(20000u) : "memory");
   return ok != 0;
 }
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {  // bounded
-  for (uint32_t i = 0; i < (1u << 18); ++i)
+constexpr uint32_t kTries = 1u << 18;
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, uint32_t tries = kTries) {  // bounded
+  for (uint32_t i = 0; i < tries; ++i)
     if (bar_try(bar, parity)) return true;
   return false;
 }
+// The same for a warp, whose lanes go on, or give up, together.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, uint32_t tries = kTries) { return __all_sync(0xffffffffu, bar_wait(bar, parity, tries)); }
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }

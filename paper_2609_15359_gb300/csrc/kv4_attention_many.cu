@@ -31,6 +31,7 @@
 // Split.  As in the other form, a call's steps are dealt out to the blocks in equal runs, whatever the
 // lengths; what a run begins or ends inside of is left as parts, which a second kernel joins.
 #include "kv4_attention.cuh"
+#include "maps_bench.h"
 
 namespace maps {
 namespace {
@@ -39,6 +40,13 @@ constexpr int kThreads = 512;
 constexpr int kItemUnits = 3;  // what an item costs besides its steps, in steps: its queries, its output, the pipeline's start
 constexpr int kRows = 256, kTok = 128, kStepGroups = kTok / kGroup;
 constexpr int kRing = 3;  // steps of the cache's records under way or waiting
+
+// Test aid (maps_test_attention_withhold): the block whose keys are never said to be there (-1: none), so that the waits of all
+// its warps run out, and the tries after which a wait gives up.
+__constant__ int32_t c_withheld = -1;
+__constant__ uint32_t c_tries = kTries;
+__device__ __forceinline__ bool one_wait(uint32_t bar, uint32_t parity) { return bar_wait(bar, parity, c_tries); }
+__device__ __forceinline__ bool all_wait(uint32_t bar, uint32_t parity) { return warp_wait(bar, parity, c_tries); }
 
 struct MReq {
   int64_t q0;
@@ -225,8 +233,7 @@ struct Lay {  // shared memory, from a 1,024-byte boundary
   static constexpr int kNan = kRow + kRows * 16;     // [4][4] bits: values held as NaN
   static constexpr int kExp = kNan + 64;             // [4] the step's exponent
   static constexpr int kAgain = kExp + 16;           // [2] a tile's scores are wanted again
-  static constexpr int kFail = kAgain + 8;           // a wait has run out
-  static constexpr int kBars = kFail + 8;
+  static constexpr int kBars = kAgain + 8;
   static constexpr int kSegAt = kBars + 8 * (2 * kRing + 14 + 2 * kSegs);
   static constexpr int kBytes = kSegAt + kSegs * static_cast<int>(sizeof(Seg));
   static constexpr int kPart = kRows * D + 2 * kRows;  // floats of a part: sums, maxima, totals
@@ -236,7 +243,7 @@ template <int D>
 constexpr bool lay_aligned() {  // to what is read and written there at once
   using L = Lay<D>;
   return L::kK % 1024 == 0 && L::kV % 1024 == 0 && L::kRingAt % 16 == 0 && L::kStep % 16 == 0 && L::kPar % 16 == 0 && L::kRow % 16 == 0 && L::kNan % 16 == 0 &&
-         L::kExp % 4 == 0 && L::kAgain % 4 == 0 && L::kFail % 4 == 0 && L::kBars % 8 == 0 && L::kSegAt % alignof(Seg) == 0;
+         L::kExp % 4 == 0 && L::kAgain % 4 == 0 && L::kBars % 8 == 0 && L::kSegAt % alignof(Seg) == 0;
 }
 static_assert(lay_aligned<64>() && lay_aligned<128>(), "alignment");
 
@@ -286,7 +293,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
   if (tid == 0) a.many_open[me].tiles = 0;
   if (U == 0) return;  // no request here has many queries
   if (tid == 0) {
-    for (int i = 0; i < 3; ++i) reinterpret_cast<int *>(smem + L::kAgain)[i] = 0;
+    for (int i = 0; i < 2; ++i) reinterpret_cast<int *>(smem + L::kAgain)[i] = 0;
     for (int i = 0; i < kRing; ++i) bar_init(step_full(i), kStepGroups), bar_init(step_free(i), 5);
     bar_init(v_full, 4), bar_init(v_free, 1);
     for (int i = 0; i < 2; ++i) {
@@ -317,10 +324,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
   auto ring_on = [&]() {
     if (++place == kRing) place = 0, round ^= 1u;
   };
-  auto hear = [&](bool &ok) {
-    ok = bar_wait(seg_full(n_seg % kSegs), n_seg / kSegs & 1);
-    return ok && reinterpret_cast<const Seg *>(smem + L::kSegAt)[n_seg % kSegs].steps >= 0;
-  };
+  auto more = [&](bool ok) { return ok && reinterpret_cast<const Seg *>(smem + L::kSegAt)[n_seg % kSegs].steps >= 0; };
+  auto hear = [&](bool &ok) { return more(ok = all_wait(seg_full(n_seg % kSegs), n_seg / kSegs & 1)); };
+  auto hear_alone = [&](bool &ok) { return more(ok = one_wait(seg_full(n_seg % kSegs), n_seg / kSegs & 1)); };
   auto told = [&]() -> const Seg & { return reinterpret_cast<const Seg *>(smem + L::kSegAt)[n_seg % kSegs]; };
   auto done = [&]() { bar_arrive(seg_free(n_seg++ % kSegs)); };  // by one lane
 
@@ -330,8 +336,13 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
     const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;  // 32 lanes of tensor memory to a warp
     const uint32_t s_at = tmem + lanes + t * 128, o_at = tmem + lanes + 256 + t * 128;
     uint32_t c = 0, n_s = 0, n_o = 0;  // steps, scores and sums so far
+    // A wait that has run out in one warp ends the four warps of its tile together, at their next vote: a warp that left alone
+    // would leave the others in a barrier without an end.  So between votes a failure is carried on.
     bool ok = true, failed = false;
-    while (hear(ok)) {
+    for (;;) {
+      const bool another = ok && hear(ok);
+      ok = !tile_any(1 + t, !ok);
+      if (!ok || !another) break;
       const Seg &w = told();
       const int steps = w.steps, tok_at = w.token;
       if (t == 1 && !w.second) {
@@ -433,7 +444,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
 
       for (int j = 0; j < steps; ++j, ++c) {
         const int buf = c & 3;
-        ok = bar_wait(s_full(t), n_s & 1);
+        ok = all_wait(s_full(t), n_s & 1);
         ++n_s;
         tc_after();
         const uint4 *par = reinterpret_cast<const uint4 *>(smem + L::kPar + buf * kTok * 8);
@@ -487,7 +498,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
         const int E = reinterpret_cast<const int *>(smem + L::kExp)[buf];
         // the sums so far to the maxima in top, where larger, and to exponent en: the product before has to be done
         auto rescale = [&](int en) {
-          if (j > 0 && !bar_wait(o_full(t), (n_o - 1) & 1)) failed = true;
+          if (j > 0 && !all_wait(o_full(t), (n_o - 1) & 1)) failed = true;
           tc_after();
           const float f_run = ex2(static_cast<float>(run - en));
           float f[4];
@@ -581,9 +592,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
           pending |= top[e] > fm[e] + kSlack;
         }
         pending = __any_sync(0xffffffffu, pending);
-        if (!ok || failed) *reinterpret_cast<volatile int *>(smem + L::kFail) = 1;
         if (tile_any(1 + t, again || !ok || failed)) {  // every warp of the tile comes here once for every wait on s_full
-          ok = !*reinterpret_cast<volatile int *>(smem + L::kFail);
+          ok = !tile_any(1 + t, !ok || failed);
           if (!ok) break;
           rescale(run);
           if (lane == 0 && (warp & 3) == 0) reinterpret_cast<volatile int *>(smem + L::kAgain)[t] = 1;
@@ -636,8 +646,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
       const bool whole = w.whole;
       const uint32_t id = w.id;
       if (steps > 0) {
-        ok = bar_wait(o_full(t), (n_o - 1) & 1);
-        if (!ok) break;
+        ok = all_wait(o_full(t), (n_o - 1) & 1);
+        if (!ok) continue;  // to the vote
         tc_after();
       }
       const float f = whole ? (l == 0.0f ? 0.0f : ex2(static_cast<float>(run)) / l) : run == kNoExp ? 0.0f : ex2(static_cast<float>(run));
@@ -694,7 +704,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
     while (hear(ok)) {
       const int steps = told().steps, tok_at = told().token, hi = told().hi;
       for (int j = 0; j < steps; ++j, ++c) {
-        ok = bar_wait(step_full(place), round);
+        ok = all_wait(step_full(place), round);
         if (!ok) break;
         const int32_t tok0 = tok_at + j * kTok;
         auto record = [&](int g) -> const uint8_t * { return smem + L::kRingAt + place * L::kStep + g * kv4_group_bytes(D); };
@@ -724,7 +734,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
           vs[e] = pack_half(p0.x * down, p1.x * down);
           vz[e] = pack_half(p0.y * down, p1.y * down);
         }
-        ok = bar_wait(v_free, (c & 1) ^ 1);
+        ok = all_wait(v_free, (c & 1) ^ 1);
         if (!ok) break;
         uint8_t *V = smem + L::kV;
 #pragma unroll 1
@@ -808,12 +818,12 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
           mma_ts(256 + t * 128, t * 128 + 8 * k, rows_desc(base + L::kV) + (k / 4 * (D * 8) + k % 4 * 2), kPV, more || k > 0);
         tc_commit(o_full(t));
       };
-      while (hear(ok)) {
+      while (hear_alone(ok)) {
         const int steps = told().steps, tiles = told().second ? 2 : 1;
         done();
         if (steps == 0) continue;
-        for (int t = 0; t < tiles && ok; ++t) ok = bar_wait(q_full(t), n_q[t]++ & 1);
-        ok = ok && bar_wait(k_full(c & 1), c >> 1 & 1);
+        for (int t = 0; t < tiles && ok; ++t) ok = one_wait(q_full(t), n_q[t]++ & 1);
+        ok = ok && one_wait(k_full(c & 1), c >> 1 & 1);
         if (!ok) break;
         tc_after();
         for (int t = 0; t < tiles; ++t) scores(t, c & 1);
@@ -821,7 +831,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
           const int buf = c & 1;
           for (int t = 0; t < tiles; ++t) {
             for (;;) {
-              ok = bar_wait(p_full(t), n_p[t]++ & 1);
+              ok = one_wait(p_full(t), n_p[t]++ & 1);
               if (!ok) break;
               tc_after();
               volatile int *again = reinterpret_cast<volatile int *>(smem + L::kAgain) + t;
@@ -831,14 +841,14 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
             }
             if (!ok) break;
             if (t == tiles - 1) tc_commit(k_free(buf));  // nobody wants these scores again
-            ok = t > 0 || bar_wait(v_full, c & 1);
+            ok = t > 0 || one_wait(v_full, c & 1);
             if (!ok) break;
             tc_after();
             sums(t, j > 0);
             if (t == tiles - 1) tc_commit(v_free);
             if (j + 1 < steps) {
               if (t == 0) {
-                ok = bar_wait(k_full(buf ^ 1), (c + 1) >> 1 & 1);
+                ok = one_wait(k_full(buf ^ 1), (c + 1) >> 1 & 1);
                 if (!ok) break;
                 tc_after();
               }
@@ -871,7 +881,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
               }
               at = block * a.block_bytes + (head_groups + grp - page * a.block_groups) * static_cast<int64_t>(kv4_group_bytes(D));
             }
-            ok = bar_wait(step_free(place), round ^ 1u);
+            ok = one_wait(step_free(place), round ^ 1u);
             if (ok) {
               bar_expect(step_full(place), load ? kv4_group_bytes(D) : 0);
               if (load) bulk_load(base + L::kRingAt + place * L::kStep + lane * kv4_group_bytes(D), a.cache + at, kv4_group_bytes(D), step_full(place));
@@ -885,7 +895,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
       if (!ok) {
         if (lane == 0) flag_error(a.status, MAPS_E_TIMEOUT);
         // let what is under way land: a step's barrier is over once all of it has
-        for (int i = 0; i < kRing; ++i) (void)bar_wait(step_full(i), 0), (void)bar_wait(step_full(i), 1);
+        for (int i = 0; i < kRing; ++i) (void)all_wait(step_full(i), 0), (void)all_wait(step_full(i), 1);
       }
     } else if (warp == 15) {
       // ====================================================================== keys
@@ -895,7 +905,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
         const int steps = told().steps, tok_at = told().token, hi = told().hi;
         for (int j = 0; j < steps; ++j, ++c) {
           const int buf = c & 1;
-          ok = bar_wait(step_full(place), round) && bar_wait(k_free(buf), (c >> 1 & 1) ^ 1);
+          ok = all_wait(step_full(place), round) && all_wait(k_free(buf), (c >> 1 & 1) ^ 1);
           if (!ok) break;
           const int32_t tok0 = tok_at + j * kTok;
           auto record = [&](int g) -> const uint8_t * { return smem + L::kRingAt + place * L::kStep + g * kv4_group_bytes(D); };
@@ -961,7 +971,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
         }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
-          if (lane == 0) bar_arrive(step_free(place)), bar_arrive(k_full(buf));
+          if (lane == 0) {
+            bar_arrive(step_free(place));
+            if (static_cast<int>(me) != c_withheld) bar_arrive(k_full(buf));
+          }
           ring_on();
         }
         if (!ok) break;
@@ -974,7 +987,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
       // ====================================================================== the block's items
       bool ok = true;
       auto tell = [&](const Seg &x) {
-        ok = bar_wait(seg_free(n_seg % kSegs), (n_seg / kSegs & 1) ^ 1);
+        ok = one_wait(seg_free(n_seg % kSegs), (n_seg / kSegs & 1) ^ 1);
         if (!ok) return;
         reinterpret_cast<Seg *>(smem + L::kSegAt)[n_seg % kSegs] = x;
         bar_arrive(seg_full(n_seg++ % kSegs));
@@ -1099,3 +1112,11 @@ int attn_many(int32_t dtype, int D, const AttnArgs &a, cudaStream_t s) {
 }
 
 }  // namespace maps
+
+extern "C" int maps_test_attention_withhold(int32_t block, uint32_t spin_limit) {
+  using namespace maps;
+  const uint32_t tries = spin_limit == 0 ? kTries : spin_limit;
+  MAPS_TRY(cuda_ok(cudaMemcpyToSymbol(c_withheld, &block, sizeof(block))));
+  MAPS_TRY(cuda_ok(cudaMemcpyToSymbol(c_tries, &tries, sizeof(tries))));
+  return MAPS_OK;
+}
