@@ -564,13 +564,13 @@ int maps_kv4_read(int32_t dtype, int64_t T, int32_t H, int32_t D, int32_t S, con
  * not used, whatever it is.
  *
  *   dtype               MAPS_BF16 or MAPS_F16, of q and out.
- *   B, T                requests (>= 0) and rows of q (T <= 2^30).
+ *   B, T                requests (>= 0) and rows of q (T <= 2^30, T * Hq <= 2^31 - 1,024).
  *   Hq, Hkv             query and KV heads, Hq a multiple of Hkv, Hq <= 65,535.
  *   D, S, cache, n_blocks   as for maps_kv4_append.
  *   q, out              element (i, x, d) is at i * row + x * head + d; rows
  *                       that no request has are neither read nor written.
  *   qo_off              [B + 1] int64, non-decreasing within [0, T].
- *   kv_len              [B] int32 tokens in the cache, in [0, max_blocks * S].
+ *   kv_len              [B] int32 tokens in the cache, in [0, max_blocks * S] and at most 2^31 - 1,024.
  *   table               [B][max_blocks] int32 block tables.
  *   causal, window      0 or 1; 0 (no window) or the keys seen, >= 1.
  *   lse                 [T][Hq] float output, natural logarithm, or NULL.

@@ -104,7 +104,7 @@ __device__ __forceinline__ Req request(const AttnArgs &a, int b, int32_t over) {
   const int64_t q0 = a.off[b], q1 = a.off[b + 1];
   int32_t n = a.len[b];
   int64_t m = q1 - q0;
-  if (n < 0 || n > a.max_blocks * a.S) {
+  if (!length_ok(a, n)) {
     flag_error(a.status, MAPS_E_RANGE);
     n = 0;
   }
@@ -842,7 +842,7 @@ int maps_kv4_attention(int32_t dtype, int32_t B, int64_t T, int32_t Hq, int32_t 
   using namespace maps;
   if ((dtype != MAPS_BF16 && dtype != MAPS_F16) || !kv4_dim_ok(D) || !kv4_block_ok(S) || B < 0 ||
       T < 0 || T > (int64_t(1) << 30) || Hkv < 1 || Hq < Hkv || Hq % Hkv != 0 || Hq > 65535 ||
-      T > ((int64_t(1) << 31) - 64) / Hq || max_blocks < 0 || max_blocks > 0x7fffffff || n_blocks < 0 || window < 0 ||
+      T > ((int64_t(1) << 31) - 1024) / Hq || max_blocks < 0 || max_blocks > 0x7fffffff || n_blocks < 0 || window < 0 ||
       (causal != 0 && causal != 1) || !(sm_scale - sm_scale == 0.0f))
     return MAPS_E_INVALID;
   MAPS_TRY(check_ws(ws, ws_bytes, maps_kv4_attention_workspace_size(B, T, Hq, Hkv, D)));

@@ -30,6 +30,9 @@ inline int attn_grid() { return sm_count() < kMaxGrid ? sm_count() : kMaxGrid; }
 
 struct Part;
 
+// Tokens a request can have: places a unit or a step past them are still counted in 32 bits.
+constexpr int32_t kMaxLen = 0x7fffffff - 1023;
+
 struct AttnArgs {
   int32_t B, Hq, Hkv, S;
   int64_t T, n_blocks, max_blocks;
@@ -63,6 +66,8 @@ struct Part {
   uint32_t id, tiles;
   int32_t rows, h, rt;
 };
+
+__device__ __forceinline__ bool length_ok(const AttnArgs &a, int32_t n) { return n >= 0 && n <= kMaxLen && n <= a.max_blocks * a.S; }
 
 // ---------------------------------------------------------------------------- small device helpers
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
@@ -144,7 +149,7 @@ __device__ __forceinline__ int32_t many_over(const AttnArgs &a) {
   for (int b = threadIdx.x; b < a.B; b += kN) {
     const int64_t q0 = a.off[b], q1 = a.off[b + 1], rows = (q1 - q0) * group;
     const int32_t n = a.len[b];
-    if (n < 0 || n > a.max_blocks * a.S || q0 < 0 || q1 < q0 || q1 > a.T || rows <= a.few_rows) continue;
+    if (!length_ok(a, n) || q0 < 0 || q1 < q0 || q1 > a.T || rows <= a.few_rows) continue;
     pairs += min(static_cast<uint64_t>(rows) * static_cast<uint64_t>(n), uint64_t(1) << 32);
   }
   if (pairs) atomicAdd(&s_pairs, static_cast<unsigned long long>(pairs));

@@ -58,7 +58,7 @@ __device__ __forceinline__ MReq many_request(const AttnArgs &a, int b) {
   const int64_t q0 = a.off[b], q1 = a.off[b + 1];
   int64_t m = q1 - q0;
   int32_t n = a.len[b];
-  if (n < 0 || n > a.max_blocks * a.S || q0 < 0 || m < 0 || q1 > a.T) n = 0, m = 0;  // the other form has reported it
+  if (!length_ok(a, n) || q0 < 0 || m < 0 || q1 > a.T) n = 0, m = 0;  // the other form has reported it
   const int64_t rows = m * (a.Hq / a.Hkv);
   r.q0 = q0;
   r.n = n;
