@@ -468,7 +468,7 @@ int maps_rr_pressure(const maps_rr_cfg *cfg, int64_t n_real, const int64_t *arri
  *   3. the new tokens of r are the positions held .. want - 1, at the indices
  *      slot_off_out[r] .. slot_off_out[r + 1] of the outputs, granted or not.
  *
- *   R, S                requests (>= 0) and block size (>= 1).
+ *   R, S                requests (0 .. 2^30) and block size (>= 1).
  *   held, want          [R] int32 tokens, in [0, max_blocks * S].
  *   order               [R] int32 permutation of the requests (such as
  *                       maps_order_local's), or NULL for index order.

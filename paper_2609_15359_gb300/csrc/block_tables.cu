@@ -452,7 +452,8 @@ int maps_block_tables(int32_t R, int32_t S, const int32_t *held, const int32_t *
                       int64_t *slots_out, int64_t slots_cap, int32_t *pos_out, void *ws,
                       size_t ws_bytes, void *stream) {
   using namespace maps;
-  if (R < 0 || S < 1 || max_blocks < 0 || pool < 0 || slots_cap < 0 ||
+  // R: a thread's place in the last tile of 1,024 requests stays a 32-bit number
+  if (R < 0 || R > 1 << 30 || S < 1 || max_blocks < 0 || pool < 0 || slots_cap < 0 ||
       slots_cap > (int64_t(1) << 38))
     return MAPS_E_INVALID;
   if (n_free == nullptr || n_free_out == nullptr || slot_off_out == nullptr) return MAPS_E_INVALID;
