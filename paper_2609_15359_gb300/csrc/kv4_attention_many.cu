@@ -612,7 +612,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
           y.v = total[e];
           fl[e] = fmaf(y.f[0] + y.f[1], up, fl[e]);
         }
-        // a value held as NaN is left out of the product, and makes a row that sees it NaN here
+        // A value held as NaN is left out of the product.  A row that sees one is marked, in the place of what a score is to be
+        // multiplied by, which is in registers: its output is NaN, its sum of weights is not.
         const uint4 nans = reinterpret_cast<const uint4 *>(smem + L::kNan)[buf];
         if (nans.x | nans.y | nans.z | nans.w) {
 #pragma unroll 1
@@ -621,7 +622,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
             if (!(word >> (col & 31) & 1u)) continue;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              if (tok0 + col >= flo[e] && tok0 + col < fhi[e]) fl[e] = NAN;
+              if (tok0 + col >= flo[e] && tok0 + col < fhi[e]) row_of[(warp & 3) * 32 + 8 * e + (lane >> 2)].y = NAN;
           }
         }
         tm_wait_store();
@@ -650,7 +651,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
         if (!ok) continue;  // to the vote
         tc_after();
       }
-      const float f = whole ? (l == 0.0f ? 0.0f : ex2(static_cast<float>(run)) / l) : run == kNoExp ? 0.0f : ex2(static_cast<float>(run));
+      __syncwarp();
+      const bool nan = steps > 0 && isnan(row_of[row].y);
+      const float f = nan ? NAN : whole ? (l == 0.0f ? 0.0f : ex2(static_cast<float>(run)) / l) : run == kNoExp ? 0.0f : ex2(static_cast<float>(run));
       T *dst = static_cast<T *>(a.out) + i * a.o_row + hq * a.o_head;
       const int at = t * 128 + row;
       float *part = a.many_parts + (static_cast<int64_t>(me) * 2 + (id < u0 ? 0 : 1)) * L::kPart;
