@@ -153,20 +153,58 @@ def _ptr(t, dtype=None) -> int | None:
 
 
 class Workspace:
-    """Zero-filled device scratch owned by the caller, grown on demand."""
+    """Zero-filled device scratch owned by the caller, grown on demand.
 
-    def __init__(self, nbytes: int = 0, device=None):
+    It is allocated and zero-filled on the stream of the call that needs it (the
+    current one where it is made beforehand).  A call on another stream first waits
+    for that, and the memory is not handed out again before that stream is done."""
+
+    def __init__(self, nbytes: int = 0, device=None, stream=None):
         self.device = torch.device("cuda") if device is None else torch.device(device)
-        self._take(max(int(nbytes), 256))
+        self.on_gpu = self.device.type == "cuda"
+        self._take(max(int(nbytes), 256), stream)
 
-    def _take(self, nbytes: int) -> None:
-        self.buf = torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
+    def _take(self, nbytes: int, stream=None) -> None:
+        self.filled, self.known = None, set()  # the zero-fill, and the streams that are behind it
+        if self.on_gpu:
+            s = torch.cuda.current_stream(self.device) if stream is None else stream
+            with torch.cuda.stream(s):
+                self.buf = torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
+                if not torch.cuda.is_current_stream_capturing():
+                    self.filled = torch.cuda.Event()
+                    self.filled.record(s)
+            self.known.add(s.cuda_stream)
+        else:
+            self.buf = torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
+            self.known.add(None)
         self.ptr, self.nbytes = self.buf.data_ptr(), nbytes
 
-    def ensure(self, nbytes: int) -> "Workspace":
+    def _meet(self, stream) -> None:
+        s = torch.cuda.current_stream(self.device) if stream is None else stream
+        with torch.cuda.stream(s):
+            # what was queued before a capture began is done by the time that its graph runs
+            if self.filled is not None and not torch.cuda.is_current_stream_capturing():
+                s.wait_event(self.filled)
+        self.buf.record_stream(s)
+        self.known.add(s.cuda_stream)
+
+    def ensure(self, nbytes: int, stream=None) -> "Workspace":
+        """At least `nbytes`, to be used by work on `stream` (the current one)."""
         if nbytes > self.nbytes:
-            self._take(int(nbytes))
+            self._take(int(nbytes), stream)
+        elif self.on_gpu and _stream(stream) not in self.known:
+            self._meet(stream)
         return self
+
+
+def _scratch(ws: Workspace | None, nbytes: int, stream):
+    """The workspace of a call that needs `nbytes`, and its stream's handle."""
+    if ws is None:
+        ws = Workspace(nbytes, stream=stream)
+    on = _stream(stream) if ws.on_gpu else None
+    if nbytes > ws.nbytes or on not in ws.known:
+        ws.ensure(nbytes, stream)
+    return ws, on
 
 
 @functools.lru_cache(maxsize=4096)
@@ -194,14 +232,13 @@ def maps_calibrate(true_len, pred_len, alpha_ppm: int, query_pred=None, bound_ou
     """Returns (status, q) where q is the host quantile when ``q_host``."""
     n = true_len.numel()
     m = 0 if query_pred is None else query_pred.numel()
-    ws = ws or Workspace()
-    ws.ensure(lib.maps_calibrate_workspace_size(n, m))
+    ws, on = _scratch(ws, lib.maps_calibrate_workspace_size(n, m), stream)
     qh = ctypes.c_int32(0)
     st = lib.maps_calibrate(_ptr(true_len, torch.int32), _ptr(pred_len, torch.int32), n,
                             int(alpha_ppm), _ptr(query_pred, torch.int32), m,
                             _ptr(bound_out, torch.int32), _ptr(q_dev_out, torch.int32),
                             ctypes.byref(qh) if q_host else None, ws.ptr, ws.nbytes,
-                            _stream(stream))
+                            on)
     return st, (int(qh.value) if q_host else None)
 
 
@@ -213,13 +250,12 @@ def kmax_shape(D: int, H: int) -> tuple[int, int]:
 def maps_project_occupancy(D: int, H: int, res_off, prompt, gen, bound, K_out, kmax_out=None,
                            ws: Workspace | None = None, stream=None) -> int:
     R = prompt.numel()
-    ws = ws or Workspace()
-    ws.ensure(lib.maps_project_occupancy_workspace_size(D, H, R))
+    ws, on = _scratch(ws, lib.maps_project_occupancy_workspace_size(D, H, R), stream)
     return lib.maps_project_occupancy(D, H, _ptr(res_off, torch.int64), R,
                                       _ptr(prompt, torch.int32), _ptr(gen, torch.int32),
                                       _ptr(bound, torch.int32), _ptr(K_out, torch.int32),
                                       _ptr(kmax_out, torch.int32), ws.ptr, ws.nbytes,
-                                      _stream(stream))
+                                      on)
 
 
 def maps_dispatch(mode: int, D: int, H: int, S: int, K, cap, Q, cand_prompt, cand_bound,
@@ -227,8 +263,7 @@ def maps_dispatch(mode: int, D: int, H: int, S: int, K, cap, Q, cand_prompt, can
                   bound=None, kmax=None, ws: Workspace | None = None, stream=None) -> int:
     J = cand_prompt.numel()
     R = 0 if prompt is None else prompt.numel()
-    ws = ws or Workspace()
-    ws.ensure(lib.maps_dispatch_workspace_size(mode, D, H, J))
+    ws, on = _scratch(ws, lib.maps_dispatch_workspace_size(mode, D, H, J), stream)
     return lib.maps_dispatch(mode, D, H, S, _ptr(K, torch.int32), _ptr(kmax, torch.int32),
                              _ptr(cap, torch.int32),
                              _ptr(Q, torch.int32), _ptr(res_off, torch.int64), R,
@@ -236,19 +271,18 @@ def maps_dispatch(mode: int, D: int, H: int, S: int, K, cap, Q, cand_prompt, can
                              _ptr(bound, torch.int32), J, _ptr(cand_prompt, torch.int32),
                              _ptr(cand_bound, torch.int32), _ptr(choice_out, torch.int32),
                              _ptr(headroom_out, torch.int64), ws.ptr, ws.nbytes,
-                             _stream(stream))
+                             on)
 
 
 def maps_order_local(D: int, dec, bound, wait, arrival, max_wait: int, perm_out, seg_off_out,
                      ws: Workspace | None = None, stream=None) -> int:
     N = dec.numel()
-    ws = ws or Workspace()
-    ws.ensure(lib.maps_order_local_workspace_size(N, D))
+    ws, on = _scratch(ws, lib.maps_order_local_workspace_size(N, D), stream)
     return lib.maps_order_local(N, D, _ptr(dec, torch.int32), _ptr(bound, torch.int32),
                                 _ptr(wait, torch.int32), _ptr(arrival, torch.int32),
                                 int(max_wait), _ptr(perm_out, torch.int32),
                                 _ptr(seg_off_out, torch.int64), ws.ptr, ws.nbytes,
-                                _stream(stream))
+                                on)
 
 
 def maps_order_local_static(D: int, dec, bound, wait, arrival, max_wait: int, perm_out,
@@ -280,15 +314,14 @@ def maps_stream_run(cfg: StreamCfg, arrival_ms, prompt, true_len, pred, choice_o
     """The whole streaming loop on the device; returns the full status.
     dec_stats_out: optional [D][4] int64 per-decoder statistics; pred_delay:
     [N] int32 prediction delays (required when cfg.beta >= 0)."""
-    ws = ws or Workspace()
-    ws.ensure(lib.maps_stream_workspace_size(ctypes.byref(cfg)))
+    ws, on = _scratch(ws, lib.maps_stream_workspace_size(ctypes.byref(cfg)), stream)
     return lib.maps_stream_run(ctypes.byref(cfg), _ptr(arrival_ms, torch.int64),
                                _ptr(prompt, torch.int32), _ptr(true_len, torch.int32),
                                _ptr(pred, torch.int32), _ptr(pred_delay, torch.int32),
                                _ptr(choice_out, torch.int32),
                                _ptr(q_out, torch.int32), _ptr(stats_out, torch.int64),
                                _ptr(dec_stats_out, torch.int64), ws.ptr, ws.nbytes,
-                               _stream(stream))
+                               on)
 
 
 def maps_rr_pressure(N: int, C: int, t_tok_us: int, theta_ppm: int, arrival_us, prompt, out_len,
@@ -300,13 +333,12 @@ def maps_rr_pressure(N: int, C: int, t_tok_us: int, theta_ppm: int, arrival_us, 
     t_sim [n_real] int64."""
     n_real, n_req = arrival_us.shape
     cfg = RRCfg(int(n_req), int(N), int(C), int(t_tok_us), int(theta_ppm))
-    ws = ws or Workspace()
-    ws.ensure(lib.maps_rr_pressure_workspace_size(ctypes.byref(cfg), n_real))
+    ws, on = _scratch(ws, lib.maps_rr_pressure_workspace_size(ctypes.byref(cfg), n_real), stream)
     return lib.maps_rr_pressure(ctypes.byref(cfg), n_real, _ptr(arrival_us, torch.int64),
                                 _ptr(prompt, torch.int32), _ptr(out_len, torch.int32),
                                 _ptr(admit_out, torch.int64), _ptr(done_out, torch.int64),
                                 _ptr(stats_out, torch.int64), _ptr(t_sim_out, torch.int64),
-                                ws.ptr, ws.nbytes, _stream(stream))
+                                ws.ptr, ws.nbytes, on)
 
 
 def maps_block_tables(S: int, held, want, table, free_blocks, n_free, n_free_out, got_out,
@@ -315,8 +347,7 @@ def maps_block_tables(S: int, held, want, table, free_blocks, n_free, n_free_out
     """Hands out the KV blocks: table [R][max_blocks] and free_blocks [pool]
     int32 are updated in place; slots_out [cap] int64 holds the new tokens'."""
     R = held.numel()
-    ws = ws or Workspace()
-    ws.ensure(_need("maps_block_tables_workspace_size", R))
+    ws, on = _scratch(ws, _need("maps_block_tables_workspace_size", R), stream)
     return lib.maps_block_tables(R, S, _ptr(held, torch.int32), _ptr(want, torch.int32),
                                  _ptr(order, torch.int32), _ptr(table, torch.int32),
                                  table.shape[1], _ptr(free_blocks, torch.int32),
@@ -324,7 +355,7 @@ def maps_block_tables(S: int, held, want, table, free_blocks, n_free, n_free_out
                                  _ptr(n_free_out, torch.int32), _ptr(got_out, torch.int32),
                                  _ptr(slot_off_out, torch.int64), _ptr(slots_out, torch.int64),
                                  slots_out.numel(), _ptr(pos_out, torch.int32), ws.ptr, ws.nbytes,
-                                 _stream(stream))
+                                 on)
 
 
 def _rows(t, dtype=None):
@@ -370,11 +401,10 @@ def maps_kv4_append(k, v, slots, cache, S: int, ws: Workspace | None = None, str
     T, H, D = k.shape
     if v.shape != k.shape or slots.numel() != T:
         raise ValueError("k, v and slots differ in size")
-    ws = ws or Workspace()
-    ws.ensure(_need("maps_kv4_workspace_size"))
+    ws, on = _scratch(ws, _need("maps_kv4_workspace_size"), stream)
     return lib.maps_kv4_append(_dtype(k), T, H, D, S, *_rows(k), *_rows(v, k.dtype),
                                _ptr(slots, torch.int64), _kv4(cache, S, D, H), cache.shape[0],
-                               ws.ptr, ws.nbytes, _stream(stream))
+                               ws.ptr, ws.nbytes, on)
 
 
 def maps_kv4_read(slots, cache, S: int, k_out, v_out, ws: Workspace | None = None,
@@ -383,11 +413,10 @@ def maps_kv4_read(slots, cache, S: int, k_out, v_out, ws: Workspace | None = Non
     T, H, D = k_out.shape
     if v_out.shape != k_out.shape or slots.numel() != T:
         raise ValueError("k_out, v_out and slots differ in size")
-    ws = ws or Workspace()
-    ws.ensure(_need("maps_kv4_workspace_size"))
+    ws, on = _scratch(ws, _need("maps_kv4_workspace_size"), stream)
     return lib.maps_kv4_read(_dtype(k_out), T, H, D, S, _ptr(slots, torch.int64),
                              _kv4(cache, S, D, H), cache.shape[0], *_rows(k_out),
-                             *_rows(v_out, k_out.dtype), ws.ptr, ws.nbytes, _stream(stream))
+                             *_rows(v_out, k_out.dtype), ws.ptr, ws.nbytes, on)
 
 
 def maps_kv4_attention(q, qo_off, kv_len, table, cache, S: int, sm_scale: float, out, lse_out=None,
@@ -402,12 +431,11 @@ def maps_kv4_attention(q, qo_off, kv_len, table, cache, S: int, sm_scale: float,
         raise ValueError("q, out, qo_off, kv_len and table differ in size")
     if lse_out is not None and tuple(lse_out.shape) != (T, Hq):
         raise ValueError("lse_out is [T, Hq]")
-    ws = ws or Workspace()
-    ws.ensure(_need("maps_kv4_attention_workspace_size", B, T, Hq, Hkv, D))
+    ws, on = _scratch(ws, _need("maps_kv4_attention_workspace_size", B, T, Hq, Hkv, D), stream)
     return lib.maps_kv4_attention(_dtype(q), B, T, Hq, Hkv, D, S, *_rows(q),
                                   _ptr(qo_off, torch.int64), _ptr(kv_len, torch.int32),
                                   _ptr(table, torch.int32), table.shape[1],
                                   _kv4(cache, S, D, Hkv), cache.shape[0], float(sm_scale),
                                   int(bool(causal)), int(window), *_rows(out, q.dtype),
                                   _ptr(lse_out, torch.float32), ws.ptr, ws.nbytes,
-                                  _stream(stream))
+                                  on)
