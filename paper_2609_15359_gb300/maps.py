@@ -157,7 +157,9 @@ class Workspace:
 
     It is allocated and zero-filled on the stream of the call that needs it (the
     current one where it is made beforehand).  A call on another stream first waits
-    for that, and the memory is not handed out again before that stream is done."""
+    for that, and the memory is not handed out again before that stream is done.
+    Growing keeps the status word, so maps_check still reads what earlier calls
+    recorded; a call without a workspace has nobody to read its data errors."""
 
     def __init__(self, nbytes: int = 0, device=None, stream=None):
         self.device = torch.device("cuda") if device is None else torch.device(device)
@@ -165,11 +167,16 @@ class Workspace:
         self._take(max(int(nbytes), 256), stream)
 
     def _take(self, nbytes: int, stream=None) -> None:
+        old = getattr(self, "buf", None)
+        if old is not None and self.on_gpu and _stream(stream) not in self.known:
+            self._meet(stream)
         self.filled, self.known = None, set()  # the zero-fill, and the streams that are behind it
         if self.on_gpu:
             s = torch.cuda.current_stream(self.device) if stream is None else stream
             with torch.cuda.stream(s):
                 self.buf = torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
+                if old is not None:
+                    self.buf[:4].copy_(old[:4])
                 if not torch.cuda.is_current_stream_capturing():
                     self.filled = torch.cuda.Event()
                     self.filled.record(s)

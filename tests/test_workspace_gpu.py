@@ -62,3 +62,19 @@ def test_attention_on_another_stream(M, kind, lens, n_q):
     torch.cuda.synchronize()
     assert ws is None or M.maps_check(ws, side) == 0
     assert torch.equal(out, plain) and len(later) == 4
+
+
+def test_an_error_of_the_first_call_outlives_growth(M):
+    """Block tables report a bad length; append and attention then make the shared workspace grow."""
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    ws = M.Workspace()
+    table, free, got = i32(0, 1, 2, 3).view(2, 2), i32(4, 5, 6, 7), i32(0, 0)
+    off, slots = torch.zeros(3, dtype=torch.int64, device="cuda"), torch.zeros(2, dtype=torch.int64, device="cuda")
+    assert M.maps_block_tables(16, i32(5, -1), i32(6, 1), table, free, i32(4), i32(0), got, off, slots, ws=ws) == 0
+    size = ws.nbytes
+    q = torch.zeros(200, 4, 64, dtype=torch.bfloat16, device="cuda")
+    cache = torch.zeros(M.kv4_cache_shape(8, 2, 16, 64), dtype=torch.uint8, device="cuda")
+    assert M.maps_kv4_attention(q, torch.tensor([0, 100, 200], device="cuda"), i32(20, 20), table, cache, 16, 0.1, torch.empty_like(q),
+                                ws=ws) == 0
+    assert ws.nbytes > size
+    assert M.maps_check(ws) == M.MAPS_E_RANGE and M.maps_check(ws) == 0

@@ -16,8 +16,15 @@ class Stream:
 
 
 class Buffer:
-    def __init__(self, n, log):
-        self.n, self.log = n, log
+    def __init__(self, n, log, now):
+        self.n, self.log, self.now = n, log, now
+
+    def __getitem__(self, word):
+        assert word == slice(None, 4)
+        return self
+
+    def copy_(self, other):
+        self.log.append(("copy", self.n, other.n, self.now[-1].cuda_stream))
 
     def data_ptr(self):
         return 4096 * (1 + self.n)
@@ -47,7 +54,7 @@ def fake(monkeypatch):
 
     def zeros(n, dtype=None, device=None):
         log.append(("zeros", n, now[-1].cuda_stream))
-        return Buffer(n, log)
+        return Buffer(n, log, now)
 
     monkeypatch.setattr(torch, "zeros", zeros)
     monkeypatch.setattr(torch.cuda, "stream", on)
@@ -94,3 +101,11 @@ def test_a_captured_call_waits_for_nothing_outside_its_graph(fake):
     capturing.append(1)
     M._scratch(ws, 1000, None)
     assert log[1:] == [("keep", 1000, 5)]
+
+
+def test_growth_keeps_the_recorded_error(fake):
+    """The status that an earlier call recorded is not lost where a later call needs more."""
+    M, log, _, _ = fake
+    ws, side = M.Workspace(), Stream(2, log)
+    M._scratch(ws, 5000, side)
+    assert log == [("zeros", 256, 1), ("wait", 2, 1), ("keep", 256, 2), ("zeros", 5000, 2), ("copy", 5000, 256, 2)]
