@@ -556,10 +556,11 @@ int maps_kv4_read(int32_t dtype, int64_t T, int32_t H, int32_t D, int32_t S, con
  * at a position below 0 it sees none.  With query head x on KV head x / (Hq / Hkv),
  *     w_j = sm_scale * (q . k_j),  out = sum_j exp(w_j) v_j / sum_j exp(w_j),
  *     lse = log(sum_j exp(w_j)).
- * Scores, maxima, sums and lse are held in 32 bits; a weight is rounded to 11
+ * Scores, maxima, sums and lse are held in 32 bits.  A weight is rounded to 11
  * bits where it meets its value (with many queries a request, a value is too);
- * out is rounded once more.  The order of the sums depends on sizes and lengths alone, so
- * a call repeated gives the same bits.  A query that sees no key has out = 0
+ * one that is, times its value, below 2^-14 of the row's largest is rounded
+ * to 2^-25 of that.  out is rounded once more.  The order of the sums depends
+ * on sizes and lengths alone, so a call repeated gives the same bits.  A query that sees no key has out = 0
  * and lse = -infinity.  What the cache holds at places that no query sees is
  * not used, whatever it is.
  *

@@ -16,10 +16,11 @@
 //
 // Keys enter the first product as bare codes (subnormal halves, exact; the odd pairs' factor of 16 is taken
 // off in Q) and s, z come in with the row's sum of Q in 32 bits, as in the form for few queries: two packed
-// operations for two scores.  Values become halves of their own: v 2^-E with a power of two common to the step's
-// 128 tokens, so any magnitude fits and a value keeps 11 bits; the running sum carries its own exponent.
-// Both would cost a score more work the other way round: a value's scale on the weights takes three operations
-// a score and eight warps' registers, on the values two for two of them.
+// operations for two scores.  Values become halves of their own: v 2^-E with a power of two of their token's, so any
+// magnitude fits and a value keeps 11 bits.  2^E goes with the weight, so that what enters the running maximum is a weight times
+// its value, and rows that a query hardly weighs, or does not see, take no bits from the others however large they are.  That is
+// one packed addition for two scores (753 -> 783 us below); with a power of two common to a step, value rows 2^16 times
+// the others left later steps' weights below half's range.  The whole scale on the weights would be three operations a score.
 //
 // Bound.  A step's four products take the tensor cores about 2,200 cycles at D = 128 where nothing else runs, but a step
 // takes 6,800: each tile's chain of softmax (3,500 cycles: scores, weights, the tile's vote, P) and products (3,100 from P to the next
@@ -228,11 +229,11 @@ struct Lay {  // shared memory, from a 1,024-byte boundary
   static constexpr int kTile = 128 * D * 2;          // Q of a tile, K or V of a step
   static constexpr int kStep = kStepGroups * kv4_group_bytes(D);  // records
   static constexpr int kQ = 0, kK = 2 * kTile, kV = 4 * kTile, kRingAt = 5 * kTile;
-  static constexpr int kPar = kRingAt + kRing * kStep;  // [4][64] {scale, scale, zero, zero} of two keys
-  static constexpr int kRow = kPar + 4 * kTok * 8;   // [256] a row's sum, what a score is to be multiplied by, and the keys that it sees
+  // [4][64][2] of two tokens: {scale, scale, zero, zero} of the keys, {exponent, exponent, and 2 to minus them} of the values
+  static constexpr int kPar = kRingAt + kRing * kStep;
+  static constexpr int kRow = kPar + 4 * kTok * 16;  // [256] a row's sum, what a score is to be multiplied by, and the keys that it sees
   static constexpr int kNan = kRow + kRows * 16;     // [4][4] bits: values held as NaN
-  static constexpr int kExp = kNan + 64;             // [4] the step's exponent
-  static constexpr int kAgain = kExp + 16;           // [2] a tile's scores are wanted again
+  static constexpr int kAgain = kNan + 64;           // [2] a tile's scores are wanted again
   static constexpr int kBars = kAgain + 8;
   static constexpr int kSegAt = kBars + 8 * (2 * kRing + 14 + 2 * kSegs);
   static constexpr int kBytes = kSegAt + kSegs * static_cast<int>(sizeof(Seg));
@@ -243,13 +244,20 @@ template <int D>
 constexpr bool lay_aligned() {  // to what is read and written there at once
   using L = Lay<D>;
   return L::kK % 1024 == 0 && L::kV % 1024 == 0 && L::kRingAt % 16 == 0 && L::kStep % 16 == 0 && L::kPar % 16 == 0 && L::kRow % 16 == 0 && L::kNan % 16 == 0 &&
-         L::kExp % 4 == 0 && L::kAgain % 4 == 0 && L::kBars % 8 == 0 && L::kSegAt % alignof(Seg) == 0;
+         L::kAgain % 4 == 0 && L::kBars % 8 == 0 && L::kSegAt % alignof(Seg) == 0;
 }
 static_assert(lay_aligned<64>() && lay_aligned<128>(), "alignment");
 
-constexpr int kNoExp = -400;     // of a step without a value
-constexpr float kSlack = 8.0f;   // powers of two that a weight may exceed 1 by before the sums are rescaled at the next step
-constexpr float kMost = 15.0f;   // and that it may at all, for half's range
+// Weights are halves against the largest weight times value so far, which counts as 2^kBias: what is 2^21 times smaller still
+// has 11 bits.  They may exceed it by 2^kSlack before the sums are rescaled at the next step, and by 2^kMost at all, for half's range.
+constexpr float kBias = 7.0f, kSlack = 6.0f, kMost = 8.75f;
+
+// A value's power of two, by which it is taken out: v 2^-E is in 2^14 .. 2^15, or less where the row is tiny or zero or, being
+// held as NaN (both comparisons fail), left out.
+__device__ __forceinline__ int value_exponent(float2 p) {
+  const float big = fmaxf(fabsf(p.y), fabsf(fmaf(15.0f, p.x, p.y)));
+  return big == big ? max(static_cast<int>(__float_as_uint(big) >> 23) - 141, -60) : -60;
+}
 
 // Whether any of a tile's 128 threads says so; barrier `id` of the block.
 __device__ __forceinline__ bool tile_any(int id, bool x) {
@@ -352,7 +360,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
         ++n_seg;
         continue;
       }
-      int run = kNoExp;
       float4 *row_of = reinterpret_cast<float4 *>(smem + L::kRow) + t * 128;
       const int R = w.rt * kRows + t * 128 + row;
       const bool there = R < w.rows;
@@ -427,7 +434,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float4 x = row_of[(warp & 3) * 32 + 8 * e + (lane >> 2)];
-        fsum[e] = x.x;
+        fsum[e] = x.x * x.y;
         funit[e] = x.y;
         flo[e] = __float_as_int(x.z);
         fhi[e] = __float_as_int(x.w);
@@ -447,11 +454,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
         ok = all_wait(s_full(t), n_s & 1);
         ++n_s;
         tc_after();
-        const uint4 *par = reinterpret_cast<const uint4 *>(smem + L::kPar + buf * kTok * 8);
+        const uint4 *par = reinterpret_cast<const uint4 *>(smem + L::kPar + buf * kTok * 16);
         const int32_t tok0 = tok_at + j * kTok;
         const bool every = tok0 >= all_lo && tok0 + kTok <= all_hi;
-        // S is taken in eighths of 16 keys.  x[4 h + 2 i + e]: columns 8 i .. of row 2 h + e; scores, up to the row's
-        // factor, in place of their products.
+        // S is taken in eighths of 16 keys.  x[4 h + 2 i + e]: columns 8 i .. of row 2 h + e; what a weight times its value is,
+        // as a power of two, in place of their products.
         auto load = [&](uint64_t *x, int k) {
           tm_load_frag2(s_at + 16 * k, reinterpret_cast<uint32_t *>(x));
           tm_load_frag2(s_at + (16u << 16) + 16 * k, reinterpret_cast<uint32_t *>(x) + 8);
@@ -460,13 +467,15 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
         auto scores = [&](auto all, uint64_t *x, int k) {  // all: every row sees every key
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            const uint4 p = par[8 * k + 4 * i + (lane & 3)];
-            F2 s, z;
-            s.u[0] = p.x, s.u[1] = p.y, z.u[0] = p.z, z.u[1] = p.w;
+            const int at = 2 * (8 * k + 4 * i + (lane & 3));
+            const uint4 p = par[at];
+            const uint2 q = *reinterpret_cast<const uint2 *>(par + at + 1);
+            F2 s, z, ve;
+            s.u[0] = p.x, s.u[1] = p.y, z.u[0] = p.z, z.u[1] = p.w, ve.u[0] = q.x, ve.u[1] = q.y;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               uint64_t &y = x[4 * (e >> 1) + 2 * i + (e & 1)];
-              y = fma2(s.v, y, mul2(z.v, two(fsum[e], fsum[e])));
+              y = fma2(mul2(s.v, two(funit[e], funit[e])), y, fma2(z.v, two(fsum[e], fsum[e]), ve.v));
               if (!decltype(all)::value) {
                 const int tok = tok0 + 16 * k + 8 * i + 2 * (lane & 3);
                 F2 v;
@@ -492,24 +501,21 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], 1));
-            top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], 2)) * funit[e];
+            top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], 2));
           }
         };
-        const int E = reinterpret_cast<const int *>(smem + L::kExp)[buf];
-        // the sums so far to the maxima in top, where larger, and to exponent en: the product before has to be done
-        auto rescale = [&](int en) {
+        // the sums so far to the maxima in top, where larger: the product before has to be done
+        auto rescale = [&]() {
           if (j > 0 && !all_wait(o_full(t), (n_o - 1) & 1)) failed = true;
           tc_after();
-          const float f_run = ex2(static_cast<float>(run - en));
           float f[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float mn = fmaxf(fm[e], top[e]), down = mn == -INFINITY ? 1.0f : ex2(fm[e] - mn);
-            f[e] = down * f_run;
-            fl[e] *= down;
+            const float mn = fmaxf(fm[e], top[e]);
+            f[e] = mn == -INFINITY ? 1.0f : ex2(fm[e] - mn);
+            fl[e] *= f[e];
             fm[e] = mn;
           }
-          run = en;
 #pragma unroll 1
           for (int k = 0; k < 2 * D; k += 32) {
             uint32_t o[16];
@@ -536,19 +542,17 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
           join_top();
 #pragma unroll
           for (int e = 0; e < 4; ++e) fm[e] = top[e];
-          run = E;
-        } else if (ok && (pending || E > run)) {
-          rescale(max(run, E));
+        } else if (ok && pending) {
+          rescale();
         }
-        // Weights against the maxima so far, in the place of the scores that have been read.  A weight may be up to
-        // 2^15 then; a row that has grown past that, and with it the whole tile, has its scores computed again.
-        const float lag = static_cast<float>(max(E - run, -60));  // this step's values lie so many powers of two lower
+        // Weights against the maxima so far, in the place of the scores that have been read.  A row that has grown past what
+        // a half can hold, and with it the whole tile, has its scores computed again.
         uint64_t total[4];
         auto weigh = [&](auto all) {
           float ref[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            ref[e] = lag - (fm[e] == -INFINITY ? 0.0f : fm[e]);
+            ref[e] = kBias - (fm[e] == -INFINITY ? 0.0f : fm[e]);
             total[e] = 0;
             top[e] = -INFINITY;
           }
@@ -562,17 +566,19 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
             larger(z);
             uint32_t p[8];
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < 2; ++i) {
+              const uint64_t weight = reinterpret_cast<const uint64_t *>(par)[4 * (8 * k + 4 * i + (lane & 3)) + 3];  // without the value
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
                 const int at = 4 * (e >> 1) + 2 * i + (e & 1);
                 F2 v;
-                v.v = fma2(z[at], two(funit[e], funit[e]), two(ref[e], ref[e]));
+                v.v = add2(z[at], two(ref[e], ref[e]));
                 v.f[0] = ex2(v.f[0]);
                 v.f[1] = ex2(v.f[1]);
-                total[e] = add2(total[e], v.v);
+                total[e] = fma2(v.v, weight, total[e]);
                 p[at] = pack_half(v.f[0], v.f[1]);
               }
+            }
             tm_store_halves(s_at + 8 * k, p);
             tm_store_halves(s_at + (16u << 16) + 8 * k, p + 4);
           }
@@ -595,7 +601,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
         if (tile_any(1 + t, again || !ok || failed)) {  // every warp of the tile comes here once for every wait on s_full
           ok = !tile_any(1 + t, !ok || failed);
           if (!ok) break;
-          rescale(run);
+          rescale();
           if (lane == 0 && (warp & 3) == 0) reinterpret_cast<volatile int *>(smem + L::kAgain)[t] = 1;
           pending = false;
           tm_wait_store();  // the weights have to be there before the next scores take their place
@@ -605,12 +611,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
           --j, --c;  // the same step
           continue;
         }
-        const float up = ex2(-lag);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           F2 y;
           y.v = total[e];
-          fl[e] = fmaf(y.f[0] + y.f[1], up, fl[e]);
+          fl[e] += y.f[0] + y.f[1];
         }
         // A value held as NaN is left out of the product.  A row that sees one is marked, in the place of what a score is to be
         // multiplied by, which is in registers: its output is NaN, its sum of weights is not.
@@ -653,7 +658,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
       }
       __syncwarp();
       const bool nan = steps > 0 && isnan(row_of[row].y);
-      const float f = nan ? NAN : whole ? (l == 0.0f ? 0.0f : ex2(static_cast<float>(run)) / l) : run == kNoExp ? 0.0f : ex2(static_cast<float>(run));
+      const float f = nan ? NAN : whole ? (l == 0.0f ? 0.0f : 1.0f / l) : 1.0f;
       T *dst = static_cast<T *>(a.out) + i * a.o_row + hq * a.o_head;
       const int at = t * 128 + row;
       float *part = a.many_parts + (static_cast<int64_t>(me) * 2 + (id < u0 ? 0 : 1)) * L::kPart;
@@ -687,11 +692,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
         }
       }
       if (!whole) {
-        part[kRows * D + at] = m;
+        part[kRows * D + at] = m - kBias;
         part[kRows * D + kRows + at] = l;
         if (tid == 0 && id >= u0) a.many_open[me] = {w.q0, id, w.tiles, w.rows, w.h, w.rt};
       } else if (there && a.lse) {
-        a.lse[i * a.Hq + hq] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+        a.lse[i * a.Hq + hq] = l == 0.0f ? -INFINITY : (m - kBias + log2f(l)) * 0.6931471805599453f;
       }
       tc_before();  // the sums have been read, before the next item's first product
       __syncwarp();
@@ -711,22 +716,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
         if (!ok) break;
         const int32_t tok0 = tok_at + j * kTok;
         auto record = [&](int g) -> const uint8_t * { return smem + L::kRingAt + place * L::kStep + g * kv4_group_bytes(D); };
-        // ---- the step's largest value, from 4 tokens a lane; every warp finds it
+        // ---- scales and zeros of the lane's 4 tokens, two side by side, against each value's own power of two; those left out are zero
         const uint4 v4 = *reinterpret_cast<const uint4 *>(record(lane >> 2) + 16 * D + 64 + (lane & 3) * 16);
         const uint32_t vp[4] = {v4.x, v4.y, v4.z, v4.w};
-        float big = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float2 p = kv4_param(vp[e]);
-          if (tok0 + 4 * lane + e >= hi) continue;
-          if (p.x == p.x && p.y == p.y) big = fmaxf(big, fmaxf(fabsf(p.y), fabsf(fmaf(15.0f, p.x, p.y))));
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
-        // v 2^-E is below 2^15
-        const int E = big == 0.0f ? kNoExp : max(static_cast<int>(__float_as_uint(big) >> 23) - 141, -112);
-        const float down = big == 0.0f ? 0.0f : __uint_as_float(static_cast<uint32_t>(127 - E) << 23);
-        // scales and zeros of the lane's tokens, two side by side; those left out are zero
         uint32_t vs[2], vz[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
@@ -734,8 +726,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
           const int32_t tok = tok0 + 4 * lane + 2 * e;
           if (tok >= hi || p0.x != p0.x || p0.y != p0.y) p0 = make_float2(0.0f, 0.0f);
           if (tok + 1 >= hi || p1.x != p1.x || p1.y != p1.y) p1 = make_float2(0.0f, 0.0f);
-          vs[e] = pack_half(p0.x * down, p1.x * down);
-          vz[e] = pack_half(p0.y * down, p1.y * down);
+          const float d0 = __uint_as_float(static_cast<uint32_t>(127 - value_exponent(p0)) << 23), d1 = __uint_as_float(static_cast<uint32_t>(127 - value_exponent(p1)) << 23);
+          vs[e] = pack_half(p0.x * d0, p1.x * d1);
+          vz[e] = pack_half(p0.y * d0, p1.y * d1);
         }
         ok = all_wait(v_free, (c & 1) ^ 1);
         if (!ok) break;
@@ -936,29 +929,24 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
             }
           }
           }
-        // ---- the step's largest value, and the values held as NaN, from 4 tokens a lane
+        // ---- the values' powers of two, and those held as NaN, from 4 tokens a lane
         const uint4 v4 = *reinterpret_cast<const uint4 *>(record(lane >> 2) + 16 * D + 64 + (lane & 3) * 16);
         const uint32_t vp[4] = {v4.x, v4.y, v4.z, v4.w};
-        float big = 0.0f;
         uint32_t bad = 0;
+        float ve[4], weight[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float2 p = kv4_param(vp[e]);
-          if (tok0 + 4 * lane + e >= hi) continue;
-          if (p.x != p.x || p.y != p.y)
-            bad |= 1u << e;
-          else
-            big = fmaxf(big, fmaxf(fabsf(p.y), fabsf(fmaf(15.0f, p.x, p.y))));
+          const bool there = tok0 + 4 * lane + e < hi;
+          if (there && (p.x != p.x || p.y != p.y)) bad |= 1u << e;
+          const int E = there ? value_exponent(p) : -60;
+          ve[e] = static_cast<float>(E);
+          weight[e] = __uint_as_float(static_cast<uint32_t>(127 - E) << 23);
         }
         bad <<= (lane & 7) * 4;
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
-#pragma unroll
         for (int o = 4; o > 0; o >>= 1) bad |= __shfl_xor_sync(0xffffffffu, bad, o);
-        // v 2^-E is below 2^15
-        const int E = big == 0.0f ? kNoExp : max(static_cast<int>(__float_as_uint(big) >> 23) - 141, -112);
         if ((lane & 7) == 0) reinterpret_cast<uint32_t *>(smem + L::kNan)[4 * (c & 3) + (lane >> 3)] = bad;
-        if (lane == 0) reinterpret_cast<int *>(smem + L::kExp)[c & 3] = E;
         // ---- keys' scales and zeros, two tokens side by side
         {
           const uint4 k4 = *reinterpret_cast<const uint4 *>(record(lane >> 2) + 16 * D + (lane & 3) * 16);
@@ -968,8 +956,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
             float2 p0 = kv4_param(kp[e]), p1 = kv4_param(kp[e + 1]);
             if (tok0 + 4 * lane + e >= hi) p0 = make_float2(0.0f, 0.0f);
             if (tok0 + 4 * lane + e + 1 >= hi) p1 = make_float2(0.0f, 0.0f);
-            reinterpret_cast<float4 *>(smem + L::kPar + (c & 3) * kTok * 8)[2 * lane + e / 2] =
-                make_float4(p0.x * (k_sign * kEven), p1.x * (k_sign * kEven), p0.y * k_sign, p1.y * k_sign);
+            float4 *par = reinterpret_cast<float4 *>(smem + L::kPar + (c & 3) * kTok * 16) + 4 * lane + e;
+            par[0] = make_float4(p0.x * (k_sign * kEven), p1.x * (k_sign * kEven), p0.y * k_sign, p1.y * k_sign);
+            par[1] = make_float4(ve[e], ve[e + 1], weight[e], weight[e + 1]);
           }
         }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
