@@ -7,7 +7,7 @@
 // sum p v = sum (p s) c + sum p z: the matrix products run on bare codes, and scales and zeros cost
 // a few operations a token instead of D.  A code is a half number as it stands (codes_of), so eight
 // codes take five operations.  q is scaled by a power of two to fill half's range; p s is held
-// relative to the largest p s so far, so it is at most 1.
+// relative to the largest p s so far.
 //
 // Bound.  A key and value of D channels are D + 8 bytes and serve the few query rows (queries x
 // heads of one KV head) of one request, so long calls are bound by the cache's bytes: 128 requests
@@ -236,8 +236,9 @@ struct Sum {
 };
 
 // Weights are held relative to the largest weight times value scale seen, so that what enters the
-// second product is at most 1; scales count as at least 2^-60 there, so that a weight itself stays finite.
-constexpr float kMinLog = -60.0f;
+// second product has a largest size; scales count as at least 2^-60 there, so that a weight itself stays finite.
+// The largest counts as 2^kBias, near half's end: what is 2^28 times smaller still has 11 bits.
+constexpr float kMinLog = -60.0f, kBias = 14.0f;
 
 // ---------------------------------------------------------------------------- the kernel
 template <class T, int D, int NT>
@@ -522,7 +523,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(con
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) ref[nt][e] = m[nt][e] == -INFINITY ? 0.0f : -m[nt][e];
+            for (int e = 0; e < 2; ++e) ref[nt][e] = kBias - (m[nt][e] == -INFINITY ? 0.0f : m[nt][e]);
 
           // ---- weights and sums over the values
 #pragma unroll
@@ -619,7 +620,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(con
 #pragma unroll
               for (int c = 0; c < kCh; ++c) dst[c] = y[c];
             }
-            if (a.lse && g == 0) a.lse[i * a.Hq + hq] = l[nt][e] == 0.0f ? -INFINITY : (m[nt][e] + log2f(l[nt][e])) * 0.6931471805599453f;
+            if (a.lse && g == 0) a.lse[i * a.Hq + hq] = l[nt][e] == 0.0f ? -INFINITY : (m[nt][e] - kBias + log2f(l[nt][e])) * 0.6931471805599453f;
           }
       } else {
         // a run's first part goes to its own place, its last to the ring, which has been read to the end
@@ -637,7 +638,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(con
                   make_float4(fmaf(o[nt][j][e], Value<T>::kEvenBy, w[nt][e]), fmaf(o[nt][j][2 + e], Value<T>::kOddBy, w[nt][e]),
                               fmaf(o[nt][j + 1][e], Value<T>::kEvenBy, w[nt][e]), fmaf(o[nt][j + 1][2 + e], Value<T>::kOddBy, w[nt][e]));
             if (g == 0) {
-              part[Sh::kRows * D + R] = m[nt][e];
+              part[Sh::kRows * D + R] = m[nt][e] - kBias;
               part[Sh::kRows * D + Sh::kRows + R] = l[nt][e];
             }
           }

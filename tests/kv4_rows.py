@@ -22,15 +22,17 @@ import kv4_oracle as K
 U = {"bf16": 2.0**-8, "fp16": 2.0**-11}
 
 
-def held(x):
-    """(values, magnitudes, rows held as NaN) of rows in 64 bits; what is held as NaN counts as 0."""
+def held(x, centre=0):
+    """(values, magnitudes, rows held as NaN) of rows in 64 bits; what is held as NaN counts as 0.
+    centre: what the codes are taken about; the few-query form takes half outputs' values about 8, so that
+    s |c - 8| + |z + 8 s| is what is summed there."""
     c, s, z = K.quantise(x)
     bad = np.isnan(s[..., 0])
     s, z = (np.where(bad[..., None], 0, y).astype(np.float64) for y in (s, z))
-    return s * c + z, s * c + np.abs(z), bad
+    return s * c + z, s * np.abs(c - float(centre)) + np.abs(z + centre * s), bad
 
 
-def expect(name, q, off, lens, k, v, Hkv, scale, causal=True, window=0):
+def expect(name, q, off, lens, k, v, Hkv, scale, causal=True, window=0, centre=0):
     """out, lse and what they may be off by, in 64 bits.  q [T, Hq, D]; k, v: per request [n, Hkv, D] as given to the cache."""
     T, Hq, D = q.shape
     e = dict(out=np.zeros((T, Hq, D)), lse=np.full((T, Hq), -np.inf), tol=np.zeros((T, Hq, D)),
@@ -56,7 +58,7 @@ def expect(name, q, off, lens, k, v, Hkv, scale, causal=True, window=0):
             continue
         for h in range(Hkv):
             kv, ka, kbad = held(k[b][:, h])
-            vv, va, vbad = held(v[b][:, h])
+            vv, va, vbad = held(v[b][:, h], centre)
             for x in range(h * group, (h + 1) * group):
                 qx = q[rows, x].astype(np.float64)
                 w = np.where(seen, qx @ kv.T * scale, -np.inf)

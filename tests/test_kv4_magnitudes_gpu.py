@@ -32,9 +32,9 @@ def inputs(rng, name, D, form, size=2.0**-10):
     return lens, n_q, k, v, R.rounded(q.astype(np.float32), name), along / D ** 0.5
 
 
-def compare(M, rng, name, D, lens, n_q, k, v, q):
+def compare(M, rng, name, D, lens, n_q, k, v, q, centre=0):
     k, v = ([R.rounded(x.astype(np.float32), name) for x in y] for y in (k, v))
-    e = R.expect(name, q, np.concatenate([[0], np.cumsum(n_q)]), lens, k, v, H, D ** -0.5)
+    e = R.expect(name, q, np.concatenate([[0], np.cumsum(n_q)]), lens, k, v, H, D ** -0.5, centre=centre)
     assert np.isfinite(e["out"]).all()
     out, lse = R.run(M, rng, name, q, lens, n_q, k, v, D ** -0.5)
     assert R.wrong(e, out, lse) is None
@@ -83,3 +83,27 @@ def test_a_silent_row_that_all_look_at(M, form, name, D, nats, size):
         k[b][0] = nats * along
         v[b][0] = 0.0
     compare(M, rng, name, D, lens, n_q, k, v, q)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("name", ["bf16", "fp16"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("nats", [10, 12, 13, 14, 15, 16, 18])
+def test_a_flat_tail_behind_one_row(M, form, name, D, nats):
+    """One key outweighs each of the others by e^nats, and its value is zero but in one channel: the
+    others' weights, all alike, are all that the other channels are made of.  (Few queries: as many
+    requests as it takes for one warp to have most of a request; for half outputs the row is one whose
+    zeros are held as the code in the middle.)"""
+    rng = np.random.default_rng(nats)
+    lens, n_q = ([300] * 800, [1] * 800) if form == "few" else FORMS[form]
+    along = rng.choice([-1.0, 1.0], (H, D))
+    k = [np.zeros((n, H, D)) for n in lens]
+    v = [1 + 0.25 * rng.normal(size=(n, H, D)) for n in lens]
+    q = R.rounded(np.repeat(np.repeat(along, HQ // H, 0)[None], sum(n_q), 0).astype(np.float32), name)
+    for b in range(len(lens)):
+        k[b][0] = nats * along / D ** 0.5
+        v[b][0] = 0.0
+        v[b][0, :, 7] = 4.0
+        if form == "few" and name == "fp16":
+            v[b][0, :, 7], v[b][0, :, 8] = 3.5, -4.0
+    compare(M, rng, name, D, lens, n_q, k, v, q, centre=8 if form == "few" and name == "fp16" else 0)
