@@ -239,6 +239,8 @@ struct Sum {
 // second product has a largest size; scales count as at least 2^-60 there, so that a weight itself stays finite.
 // The largest counts as 2^kBias, near half's end: what is 2^28 times smaller still has 11 bits.
 constexpr float kMinLog = -60.0f, kBias = 14.0f;
+// A row of one value has scale 0.  It counts with 2^-20 of its zero, or weight times zero would pass the 32-bit range from zeros of 2^54 on.
+constexpr float kLeastScale = 9.5367431640625e-7f;
 
 // ---------------------------------------------------------------------------- the kernel
 template <class T, int D, int NT>
@@ -478,8 +480,9 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(con
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
               const float2 p = kv4_param(par[g + 8 * half]);
-              vs[gr][half] = kv4_param(par[16 + g + 8 * half]).x;
-              const float ks = p.x * k_unit, kz = p.y * k_sign, ls = fmaxf(lg2(vs[gr][half]), kMinLog);
+              const float2 v = kv4_param(par[16 + g + 8 * half]);
+              vs[gr][half] = v.x;
+              const float ks = p.x * k_unit, kz = p.y * k_sign, ls = fmaxf(lg2(fmaxf(v.x, fabsf(v.y) * kLeastScale)), kMinLog);
               const int32_t tok = tok0 + gr * kGroup + g + 8 * half;
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt)

@@ -107,3 +107,19 @@ def test_a_flat_tail_behind_one_row(M, form, name, D, nats):
         if form == "few" and name == "fp16":
             v[b][0, :, 7], v[b][0, :, 8] = 3.5, -4.0
     compare(M, rng, name, D, lens, n_q, k, v, q, centre=8 if form == "few" and name == "fp16" else 0)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("power", [0, 40, 60, 100, 126])
+@pytest.mark.parametrize("share", [1.0, 0.2])
+def test_rows_of_one_value(M, form, D, power, share):
+    """Value rows whose channels are all alike, up to the end of bfloat16's range: their step is zero, and the value comes
+    in with the zero point alone.  All rows, or a fifth of them among others of their size."""
+    rng = np.random.default_rng(power + D)
+    lens, n_q, k, v, q, _ = inputs(rng, "bf16", D, form, 0.25)
+    for b, n in enumerate(lens):
+        alike = rng.random(n) < share
+        v[b][alike] = rng.uniform(-1.9, 1.9, (alike.sum(), H, 1))
+        v[b] *= 2.0**power
+    compare(M, rng, "bf16", D, lens, n_q, k, v, q)
