@@ -484,8 +484,8 @@ int maps_rr_pressure(const maps_rr_cfg *cfg, int64_t n_real, const int64_t *arri
  *                       every new token, -1 where r was refused.
  *   pos_out             [slots_cap] int32 positions, or NULL.
  * A call repeated on the same held, want, n_free and stack gives the same
- * result.  Lengths out of their domain, an order entry outside [0, R), more
- * new tokens than slots_cap or more returned blocks than the stack has room
+ * result.  Lengths out of their domain, an order entry outside [0, R) or there
+ * twice (what it leaves out gets no block), more new tokens than slots_cap or more returned blocks than the stack has room
  * for are MAPS_E_RANGE (via maps_check).
  * ---------------------------------------------------------------------- */
 size_t maps_block_tables_workspace_size(int32_t R);

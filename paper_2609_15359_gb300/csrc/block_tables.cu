@@ -46,6 +46,7 @@ struct alignas(32) Request {
   int64_t begin;   // its first new token
   int64_t before;  // blocks granted ahead of its first, -1 where it is refused
   int32_t held, last;  // tokens held, and the block of the last of them (where it is not full)
+  int32_t named;       // whether the order has named it
 };
 // The sums over all, for the kernels that expand them.
 struct alignas(32) Totals {
@@ -263,6 +264,7 @@ __global__ void __launch_bounds__(kScanThreads) bt_scan_kernel(const BTArgs a) {
       a.off[r] = sy, a.back[r] = sx;
       Request &q = a.requests[r];
       q.begin = sy, q.held = n.held, q.last = last;
+      if (a.order) q.before = -1, q.named = 0;  // one that the order leaves out gets nothing
       set_marks(a.coarse, r, sy, y, mark_shift(toks));
       set_marks(a.coarse + kCoarse + 2, r, sx, x, mark_shift(back));
     }
@@ -295,6 +297,7 @@ __global__ void __launch_bounds__(kScanThreads) bt_scan_kernel(const BTArgs a) {
     cluster_sums<kBlocks>(tx, 0, ahead, unused, all, unused);
   }
   int64_t granted = 0;  // the needs up to the last one granted
+  int32_t twice_named = 0;
   for (int base = r0, k = 0; k < each; base += kScanThreads, ++k) {
     int r;
     const int64_t x = place(base + tid, r, n);
@@ -304,6 +307,7 @@ __global__ void __launch_bounds__(kScanThreads) bt_scan_kernel(const BTArgs a) {
     sx += ahead;
     if (r >= 0) {
       const bool ok = x == 0 || sx + x <= N;
+      if (a.order) twice_named |= atomicExch(&a.requests[r].named, 1);
       a.requests[r].before = ok ? sx : -1;
       a.got[r] = n.want < n.held || ok ? n.want : n.held;
       if (ok && x) granted = sx + x;
@@ -318,6 +322,7 @@ __global__ void __launch_bounds__(kScanThreads) bt_scan_kernel(const BTArgs a) {
   for (int o = 16; o > 0; o >>= 1) granted = max(granted, static_cast<int64_t>(__shfl_xor_sync(0xffffffffu, granted, o)));
   if ((tid & 31) == 0 && granted) atomicMax(&s_granted, static_cast<unsigned long long>(granted));
   __syncthreads();
+  if (twice_named) flag_error(a.status, MAPS_E_RANGE);
   int64_t most = static_cast<int64_t>(s_granted);
   if (kBlocks > 1) {
     cg::cluster_group cl = cg::this_cluster();
@@ -369,7 +374,7 @@ __global__ void __launch_bounds__(kFillThreads) bt_fill_many_kernel(const BTArgs
   int64_t end = 0;
   int r = -1;
   uint32_t hb = 0;
-  Request q = {0, -1, 0, -1};
+  Request q = {0, -1, 0, -1, 0};
 #pragma unroll
   for (int i = 0; i < kManyEach; ++i) {
     const int64_t j = j0 + 32 * i;
