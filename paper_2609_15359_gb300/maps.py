@@ -215,8 +215,8 @@ def _scratch(ws: Workspace | None, nbytes: int, stream):
 
 
 @functools.lru_cache(maxsize=4096)
-def _need(query: str, *sizes: int) -> int:
-    """A workspace size query: it depends on the sizes alone."""
+def _need(device: int | None, query: str, *sizes: int) -> int:
+    """A size query: it depends on the sizes alone, or on the multiprocessors of `device` too."""
     return getattr(lib, query)(*sizes)
 
 
@@ -354,7 +354,7 @@ def maps_block_tables(S: int, held, want, table, free_blocks, n_free, n_free_out
     """Hands out the KV blocks: table [R][max_blocks] and free_blocks [pool]
     int32 are updated in place; slots_out [cap] int64 holds the new tokens'."""
     R = held.numel()
-    ws, on = _scratch(ws, _need("maps_block_tables_workspace_size", R), stream)
+    ws, on = _scratch(ws, _need(None, "maps_block_tables_workspace_size", R), stream)
     return lib.maps_block_tables(R, S, _ptr(held, torch.int32), _ptr(want, torch.int32),
                                  _ptr(order, torch.int32), _ptr(table, torch.int32),
                                  table.shape[1], _ptr(free_blocks, torch.int32),
@@ -390,7 +390,7 @@ def _dtype(t) -> int:
 
 def kv4_cache_shape(n_blocks: int, H: int, S: int, D: int) -> tuple[int, int, int]:
     """Shape of a 4-bit cache (uint8): [blocks][KV heads][record bytes]."""
-    nbytes = _need("maps_kv4_record_bytes", S, D)
+    nbytes = _need(None, "maps_kv4_record_bytes", S, D)
     if nbytes == 0:
         raise ValueError(f"no 4-bit cache for blocks of {S} tokens and {D} channels")
     return n_blocks, H, nbytes
@@ -408,7 +408,7 @@ def maps_kv4_append(k, v, slots, cache, S: int, ws: Workspace | None = None, str
     T, H, D = k.shape
     if v.shape != k.shape or slots.numel() != T:
         raise ValueError("k, v and slots differ in size")
-    ws, on = _scratch(ws, _need("maps_kv4_workspace_size"), stream)
+    ws, on = _scratch(ws, _need(None, "maps_kv4_workspace_size"), stream)
     return lib.maps_kv4_append(_dtype(k), T, H, D, S, *_rows(k), *_rows(v, k.dtype),
                                _ptr(slots, torch.int64), _kv4(cache, S, D, H), cache.shape[0],
                                ws.ptr, ws.nbytes, on)
@@ -420,7 +420,7 @@ def maps_kv4_read(slots, cache, S: int, k_out, v_out, ws: Workspace | None = Non
     T, H, D = k_out.shape
     if v_out.shape != k_out.shape or slots.numel() != T:
         raise ValueError("k_out, v_out and slots differ in size")
-    ws, on = _scratch(ws, _need("maps_kv4_workspace_size"), stream)
+    ws, on = _scratch(ws, _need(None, "maps_kv4_workspace_size"), stream)
     return lib.maps_kv4_read(_dtype(k_out), T, H, D, S, _ptr(slots, torch.int64),
                              _kv4(cache, S, D, H), cache.shape[0], *_rows(k_out),
                              *_rows(v_out, k_out.dtype), ws.ptr, ws.nbytes, on)
@@ -438,7 +438,7 @@ def maps_kv4_attention(q, qo_off, kv_len, table, cache, S: int, sm_scale: float,
         raise ValueError("q, out, qo_off, kv_len and table differ in size")
     if lse_out is not None and tuple(lse_out.shape) != (T, Hq):
         raise ValueError("lse_out is [T, Hq]")
-    ws, on = _scratch(ws, _need("maps_kv4_attention_workspace_size", B, T, Hq, Hkv, D), stream)
+    ws, on = _scratch(ws, _need(torch.cuda.current_device(), "maps_kv4_attention_workspace_size", B, T, Hq, Hkv, D), stream)
     return lib.maps_kv4_attention(_dtype(q), B, T, Hq, Hkv, D, S, *_rows(q),
                                   _ptr(qo_off, torch.int64), _ptr(kv_len, torch.int32),
                                   _ptr(table, torch.int32), table.shape[1],

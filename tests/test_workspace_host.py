@@ -109,3 +109,25 @@ def test_growth_keeps_the_recorded_error(fake):
     ws, side = M.Workspace(), Stream(2, log)
     M._scratch(ws, 5000, side)
     assert log == [("zeros", 256, 1), ("wait", 2, 1), ("keep", 256, 2), ("zeros", 5000, 2), ("copy", 5000, 256, 2)]
+
+
+def test_attention_asks_for_its_workspace_on_every_device(fake, monkeypatch):
+    """The size grows with a device's multiprocessors: one device's does not serve another."""
+    M, _, _, _ = fake
+    device, asked = [0], []
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: device[0])
+    monkeypatch.setattr(M.lib, "maps_kv4_attention_workspace_size", lambda *sizes: 1000 * (1 + device[0]))
+
+    class Enough(Exception):
+        pass
+
+    def scratch(ws, nbytes, stream):
+        asked.append(nbytes)
+        raise Enough
+
+    monkeypatch.setattr(M, "_scratch", scratch)
+    q, cache = torch.empty(3, 4, 64), torch.empty(5, 2, 1152, dtype=torch.uint8)
+    for device[0] in (0, 1, 0, 1):
+        with pytest.raises(Enough):
+            M.maps_kv4_attention(q, torch.empty(3), torch.empty(2), torch.empty(2, 4), cache, 16, 0.1, torch.empty(3, 4, 64))
+    assert asked == [1000, 2000, 1000, 2000]
