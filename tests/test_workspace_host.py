@@ -131,3 +131,16 @@ def test_attention_asks_for_its_workspace_on_every_device(fake, monkeypatch):
         with pytest.raises(Enough):
             M.maps_kv4_attention(q, torch.empty(3), torch.empty(2), torch.empty(2, 4), cache, 16, 0.1, torch.empty(3, 4, 64))
     assert asked == [1000, 2000, 1000, 2000]
+
+
+def test_the_current_stream_without_the_private_function(monkeypatch):
+    """The binding loads and finds the current stream on a PyTorch that lacks the function it prefers."""
+    import importlib.util
+
+    from paper_2609_15359_gb300 import maps as M
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream")
+    spec = importlib.util.spec_from_file_location("maps_without", M.__file__)
+    other = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(other)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: Stream(17, []))
+    assert other._stream(None) == 17 and other._stream(Stream(5, [])) == 5
