@@ -380,7 +380,7 @@ def _rows(t, dtype=None):
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"expected {dtype}, got {t.dtype}")
     row, head, channel = t.stride()
-    if channel != 1:
+    if channel != 1 and t.numel() > 0:  # the strides of an empty tensor say nothing
         raise TypeError("expected [rows, heads, channels] with contiguous channels")
     return t.data_ptr(), row, head
 
