@@ -481,7 +481,9 @@ int maps_rr_pressure(const maps_rr_cfg *cfg, int64_t n_real, const int64_t *arri
  *   got_out             [R] int32: want where granted or shrunk, else held.
  *   slot_off_out        [R + 1] int64.
  *   slots_out           [slots_cap] int64: block * S + position mod S for
- *                       every new token, -1 where r was refused.
+ *                       every new token, -1 where r was refused.  Its tokens
+ *                       keep their places in a batch of slots_out's rows: with
+ *                       kv_len 0 for r, maps_kv4_attention gives them zeros.
  *   pos_out             [slots_cap] int32 positions, or NULL.
  * A call repeated on the same held, want, n_free and stack gives the same
  * result.  Lengths out of their domain, an order entry outside [0, R) or there
