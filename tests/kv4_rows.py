@@ -32,8 +32,10 @@ def held(x, centre=0):
     return s * c + z, s * np.abs(c - float(centre)) + np.abs(z + centre * s), bad
 
 
-def expect(name, q, off, lens, k, v, Hkv, scale, causal=True, window=0, centre=0):
-    """out, lse and what they may be off by, in 64 bits.  q [T, Hq, D]; k, v: per request [n, Hkv, D] as given to the cache."""
+def expect(name, q, off, lens, k, v, Hkv, scale, causal=True, window=0, centre=0, run=None):
+    """out, lse and what they may be off by, in 64 bits.  q [T, Hq, D]; k, v: per request [n, Hkv, D] as given to the cache.
+    run: the most keys that are summed one after another where that is known, and not more than 164 parts of
+    such sums are joined; with it a row's error as a vector takes the scores' roundings as independent too."""
     T, Hq, D = q.shape
     e = dict(out=np.zeros((T, Hq, D)), lse=np.full((T, Hq), -np.inf), tol=np.zeros((T, Hq, D)),
              norm=np.zeros((T, Hq)), lse_tol=np.zeros((T, Hq)), has=np.zeros(T, bool))
@@ -71,11 +73,14 @@ def expect(name, q, off, lens, k, v, Hkv, scale, causal=True, window=0, centre=0
                 out, A = p @ vv, p @ va
                 spread = np.sqrt((p * p) @ (va * va))
                 most = (p * va.max(1)).max(1)
-                sums = (keys / 16 + 64) * 2.0**-23
+                sums = (keys / 16 + 64 if run is None else np.minimum(keys, run) / 16 + 64 + 164) * 2.0**-23
                 rest = ((2 * score + sums)[:, None] * A + (keys * 2.0**-32 * most)[:, None])
                 e["out"][rows, x] = np.where((seen & (kbad | vbad)).any(1)[:, None], np.nan, out)
                 e["tol"][rows, x] = u * np.abs(out) + 2.0**-10 * (1 + 2.0**-9) * A + rest
-                e["norm"][rows, x] = (u * np.linalg.norm(out, axis=1) + 4 * 2.0**-11 * np.linalg.norm(spread, axis=1) +
+                eleven = 4 * 2.0**-11
+                if run is not None:
+                    eleven, rest = eleven + 8 * score, sums[:, None] * A + (keys * 2.0**-32 * most)[:, None]
+                e["norm"][rows, x] = (u * np.linalg.norm(out, axis=1) + eleven * np.linalg.norm(spread, axis=1) +
                                       np.linalg.norm(rest, axis=1))
                 lse = (m + np.log(total))[:, 0]
                 e["lse"][rows, x] = np.where((seen & kbad).any(1), np.nan, lse)
