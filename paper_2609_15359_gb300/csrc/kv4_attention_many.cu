@@ -232,7 +232,7 @@ struct Lay {  // shared memory, from a 1,024-byte boundary
   // [4][64][2] of two tokens: {scale, scale, zero, zero} of the keys, {exponent, exponent, and 2 to minus them} of the values
   static constexpr int kPar = kRingAt + kRing * kStep;
   static constexpr int kRow = kPar + 4 * kTok * 16;  // [256] a row's sum, what a score is to be multiplied by, and the keys that it sees
-  static constexpr int kNan = kRow + kRows * 16;     // [4][4] bits: values held as NaN
+  static constexpr int kNan = kRow + kRows * 16;     // [4][4] bits: values that are not finite
   static constexpr int kAgain = kNan + 64;           // [2] a tile's scores are wanted again
   static constexpr int kBars = kAgain + 8;
   static constexpr int kSegAt = kBars + 8 * (2 * kRing + 14 + 2 * kSegs);
@@ -252,11 +252,12 @@ static_assert(lay_aligned<64>() && lay_aligned<128>(), "alignment");
 // has 11 bits.  They may exceed it by 2^kSlack before the sums are rescaled at the next step, and by 2^kMost at all, for half's range.
 constexpr float kBias = 7.0f, kSlack = 6.0f, kMost = 8.75f;
 
-// A value's power of two, by which it is taken out: v 2^-E is in 2^14 .. 2^15, or less where the row is tiny or zero or, being
-// held as NaN (both comparisons fail), left out.
+// A token's values are left out of the product where they are no finite numbers: held as NaN, or, at places that no query
+// sees, whatever lies there.  0 times what is not finite would reach every row.  (Halves: the largest may round past 32 bits.)
+__device__ __forceinline__ bool value_finite(float2 p) { return fabsf(fmaf(7.5f, p.x, 0.5f * p.y)) < INFINITY && fabsf(p.y) < INFINITY; }
+// The power of two by which they are taken out: v 2^-E is in 2^14 .. 2^15, or less where the row is tiny or zero.
 __device__ __forceinline__ int value_exponent(float2 p) {
-  const float big = fmaxf(fabsf(p.y), fabsf(fmaf(15.0f, p.x, p.y)));
-  return big == big ? max(static_cast<int>(__float_as_uint(big) >> 23) - 141, -60) : -60;
+  return max(static_cast<int>(__float_as_uint(fmaxf(fabsf(0.5f * p.y), fabsf(fmaf(7.5f, p.x, 0.5f * p.y)))) >> 23) - 140, -60);
 }
 
 // Whether any of a tile's 128 threads says so; barrier `id` of the block.
@@ -617,7 +618,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
           y.v = total[e];
           fl[e] += y.f[0] + y.f[1];
         }
-        // A value held as NaN is left out of the product.  A row that sees one is marked, in the place of what a score is to be
+        // A value that is not finite is left out of the product.  A row that sees one is marked, in the place of what a score is to be
         // multiplied by, which is in registers: its output is NaN, its sum of weights is not.
         const uint4 nans = reinterpret_cast<const uint4 *>(smem + L::kNan)[buf];
         if (nans.x | nans.y | nans.z | nans.w) {
@@ -724,8 +725,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
         for (int e = 0; e < 2; ++e) {
           float2 p0 = kv4_param(vp[2 * e]), p1 = kv4_param(vp[2 * e + 1]);
           const int32_t tok = tok0 + 4 * lane + 2 * e;
-          if (tok >= hi || p0.x != p0.x || p0.y != p0.y) p0 = make_float2(0.0f, 0.0f);
-          if (tok + 1 >= hi || p1.x != p1.x || p1.y != p1.y) p1 = make_float2(0.0f, 0.0f);
+          if (tok >= hi || !value_finite(p0)) p0 = make_float2(0.0f, 0.0f);
+          if (tok + 1 >= hi || !value_finite(p1)) p1 = make_float2(0.0f, 0.0f);
           const float d0 = __uint_as_float(static_cast<uint32_t>(127 - value_exponent(p0)) << 23), d1 = __uint_as_float(static_cast<uint32_t>(127 - value_exponent(p1)) << 23);
           vs[e] = pack_half(p0.x * d0, p1.x * d1);
           vz[e] = pack_half(p0.y * d0, p1.y * d1);
@@ -929,7 +930,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
             }
           }
           }
-        // ---- the values' powers of two, and those held as NaN, from 4 tokens a lane
+        // ---- the values' powers of two, and those that are not finite, from 4 tokens a lane
         const uint4 v4 = *reinterpret_cast<const uint4 *>(record(lane >> 2) + 16 * D + 64 + (lane & 3) * 16);
         const uint32_t vp[4] = {v4.x, v4.y, v4.z, v4.w};
         uint32_t bad = 0;
@@ -938,8 +939,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
         for (int e = 0; e < 4; ++e) {
           const float2 p = kv4_param(vp[e]);
           const bool there = tok0 + 4 * lane + e < hi;
-          if (there && (p.x != p.x || p.y != p.y)) bad |= 1u << e;
-          const int E = there ? value_exponent(p) : -60;
+          const bool finite = value_finite(p);
+          if (there && !finite) bad |= 1u << e;
+          const int E = there && finite ? value_exponent(p) : -60;
           ve[e] = static_cast<float>(E);
           weight[e] = __uint_as_float(static_cast<uint32_t>(127 - E) << 23);
         }
