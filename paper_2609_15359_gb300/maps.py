@@ -361,14 +361,19 @@ def maps_block_tables(S: int, held, want, table, free_blocks, n_free, n_free_out
     """Hands out the KV blocks: table [R][max_blocks] and free_blocks [pool]
     int32 are updated in place; slots_out [cap] int64 holds the new tokens'."""
     R = held.numel()
+    rows, max_blocks = table.shape
+    cap = slots_out.numel()
+    if (want.numel() < R or got_out.numel() < R or slot_off_out.numel() <= R or rows < R or
+            order is not None and order.numel() < R or pos_out is not None and pos_out.numel() < cap):
+        raise ValueError("want, order, table, got_out, slot_off_out or pos_out has too few elements")
     ws, on = _scratch(ws, _need(None, "maps_block_tables_workspace_size", R), stream)
     return lib.maps_block_tables(R, S, _ptr(held, torch.int32), _ptr(want, torch.int32),
                                  _ptr(order, torch.int32), _ptr(table, torch.int32),
-                                 table.shape[1], _ptr(free_blocks, torch.int32),
+                                 max_blocks, _ptr(free_blocks, torch.int32),
                                  free_blocks.numel(), _ptr(n_free, torch.int32),
                                  _ptr(n_free_out, torch.int32), _ptr(got_out, torch.int32),
                                  _ptr(slot_off_out, torch.int64), _ptr(slots_out, torch.int64),
-                                 slots_out.numel(), _ptr(pos_out, torch.int32), ws.ptr, ws.nbytes,
+                                 cap, _ptr(pos_out, torch.int32), ws.ptr, ws.nbytes,
                                  on)
 
 
