@@ -382,44 +382,44 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
         constexpr int kBatch = 8;  // loads under way at once
 #pragma unroll 1
         for (int x0 = 0; x0 < kLanes; x0 += kBatch) {
-        uint4 raws[kBatch];
+          uint4 raws[kBatch];
 #pragma unroll
-        for (int x = 0; x < kBatch; ++x) {
-          const int Rx = w.rt * kRows + t * 128 + (warp & 3) * 32 + (x0 + x) * kAt + lane / kLanes;
-          raws[x] = make_uint4(0, 0, 0, 0);
-          if (Rx < rows) {
-            const T *src = static_cast<const T *>(a.q) + (q0 + Rx / group) * a.q_row + (h0 + Rx % group) * a.q_head + 8 * (lane % kLanes);
-            if (a.wide) {
-              raws[x] = *reinterpret_cast<const uint4 *>(src);
-            } else {
-              T *z = reinterpret_cast<T *>(&raws[x]);
+          for (int x = 0; x < kBatch; ++x) {
+            const int Rx = w.rt * kRows + t * 128 + (warp & 3) * 32 + (x0 + x) * kAt + lane / kLanes;
+            raws[x] = make_uint4(0, 0, 0, 0);
+            if (Rx < rows) {
+              const T *src = static_cast<const T *>(a.q) + (q0 + Rx / group) * a.q_row + (h0 + Rx % group) * a.q_head + 8 * (lane % kLanes);
+              if (a.wide) {
+                raws[x] = *reinterpret_cast<const uint4 *>(src);
+              } else {
+                T *z = reinterpret_cast<T *>(&raws[x]);
 #pragma unroll
-              for (int e = 0; e < 8; ++e) z[e] = src[e];
+                for (int e = 0; e < 8; ++e) z[e] = src[e];
+              }
             }
           }
-        }
 #pragma unroll
-        for (int x = 0; x < kBatch; ++x) {
-          const int r = (warp & 3) * 32 + (x0 + x) * kAt + lane / kLanes, at = lane % kLanes;
-          const T *y = reinterpret_cast<const T *>(&raws[x]);
-          float q[8], top = 0.0f, sum = 0.0f;
+          for (int x = 0; x < kBatch; ++x) {
+            const int r = (warp & 3) * 32 + (x0 + x) * kAt + lane / kLanes, at = lane % kLanes;
+            const T *y = reinterpret_cast<const T *>(&raws[x]);
+            float q[8], top = 0.0f, sum = 0.0f;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) q[e] = Cvt<T>::to(y[e]), top = fmaxf(top, fabsf(q[e]));
+            for (int e = 0; e < 8; ++e) q[e] = Cvt<T>::to(y[e]), top = fmaxf(top, fabsf(q[e]));
 #pragma unroll
-          for (int o = kLanes / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-          const int ef = min(max(static_cast<int>(__float_as_uint(top) >> 23), 20), 254);
-          const float up = __uint_as_float(static_cast<uint32_t>(268 - ef) << 23);
+            for (int o = kLanes / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            const int ef = min(max(static_cast<int>(__float_as_uint(top) >> 23), 20), 254);
+            const float up = __uint_as_float(static_cast<uint32_t>(268 - ef) << 23);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) q[e] *= up, sum += q[e];
+            for (int e = 0; e < 8; ++e) q[e] *= up, sum += q[e];
 #pragma unroll
-          for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-          const uint4 z = make_uint4(pack_half(q[0], q[4]), pack_half(q[1] * 0.0625f, q[5] * 0.0625f), pack_half(q[2], q[6]),
-                                     pack_half(q[3] * 0.0625f, q[7] * 0.0625f));
-          *reinterpret_cast<uint4 *>(smem + L::kQ + t * L::kTile + at / 8 * 16384 + r * 128 + ((at % 8 ^ (r & 7)) << 4)) = z;
-          if (at == 0)
-            *reinterpret_cast<float2 *>(row_of + r) =
-                make_float2(sum, fmaxf(fabsf(sl2) * __uint_as_float(static_cast<uint32_t>(ef - 14) << 23), 1.17549435e-38f));
-        }
+            for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            const uint4 z = make_uint4(pack_half(q[0], q[4]), pack_half(q[1] * 0.0625f, q[5] * 0.0625f), pack_half(q[2], q[6]),
+                                       pack_half(q[3] * 0.0625f, q[7] * 0.0625f));
+            *reinterpret_cast<uint4 *>(smem + L::kQ + t * L::kTile + at / 8 * 16384 + r * 128 + ((at % 8 ^ (r & 7)) << 4)) = z;
+            if (at == 0)
+              *reinterpret_cast<float2 *>(row_of + r) =
+                  make_float2(sum, fmaxf(fabsf(sl2) * __uint_as_float(static_cast<uint32_t>(ef - 14) << 23), 1.17549435e-38f));
+          }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
@@ -910,59 +910,59 @@ __global__ void __launch_bounds__(kThreads, 1) attn_many_kernel(const AttnArgs a
 #pragma unroll 1
           for (int g = 0; g < kStepGroups; ++g) {
             const uint8_t *rec = record(g);
-          // ---- keys: a token's row, 8 channels to 16 bytes
+            // ---- keys: a token's row, 8 channels to 16 bytes
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            const int tr = half * 8 + (lane >> 2), t = lane & 3, row = g * kGroup + tr;
-            uint32_t words[D / 32];
-            if (D == 64)
-              *reinterpret_cast<uint2 *>(words) = *reinterpret_cast<const uint2 *>(rec + tr * (D / 2) + t * (D / 8));
-            else
-              *reinterpret_cast<uint4 *>(words) = *reinterpret_cast<const uint4 *>(rec + tr * (D / 2) + t * (D / 8));
+            for (int half = 0; half < 2; ++half) {
+              const int tr = half * 8 + (lane >> 2), t = lane & 3, row = g * kGroup + tr;
+              uint32_t words[D / 32];
+              if (D == 64)
+                *reinterpret_cast<uint2 *>(words) = *reinterpret_cast<const uint2 *>(rec + tr * (D / 2) + t * (D / 8));
+              else
+                *reinterpret_cast<uint4 *>(words) = *reinterpret_cast<const uint4 *>(rec + tr * (D / 2) + t * (D / 8));
 #pragma unroll
-            for (int x = 0; x < D / 32; ++x) {
-              // lanes of the second 64 channels take their words in another order, so that eight lanes write to eight different banks
-              const bool other = D == 128 && (t & 2);
-              const int y = other ? x ^ 2 : x;
-              const Codes z = codes_of(D == 128 && other ? words[(x ^ 2) % (D / 32)] : words[x]);
-              const int chunk = t * (D / 32) + y;
-              *reinterpret_cast<uint4 *>(K + chunk / 8 * 16384 + row * 128 + ((chunk % 8 ^ (row & 7)) << 4)) = make_uint4(z.x[0], z.x[1], z.x[2], z.x[3]);
+              for (int x = 0; x < D / 32; ++x) {
+                // lanes of the second 64 channels take their words in another order, so that eight lanes write to eight different banks
+                const bool other = D == 128 && (t & 2);
+                const int y = other ? x ^ 2 : x;
+                const Codes z = codes_of(D == 128 && other ? words[(x ^ 2) % (D / 32)] : words[x]);
+                const int chunk = t * (D / 32) + y;
+                *reinterpret_cast<uint4 *>(K + chunk / 8 * 16384 + row * 128 + ((chunk % 8 ^ (row & 7)) << 4)) = make_uint4(z.x[0], z.x[1], z.x[2], z.x[3]);
+              }
             }
           }
+          // ---- the values' powers of two, and those that are not finite, from 4 tokens a lane
+          const uint4 v4 = *reinterpret_cast<const uint4 *>(record(lane >> 2) + 16 * D + 64 + (lane & 3) * 16);
+          const uint32_t vp[4] = {v4.x, v4.y, v4.z, v4.w};
+          uint32_t bad = 0;
+          float ve[4], weight[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float2 p = kv4_param(vp[e]);
+            const bool there = tok0 + 4 * lane + e < hi;
+            const bool finite = value_finite(p);
+            if (there && !finite) bad |= 1u << e;
+            const int E = there && finite ? value_exponent(p) : -60;
+            ve[e] = static_cast<float>(E);
+            weight[e] = __uint_as_float(static_cast<uint32_t>(127 - E) << 23);
           }
-        // ---- the values' powers of two, and those that are not finite, from 4 tokens a lane
-        const uint4 v4 = *reinterpret_cast<const uint4 *>(record(lane >> 2) + 16 * D + 64 + (lane & 3) * 16);
-        const uint32_t vp[4] = {v4.x, v4.y, v4.z, v4.w};
-        uint32_t bad = 0;
-        float ve[4], weight[4];
+          bad <<= (lane & 7) * 4;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float2 p = kv4_param(vp[e]);
-          const bool there = tok0 + 4 * lane + e < hi;
-          const bool finite = value_finite(p);
-          if (there && !finite) bad |= 1u << e;
-          const int E = there && finite ? value_exponent(p) : -60;
-          ve[e] = static_cast<float>(E);
-          weight[e] = __uint_as_float(static_cast<uint32_t>(127 - E) << 23);
-        }
-        bad <<= (lane & 7) * 4;
+          for (int o = 4; o > 0; o >>= 1) bad |= __shfl_xor_sync(0xffffffffu, bad, o);
+          if ((lane & 7) == 0) reinterpret_cast<uint32_t *>(smem + L::kNan)[4 * (c & 3) + (lane >> 3)] = bad;
+          // ---- keys' scales and zeros, two tokens side by side
+          {
+            const uint4 k4 = *reinterpret_cast<const uint4 *>(record(lane >> 2) + 16 * D + (lane & 3) * 16);
+            const uint32_t kp[4] = {k4.x, k4.y, k4.z, k4.w};
 #pragma unroll
-        for (int o = 4; o > 0; o >>= 1) bad |= __shfl_xor_sync(0xffffffffu, bad, o);
-        if ((lane & 7) == 0) reinterpret_cast<uint32_t *>(smem + L::kNan)[4 * (c & 3) + (lane >> 3)] = bad;
-        // ---- keys' scales and zeros, two tokens side by side
-        {
-          const uint4 k4 = *reinterpret_cast<const uint4 *>(record(lane >> 2) + 16 * D + (lane & 3) * 16);
-          const uint32_t kp[4] = {k4.x, k4.y, k4.z, k4.w};
-#pragma unroll
-          for (int e = 0; e < 4; e += 2) {
-            float2 p0 = kv4_param(kp[e]), p1 = kv4_param(kp[e + 1]);
-            if (tok0 + 4 * lane + e >= hi) p0 = make_float2(0.0f, 0.0f);
-            if (tok0 + 4 * lane + e + 1 >= hi) p1 = make_float2(0.0f, 0.0f);
-            float4 *par = reinterpret_cast<float4 *>(smem + L::kPar + (c & 3) * kTok * 16) + 4 * lane + e;
-            par[0] = make_float4(p0.x * (k_sign * kEven), p1.x * (k_sign * kEven), p0.y * k_sign, p1.y * k_sign);
-            par[1] = make_float4(ve[e], ve[e + 1], weight[e], weight[e + 1]);
+            for (int e = 0; e < 4; e += 2) {
+              float2 p0 = kv4_param(kp[e]), p1 = kv4_param(kp[e + 1]);
+              if (tok0 + 4 * lane + e >= hi) p0 = make_float2(0.0f, 0.0f);
+              if (tok0 + 4 * lane + e + 1 >= hi) p1 = make_float2(0.0f, 0.0f);
+              float4 *par = reinterpret_cast<float4 *>(smem + L::kPar + (c & 3) * kTok * 16) + 4 * lane + e;
+              par[0] = make_float4(p0.x * (k_sign * kEven), p1.x * (k_sign * kEven), p0.y * k_sign, p1.y * k_sign);
+              par[1] = make_float4(ve[e], ve[e + 1], weight[e], weight[e + 1]);
+            }
           }
-        }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
           if (lane == 0) {
