@@ -174,7 +174,7 @@ class Workspace:
         self._take(max(int(nbytes), 256), stream)
 
     def _take(self, nbytes: int, stream=None) -> None:
-        old = getattr(self, "buf", None)
+        old = getattr(self, "_buf", None)
         if old is not None and self.on_gpu and _stream(stream) not in self.known:
             self._meet(stream)
         self.filled, self.known = None, set()  # the zero-fill, and the streams that are behind it
@@ -191,7 +191,14 @@ class Workspace:
         else:
             self.buf = torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
             self.known.add(None)
-        self.ptr, self.nbytes = self.buf.data_ptr(), nbytes
+
+    @property
+    def buf(self):
+        return self._buf
+
+    @buf.setter
+    def buf(self, buf) -> None:
+        self._buf, self.ptr, self.nbytes = buf, ctypes.c_void_p(buf.data_ptr()), buf.numel()
 
     def _meet(self, stream) -> None:
         s = torch.cuda.current_stream(self.device) if stream is None else stream

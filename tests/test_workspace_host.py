@@ -29,6 +29,9 @@ class Buffer:
     def data_ptr(self):
         return 4096 * (1 + self.n)
 
+    def numel(self):
+        return self.n
+
     def record_stream(self, s):
         self.log.append(("keep", self.n, s.cuda_stream))
 
@@ -144,3 +147,17 @@ def test_the_current_stream_without_the_private_function(monkeypatch):
     spec.loader.exec_module(other)
     monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: Stream(17, []))
     assert other._stream(None) == 17 and other._stream(Stream(5, [])) == 5
+
+
+def test_pointer_and_size_are_the_buffers():
+    """`ptr` is a pointer for any ctypes call, one without declared arguments too, and follows a buffer that its owner puts in."""
+    import ctypes
+
+    from paper_2609_15359_gb300 import maps as M
+    ws = M.Workspace(1000, device="cpu")
+    assert isinstance(ws.ptr, ctypes.c_void_p) and ws.ptr.value == ws.buf.data_ptr() and ws.nbytes == 1000
+    mine = torch.zeros(4096, dtype=torch.uint8)
+    ws.buf = mine
+    assert ws.buf is mine and ws.ptr.value == mine.data_ptr() and ws.nbytes == 4096
+    ws.ensure(5000)
+    assert ws.nbytes == 5000 == ws.buf.numel() and ws.ptr.value == ws.buf.data_ptr()
