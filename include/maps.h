@@ -578,11 +578,15 @@ int maps_kv4_read(int32_t dtype, int64_t T, int32_t H, int32_t D, int32_t S, con
  *   table               [B][max_blocks] int32 block tables.
  *   causal, window      0 or 1; 0 (no window) or the keys seen, >= 1.
  *   lse                 [T][Hq] float output, natural logarithm, or NULL.
- *   ws                  about 5 MB, and 40 MB more where a request can have more
- *                       than 96 query rows to a KV head (D = 64, 128).  After
- *                       MAPS_E_TIMEOUT it is to be zero-filled anew.
+ *   ws                  2.6 MB, and 20 (D = 64) or 40 MB (128) more where a
+ *                       request can have more than 96 query rows to a KV head,
+ *                       on a device of 152 multiprocessors, with which it
+ *                       grows.  After MAPS_E_TIMEOUT it is to be zero-filled
+ *                       anew.
  * A length or a used table entry out of its domain is MAPS_E_RANGE (via
- * maps_check); nothing outside the cache is read.
+ * maps_check); nothing outside the cache is read.  So is a call of 2^31 units of
+ * work or more, of which no output is written: a unit is 32 to 96 keys of a KV
+ * head for 8 or 16 query rows, or, with many queries, 128 keys for 256.
  * ---------------------------------------------------------------------- */
 size_t maps_kv4_attention_workspace_size(int32_t B, int64_t T, int32_t Hq, int32_t Hkv, int32_t D);
 int maps_kv4_attention(int32_t dtype, int32_t B, int64_t T, int32_t Hq, int32_t Hkv, int32_t D,

@@ -480,6 +480,8 @@ int maps_block_tables(int32_t R, int32_t S, const int32_t *held, const int32_t *
   // A decode step's worth in one kernel: what one block has to expand besides costs less than a launch (64 requests, a token
   // each: 3.9 us, 4.7 with two kernels; 256 with 8 tokens 5.4, 5.9; with 16 tokens 7.1, 6.3).  The sums are one block's up to
   // its threads, then a cluster's of eight (1,024 requests: 7.8, 11.1 us; 2,048: 16.0, 15.6; 4,096: 24.2, 16.0).
+  // The pool bounds the blocks that one block may have to put back (256 requests of 32 blocks, one kernel and two: none finish
+  // 5.1, 5.9 us; 32 do 6.3, 7.1; 128 do 8.1, 6.9; all do 9.5, 7.5); from a larger pool they could be more.
   const bool all = R <= kScanThreads && slots_cap <= 2 * kScanThreads && pool <= 16 * kScanThreads;
   if (all)
     launch_pdl(bt_scan_kernel<1, true>, 1, kScanThreads, 0, s, a);

@@ -359,7 +359,8 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn_few_kernel(con
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         const int R = at.rt * Sh::kRows + nt * 8 + g;
-        // A row is scaled by a power of two to fill half's range; only its smallest channels, below 2^-38 of the largest, lose bits.
+        // A row is scaled by a power of two to fill half's range.  Only its smallest channels lose bits: below 2^-31 of the largest
+        // (bfloat16) or 2^-28 (half), and the odd ones, which enter divided by 16, below 2^-27 and 2^-24.
         float x[kSteps * 4], top = 0.0f;
         const bool there = R < rows;
         const T *src = static_cast<const T *>(a.q) + (there ? (q0 + R / group) * a.q_row + (at.h * group + R % group) * a.q_head + t * (D / 4) : 0);
@@ -825,7 +826,8 @@ static void carve(maps::Carve &c, maps::AttnArgs &a, int32_t B, int64_t T, int32
   a.parts = c.take<float>(static_cast<size_t>(attn_grid()) * 2 * kMaxParts);
   a.starts = c.take<Start>(B > kMaxLocalB ? static_cast<size_t>(attn_grid()) * kMaxWarps : 0);
   a.units = c.take<uint32_t>(2);
-  // requests with many queries there can only be where there are more rows than requests
+  // A decode step has as many rows as requests and spends no launches on the other form; so has a batch of fewer rows than
+  // requests, whose chunks, where it has any, are served here too.
   a.few_rows = Hkv > 0 && attn_many_dim(D) && T > B && T * (Hq / Hkv) > kFewRows ? kFewRows : 0;
   if (a.few_rows) attn_many_carve(c, a, B, D);
 }

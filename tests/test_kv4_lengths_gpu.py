@@ -51,3 +51,18 @@ def test_the_longest_request(M, D, n_q):
     for n in (LAST + 1, 2**31 - 97, 2**31 - 1):
         assert status(n) == M.MAPS_E_RANGE
     assert status(LAST) == 0
+
+
+@pytest.mark.parametrize("n_q", [1, 300])
+def test_more_work_than_a_call_can_count(M, n_q):
+    """2^31 units and more are refused before any of them is begun: nothing is written."""
+    S, B, D = 4096, 140, 64
+    cache = torch.zeros(M.kv4_cache_shape(1, 1, S, D), dtype=torch.uint8, device="cuda")
+    table = torch.zeros(B, 2**31 // S, dtype=torch.int32, device="cuda")
+    q = torch.zeros(B * n_q, 1, D, dtype=torch.float16, device="cuda")
+    out = torch.full_like(q, 7.0)
+    ws = M.Workspace()
+    off = torch.arange(B + 1, device="cuda") * n_q
+    assert M.maps_kv4_attention(q, off, torch.full((B,), LAST, dtype=torch.int32, device="cuda"), table, cache, S, 0.1, out, ws=ws) == 0
+    assert M.maps_check(ws) == M.MAPS_E_RANGE
+    assert (out == 7).all()
