@@ -46,7 +46,7 @@ struct alignas(32) Request {
   int64_t begin;   // its first new token
   int64_t before;  // blocks granted ahead of its first, -1 where it is refused
   int32_t held, last;  // tokens held, and the block of the last of them (where it is not full)
-  int32_t named;       // whether the order has named it
+  uint32_t named;      // whether the order has named it (where several blocks take the sums)
 };
 // The sums over all, for the kernels that expand them.
 struct alignas(32) Totals {
@@ -215,8 +215,10 @@ __device__ __forceinline__ void fill_token(const BTArgs &a, const Totals &t, int
 
 template <int kBlocks, bool kAll>  // kAll: and expands the sums too
 __global__ void __launch_bounds__(kScanThreads) bt_scan_kernel(const BTArgs a) {
-  pdl_prologue();
+  __shared__ uint32_t s_named[kBlocks == 1 ? kScanThreads / 32 : 1];  // one block: the requests that the order has named
   const int tid = threadIdx.x;
+  if (kBlocks == 1 && tid < kScanThreads / 32) s_named[tid] = 0;
+  pdl_prologue();
   // the block's tiles of 1,024 requests; where it has more than one, a first pass sums them up
   const int tiles = (a.R + kScanThreads - 1) / kScanThreads, each = (tiles + kBlocks - 1) / kBlocks;
   const int r0 = static_cast<int>(min(static_cast<int64_t>(blockIdx.x) * each * kScanThreads, static_cast<int64_t>(a.R)));
@@ -264,7 +266,7 @@ __global__ void __launch_bounds__(kScanThreads) bt_scan_kernel(const BTArgs a) {
       a.off[r] = sy, a.back[r] = sx;
       Request &q = a.requests[r];
       q.begin = sy, q.held = n.held, q.last = last;
-      if (a.order) q.before = -1, q.named = 0;  // one that the order leaves out gets nothing
+      if (a.order) q.before = -1, q.named = 0u;  // one that the order leaves out gets nothing
       set_marks(a.coarse, r, sy, y, mark_shift(toks));
       set_marks(a.coarse + kCoarse + 2, r, sx, x, mark_shift(back));
     }
@@ -297,7 +299,7 @@ __global__ void __launch_bounds__(kScanThreads) bt_scan_kernel(const BTArgs a) {
     cluster_sums<kBlocks>(tx, 0, ahead, unused, all, unused);
   }
   int64_t granted = 0;  // the needs up to the last one granted
-  int32_t twice_named = 0;
+  uint32_t twice_named = 0;
   for (int base = r0, k = 0; k < each; base += kScanThreads, ++k) {
     int r;
     const int64_t x = place(base + tid, r, n);
@@ -307,7 +309,12 @@ __global__ void __launch_bounds__(kScanThreads) bt_scan_kernel(const BTArgs a) {
     sx += ahead;
     if (r >= 0) {
       const bool ok = x == 0 || sx + x <= N;
-      if (a.order) twice_named |= atomicExch(&a.requests[r].named, 1);
+      if (a.order) {
+        if (kBlocks == 1)
+          twice_named |= atomicOr(&s_named[r >> 5], 1u << (r & 31)) >> (r & 31) & 1u;
+        else
+          twice_named |= atomicExch(&a.requests[r].named, 1u);
+      }
       a.requests[r].before = ok ? sx : -1;
       a.got[r] = n.want < n.held || ok ? n.want : n.held;
       if (ok && x) granted = sx + x;
@@ -481,7 +488,7 @@ int maps_block_tables(int32_t R, int32_t S, const int32_t *held, const int32_t *
   // each: 3.9 us, 4.7 with two kernels; 256 with 8 tokens 5.4, 5.9; with 16 tokens 7.1, 6.3).  The sums are one block's up to
   // its threads, then a cluster's of eight (1,024 requests: 7.8, 11.1 us; 2,048: 16.0, 15.6; 4,096: 24.2, 16.0).
   // The pool bounds the blocks that one block may have to put back (256 requests of 32 blocks, one kernel and two: none finish
-  // 5.1, 5.9 us; 32 do 6.3, 7.1; 128 do 8.1, 6.9; all do 9.5, 7.5); from a larger pool they could be more.
+  // 4.5, 5.3 us; 32 do 5.8, 6.8; 128 do 7.4, 7.1; all do 8.7, 7.0); from a larger pool they could be more.
   const bool all = R <= kScanThreads && slots_cap <= 2 * kScanThreads && pool <= 16 * kScanThreads;
   if (all)
     launch_pdl(bt_scan_kernel<1, true>, 1, kScanThreads, 0, s, a);
