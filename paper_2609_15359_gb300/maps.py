@@ -174,23 +174,20 @@ class Workspace:
         self._take(max(int(nbytes), 256), stream)
 
     def _take(self, nbytes: int, stream=None) -> None:
+        on = _stream(stream) if self.on_gpu else None
+        if on is not None and on != _stream(None):
+            with torch.cuda.stream(stream):
+                return self._take(nbytes)
         old = getattr(self, "_buf", None)
-        if old is not None and self.on_gpu and _stream(stream) not in self.known:
+        if old is not None and on not in self.known:
             self._meet(stream)
-        self.filled, self.known = None, set()  # the zero-fill, and the streams that are behind it
-        if self.on_gpu:
-            s = torch.cuda.current_stream(self.device) if stream is None else stream
-            with torch.cuda.stream(s):
-                self.buf = torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
-                if old is not None:
-                    self.buf[:4].copy_(old[:4])
-                if not torch.cuda.is_current_stream_capturing():
-                    self.filled = torch.cuda.Event()
-                    self.filled.record(s)
-            self.known.add(s.cuda_stream)
-        else:
-            self.buf = torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
-            self.known.add(None)
+        self.filled, self.known = None, {on}  # the zero-fill, and the streams that are behind it
+        self.buf = torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
+        if old is not None:
+            self._buf[:4].copy_(old[:4])
+        if self.on_gpu and not torch.cuda.is_current_stream_capturing():
+            self.filled = torch.cuda.Event()
+            self.filled.record(torch.cuda.current_stream(self.device))
 
     @property
     def buf(self):
@@ -206,7 +203,7 @@ class Workspace:
             # what was queued before a capture began is done by the time that its graph runs
             if self.filled is not None and not torch.cuda.is_current_stream_capturing():
                 s.wait_event(self.filled)
-        self.buf.record_stream(s)
+        self._buf.record_stream(s)
         self.known.add(s.cuda_stream)
 
     def ensure(self, nbytes: int, stream=None) -> "Workspace":
