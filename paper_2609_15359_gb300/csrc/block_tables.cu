@@ -19,7 +19,7 @@
 // onto the stack first and a token costs one load of it.
 //
 // Bound: a decode step (64 requests) by latency, 4.5 us for a launch and three rounds of dependent loads;
-// 4,096 requests with prompts up to 8,192 tokens, 32 MB mostly written, 26 us: 16 of them are sums and
+// 4,096 requests with prompts up to 8,192 tokens, 32 MB mostly written, 27 us: 16 of them are sums and
 // launches, in the rest slots and positions are written at about 3 TB/s.
 #include <cooperative_groups.h>
 

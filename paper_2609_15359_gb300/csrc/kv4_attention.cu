@@ -35,8 +35,8 @@ namespace {
 
 constexpr int kMaxWarps = 16;  // of a block
 // Query rows of a request to a KV head up to which this form serves it where the other may.  Both grow with the rows, this
-// one by tiles of 16: 32 requests of 4,096 tokens, 128 channels: 64 rows 160 us here, 218 there; 96 rows 231, 218;
-// 128 rows 299, 219.  With 64 channels 171, 176 at 96; with 4 requests 46, 56 at 96 and 89, 68 at 256.
+// one by tiles of 16: 32 requests of 4,096 random tokens, 128 channels: 64 rows 189 us here, 229 there; 96 rows 265, 229;
+// 128 rows 343, 231.  With 64 channels 191, 181 at 96; with 4 requests 53, 57 at 96 and 100, 69 at 256.
 constexpr int kFewRows = 96;
 
 __device__ __forceinline__ uint32_t transpose8(uint32_t x) {

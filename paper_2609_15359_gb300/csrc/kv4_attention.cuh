@@ -133,8 +133,8 @@ struct Deal {
 
 // Query rows x keys x KV heads of all requests that may go to the form for many queries, up to which none does: its queries,
 // parts and joins cost 40 us and more whatever the lengths (a window, which lessens both forms' work, is left out of account).
-// 128 channels, one request of 256 rows and 4,096 tokens (8 million): 36 us with few, 72 with many; four of 128 rows
-// (17 million) 54, 57; 32 of 128 rows and 500 tokens (16 million) 75, 69; four of 256 rows (34 million) 89, 68.
+// 128 channels, one request of 256 rows and 4,096 tokens (8 million): 44 us with few, 76 with many; four of 128 rows
+// (17 million) 63, 58; 32 of 128 rows and 500 tokens (16 million) 76, 73; four of 256 rows (34 million) 100, 69.
 constexpr uint64_t kFewPairs = uint64_t(1) << 24;
 
 // The rows over which a request of this call goes to the form for many queries; 0: none does.  All kN threads call it.

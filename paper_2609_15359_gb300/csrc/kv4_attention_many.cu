@@ -23,10 +23,10 @@
 // the others left later steps' weights below half's range.  The whole scale on the weights would be three operations a score.
 //
 // Bound.  A step's four products take the tensor cores about 2,200 cycles at D = 128 where nothing else runs, but a step
-// takes 6,800: each tile's chain of softmax (3,500 cycles: scores, weights, the tile's vote, P) and products (3,100 from P to the next
-// S, which replaces P), in which the products take two and a half times as long to issue as alone.  The tensor
-// cores work 28 % of the time, and issue slots are 43 % taken.  Six chunks of 1,024 queries, 32 heads on 8, behind 1,500
-// to 9,000 tokens: 782 us, 552 TFLOP/s of 432 GFLOP (0.29 of the measured dense rate).  S in halves of 64 keys, the first beside
+// takes 6,800: each tile's chain of softmax (some 3,500 cycles: scores, weights, the tile's vote, P) and products (3,100 from P to the
+// next S, which replaces P), in which the products take two and a half times as long to issue as alone.  The tensor
+// cores' pipe is active 24 % of the time, and issue slots are 46 % taken.  Six chunks of 1,024 queries, 32 heads on 8, behind 1,500
+// to 9,000 tokens: 783 us, 552 TFLOP/s of 432 GFLOP (0.29 of the measured dense rate); with 64 channels 636.  S in halves of 64 keys, the first beside
 // P, so that the softmax need not wait for the sums, was 894 us: more and smaller products for the same thread.
 //
 // Split.  As in the other form, a call's steps are dealt out to the blocks in equal runs, whatever the
