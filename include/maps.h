@@ -561,10 +561,12 @@ int maps_kv4_read(int32_t dtype, int64_t T, int32_t H, int32_t D, int32_t S, con
  * Scores, maxima, sums and lse are held in 32 bits.  A weight is rounded to 11
  * bits where it meets its value's code (taken about 0, for MAPS_F16 about 8),
  * or, with many queries a request, its value, which is rounded to 11 bits too;
- * one that is, times its value, below 2^-21 of the row's largest is rounded
- * to 2^-32 of that.  out is rounded once more.  The order of the sums depends
- * on sizes and lengths alone, so a call repeated gives the same bits.  A query that sees no key has out = 0
- * and lse = -infinity.  What the cache holds at places that no query sees is
+ * one that is, times its value (which counts as 2^-60 at least), below 2^-21 of
+ * the row's largest is rounded to 2^-32 of that.  Rows of values below 2^-60,
+ * zeros too, may lose their part in the sums of weights beside values past
+ * 2^60.  out is rounded once more.  The order of the sums depends on sizes and
+ * lengths alone, so a call repeated gives the same bits.  A query that sees no
+ * key has out = 0 and lse = -infinity.  What the cache holds at places that no query sees is
  * not used, whatever it is.
  *
  *   dtype               MAPS_BF16 or MAPS_F16, of q and out.
