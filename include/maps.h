@@ -598,6 +598,133 @@ int maps_kv4_attention(int32_t dtype, int32_t B, int64_t T, int32_t Hq, int32_t 
                        int32_t causal, int32_t window, void *out, int64_t o_row, int64_t o_head,
                        float *lse, void *ws, size_t ws_bytes, void *stream);
 
+/* ------------------------------------------------------------------------
+ * maps_kv4_append for models with rotary positions: keys are turned by their
+ * tokens' positions on the way into the cache, and the batch's queries with
+ * them.  A position may have several axes (one for text; time, height and
+ * width for images and video).
+ *
+ * The first `rot` channels of a row are rot/2 pairs, pair f being channels f
+ * and f + rot/2, or 2f and 2f + 1 where interleaved; the others stay as they
+ * are.  With p = pos[axis[f]][i] the position of token i on the pair's axis,
+ * c = cos_sin[p][f] and s = cos_sin[p][rot/2 + f], a pair (a, b) becomes
+ *     (a c - b s, b c + a s),
+ * in 32 bits, each product, difference and sum rounded to nearest.  A query is
+ * then rounded to its type.  A key is quantised as maps_kv4_append does it, but
+ * from the 32 bits; a value as maps_kv4_append does it.
+ *
+ *   Hq                  query heads (>= 0; 0: no queries, q and q_out NULL);
+ *                       T * (Hq + H) <= 2^30.
+ *   q, q_out            [T][Hq][D] with any strides, like k and v; q_out may be
+ *                       q itself, with the same strides, and otherwise shares no
+ *                       memory with q, k or v.  A token without a slot has its
+ *                       queries turned like any other.
+ *   axes, pos           axes (1 .. 8) and [axes][T] int32 positions.
+ *   axis                [rot/2] int32, the axis of each pair, or NULL: all on
+ *                       axis 0.
+ *   rot, interleaved    channels that are turned: a multiple of 16 up to D, 0
+ *                       for none; 0 or 1.
+ *   cos_sin, n_pos      [n_pos][rot] float: a position's cosines, then its sines.
+ *   all others          as for maps_kv4_append.
+ * A position outside [0, n_pos) or an axis outside [0, axes) is MAPS_E_RANGE (via
+ * maps_check), and pairs on it are not turned.
+ * ---------------------------------------------------------------------- */
+int maps_kv4_append_rotated(int32_t dtype, int64_t T, int32_t Hq, int32_t H, int32_t D, int32_t S,
+                            const void *q, int64_t q_row, int64_t q_head, const void *k,
+                            int64_t k_row, int64_t k_head, const void *v, int64_t v_row,
+                            int64_t v_head, int32_t axes, const int32_t *pos, const int32_t *axis,
+                            int32_t rot, int32_t interleaved, const float *cos_sin, int64_t n_pos,
+                            const int64_t *slots, void *cache, int64_t n_blocks, void *q_out,
+                            int64_t qo_row, int64_t qo_head, void *ws, size_t ws_bytes,
+                            void *stream);
+
+/* ------------------------------------------------------------------------
+ * Sparse decoding: a query attends over those blocks of the cache alone that a
+ * cheap score ranks highest.  Three calls: the ranges that each block's keys lie
+ * in (after maps_kv4_append or maps_kv4_append_rotated, for the blocks that new
+ * tokens went to), the blocks of each query, and attention over them.
+ *
+ * maps_kv4_block_ranges: of every KV head of the blocks j of request b with
+ * min(held, n) < (j + 1) S and j S < n, n = kv_len[b] (so of those that tokens
+ * were written to since there were `held`, or cut off), over their places below n:
+ * with lo_d, hi_d the least and the greatest key of channel d, as they are held
+ * (scale * code + zero, rounded to 32 bits),
+ *     scale = the least bfloat16 number with 127 scale >= |lo_d|, |hi_d| for
+ *             all d, or 0 where that is below 2^-126,
+ *     codes = floor(lo_d / scale) and ceil(hi_d / scale), or 0 where scale is 0,
+ * so that every key lies between its channel's codes times the scale, but for
+ * those below 2^-119 of a block of nothing else.  Where a key is held as NaN, or
+ * one passes the 32-bit range, scale is NaN and the codes are 0.
+ *
+ *   B                   requests (0 .. 2^30).
+ *   held, kv_len        [B] int32 tokens before and now, kv_len in [0, max_blocks *
+ *                       S] and at most 2^31 - 1,024, held >= 0; held may be NULL
+ *                       (none held before).
+ *   table, max_blocks, cache, n_blocks   as for maps_kv4_attention.
+ *   codes               [n_blocks][H][2][D] int8: the least, then the greatest;
+ *                       16-byte aligned.
+ *   scale               [n_blocks][H] float.
+ *   ws                  maps_kv4_workspace_size() bytes.
+ * Entries of other blocks are left as they are.  A block in two tables is written
+ * for both: the same values where both hold all that they see of it.
+ *
+ * maps_kv4_select_blocks: query row i at position p of its request (as for
+ * maps_kv4_attention, causal) sees the blocks 0 .. p / S.  For each KV head, with
+ * N_d and P_d the sums of its query heads' negative and of their positive parts
+ * (summed with 48 bits or more, rounded to 32),
+ *     inv = 1 / (max_d max(P_d, -N_d) * (1/127)), or 0 where that is below 2^-126,
+ *     w   = min(max(round(N_d inv), -127), 127), and the same of P_d,
+ *     score of a block = (sum_d w[N_d] lo code_d + w[P_d] hi code_d) * scale,
+ * the sum exact, its product rounded to 32 bits: a bound of the sum of the query
+ * heads' products with any key of the block, up to the 8 bits' rounding.  The list
+ * holds the first `first` blocks and the last `last`, always, then the others of
+ * the highest scores (NaN above all, ties to the earlier block), n_list in all or
+ * as many as there are, in the order of their keys.
+ *
+ *   T, Hq, H, q         as for maps_kv4_attention; T * H <= 2^31 - 1.
+ *   qo_off, kv_len, table, max_blocks   as for maps_kv4_attention.
+ *   codes, scale, n_blocks   as maps_kv4_block_ranges leaves them.
+ *   first, last         >= 0 and >= 1, first + last <= n_list.
+ *   n_list              1 .. 2^20, n_list * S <= 2^31 - 1,024.
+ *   blocks              [T][H][n_list] int32 out: the blocks of the cache, then -1.
+ *   tokens              [T][H] int32 out: the tokens of the list, of which only the
+ *                       last block may have less than S; 0: the row sees no key.
+ *   ws                  maps_kv4_select_blocks_workspace_size bytes; more than the
+ *                       256 of the control block only where max_blocks passes 32,768.
+ * Rows that no request has are left as they are.  A length, an offset or a used table
+ * entry out of its domain is MAPS_E_RANGE (via maps_check); such a request's rows get
+ * empty lists, such a block has score NaN, and nothing outside the arrays is read.
+ *
+ * maps_kv4_attention_blocks: attention as maps_kv4_attention has it, of query head x
+ * of row i over the first tokens[i][h] tokens of the blocks blocks[i][h][..], h = x /
+ * (Hq / H), all of which it sees.  Its results keep to the same limits.
+ *
+ *   T                   rows (<= 2^30, T * Hq <= 2^31 - 1,024).
+ *   blocks, tokens, n_list   as maps_kv4_select_blocks leaves them, or any others; a block
+ *                       may be in a list twice, and counts twice.  tokens in [0, n_list *
+ *                       S], 0 giving zeros; with a negative number a row's heads are
+ *                       neither read nor written, as for rows that no request has.
+ *   all others          as for maps_kv4_attention.
+ * ---------------------------------------------------------------------- */
+int maps_kv4_block_ranges(int32_t B, int32_t H, int32_t D, int32_t S, const int32_t *held,
+                          const int32_t *kv_len, const int32_t *table, int64_t max_blocks,
+                          const void *cache, int64_t n_blocks, int8_t *codes, float *scale,
+                          void *ws, size_t ws_bytes, void *stream);
+size_t maps_kv4_select_blocks_workspace_size(int64_t T, int32_t H, int64_t max_blocks);
+int maps_kv4_select_blocks(int32_t dtype, int32_t B, int64_t T, int32_t Hq, int32_t H, int32_t D,
+                           int32_t S, const void *q, int64_t q_row, int64_t q_head,
+                           const int64_t *qo_off, const int32_t *kv_len, const int32_t *table,
+                           int64_t max_blocks, const int8_t *codes, const float *scale,
+                           int64_t n_blocks, int32_t first, int32_t last, int32_t n_list,
+                           int32_t *blocks, int32_t *tokens, void *ws, size_t ws_bytes,
+                           void *stream);
+size_t maps_kv4_attention_blocks_workspace_size(int64_t T, int32_t Hq, int32_t H, int32_t D);
+int maps_kv4_attention_blocks(int32_t dtype, int64_t T, int32_t Hq, int32_t H, int32_t D, int32_t S,
+                              const void *q, int64_t q_row, int64_t q_head, const int32_t *blocks,
+                              const int32_t *tokens, int64_t n_list, const void *cache,
+                              int64_t n_blocks, float sm_scale, void *out, int64_t o_row,
+                              int64_t o_head, float *lse, void *ws, size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,169 @@
+// kv4_rows.cuh -- rows of keys and values on their way into the 4-bit cache and out of it: where a slot lies, a row's
+// codes, and moving 8 channels.
+#pragma once
+
+#include "kv4.cuh"
+
+namespace maps {
+namespace {
+
+struct KVArgs {
+  int64_t T, n_blocks;
+  int32_t H, S;
+  const void *k, *v;
+  void *ko, *vo;
+  int64_t k_row, k_head, v_row, v_head;  // elements
+  const int64_t *slots;
+  uint8_t *cache;
+  int32_t *status;
+};
+
+// Where a slot's token lies: its group's first byte and its place there; false for a slot that is none.
+__device__ __forceinline__ bool locate(const KVArgs &a, int64_t slot, int h, int group_bytes, uint8_t *&group, int &tau) {
+  if (slot < 0) return false;
+  const int64_t block = slot / a.S;
+  if (block >= a.n_blocks) {
+    flag_error(a.status, MAPS_E_RANGE);
+    return false;
+  }
+  const int within = static_cast<int>(slot - block * a.S);
+  tau = within % kGroup;
+  group = a.cache + ((block * a.H + h) * (a.S / kGroup) + within / kGroup) * group_bytes;
+  return true;
+}
+
+// 16-bit pairs of either type, with NaN in either argument kept.
+template <class T>
+struct Pair;
+template <>
+struct Pair<__nv_bfloat16> {
+  using V = __nv_bfloat162;
+};
+template <>
+struct Pair<__half> {
+  using V = __half2;
+};
+
+// Codes and {scale, zero} of a row's 8 values y, the row's extremes given.
+__device__ __forceinline__ void encode(const float (&y)[8], float low, float high, uint32_t &codes, uint32_t &param) {
+  const float spread = __fsub_rn(high, low);
+  const bool bad = !isfinite(low) || !isfinite(high) || !isfinite(spread);
+  const float scale = __bfloat162float(__float2bfloat16_rn(__fmul_rn(spread, 1.0f / 15.0f)));
+  const float zero = __bfloat162float(__float2bfloat16_rn(low));
+  const float inv = scale >= 1.17549435e-38f ? __fdiv_rn(1.0f, scale) : 0.0f;  // smallest normal number
+  // adding 1.5 * 2^23 rounds to an integer in the low bits; the sum of those times 16^i then has 8 known offsets to take off
+  uint32_t sum = 0;
+#pragma unroll
+  for (int i = 7; i >= 0; --i) {
+    const float c = fminf(fmaxf(__fmul_rn(__fsub_rn(y[i], zero), inv), 0.0f), 15.0f);
+    sum = sum * 16u + __float_as_uint(__fadd_rn(c, 12582912.0f));
+  }
+  codes = bad ? 0u : sum - 0x4b400000u * 0x11111111u;
+  param = bad ? 0x7fff7fffu : __float_as_uint(scale) >> 16 | (__float_as_uint(zero) & 0xffff0000u);
+}
+
+// A row's 8 channels of this lane: codes (channel i in bits 4i) and {scale, zero} of the row, whose
+// kLanes lanes have it between them.
+template <class T, int kLanes>
+__device__ __forceinline__ void quantise(const uint4 raw, unsigned mask, uint32_t &codes, uint32_t &param) {
+  using V = typename Pair<T>::V;
+  const V *x = reinterpret_cast<const V *>(&raw);
+  V lo = __hmin2_nan(__hmin2_nan(x[0], x[1]), __hmin2_nan(x[2], x[3]));
+  V hi = __hmax2_nan(__hmax2_nan(x[0], x[1]), __hmax2_nan(x[2], x[3]));
+  // {min, -max} in one word, so a step of the join is one shuffle and one minimum
+  V ends;
+  ends.x = __hmin_nan(lo.x, lo.y);
+  ends.y = __hneg(__hmax_nan(hi.x, hi.y));
+#pragma unroll
+  for (int o = kLanes / 2; o > 0; o >>= 1) {
+    const uint32_t u = __shfl_xor_sync(mask, *reinterpret_cast<const uint32_t *>(&ends), o);
+    ends = __hmin2_nan(ends, *reinterpret_cast<const V *>(&u));
+  }
+  float y[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) y[i] = Cvt<T>::to(i % 2 ? x[i / 2].y : x[i / 2].x);
+  encode(y, Cvt<T>::to(ends.x), -Cvt<T>::to(ends.y), codes, param);
+}
+
+// The same of a row in 32 bits.
+__device__ __forceinline__ float min_nan(float a, float b) {
+  float y;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
+}
+template <int kLanes>
+__device__ __forceinline__ void quantise32(const float (&y)[8], unsigned mask, uint32_t &codes, uint32_t &param) {
+  float low = y[0], high = y[0];
+#pragma unroll
+  for (int i = 1; i < 8; ++i) low = min_nan(low, y[i]), high = max_nan(high, y[i]);
+#pragma unroll
+  for (int o = kLanes / 2; o > 0; o >>= 1) {
+    low = min_nan(low, __shfl_xor_sync(mask, low, o));
+    high = max_nan(high, __shfl_xor_sync(mask, high, o));
+  }
+  encode(y, low, high, codes, param);
+}
+
+// The values of 8 codes.
+template <class T>
+__device__ __forceinline__ uint4 values(uint32_t codes, uint32_t param) {
+  const float2 p = kv4_param(param);
+  uint4 y;
+  T *z = reinterpret_cast<T *>(&y);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float c = __uint_as_float(0x4b000000u | (codes >> (4 * i) & 15u)) - 8388608.0f;
+    z[i] = Cvt<T>::from(fmaf(p.x, c, p.y));
+  }
+  return y;
+}
+
+template <class T, bool kWide>
+__device__ __forceinline__ uint4 load8(const T *src) {
+  if (kWide) return *reinterpret_cast<const uint4 *>(src);
+  uint4 raw;
+  T *x = reinterpret_cast<T *>(&raw);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = src[i];
+  return raw;
+}
+template <class T, bool kWide>
+__device__ __forceinline__ void store8(T *dst, uint4 y) {
+  if (kWide) {
+    *reinterpret_cast<uint4 *>(dst) = y;
+  } else {
+    const T *x = reinterpret_cast<const T *>(&y);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) dst[i] = x[i];
+  }
+}
+
+template <int D>
+__device__ __forceinline__ void put_row(uint8_t *group, int tau, bool is_v, int l, uint32_t codes, uint32_t param) {
+  if (is_v) {
+    *reinterpret_cast<uint16_t *>(group + 8 * D + kv4_v_unit<D>(tau, 2 * l)) = static_cast<uint16_t>(codes);
+    *reinterpret_cast<uint16_t *>(group + 8 * D + kv4_v_unit<D>(tau, 2 * l + 1)) = static_cast<uint16_t>(codes >> 16);
+  } else {
+    *reinterpret_cast<uint32_t *>(group + tau * (D / 2) + 4 * l) = codes;
+  }
+  if (l == 0) reinterpret_cast<uint32_t *>(group + 16 * D)[(is_v ? 16 : 0) + tau] = param;
+}
+template <int D>
+__device__ __forceinline__ void get_row(const uint8_t *group, int tau, bool is_v, int l, uint32_t &codes, uint32_t &param) {
+  if (is_v)
+    codes = *reinterpret_cast<const uint16_t *>(group + 8 * D + kv4_v_unit<D>(tau, 2 * l)) |
+            static_cast<uint32_t>(*reinterpret_cast<const uint16_t *>(group + 8 * D + kv4_v_unit<D>(tau, 2 * l + 1))) << 16;
+  else
+    codes = *reinterpret_cast<const uint32_t *>(group + tau * (D / 2) + 4 * l);
+  param = reinterpret_cast<const uint32_t *>(group + 16 * D)[(is_v ? 16 : 0) + tau];
+}
+
+inline bool wide(const void *p, int64_t row, int64_t head) { return aligned(p, 16) && row % 8 == 0 && head % 8 == 0; }
+
+}  // namespace
+}  // namespace maps

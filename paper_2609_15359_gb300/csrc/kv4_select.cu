@@ -1,0 +1,306 @@
+// kv4_select.cu -- the blocks of the cache that a cheap score ranks highest, for each query row and KV head.
+//
+// Score.  With lo <= k <= hi in every channel, q . k <= sum_d max(q_d lo_d, q_d hi_d); summed over the query heads x of a KV head
+// that is sum_d N_d lo_d + P_d hi_d, N and P the sums of the heads' negative and positive parts.  So a group of heads costs one
+// row of 2 D products, in 8 bits on both sides: whole numbers below 2^23, exact in any order, and one rounding with the scale.
+// The same list comes out whatever the split.
+//
+// A block takes a row and KV head: its scores become keys, whole numbers in the scores' order; the least key that is taken
+// is found by histograms of the keys that are still in question, ten bits at a time; then the list is written in order.
+#include "kv4.cuh"
+
+namespace maps {
+namespace {
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kBinBits = 10, kBins = 1 << kBinBits;
+constexpr int kSmemKeys = 32768;  // longer rows of keys lie in the workspace
+
+struct SelectArgs {
+  int32_t B, Hq, H, S;
+  int64_t T, max_blocks, n_blocks;
+  const void *q;
+  int64_t q_row, q_head;
+  const int64_t *off;
+  const int32_t *len, *table;
+  const int8_t *codes;
+  const float *scale;
+  int32_t first, last, n_list;
+  int32_t *blocks, *tokens;
+  uint32_t *keys;  // [T * H][max_blocks], or NULL: in shared memory
+  int32_t *status;
+};
+
+// Whole numbers in the order of the scores, NaN above all.
+__device__ __forceinline__ uint32_t key_of(float x) {
+  const uint32_t u = __float_as_uint(x + 0.0f);  // one zero
+  return x != x ? 0xfffffffeu : u >> 31 ? ~u : u | 0x80000000u;
+}
+
+// Adds x to the running sum s + e, of which e holds what s's roundings lost: 48 bits.
+__device__ __forceinline__ void add_twice(float &s, float &e, float x) {
+  const float t = __fadd_rn(s, x), y = __fsub_rn(t, s);
+  e = __fadd_rn(e, __fadd_rn(__fsub_rn(s, __fsub_rn(t, y)), __fsub_rn(x, y)));
+  s = t;
+}
+
+// The greatest b with off[b] <= i of b in [0, B], -1 where there is none.  All threads call it.
+__device__ __forceinline__ int request_of(const int64_t *off, int B, int64_t i) {
+  int64_t lo = 0, n = static_cast<int64_t>(B) + 1;
+  for (;;) {
+    const int64_t step = (n + kThreads - 1) / kThreads, at = threadIdx.x * step;
+    const int count = __syncthreads_count(at < n && off[lo + at] <= i);
+    if (count == 0) return -1;
+    lo += (count - 1) * step;
+    if (step == 1) return static_cast<int>(lo);
+    n = min(step, n - (count - 1) * step);
+  }
+}
+
+template <class T, int D>
+__global__ void __launch_bounds__(kThreads) kv4_select_kernel(const SelectArgs a) {
+  constexpr int kLanes = D / 8, kSub = 32 / kLanes;  // lanes of a block's 2 D codes, and blocks of a warp's load
+  constexpr int kBatch = kLanes < 8 ? kLanes : 8;    // loads under way at once
+  extern __shared__ uint32_t s_keys[];
+  __shared__ __align__(16) int8_t s_w[2 * D];
+  __shared__ uint32_t s_hist[kBins];
+  __shared__ uint32_t s_warp[kWarps][2];
+  __shared__ uint32_t s_found[3];
+  __shared__ float s_step[kWarps];
+  pdl_prologue();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int64_t item = blockIdx.x, i = item / a.H;
+  const int h = static_cast<int>(item - i * a.H);
+  const int b = request_of(a.off, a.B, i);
+  if (b < 0 || b == a.B) return;  // no request's
+  const int64_t q0 = a.off[b], q1 = a.off[b + 1];
+  int32_t n = a.len[b];
+  int32_t *out = a.blocks + item * a.n_list;
+  if (q0 < 0 || q1 > a.T || i >= q1 || n < 0 || n > 0x7fffffff - 1023 || n > a.max_blocks * a.S) {
+    if (tid == 0) flag_error(a.status, MAPS_E_RANGE);
+    n = 0;
+  }
+  const int64_t seen = n - (q1 - i) + 1;  // keys
+  if (n == 0 || seen <= 0) {
+    for (int x = tid; x < a.n_list; x += kThreads) out[x] = -1;
+    if (tid == 0) a.tokens[item] = 0;
+    return;
+  }
+  const int32_t nb = static_cast<int32_t>((seen + a.S - 1) / a.S), count = min(nb, a.n_list);
+  const int32_t *table = a.table + b * a.max_blocks;
+  if (tid == 0) a.tokens[item] = static_cast<int32_t>((count - 1) * static_cast<int64_t>(a.S) + seen - (nb - 1) * static_cast<int64_t>(a.S));
+  for (int x = count + tid; x < a.n_list; x += kThreads) out[x] = -1;
+  if (nb <= a.n_list) {  // all of them
+    for (int x = tid; x < nb; x += kThreads) out[x] = table[x];
+    return;
+  }
+  for (int x = tid; x < a.first; x += kThreads) out[x] = table[x];
+  for (int x = tid; x < a.last; x += kThreads) out[count - a.last + x] = table[nb - a.last + x];
+  uint32_t need = a.n_list - a.first - a.last;  // of the others
+  if (need == 0) return;
+  const int32_t N = nb - a.first - a.last;
+  table += a.first;
+  out += a.first;
+
+  // ---- the queries' weights
+  const int group = a.Hq / a.H;
+  float P = 0.0f, Pe = 0.0f, M = 0.0f, Me = 0.0f;
+  if (tid < D) {
+    const T *src = static_cast<const T *>(a.q) + i * a.q_row + static_cast<int64_t>(h) * group * a.q_head + tid;
+    for (int x = 0; x < group; ++x) {
+      const float y = Cvt<T>::to(src[x * a.q_head]);
+      add_twice(P, Pe, y > 0.0f || y != y ? y : 0.0f);
+      add_twice(M, Me, y < 0.0f || y != y ? y : 0.0f);
+    }
+    P = __fadd_rn(P, Pe);
+    M = __fadd_rn(M, Me);
+  }
+  // NaN's bits are above infinity's
+  const uint32_t most = __reduce_max_sync(0xffffffffu, max(__float_as_uint(P) & 0x7fffffffu, __float_as_uint(M) & 0x7fffffffu));
+  if (lane == 0) s_step[warp] = __uint_as_float(most);
+  __syncthreads();
+  uint32_t top = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) top = max(top, __float_as_uint(s_step[w]));
+  const float step = __fmul_rn(__uint_as_float(top), 1.0f / 127.0f);
+  const bool no_number = !(step < INFINITY);
+  const float inv = step >= 1.17549435e-38f ? __fdiv_rn(1.0f, step) : 0.0f;
+  if (tid < D && !no_number) {
+    s_w[tid] = static_cast<int8_t>(fminf(fmaxf(rintf(__fmul_rn(M, inv)), -127.0f), 127.0f));
+    s_w[D + tid] = static_cast<int8_t>(fminf(fmaxf(rintf(__fmul_rn(P, inv)), -127.0f), 127.0f));
+  }
+  __syncthreads();
+
+  // ---- keys
+  uint32_t *keys = a.keys ? a.keys + item * a.max_blocks : s_keys;
+  uint32_t least = 0xffffffffu, greatest = 0;
+  const int l = lane % kLanes, sub = lane / kLanes;
+  const int4 w = *reinterpret_cast<const int4 *>(s_w + 16 * l);
+  for (int j0 = warp * 32; j0 < N; j0 += kThreads) {
+    const int j = j0 + l * kSub + sub;  // the block whose score this lane ends up with
+    int32_t block = -1;
+    float sc = 0.0f;
+    if (j < N) {
+      block = table[j];
+      if (block < 0 || block >= a.n_blocks) {
+        flag_error(a.status, MAPS_E_RANGE);
+        block = -1;
+      } else {
+        sc = a.scale[static_cast<int64_t>(block) * a.H + h];
+      }
+    }
+    int acc[kLanes];
+#pragma unroll
+    for (int k0 = 0; k0 < kLanes; k0 += kBatch) {
+      int4 c[kBatch];
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        const int32_t blk = __shfl_sync(0xffffffffu, block, sub * kLanes + k0 + k);
+        c[k] = make_int4(0, 0, 0, 0);
+        if (blk >= 0) c[k] = *reinterpret_cast<const int4 *>(a.codes + (static_cast<int64_t>(blk) * a.H + h) * (2 * D) + 16 * l);
+      }
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) acc[k0 + k] = __dp4a(c[k].x, w.x, __dp4a(c[k].y, w.y, __dp4a(c[k].z, w.z, __dp4a(c[k].w, w.w, 0))));
+    }
+#pragma unroll
+    for (int o = kLanes / 2; o > 0; o >>= 1) {
+      const bool up = l & o;
+#pragma unroll
+      for (int k = 0; k < o; ++k) {
+        const int send = up ? acc[k] : acc[k + o], keep = up ? acc[k + o] : acc[k];
+        acc[k] = keep + __shfl_xor_sync(0xffffffffu, send, o);
+      }
+    }
+    if (j < N) {
+      const uint32_t key = no_number || block < 0 ? 0xfffffffeu : key_of(__fmul_rn(static_cast<float>(acc[0]), sc));
+      keys[j] = key;
+      least = min(least, key);
+      greatest = max(greatest, key);
+    }
+  }
+  least = __reduce_min_sync(0xffffffffu, least);
+  greatest = __reduce_max_sync(0xffffffffu, greatest);
+  if (lane == 0) s_warp[warp][0] = least, s_warp[warp][1] = greatest;
+  __syncthreads();
+  uint32_t lo = 0xffffffffu, hi = 0;
+#pragma unroll
+  for (int x = 0; x < kWarps; ++x) lo = min(lo, s_warp[x][0]), hi = max(hi, s_warp[x][1]);
+
+  // ---- the least key that is taken: the keys in question are those of [lo, hi], of which `need` are wanted, the greatest first
+  while (lo < hi) {
+    const int shift = max(0, 32 - __clz(hi - lo) - kBinBits);
+    for (int x = tid; x < kBins; x += kThreads) s_hist[x] = 0;
+    __syncthreads();
+    for (int j = tid; j < N; j += kThreads) {
+      const uint32_t key = keys[j];
+      if (key >= lo && key <= hi) atomicAdd(&s_hist[(key - lo) >> shift], 1u);
+    }
+    __syncthreads();
+    constexpr int kOwn = kBins / kThreads;  // bins of a thread, from the top down
+    uint32_t own[kOwn], mine = 0;
+#pragma unroll
+    for (int x = 0; x < kOwn; ++x) own[x] = s_hist[kBins - 1 - (tid * kOwn + x)], mine += own[x];
+    uint32_t sum = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t y = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += y;
+    }
+    if (lane == 31) s_warp[warp][0] = sum;
+    __syncthreads();
+    uint32_t above = sum - mine;
+    for (int x = 0; x < warp; ++x) above += s_warp[x][0];
+#pragma unroll
+    for (int x = 0; x < kOwn; ++x) {
+      if (above < need && need <= above + own[x]) s_found[0] = kBins - 1 - (tid * kOwn + x), s_found[1] = above, s_found[2] = own[x];
+      above += own[x];
+    }
+    __syncthreads();
+    lo += s_found[0] << shift;
+    need -= s_found[1];
+    const bool all = s_found[2] == need;
+    hi = lo + min(hi - lo, (1u << shift) - 1u);
+    __syncthreads();
+    if (all) {
+      need = 0;
+      break;
+    }
+  }
+  // taken: keys above hi, with need == 0 those from lo on, else the first `need` of those that are lo
+  const uint32_t from = need == 0 ? lo : lo + 1;
+
+  // ---- the list, in the order of the blocks
+  const int span = (N + kThreads - 1) / kThreads * 32;  // of a warp
+  const int j0 = min(warp * span, N), j1 = min(j0 + span, N);
+  uint32_t over = 0, same = 0;
+  for (int j = j0 + lane; j - lane < j1; j += 32) {
+    const uint32_t key = j < j1 ? keys[j] : 0;
+    over += __popc(__ballot_sync(0xffffffffu, j < j1 && key >= from));
+    same += __popc(__ballot_sync(0xffffffffu, j < j1 && key == lo));
+  }
+  if (lane == 0) s_warp[warp][0] = over, s_warp[warp][1] = same;
+  __syncthreads();
+  over = same = 0;
+  for (int x = 0; x < warp; ++x) over += s_warp[x][0], same += s_warp[x][1];
+  const unsigned below = (1u << lane) - 1u;
+  for (int j = j0 + lane; j - lane < j1; j += 32) {
+    const uint32_t key = j < j1 ? keys[j] : 0;
+    const bool is_over = j < j1 && key >= from, is_same = j < j1 && key == lo && need > 0;
+    const unsigned overs = __ballot_sync(0xffffffffu, is_over), sames = __ballot_sync(0xffffffffu, is_same);
+    const uint32_t rank = same + __popc(sames & below);
+    if (is_over || (is_same && rank < need)) out[over + __popc(overs & below) + min(rank, need)] = table[j];
+    over += __popc(overs);
+    same += __popc(sames);
+  }
+}
+
+size_t key_bytes(int64_t T, int32_t H, int64_t max_blocks) {
+  return max_blocks > kSmemKeys ? static_cast<size_t>(T) * static_cast<size_t>(H) * static_cast<size_t>(max_blocks) * 4 : 0;
+}
+
+template <class T, int D>
+int launch(const SelectArgs &a, cudaStream_t s) {
+  const size_t smem = a.keys ? 0 : static_cast<size_t>(a.max_blocks) * 4;
+  constexpr auto kernel = kv4_select_kernel<T, D>;
+  MAPS_TRY(cuda_ok(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemKeys * 4)));
+  launch_pdl(kernel, static_cast<unsigned>(a.T * a.H), kThreads, smem, s, a);
+  return launch_ok();
+}
+template <class T>
+int launch_dim(int D, const SelectArgs &a, cudaStream_t s) {
+  return D == 64 ? launch<T, 64>(a, s) : D == 128 ? launch<T, 128>(a, s) : launch<T, 256>(a, s);
+}
+
+}  // namespace
+}  // namespace maps
+
+extern "C" {
+
+size_t maps_kv4_select_blocks_workspace_size(int64_t T, int32_t H, int64_t max_blocks) {
+  using namespace maps;
+  return kCtrlBytes + (T > 0 && H > 0 && max_blocks > 0 ? (key_bytes(T, H, max_blocks) + kAlign - 1) / kAlign * kAlign : 0);
+}
+
+int maps_kv4_select_blocks(int32_t dtype, int32_t B, int64_t T, int32_t Hq, int32_t H, int32_t D, int32_t S, const void *q, int64_t q_row,
+                           int64_t q_head, const int64_t *qo_off, const int32_t *kv_len, const int32_t *table, int64_t max_blocks,
+                           const int8_t *codes, const float *scale, int64_t n_blocks, int32_t first, int32_t last, int32_t n_list,
+                           int32_t *blocks, int32_t *tokens, void *ws, size_t ws_bytes, void *stream) {
+  using namespace maps;
+  if ((dtype != MAPS_BF16 && dtype != MAPS_F16) || !kv4_dim_ok(D) || !kv4_block_ok(S) || B < 0 || T < 0 || T > (int64_t(1) << 30) || H < 1 ||
+      Hq < H || Hq % H != 0 || Hq > 65535 || T > 0x7fffffff / H || max_blocks < 0 || max_blocks > 0x7fffffff || n_blocks < 0 || first < 0 ||
+      last < 1 || n_list < 1 || n_list > (1 << 20) || first > n_list - last || static_cast<int64_t>(n_list) * S > 0x7fffffff - 1023)
+    return MAPS_E_INVALID;
+  MAPS_TRY(check_ws(ws, ws_bytes, maps_kv4_select_blocks_workspace_size(T, H, max_blocks)));
+  if (T == 0 || B == 0) return MAPS_OK;
+  if (q == nullptr || qo_off == nullptr || kv_len == nullptr || (max_blocks > 0 && table == nullptr) || blocks == nullptr || tokens == nullptr ||
+      (n_blocks > 0 && (codes == nullptr || scale == nullptr)) || !aligned(q, 2) || !aligned(codes, 16) || !aligned(scale, 4) ||
+      !aligned(qo_off, 8) || !aligned(kv_len, 4) || !aligned(table, 4) || !aligned(blocks, 4) || !aligned(tokens, 4))
+    return MAPS_E_INVALID;
+  SelectArgs a = {B, Hq, H, S, T, max_blocks, n_blocks, q, q_row, q_head, qo_off, kv_len, table, codes, scale, first, last, n_list,
+                  blocks, tokens, nullptr, status_word(ws)};
+  if (key_bytes(T, H, max_blocks)) a.keys = reinterpret_cast<uint32_t *>(static_cast<char *>(ws) + kCtrlBytes);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  return dtype == MAPS_BF16 ? launch_dim<__nv_bfloat16>(D, a, s) : launch_dim<__half>(D, a, s);
+}
+
+}  // extern "C"

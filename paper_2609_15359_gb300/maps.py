@@ -107,6 +107,17 @@ def _load():
                              sz, vp], ctypes.c_int),
         "maps_kv4_read": ([i32, i64, i32, i32, i32, vp, vp, i64, vp, i64, i64, vp, i64, i64, vp,
                            sz, vp], ctypes.c_int),
+        "maps_kv4_append_rotated": ([i32, i64, i32, i32, i32, i32, vp, i64, i64, vp, i64, i64, vp, i64, i64,
+                                     i32, vp, vp, i32, i32, vp, i64, vp, vp, i64, vp, i64, i64, vp, sz, vp],
+                                    ctypes.c_int),
+        "maps_kv4_block_ranges": ([i32, i32, i32, i32, vp, vp, vp, i64, vp, i64, vp, vp, vp, sz, vp],
+                                  ctypes.c_int),
+        "maps_kv4_select_blocks_workspace_size": ([i64, i32, i64], sz),
+        "maps_kv4_select_blocks": ([i32, i32, i64, i32, i32, i32, i32, vp, i64, i64, vp, vp, vp, i64, vp, vp,
+                                    i64, i32, i32, i32, vp, vp, vp, sz, vp], ctypes.c_int),
+        "maps_kv4_attention_blocks_workspace_size": ([i64, i32, i32, i32], sz),
+        "maps_kv4_attention_blocks": ([i32, i64, i32, i32, i32, i32, vp, i64, i64, vp, vp, i64, vp, i64, f32,
+                                       vp, i64, i64, vp, vp, sz, vp], ctypes.c_int),
         "maps_kv4_attention_workspace_size": ([i32, i64, i32, i32, i32], sz),
         "maps_kv4_attention": ([i32, i32, i64, i32, i32, i32, i32, vp, i64, i64, vp, vp, vp, i64,
                                 vp, i64, f32, i32, i32, vp, i64, i64, vp, vp, sz, vp],
@@ -131,7 +142,9 @@ EXPORTS = ("maps_version", "maps_last_cuda_error", "maps_check", "maps_set_dispa
            "maps_rr_pressure_workspace_size", "maps_rr_pressure",
            "maps_block_tables_workspace_size", "maps_block_tables", "maps_kv4_record_bytes",
            "maps_kv4_workspace_size", "maps_kv4_append", "maps_kv4_read",
-           "maps_kv4_attention_workspace_size", "maps_kv4_attention")
+           "maps_kv4_attention_workspace_size", "maps_kv4_attention", "maps_kv4_append_rotated",
+           "maps_kv4_block_ranges", "maps_kv4_select_blocks_workspace_size", "maps_kv4_select_blocks",
+           "maps_kv4_attention_blocks_workspace_size", "maps_kv4_attention_blocks")
 
 
 # The handle of the current stream without a stream object, which costs 3.2 us, a third of a call.  PyTorch promises
@@ -462,3 +475,88 @@ def maps_kv4_attention(q, qo_off, kv_len, table, cache, S: int, sm_scale: float,
                                   int(bool(causal)), int(window), *_rows(out, q.dtype),
                                   _ptr(lse_out, torch.float32), ws.ptr, ws.nbytes,
                                   on)
+
+
+def maps_kv4_append_rotated(q, k, v, pos, cos_sin, slots, cache, S: int, q_out, axis=None,
+                            interleaved: bool = False, ws: Workspace | None = None, stream=None) -> int:
+    """Turns q [T, Hq, D] into q_out and k [T, H, D] on its way into the cache by the
+    tokens' positions: pos [axes, T] (or [T]) int32, cos_sin [n_pos, rot] float32 (cosines,
+    then sines), axis [rot / 2] int32 or None; q and q_out None: keys and values alone."""
+    T, H, D = k.shape
+    if v.shape != k.shape or slots.numel() != T:
+        raise ValueError("k, v and slots differ in size")
+    if (q is None) != (q_out is None) or q is not None and (
+            q_out.shape != q.shape or q.dim() != 3 or q.shape[0] != T or q.shape[2] != D):
+        raise ValueError("q, q_out and k differ in size")
+    n_pos, rot = cos_sin.shape
+    axes = pos.shape[0] if pos.dim() == 2 else 1
+    if pos.numel() != axes * T or axis is not None and axis.numel() != rot // 2:
+        raise ValueError("pos is [axes, T], axis [rot / 2]")
+    ws, on = _scratch(ws, _need(None, "maps_kv4_workspace_size"), stream)
+    rows, rows_out, Hq = ((None, 0, 0), (None, 0, 0), 0) if q is None else (
+        _rows(q, k.dtype), _rows(q_out, k.dtype), q.shape[1])
+    return lib.maps_kv4_append_rotated(_dtype(k), T, Hq, H, D, S, *rows, *_rows(k), *_rows(v, k.dtype),
+                                       axes, _ptr(pos, torch.int32), _ptr(axis, torch.int32), rot,
+                                       int(bool(interleaved)), _ptr(cos_sin, torch.float32), n_pos,
+                                       _ptr(slots, torch.int64), _kv4(cache, S, D, H), cache.shape[0],
+                                       *rows_out, ws.ptr, ws.nbytes, on)
+
+
+def kv4_range_shape(n_blocks: int, H: int, D: int) -> tuple[int, int, int, int]:
+    """Shape of the ranges' codes (int8): [blocks][KV heads][least, greatest][channels]; their scales are [blocks][KV heads] float32."""
+    return n_blocks, H, 2, D
+
+
+def _ranges(codes, scale, n_blocks: int, H: int):
+    D = codes.shape[-1]
+    if tuple(codes.shape) != kv4_range_shape(n_blocks, H, D) or tuple(scale.shape) != (n_blocks, H):
+        raise ValueError("codes is [blocks, H, 2, D], scale [blocks, H]")
+    return _ptr(codes, torch.int8), _ptr(scale, torch.float32)
+
+
+def maps_kv4_block_ranges(held, kv_len, table, cache, S: int, codes, scale,
+                          ws: Workspace | None = None, stream=None) -> int:
+    """Ranges of the keys of the blocks that tokens went to since there were held [B]
+    int32 (None: all blocks): codes [blocks, H, 2, D] int8 and scale [blocks, H] float32."""
+    B, n_blocks, H, D = kv_len.numel(), cache.shape[0], cache.shape[1], codes.shape[-1]
+    if held is not None and held.numel() != B or table.dim() != 2 or table.shape[0] != B:
+        raise ValueError("held, kv_len and table differ in size")
+    ws, on = _scratch(ws, _need(None, "maps_kv4_workspace_size"), stream)
+    return lib.maps_kv4_block_ranges(B, H, D, S, _ptr(held, torch.int32), _ptr(kv_len, torch.int32),
+                                     _ptr(table, torch.int32), table.shape[1], _kv4(cache, S, D, H),
+                                     n_blocks, *_ranges(codes, scale, n_blocks, H), ws.ptr, ws.nbytes, on)
+
+
+def maps_kv4_select_blocks(q, qo_off, kv_len, table, codes, scale, S: int, first: int, last: int,
+                           blocks_out, tokens_out, ws: Workspace | None = None, stream=None) -> int:
+    """For each row of q [T, Hq, D] and KV head the cache blocks of the highest scores, the
+    first and last ones always: blocks_out [T, H, n_list] and tokens_out [T, H] int32."""
+    T, Hq, D = q.shape
+    B, (n_blocks, H) = kv_len.numel(), codes.shape[:2]
+    if codes.shape[-1] != D or qo_off.numel() != B + 1 or table.dim() != 2 or table.shape[0] != B:
+        raise ValueError("q, codes, qo_off, kv_len and table differ in size")
+    if blocks_out.dim() != 3 or tuple(blocks_out.shape[:2]) != (T, H) or tuple(tokens_out.shape) != (T, H):
+        raise ValueError("blocks_out is [T, H, n_list], tokens_out [T, H]")
+    ws, on = _scratch(ws, _need(None, "maps_kv4_select_blocks_workspace_size", T, H, table.shape[1]), stream)
+    return lib.maps_kv4_select_blocks(_dtype(q), B, T, Hq, H, D, S, *_rows(q), _ptr(qo_off, torch.int64),
+                                      _ptr(kv_len, torch.int32), _ptr(table, torch.int32), table.shape[1],
+                                      *_ranges(codes, scale, n_blocks, H), n_blocks, int(first), int(last),
+                                      blocks_out.shape[2], _ptr(blocks_out, torch.int32),
+                                      _ptr(tokens_out, torch.int32), ws.ptr, ws.nbytes, on)
+
+
+def maps_kv4_attention_blocks(q, blocks, tokens, cache, S: int, sm_scale: float, out, lse_out=None,
+                              ws: Workspace | None = None, stream=None) -> int:
+    """Attention of q [T, Hq, D] over the first tokens [T, H] tokens of the cache blocks
+    blocks [T, H, n_list] (both int32); out like q, lse_out [T][Hq] float32 or None."""
+    T, Hq, D = q.shape
+    H = cache.shape[1]
+    if out.shape != q.shape or blocks.dim() != 3 or tuple(blocks.shape[:2]) != (T, H) or tuple(tokens.shape) != (T, H):
+        raise ValueError("q and out are [T, Hq, D], blocks [T, H, n_list], tokens [T, H]")
+    if lse_out is not None and tuple(lse_out.shape) != (T, Hq):
+        raise ValueError("lse_out is [T, Hq]")
+    ws, on = _scratch(ws, _need(torch.cuda.current_device(), "maps_kv4_attention_blocks_workspace_size", T, Hq, H, D), stream)
+    return lib.maps_kv4_attention_blocks(_dtype(q), T, Hq, H, D, S, *_rows(q), _ptr(blocks, torch.int32),
+                                         _ptr(tokens, torch.int32), blocks.shape[2], _kv4(cache, S, D, H),
+                                         cache.shape[0], float(sm_scale), *_rows(out, q.dtype),
+                                         _ptr(lse_out, torch.float32), ws.ptr, ws.nbytes, on)
