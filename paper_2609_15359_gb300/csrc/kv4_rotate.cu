@@ -10,9 +10,13 @@
 namespace maps {
 namespace {
 
+// Warps of a multiprocessor up to which a token's heads are shared out among several.
+constexpr int kUnitWarps = 32;
+
 struct RotArgs {
   KVArgs kv;
   int32_t Hq, axes, rot;
+  bool wide_axis;
   const void *q;
   void *qo;
   int64_t q_row, q_head, qo_row, qo_head;
@@ -33,32 +37,49 @@ struct Turn {
     on = 8 * l < a.rot;
     const bool second = !kInter && 8 * l >= F;
     partner = kInter || !on ? 0 : second ? -(F / 8) : F / 8;
+#pragma unroll
+    for (int i = 0; i < kN; ++i) c[i] = 1.0f, s[i] = 0.0f;
     if (!on) return;
     const int f0 = kInter ? 4 * l : second ? 8 * l - F : 8 * l;
-    int64_t at[kN];
-    bool same = true;
-#pragma unroll
-    for (int i = 0; i < kN; ++i) {
-      const int32_t x = a.axis ? a.axis[f0 + i] : 0;
-      const bool good = x >= 0 && x < a.axes;
-      const int32_t p = good ? a.pos[x * a.kv.T + tok] : -1;
-      at[i] = p >= 0 && p < a.n_pos ? static_cast<int64_t>(p) * a.rot : -1;
-      if (at[i] < 0) flag_error(a.kv.status, MAPS_E_RANGE);
-      same &= at[i] == at[0];
-    }
-    if (same && at[0] >= 0) {
-      const float4 *src = reinterpret_cast<const float4 *>(a.cos_sin + at[0] + f0);
-      const float4 *sin = reinterpret_cast<const float4 *>(a.cos_sin + at[0] + F + f0);
+    int32_t ax[kN] = {};
+    if (a.axis) {
 #pragma unroll
       for (int i = 0; i < kN; i += 4) {
-        *reinterpret_cast<float4 *>(c + i) = src[i / 4];
-        *reinterpret_cast<float4 *>(s + i) = sin[i / 4];
+        if (a.wide_axis) {
+          *reinterpret_cast<int4 *>(ax + i) = *reinterpret_cast<const int4 *>(a.axis + f0 + i);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) ax[i + k] = a.axis[f0 + i + k];
+        }
+      }
+    }
+    // a position once for each run of pairs on one axis
+    auto row_of = [&](int32_t x) -> int64_t {
+      const int32_t p = x >= 0 && x < a.axes ? a.pos[x * a.kv.T + tok] : -1;
+      if (p < 0 || p >= a.n_pos) {
+        flag_error(a.kv.status, MAPS_E_RANGE);
+        return -1;
+      }
+      return static_cast<int64_t>(p) * a.rot;
+    };
+    int64_t at = row_of(ax[0]);
+    bool same = true;
+#pragma unroll
+    for (int i = 1; i < kN; ++i) same &= ax[i] == ax[0];
+    if (same) {
+      if (at >= 0) {
+        const float *src = a.cos_sin + at + f0;
+#pragma unroll
+        for (int i = 0; i < kN; i += 4) {
+          *reinterpret_cast<float4 *>(c + i) = *reinterpret_cast<const float4 *>(src + i);
+          *reinterpret_cast<float4 *>(s + i) = *reinterpret_cast<const float4 *>(src + F + i);
+        }
       }
     } else {
 #pragma unroll
       for (int i = 0; i < kN; ++i) {
-        c[i] = at[i] >= 0 ? a.cos_sin[at[i] + f0 + i] : 1.0f;
-        s[i] = at[i] >= 0 ? a.cos_sin[at[i] + F + f0 + i] : 0.0f;
+        if (i > 0 && ax[i] != ax[i - 1]) at = row_of(ax[i]);
+        if (at >= 0) c[i] = a.cos_sin[at + f0 + i], s[i] = a.cos_sin[at + F + f0 + i];
       }
     }
     if (!kInter && !second) {
@@ -66,9 +87,9 @@ struct Turn {
       for (int i = 0; i < kN; ++i) s[i] = -s[i];
     }
   }
-  // A row's 8 channels, turned.  `mask`: the lanes that call this, whole rows.
+  // A row's 8 channels, turned.  All lanes of the warp call it.
   template <class T>
-  __device__ __forceinline__ void apply(const uint4 raw, unsigned mask, float (&y)[8]) const {
+  __device__ __forceinline__ void apply(const uint4 raw, float (&y)[8]) const {
     const T *x = reinterpret_cast<const T *>(&raw);
     if (kInter) {
 #pragma unroll
@@ -80,10 +101,10 @@ struct Turn {
     } else {
       uint4 other;
       const int from = (threadIdx.x & 31) + partner;
-      other.x = __shfl_sync(mask, raw.x, from);
-      other.y = __shfl_sync(mask, raw.y, from);
-      other.z = __shfl_sync(mask, raw.z, from);
-      other.w = __shfl_sync(mask, raw.w, from);
+      other.x = __shfl_sync(0xffffffffu, raw.x, from);
+      other.y = __shfl_sync(0xffffffffu, raw.y, from);
+      other.z = __shfl_sync(0xffffffffu, raw.z, from);
+      other.w = __shfl_sync(0xffffffffu, raw.w, from);
       const T *z = reinterpret_cast<const T *>(&other);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -103,53 +124,86 @@ __device__ __forceinline__ uint4 rounded(const float (&y)[8]) {
   return out;
 }
 
-// ---- few rows: D/8 lanes a row and nothing else, for the shortest chain of loads
-template <class T, int D, bool kWide, bool kInter>
-__global__ void __launch_bounds__(256) kv4_rotate_few_kernel(const RotArgs a) {
+// A unit is a token and `per` of its query and key heads (queries first); a warp takes one and keeps the angles in registers for
+// all its rows, of which 32 / (D/8) pass side by side and kAhead more are under way.  Values, which do not turn, are
+// other blocks' of the same launch: row by row, or (kGroups) 16 tokens of a head to a warp, as in maps_kv4_append.
+constexpr int kAhead = 4;
+
+template <class T, int D, bool kWide, bool kInter, bool kGroups>
+__global__ void __launch_bounds__(256) kv4_rotate_kernel(const RotArgs a, const int64_t value_blocks, const int32_t units, const int32_t per) {
   pdl_prologue();
-  constexpr int kLanes = D / 8;
-  const int64_t row = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) / kLanes;
-  const int l = threadIdx.x % kLanes, per = a.Hq + 2 * a.kv.H;
-  const bool there = row < a.kv.T * per;
-  const int64_t tok = row / per;
-  const int rest = static_cast<int>(row - tok * per);
-  const bool is_q = rest < a.Hq, is_v = rest >= a.Hq + a.kv.H;
-  const unsigned turned = __ballot_sync(0xffffffffu, there && !is_v);
-  const unsigned values = __ballot_sync(0xffffffffu, there && is_v);
-  if (!there) return;  // whole rows leave together: kLanes divides 32
-  if (is_v) {
-    const int h = rest - a.Hq - a.kv.H;
-    const uint4 raw = load8<T, kWide>(static_cast<const T *>(a.kv.v) + tok * a.kv.v_row + h * a.kv.v_head + 8 * l);
-    uint32_t codes, param;
-    quantise<T, kLanes>(raw, values, codes, param);
-    uint8_t *group;
-    int tau;
-    if (locate(a.kv, a.kv.slots[tok], h, kv4_group_bytes(D), group, tau)) put_row<D>(group, tau, true, l, codes, param);
+  constexpr int kLanes = D / 8, kRows = 32 / kLanes;
+  __shared__ __align__(16) uint8_t s_stage[kGroups ? 8 : 1][kGroups ? kStageBytes<D> : 16];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l = lane % kLanes, sub = lane / kLanes;
+  uint8_t *group;
+  int tau;
+  if (blockIdx.x < value_blocks) {
+    const int64_t w = static_cast<int64_t>(blockIdx.x) * 8 + warp;
+    if (kGroups) {
+      move_groups<T, D, kWide, true, 1>(a.kv, w, s_stage[warp]);
+    } else {
+      const int64_t row = w * kRows + sub, tok = row / a.kv.H;
+      const int h = static_cast<int>(row - tok * a.kv.H);
+      const bool there = tok < a.kv.T;
+      uint4 raw = make_uint4(0, 0, 0, 0);
+      if (there) raw = load8<T, kWide>(static_cast<const T *>(a.kv.v) + tok * a.kv.v_row + h * a.kv.v_head + 8 * l);
+      const int64_t slot = there ? a.kv.slots[tok] : -1;
+      uint32_t codes, param;
+      quantise<T, kLanes>(raw, 0xffffffffu, codes, param);
+      if (locate(a.kv, slot, h, kv4_group_bytes(D), group, tau)) put_row<D>(group, tau, true, l, codes, param);
+    }
     return;
   }
-  const int h = is_q ? rest : rest - a.Hq;
-  const T *src = is_q ? static_cast<const T *>(a.q) + tok * a.q_row + h * a.q_head : static_cast<const T *>(a.kv.k) + tok * a.kv.k_row + h * a.kv.k_head;
-  const uint4 raw = load8<T, kWide>(src + 8 * l);
-  const int64_t slot = is_q ? -1 : a.kv.slots[tok];
+  const int64_t u = (static_cast<int64_t>(blockIdx.x) - value_blocks) * 8 + warp, tok = u / units;
+  if (tok >= a.kv.T) return;
+  const int first = static_cast<int>(u - tok * units) * per, end = min(first + per, a.Hq + a.kv.H);
+  const T *q = static_cast<const T *>(a.q) + tok * a.q_row + 8 * l, *k = static_cast<const T *>(a.kv.k) + tok * a.kv.k_row + 8 * l;
+  auto fetch = [&](uint4 (&raw)[kAhead], int r0) {
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x) {
+      const int r = r0 + x * kRows + sub;
+      raw[x] = make_uint4(0, 0, 0, 0);
+      if (r < end) raw[x] = load8<T, kWide>(r < a.Hq ? q + r * a.q_head : k + (r - a.Hq) * a.kv.k_head);
+    }
+  };
+  uint4 raw[kAhead];
+  fetch(raw, first);
+  const int64_t slot = end > a.Hq ? a.kv.slots[tok] : -1;
   Turn<kInter> turn;
   turn.load(a, tok, l);
-  float y[8];
-  turn.template apply<T>(raw, turned, y);
-  const unsigned keys = __ballot_sync(turned, !is_q);
-  if (is_q) {
-    store8<T, kWide>(static_cast<T *>(a.qo) + tok * a.qo_row + h * a.qo_head + 8 * l, rounded<T>(y));
-  } else {
-    uint32_t codes, param;
-    quantise32<kLanes>(y, keys, codes, param);
-    uint8_t *group;
-    int tau;
-    if (locate(a.kv, slot, h, kv4_group_bytes(D), group, tau)) put_row<D>(group, tau, false, l, codes, param);
+  for (int r0 = first; r0 < end; r0 += kAhead * kRows) {
+    if (r0 > first) fetch(raw, r0);
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x) {
+      const int r = r0 + x * kRows + sub;
+      if (r - sub >= end) break;
+      float y[8];
+      turn.template apply<T>(raw[x], y);
+      if (r < min(a.Hq, end)) store8<T, kWide>(static_cast<T *>(a.qo) + tok * a.qo_row + r * a.qo_head + 8 * l, rounded<T>(y));
+      if (r - sub + kRows > a.Hq) {  // keys among them
+        uint32_t codes, param;
+        quantise32<kLanes>(y, 0xffffffffu, codes, param);
+        if (r >= a.Hq && r < end && locate(a.kv, slot, r - a.Hq, kv4_group_bytes(D), group, tau)) put_row<D>(group, tau, false, l, codes, param);
+      }
+    }
   }
 }
 
 template <class T, int D, bool kWide, bool kInter>
 void launch_rows(const RotArgs &a, cudaStream_t s) {
-  launch_pdl(kv4_rotate_few_kernel<T, D, kWide, kInter>, static_cast<unsigned>((a.kv.T * (a.Hq + 2 * a.kv.H) * (D / 8) + 255) / 256), 256, 0, s, a);
+  constexpr int kRows = 256 / D;
+  const int64_t T_ = a.kv.T, passes = (a.Hq + a.kv.H + kRows - 1) / kRows, want = static_cast<int64_t>(sm_count()) * kUnitWarps;
+  const int64_t cut = T_ >= want ? 1 : (want + T_ - 1) / T_;  // units of a token
+  const int32_t per = static_cast<int32_t>((passes + (cut < passes ? cut : passes) - 1) / (cut < passes ? cut : passes)) * kRows;
+  const int32_t units = (a.Hq + a.kv.H + per - 1) / per;
+  const int64_t warps = T_ * units, groups = (T_ + kGroup - 1) / kGroup * a.kv.H;
+  const bool many = groups >= static_cast<int64_t>(kManyWarps) * sm_count();
+  const int64_t values = many ? (groups + 7) / 8 : (T_ * a.kv.H + 8 * kRows - 1) / (8 * kRows);
+  const unsigned grid = static_cast<unsigned>(values + (warps + 7) / 8);
+  if (many)
+    launch_pdl(kv4_rotate_kernel<T, D, kWide, kInter, true>, grid, 256, 0, s, a, values, units, per);
+  else
+    launch_pdl(kv4_rotate_kernel<T, D, kWide, kInter, false>, grid, 256, 0, s, a, values, units, per);
 }
 template <class T, int D>
 void launch_form(bool w, bool inter, const RotArgs &a, cudaStream_t s) {
@@ -186,7 +240,7 @@ extern "C" int maps_kv4_append_rotated(int32_t dtype, int64_t T, int32_t Hq, int
       (rot > 0 && (pos == nullptr || (n_pos > 0 && cos_sin == nullptr) || !aligned(pos, 4) || !aligned(axis, 4) || !aligned(cos_sin, 16))))
     return MAPS_E_INVALID;
   RotArgs a = {{T, n_blocks, H, S, k, v, nullptr, nullptr, k_row, k_head, v_row, v_head, slots, static_cast<uint8_t *>(cache), status_word(ws)},
-               Hq, axes, rot, q, q_out, q_row, q_head, qo_row, qo_head, pos, axis, cos_sin, n_pos};
+               Hq, axes, rot, aligned(axis, 16), q, q_out, q_row, q_head, qo_row, qo_head, pos, axis, cos_sin, n_pos};
   const bool w = wide(k, k_row, k_head) && wide(v, v_row, v_head) && (Hq == 0 || (wide(q, q_row, q_head) && wide(q_out, qo_row, qo_head)));
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (dtype == MAPS_BF16)

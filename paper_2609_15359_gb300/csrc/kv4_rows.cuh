@@ -7,6 +7,11 @@
 namespace maps {
 namespace {
 
+// Warps of a multiprocessor from which on a warp takes 16 tokens of a head: shared loads of slots and whole groups moved at
+// once, but fewer and longer threads.  8 heads of 128 channels, append / read, rows side by side and 16 to a warp:
+// 1,024 tokens (3 warps) 3.8 / 3.3 and 5.2 / 3.4 us; 4,096 (13) 9.7 / 7.9 and 9.4 / 4.7; 16,384 34.6 / 28.0 and 20.2 / 12.8.
+constexpr int kManyWarps = 8;
+
 struct KVArgs {
   int64_t T, n_blocks;
   int32_t H, S;
@@ -161,6 +166,123 @@ __device__ __forceinline__ void get_row(const uint8_t *group, int tau, bool is_v
   else
     codes = *reinterpret_cast<const uint32_t *>(group + tau * (D / 2) + 4 * l);
   param = reinterpret_cast<const uint32_t *>(group + 16 * D)[(is_v ? 16 : 0) + tau];
+}
+
+// ---- many rows: a warp takes 16 consecutive tokens of a head, keys and values.  Prompts fill the cache in
+// runs, and the bytes are what counts there, so a group of 16 tokens that the batch holds whole and in order is moved as a
+// whole: its V units pass through shared memory, because a token's lie 2 bytes in every 4, and reach memory as full lines.  The
+// warp whose tokens a group starts in takes it; the tokens of no whole group go one by one as few rows do.
+// w counts (16 tokens, head) over the device's warps; stage: kStageBytes of shared memory for each; kFirst 1: values alone.
+template <int D>
+constexpr int kStageBytes = 8 * D + 128;  // V codes and parameters of a group
+
+template <class T, int D, bool kWide, bool kAppend, int kFirst>
+__device__ __forceinline__ void move_groups(const KVArgs &a, int64_t w, uint8_t *stage) {
+  constexpr int kLanes = D / 8, kRows = 32 / kLanes, kPasses = kGroup / kRows;
+  constexpr int kBatch = kPasses < 8 ? kPasses : 8;  // rows' loads under way at once
+  constexpr int kStage = kStageBytes<D>;
+  const int lane = threadIdx.x & 31, l = lane % kLanes, sub = lane / kLanes;
+  const int64_t i0 = w / a.H * kGroup;
+  const int h = static_cast<int>(w % a.H);
+  if (i0 >= a.T) return;
+
+  // slots of the tokens i0 - 16 .. i0 + 31: bit q of `next` says that token i0 - 16 + q follows its predecessor's
+  auto slot_of = [&](int64_t i) -> int64_t { return i >= 0 && i < a.T ? a.slots[i] : -1; };
+  const int64_t s0 = slot_of(i0 - kGroup + lane), s1 = slot_of(i0 + kGroup + lane);
+  const int64_t p0 = __shfl_up_sync(0xffffffffu, s0, 1), last = __shfl_sync(0xffffffffu, s0, 31);
+  int64_t p1 = __shfl_up_sync(0xffffffffu, s1, 1);
+  if (lane == 0) p1 = last;
+  const unsigned n0 = __ballot_sync(0xffffffffu, lane > 0 && p0 >= 0 && s0 == p0 + 1), n1 = __ballot_sync(0xffffffffu, p1 >= 0 && s1 == p1 + 1);
+  const uint64_t next = n0 | static_cast<uint64_t>(n1) << 32;
+  const bool starts = s0 >= 0 && s0 % kGroup == 0 && s0 / a.S < a.n_blocks && ((next >> (lane + 1)) & 0x7fffu) == 0x7fffu;
+  const unsigned whole = __ballot_sync(0xffffffffu, starts);  // at most one in each half
+  const int before = __ffs(whole & 0xffffu) - 1, here = __ffs(whole >> 16) - 1;
+  const int from = before > 0 ? before : 0, to = here >= 0 ? here : kGroup;  // tokens of no whole group
+
+  if (here >= 0) {
+    const int64_t i = i0 + here, slot = __shfl_sync(0xffffffffu, s0, kGroup + here);
+    uint8_t *group;
+    int tau0;
+    (void)locate(a, slot, h, kv4_group_bytes(D), group, tau0);
+    uint32_t *par = reinterpret_cast<uint32_t *>(stage + 8 * D);
+    if (!kAppend) {
+#pragma unroll
+      for (int x = lane; x < kStage / 16; x += 32) reinterpret_cast<uint4 *>(stage)[x] = reinterpret_cast<const uint4 *>(group + 8 * D)[x];
+      __syncwarp();
+    }
+#pragma unroll
+    for (int kind = kFirst; kind < 2; ++kind) {
+      const int64_t row = kind ? a.v_row : a.k_row;
+      const int64_t at = i * row + h * (kind ? a.v_head : a.k_head) + 8 * l;
+#pragma unroll
+      for (int b = 0; b < kPasses; b += kBatch) {
+        if (kAppend) {
+          uint4 raw[kBatch];
+#pragma unroll
+          for (int p = 0; p < kBatch; ++p) raw[p] = load8<T, kWide>(static_cast<const T *>(kind ? a.v : a.k) + at + ((b + p) * kRows + sub) * row);
+#pragma unroll
+          for (int p = 0; p < kBatch; ++p) {
+            const int tau = (b + p) * kRows + sub;
+            uint32_t codes, param;
+            quantise<T, kLanes>(raw[p], 0xffffffffu, codes, param);
+            if (kind == 0) {
+              *reinterpret_cast<uint32_t *>(group + tau * (D / 2) + 4 * l) = codes;
+            } else {
+              *reinterpret_cast<uint16_t *>(stage + kv4_v_unit<D>(tau, 2 * l)) = static_cast<uint16_t>(codes);
+              *reinterpret_cast<uint16_t *>(stage + kv4_v_unit<D>(tau, 2 * l + 1)) = static_cast<uint16_t>(codes >> 16);
+            }
+            if (l == 0) par[16 * kind + tau] = param;
+          }
+        } else {
+          uint32_t codes[kBatch];
+#pragma unroll
+          for (int p = 0; p < kBatch; ++p) {
+            const int tau = (b + p) * kRows + sub;
+            if (kind == 0)
+              codes[p] = *reinterpret_cast<const uint32_t *>(group + tau * (D / 2) + 4 * l);
+            else
+              codes[p] = *reinterpret_cast<const uint16_t *>(stage + kv4_v_unit<D>(tau, 2 * l)) |
+                         static_cast<uint32_t>(*reinterpret_cast<const uint16_t *>(stage + kv4_v_unit<D>(tau, 2 * l + 1))) << 16;
+          }
+#pragma unroll
+          for (int p = 0; p < kBatch; ++p) {
+            const int tau = (b + p) * kRows + sub;
+            store8<T, kWide>(static_cast<T *>(kind ? a.vo : a.ko) + at + tau * row, values<T>(codes[p], par[16 * kind + tau]));
+          }
+        }
+      }
+    }
+    if (kAppend) {
+      __syncwarp();
+#pragma unroll
+      for (int x = lane; x < kStage / 16; x += 32) {
+        if (kFirst == 1 && x >= D / 2 && x < D / 2 + 4) continue;  // the keys' parameters are another warp's
+        reinterpret_cast<uint4 *>(group + 8 * D)[x] = reinterpret_cast<const uint4 *>(stage)[x];
+      }
+    }
+  }
+  for (int j0 = from / kRows * kRows; j0 < to; j0 += kRows) {
+    const int j = j0 + sub;
+    const int64_t i = i0 + j;
+    const bool mine = j >= from && j < to && i < a.T;
+    const int64_t slot = mine ? a.slots[i] : -1;
+#pragma unroll
+    for (int kind = kFirst; kind < 2; ++kind) {
+      const int64_t at = i * (kind ? a.v_row : a.k_row) + h * (kind ? a.v_head : a.k_head) + 8 * l;
+      uint8_t *group;
+      int tau;
+      uint32_t codes = 0, param = 0;
+      if (kAppend) {
+        uint4 raw = make_uint4(0, 0, 0, 0);
+        if (mine) raw = load8<T, kWide>(static_cast<const T *>(kind ? a.v : a.k) + at);
+        quantise<T, kLanes>(raw, 0xffffffffu, codes, param);
+        if (locate(a, slot, h, kv4_group_bytes(D), group, tau)) put_row<D>(group, tau, kind, l, codes, param);
+      } else {
+        if (locate(a, slot, h, kv4_group_bytes(D), group, tau)) get_row<D>(group, tau, kind, l, codes, param);
+        if (mine) store8<T, kWide>(static_cast<T *>(kind ? a.vo : a.ko) + at, values<T>(codes, param));
+      }
+    }
+  }
 }
 
 inline bool wide(const void *p, int64_t row, int64_t head) { return aligned(p, 16) && row % 8 == 0 && head % 8 == 0; }
