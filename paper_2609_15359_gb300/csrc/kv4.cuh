@@ -56,4 +56,7 @@ __device__ __forceinline__ float2 kv4_param(uint32_t w) {  // {scale, zero}
   return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
 }
 
+struct Yes { static constexpr bool value = true; };
+struct No { static constexpr bool value = false; };
+
 }  // namespace maps

@@ -157,9 +157,6 @@ __device__ __forceinline__ int32_t many_over(const AttnArgs &a) {
   return s_pairs > kFewPairs / a.Hkv ? a.few_rows : 0;
 }
 
-struct Yes { static constexpr bool value = true; };
-struct No { static constexpr bool value = false; };
-
 // The form for many queries (kv4_attention_many.cu).
 bool attn_many_dim(int D);
 void attn_many_carve(Carve &c, AttnArgs &a, int32_t B, int D);

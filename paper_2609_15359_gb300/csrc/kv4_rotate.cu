@@ -11,7 +11,7 @@ namespace maps {
 namespace {
 
 // Warps of a multiprocessor up to which a token's heads are shared out among several.
-constexpr int kUnitWarps = 32;
+constexpr int kUnitWarps = 16;
 
 struct RotArgs {
   KVArgs kv;
@@ -23,22 +23,24 @@ struct RotArgs {
   const int32_t *pos, *axis;
   const float *cos_sin;
   int64_t n_pos;
+  float minus_zero;
 };
 
-// The angles of this lane's channels 8l .. 8l + 7 at a token: of their 8 pairs, or, where pairs are neighbours, 4.
+// The angles of this lane's channels 8l .. 8l + 7 at a token: channel i becomes x_i c_i + z_i s_i, z its partner, the sine with
+// the sign that it has there (a c - b s is a c + b (-s), rounded alike).
 template <bool kInter>
 struct Turn {
-  static constexpr int kN = kInter ? 4 : 8;
-  float c[kN], s[kN];  // the sine with the sign that it has for this half of the pairs
-  bool on;
+  float c[8], s[8];
+  uint32_t on;  // all bits, or none: channels that do not turn, which are x 1 + 0 (-0), x itself whatever it is
   int partner;  // lanes from here
   __device__ __forceinline__ void load(const RotArgs &a, int64_t tok, int l) {
+    constexpr int kN = kInter ? 4 : 8;  // pairs
     const int F = a.rot / 2;
-    on = 8 * l < a.rot;
+    on = 8 * l < a.rot ? 0xffffffffu : 0u;
     const bool second = !kInter && 8 * l >= F;
-    partner = kInter || !on ? 0 : second ? -(F / 8) : F / 8;
+    partner = !on ? 0 : second ? -(F / 8) : F / 8;
 #pragma unroll
-    for (int i = 0; i < kN; ++i) c[i] = 1.0f, s[i] = 0.0f;
+    for (int i = 0; i < 8; ++i) c[i] = 1.0f, s[i] = -0.0f;
     if (!on) return;
     const int f0 = kInter ? 4 * l : second ? 8 * l - F : 8 * l;
     int32_t ax[kN] = {};
@@ -82,35 +84,35 @@ struct Turn {
         if (at >= 0) c[i] = a.cos_sin[at + f0 + i], s[i] = a.cos_sin[at + F + f0 + i];
       }
     }
-    if (!kInter && !second) {
-#pragma unroll
-      for (int i = 0; i < kN; ++i) s[i] = -s[i];
-    }
-  }
-  // A row's 8 channels, turned.  All lanes of the warp call it.
-  template <class T>
-  __device__ __forceinline__ void apply(const uint4 raw, float (&y)[8]) const {
-    const T *x = reinterpret_cast<const T *>(&raw);
     if (kInter) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float p = Cvt<T>::to(x[2 * i]), q = Cvt<T>::to(x[2 * i + 1]);
-        y[2 * i] = on ? __fsub_rn(__fmul_rn(p, c[i]), __fmul_rn(q, s[i])) : p;
-        y[2 * i + 1] = on ? __fadd_rn(__fmul_rn(q, c[i]), __fmul_rn(p, s[i])) : q;
-      }
+      for (int i = 3; i >= 0; --i) c[2 * i + 1] = c[2 * i] = c[i], s[2 * i + 1] = s[i], s[2 * i] = -s[i];
+    } else if (!second) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s[i] = -s[i];
+    }
+  }
+  // A row's 8 channels, turned.  All lanes of the warp call it.  A product of two is a fused one with minus_zero, which
+  // only the host knows to be -0: the compiler joins a product and a sum of two to one operation, rounded once.
+  template <class T>
+  __device__ __forceinline__ void apply(const uint4 raw, float minus_zero, float (&y)[8]) const {
+    uint4 other;
+    if (kInter) {
+      other = make_uint4(__funnelshift_l(raw.x, raw.x, 16), __funnelshift_l(raw.y, raw.y, 16), __funnelshift_l(raw.z, raw.z, 16), __funnelshift_l(raw.w, raw.w, 16));
     } else {
-      uint4 other;
       const int from = (threadIdx.x & 31) + partner;
       other.x = __shfl_sync(0xffffffffu, raw.x, from);
       other.y = __shfl_sync(0xffffffffu, raw.y, from);
       other.z = __shfl_sync(0xffffffffu, raw.z, from);
       other.w = __shfl_sync(0xffffffffu, raw.w, from);
-      const T *z = reinterpret_cast<const T *>(&other);
+    }
+    other.x &= on, other.y &= on, other.z &= on, other.w &= on;
+    const T *x = reinterpret_cast<const T *>(&raw), *z = reinterpret_cast<const T *>(&other);
+    const Two none(minus_zero, minus_zero);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float p = Cvt<T>::to(x[i]);
-        y[i] = on ? __fadd_rn(__fmul_rn(p, c[i % kN]), __fmul_rn(Cvt<T>::to(z[i]), s[i % kN])) : p;
-      }
+    for (int i = 0; i < 8; i += 2) {
+      const Two own = fused(Two(Cvt<T>::to(x[i]), Cvt<T>::to(x[i + 1])), Two(c[i], c[i + 1]), none);
+      (own + fused(Two(Cvt<T>::to(z[i]), Cvt<T>::to(z[i + 1])), Two(s[i], s[i + 1]), none)).get(y[i], y[i + 1]);
     }
   }
 };
@@ -130,7 +132,7 @@ __device__ __forceinline__ uint4 rounded(const float (&y)[8]) {
 constexpr int kAhead = 4;
 
 template <class T, int D, bool kWide, bool kInter, bool kGroups>
-__global__ void __launch_bounds__(256) kv4_rotate_kernel(const RotArgs a, const int64_t value_blocks, const int32_t units, const int32_t per) {
+__global__ void __launch_bounds__(256, 4) kv4_rotate_kernel(const RotArgs a, const int64_t value_blocks, const int32_t units, const int32_t per) {
   pdl_prologue();
   constexpr int kLanes = D / 8, kRows = 32 / kLanes;
   __shared__ __align__(16) uint8_t s_stage[kGroups ? 8 : 1][kGroups ? kStageBytes<D> : 16];
@@ -157,35 +159,43 @@ __global__ void __launch_bounds__(256) kv4_rotate_kernel(const RotArgs a, const 
   const int64_t u = (static_cast<int64_t>(blockIdx.x) - value_blocks) * 8 + warp, tok = u / units;
   if (tok >= a.kv.T) return;
   const int first = static_cast<int>(u - tok * units) * per, end = min(first + per, a.Hq + a.kv.H);
-  const T *q = static_cast<const T *>(a.q) + tok * a.q_row + 8 * l, *k = static_cast<const T *>(a.kv.k) + tok * a.kv.k_row + 8 * l;
-  auto fetch = [&](uint4 (&raw)[kAhead], int r0) {
-#pragma unroll
-    for (int x = 0; x < kAhead; ++x) {
-      const int r = r0 + x * kRows + sub;
-      raw[x] = make_uint4(0, 0, 0, 0);
-      if (r < end) raw[x] = load8<T, kWide>(r < a.Hq ? q + r * a.q_head : k + (r - a.Hq) * a.kv.k_head);
-    }
-  };
-  uint4 raw[kAhead];
-  fetch(raw, first);
   const int64_t slot = end > a.Hq ? a.kv.slots[tok] : -1;
   Turn<kInter> turn;
-  turn.load(a, tok, l);
-  for (int r0 = first; r0 < end; r0 += kAhead * kRows) {
-    if (r0 > first) fetch(raw, r0);
+  bool ready = false;
+  // Rows r .. r_end - 1 of the token's rows at `base`.  All lanes of the warp call put(row, y, whether this lane has the row).
+  auto pass = [&](const T *base, int64_t stride, int r, int r_end, auto put) {
+    const T *src = base + (r + sub) * stride;
+    for (; r < r_end; r += kAhead * kRows, src += kAhead * kRows * stride) {
+      uint4 raw[kAhead];
 #pragma unroll
-    for (int x = 0; x < kAhead; ++x) {
-      const int r = r0 + x * kRows + sub;
-      if (r - sub >= end) break;
-      float y[8];
-      turn.template apply<T>(raw[x], y);
-      if (r < min(a.Hq, end)) store8<T, kWide>(static_cast<T *>(a.qo) + tok * a.qo_row + r * a.qo_head + 8 * l, rounded<T>(y));
-      if (r - sub + kRows > a.Hq) {  // keys among them
-        uint32_t codes, param;
-        quantise32<kLanes>(y, 0xffffffffu, codes, param);
-        if (r >= a.Hq && r < end && locate(a.kv, slot, r - a.Hq, kv4_group_bytes(D), group, tau)) put_row<D>(group, tau, false, l, codes, param);
+      for (int x = 0; x < kAhead; ++x) {
+        raw[x] = make_uint4(0, 0, 0, 0);
+        if (r + x * kRows + sub < r_end) raw[x] = load8<T, kWide>(src + x * kRows * stride);
+      }
+      if (!ready) turn.load(a, tok, l), ready = true;
+#pragma unroll
+      for (int x = 0; x < kAhead; ++x) {
+        if (r + x * kRows >= r_end) break;
+        float y[8];
+        turn.template apply<T>(raw[x], a.minus_zero, y);
+        put(r + x * kRows + sub, y, r + x * kRows + sub < r_end);
       }
     }
+  };
+  if (first < a.Hq) {
+    T *out = static_cast<T *>(a.qo) + tok * a.qo_row + 8 * l;
+    pass(static_cast<const T *>(a.q) + tok * a.q_row + 8 * l, a.q_head, first, min(a.Hq, end), [&](int r, const float (&y)[8], bool mine) {
+      if (mine) store8<T, kWide>(out + r * a.qo_head, rounded<T>(y));
+    });
+  }
+  if (end > a.Hq) {
+    const bool held = locate(a.kv, slot, 0, kv4_group_bytes(D), group, tau);
+    const int64_t head = static_cast<int64_t>(a.kv.S / kGroup) * kv4_group_bytes(D);
+    pass(static_cast<const T *>(a.kv.k) + tok * a.kv.k_row + 8 * l, a.kv.k_head, max(first - a.Hq, 0), end - a.Hq, [&](int r, const float (&y)[8], bool mine) {
+      uint32_t codes, param;
+      quantise32<kLanes>(y, 0xffffffffu, codes, param);
+      if (mine && held) put_row<D>(group + r * head, tau, false, l, codes, param);
+    });
   }
 }
 
@@ -240,7 +250,7 @@ extern "C" int maps_kv4_append_rotated(int32_t dtype, int64_t T, int32_t Hq, int
       (rot > 0 && (pos == nullptr || (n_pos > 0 && cos_sin == nullptr) || !aligned(pos, 4) || !aligned(axis, 4) || !aligned(cos_sin, 16))))
     return MAPS_E_INVALID;
   RotArgs a = {{T, n_blocks, H, S, k, v, nullptr, nullptr, k_row, k_head, v_row, v_head, slots, static_cast<uint8_t *>(cache), status_word(ws)},
-               Hq, axes, rot, aligned(axis, 16), q, q_out, q_row, q_head, qo_row, qo_head, pos, axis, cos_sin, n_pos};
+               Hq, axes, rot, aligned(axis, 16), q, q_out, q_row, q_head, qo_row, qo_head, pos, axis, cos_sin, n_pos, -0.0f};
   const bool w = wide(k, k_row, k_head) && wide(v, v_row, v_head) && (Hq == 0 || (wide(q, q_row, q_head) && wide(q_out, qo_row, qo_head)));
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (dtype == MAPS_BF16)

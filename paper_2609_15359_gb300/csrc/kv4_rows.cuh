@@ -49,6 +49,25 @@ struct Pair<__half> {
   using V = __half2;
 };
 
+// Two 32-bit numbers at a time, each operation rounded as a single one is.
+struct Two {
+  uint64_t bits;
+  __device__ __forceinline__ Two(float x, float y) { asm("mov.b64 %0, {%1, %2};" : "=l"(bits) : "f"(x), "f"(y)); }
+  __device__ __forceinline__ void get(float &x, float &y) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(bits)); }
+};
+__device__ __forceinline__ Two operator+(Two x, Two y) {
+  asm("add.rn.f32x2 %0, %0, %1;" : "+l"(x.bits) : "l"(y.bits));
+  return x;
+}
+__device__ __forceinline__ Two operator*(Two x, Two y) {
+  asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(x.bits) : "l"(y.bits));
+  return x;
+}
+__device__ __forceinline__ Two fused(Two x, Two y, Two z) {
+  asm("fma.rn.f32x2 %0, %0, %1, %2;" : "+l"(x.bits) : "l"(y.bits), "l"(z.bits));
+  return x;
+}
+
 // Codes and {scale, zero} of a row's 8 values y, the row's extremes given.
 __device__ __forceinline__ void encode(const float (&y)[8], float low, float high, uint32_t &codes, uint32_t &param) {
   const float spread = __fsub_rn(high, low);
@@ -58,10 +77,14 @@ __device__ __forceinline__ void encode(const float (&y)[8], float low, float hig
   const float inv = scale >= 1.17549435e-38f ? __fdiv_rn(1.0f, scale) : 0.0f;  // smallest normal number
   // adding 1.5 * 2^23 rounds to an integer in the low bits; the sum of those times 16^i then has 8 known offsets to take off
   uint32_t sum = 0;
+  const Two off(-zero, -zero), by(inv, inv), whole(12582912.0f, 12582912.0f);
 #pragma unroll
-  for (int i = 7; i >= 0; --i) {
-    const float c = fminf(fmaxf(__fmul_rn(__fsub_rn(y[i], zero), inv), 0.0f), 15.0f);
-    sum = sum * 16u + __float_as_uint(__fadd_rn(c, 12582912.0f));
+  for (int i = 6; i >= 0; i -= 2) {
+    float c[2];
+    ((Two(y[i], y[i + 1]) + off) * by).get(c[0], c[1]);
+    (Two(fminf(fmaxf(c[0], 0.0f), 15.0f), fminf(fmaxf(c[1], 0.0f), 15.0f)) + whole).get(c[0], c[1]);
+    sum = sum * 16u + __float_as_uint(c[1]);
+    sum = sum * 16u + __float_as_uint(c[0]);
   }
   codes = bad ? 0u : sum - 0x4b400000u * 0x11111111u;
   param = bad ? 0x7fff7fffu : __float_as_uint(scale) >> 16 | (__float_as_uint(zero) & 0xffff0000u);
