@@ -5,8 +5,12 @@
 // row of 2 D products, in 8 bits on both sides: whole numbers below 2^23, exact in any order, and one rounding with the scale.
 // The same list comes out whatever the split.
 //
-// A block takes a row and KV head: its scores become keys, whole numbers in the scores' order; the least key that is taken
-// is found by histograms of the keys that are still in question, ten bits at a time; then the list is written in order.
+// A block takes a row and KV head, or a cluster of them where there are few: 256 cache blocks each in turn.  Scores become keys, whole
+// numbers in the scores' order, in the shared memory of the cluster's first block, which goes on alone (in the workspace where they
+// are too many).  The least key that is taken is found by histograms of the keys that are still in question, ten bits at a
+// time; then the list is written in order.
+#include <atomic>
+
 #include "kv4.cuh"
 
 namespace maps {
@@ -14,7 +18,10 @@ namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kBinBits = 10, kBins = 1 << kBinBits;
-constexpr int kSmemKeys = 32768;  // longer rows of keys lie in the workspace
+constexpr int kSmemKeys = 8192;   // of shared memory; longer rows of keys stay in the workspace
+constexpr int kBlocksOfSm = 8;    // blocks of a multiprocessor up to which a row and head is shared out
+constexpr int kMaxCluster = 16;
+constexpr size_t kMostKeys = size_t(1) << 26;  // in the workspace: more rows take their turns
 
 struct SelectArgs {
   int32_t B, Hq, H, S;
@@ -27,7 +34,11 @@ struct SelectArgs {
   const float *scale;
   int32_t first, last, n_list;
   int32_t *blocks, *tokens;
-  uint32_t *keys;  // [T * H][max_blocks], or NULL: in shared memory
+  int64_t row0;      // the launch's first row
+  int32_t cluster;
+  int32_t smem_keys;
+  uint32_t *keys;    // [rows of a launch * H][stride], or NULL: in shared memory
+  int64_t stride;
   int32_t *status;
 };
 
@@ -44,6 +55,14 @@ __device__ __forceinline__ void add_twice(float &s, float &e, float x) {
   s = t;
 }
 
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint32_t *of_first_block(uint32_t *p) {  // the same place in the shared memory of the cluster's first block
+  uint64_t y;
+  asm("mapa.u64 %0, %1, 0;" : "=l"(y) : "l"(reinterpret_cast<uint64_t>(p)));
+  return reinterpret_cast<uint32_t *>(y);
+}
+
 // The greatest b with off[b] <= i of b in [0, B], -1 where there is none.  All threads call it.
 __device__ __forceinline__ int request_of(const int64_t *off, int B, int64_t i) {
   int64_t lo = 0, n = static_cast<int64_t>(B) + 1;
@@ -57,56 +76,111 @@ __device__ __forceinline__ int request_of(const int64_t *off, int B, int64_t i) 
   }
 }
 
+// Sums of acc[k] over the 2 kHalf lanes that differ in their low bits, lane x keeping that of acc[x].
+template <int kHalf>
+__device__ __forceinline__ void join(int (&acc)[8], int lane) {
+#pragma unroll
+  for (int o = kHalf; o > 0; o >>= 1) {
+    const bool up = lane & o;
+#pragma unroll
+    for (int k = 0; k < o; ++k) {
+      const int send = up ? acc[k] : acc[k + o], keep = up ? acc[k + o] : acc[k];
+      acc[k] = keep + __shfl_xor_sync(0xffffffffu, send, o);
+    }
+  }
+}
+
 template <class T, int D>
-__global__ void __launch_bounds__(kThreads) kv4_select_kernel(const SelectArgs a) {
+__global__ void __launch_bounds__(kThreads, 3) kv4_select_kernel(const SelectArgs a) {
   constexpr int kLanes = D / 8, kSub = 32 / kLanes;  // lanes of a block's 2 D codes, and blocks of a warp's load
-  constexpr int kBatch = kLanes < 8 ? kLanes : 8;    // loads under way at once
-  extern __shared__ uint32_t s_keys[];
+  constexpr int kBatch = 8;                          // loads under way at once; D/8 of them make a step of 32 blocks
+  extern __shared__ __align__(16) uint32_t s_keys[];
   __shared__ __align__(16) int8_t s_w[2 * D];
   __shared__ uint32_t s_hist[kBins];
   __shared__ uint32_t s_warp[kWarps][2];
   __shared__ uint32_t s_found[3];
-  __shared__ float s_step[kWarps];
   pdl_prologue();
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int64_t item = blockIdx.x, i = item / a.H;
-  const int h = static_cast<int>(item - i * a.H);
-  const int b = request_of(a.off, a.B, i);
-  if (b < 0 || b == a.B) return;  // no request's
-  const int64_t q0 = a.off[b], q1 = a.off[b + 1];
-  int32_t n = a.len[b];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = static_cast<int>(blockIdx.x) & (a.cluster - 1);
+  const int64_t here = blockIdx.x / a.cluster, item = a.row0 * a.H + here, i = a.row0 + here / a.H;
+  const int h = static_cast<int>(here % a.H);
+  // the row's request: the one of its number, where each has one row, else searched for
+  int64_t b = i, q1 = 0;
+  int32_t n = 0;
+  bool found = false;
+  if (i < a.B) {
+    const int64_t q0 = a.off[i];
+    q1 = a.off[i + 1];
+    n = a.len[i];
+    found = q0 >= 0 && q0 <= i && i < q1;
+  }
+  if (!found) {
+    b = request_of(a.off, a.B, i);
+    if (b < 0 || b == a.B) return;  // no request's
+    q1 = a.off[b + 1];
+    n = a.len[b];
+  }
   int32_t *out = a.blocks + item * a.n_list;
-  if (q0 < 0 || q1 > a.T || i >= q1 || n < 0 || n > 0x7fffffff - 1023 || n > a.max_blocks * a.S) {
+  if (q1 > a.T || i >= q1 || n < 0 || n > 0x7fffffff - 1023 || n > a.max_blocks * a.S) {
     if (tid == 0) flag_error(a.status, MAPS_E_RANGE);
     n = 0;
   }
   const int64_t seen = n - (q1 - i) + 1;  // keys
-  if (n == 0 || seen <= 0) {
-    for (int x = tid; x < a.n_list; x += kThreads) out[x] = -1;
-    if (tid == 0) a.tokens[item] = 0;
-    return;
-  }
-  const int32_t nb = static_cast<int32_t>((seen + a.S - 1) / a.S), count = min(nb, a.n_list);
+  const int32_t nb = n == 0 || seen <= 0 ? 0 : static_cast<int32_t>((seen + a.S - 1) / a.S), count = min(nb, a.n_list);
+  const int32_t N = nb - a.first - a.last;           // blocks in question
+  uint32_t need = a.n_list - a.first - a.last;       // of which so many are taken
+  const bool all = nb <= a.n_list;
+  const int sharers = all || need == 0 ? 1 : min(a.cluster, (N + kThreads - 1) / kThreads);
+  if (rank >= sharers) return;  // the cluster's barriers count those that are left
   const int32_t *table = a.table + b * a.max_blocks;
-  if (tid == 0) a.tokens[item] = static_cast<int32_t>((count - 1) * static_cast<int64_t>(a.S) + seen - (nb - 1) * static_cast<int64_t>(a.S));
-  for (int x = count + tid; x < a.n_list; x += kThreads) out[x] = -1;
-  if (nb <= a.n_list) {  // all of them
-    for (int x = tid; x < nb; x += kThreads) out[x] = table[x];
-    return;
+  if (rank == 0) {
+    if (tid == 0) a.tokens[item] = nb == 0 ? 0 : static_cast<int32_t>((count - 1) * static_cast<int64_t>(a.S) + seen - (nb - 1) * static_cast<int64_t>(a.S));
+    for (int x = count + tid; x < a.n_list; x += kThreads) out[x] = -1;
+    if (all) {
+      for (int x = tid; x < nb; x += kThreads) out[x] = table[x];
+    } else {
+      for (int x = tid; x < a.first; x += kThreads) out[x] = table[x];
+      for (int x = tid; x < a.last; x += kThreads) out[count - a.last + x] = table[nb - a.last + x];
+    }
   }
-  for (int x = tid; x < a.first; x += kThreads) out[x] = table[x];
-  for (int x = tid; x < a.last; x += kThreads) out[count - a.last + x] = table[nb - a.last + x];
-  uint32_t need = a.n_list - a.first - a.last;  // of the others
-  if (need == 0) return;
-  const int32_t N = nb - a.first - a.last;
+  if (all || need == 0) return;
+  if (sharers > 1) cluster_arrive();  // this block runs, so its shared memory may be written
   table += a.first;
   out += a.first;
 
-  // ---- the queries' weights
+  // ---- the first blocks' codes are under way while the queries' weights are made
+  const int l = lane % kLanes, sub = lane / kLanes;
+  const int first = (rank * kWarps + warp) * 32, stride = sharers * kThreads;
+  int32_t block = -1;
+  float sc = 0.0f;
+  auto look_up = [&](int j) {  // the block whose score this lane ends up with
+    block = -1;
+    sc = 0.0f;
+    if (j >= N) return;
+    block = table[j];
+    if (block < 0 || block >= a.n_blocks) {
+      flag_error(a.status, MAPS_E_RANGE);
+      block = -1;
+    } else {
+      sc = a.scale[static_cast<int64_t>(block) * a.H + h];
+    }
+  };
+  int4 c[kBatch];
+  const int8_t *mine = a.codes + static_cast<int64_t>(h) * (2 * D) + 16 * l;
+  const int64_t block_bytes = static_cast<int64_t>(a.H) * (2 * D);
+  auto fetch = [&](int k0) {
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const int32_t blk = __shfl_sync(0xffffffffu, block, sub * kLanes + k0 + k);
+      c[k] = make_int4(0, 0, 0, 0);
+      if (blk >= 0) c[k] = *reinterpret_cast<const int4 *>(mine + blk * block_bytes);
+    }
+  };
+  look_up(first + l * kSub + sub);
   const int group = a.Hq / a.H;
   float P = 0.0f, Pe = 0.0f, M = 0.0f, Me = 0.0f;
   if (tid < D) {
     const T *src = static_cast<const T *>(a.q) + i * a.q_row + static_cast<int64_t>(h) * group * a.q_head + tid;
+#pragma unroll 4
     for (int x = 0; x < group; ++x) {
       const float y = Cvt<T>::to(src[x * a.q_head]);
       add_twice(P, Pe, y > 0.0f || y != y ? y : 0.0f);
@@ -115,13 +189,14 @@ __global__ void __launch_bounds__(kThreads) kv4_select_kernel(const SelectArgs a
     P = __fadd_rn(P, Pe);
     M = __fadd_rn(M, Me);
   }
+  fetch(0);
   // NaN's bits are above infinity's
   const uint32_t most = __reduce_max_sync(0xffffffffu, max(__float_as_uint(P) & 0x7fffffffu, __float_as_uint(M) & 0x7fffffffu));
-  if (lane == 0) s_step[warp] = __uint_as_float(most);
+  if (lane == 0) s_warp[warp][0] = most;
   __syncthreads();
   uint32_t top = 0;
 #pragma unroll
-  for (int w = 0; w < kWarps; ++w) top = max(top, __float_as_uint(s_step[w]));
+  for (int w = 0; w < kWarps; ++w) top = max(top, s_warp[w][0]);
   const float step = __fmul_rn(__uint_as_float(top), 1.0f / 127.0f);
   const bool no_number = !(step < INFINITY);
   const float inv = step >= 1.17549435e-38f ? __fdiv_rn(1.0f, step) : 0.0f;
@@ -132,75 +207,84 @@ __global__ void __launch_bounds__(kThreads) kv4_select_kernel(const SelectArgs a
   __syncthreads();
 
   // ---- keys
-  uint32_t *keys = a.keys ? a.keys + item * a.max_blocks : s_keys;
-  uint32_t least = 0xffffffffu, greatest = 0;
-  const int l = lane % kLanes, sub = lane / kLanes;
+  const bool fits = N <= a.smem_keys;
+  uint32_t *keys = !fits ? a.keys + here * a.stride : sharers > 1 ? of_first_block(s_keys) : s_keys;
+  uint32_t lo = 0xffffffffu, hi = 0;
   const int4 w = *reinterpret_cast<const int4 *>(s_w + 16 * l);
-  for (int j0 = warp * 32; j0 < N; j0 += kThreads) {
-    const int j = j0 + l * kSub + sub;  // the block whose score this lane ends up with
-    int32_t block = -1;
-    float sc = 0.0f;
+  if (sharers > 1) cluster_wait();
+  for (int j0 = first; j0 < N; j0 += stride) {
+    // a step's D/8 loads eight at a time: their sums over 8 lanes, lane x keeping that of load x; then over the rest of a block's lanes
+    int part[kLanes / 8];
+#pragma unroll
+    for (int k0 = 0; k0 < kLanes; k0 += 8) {
+      if (k0 > 0) fetch(k0);
+      int acc[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) acc[k] = __dp4a(c[k].x, w.x, __dp4a(c[k].y, w.y, __dp4a(c[k].z, w.z, __dp4a(c[k].w, w.w, 0))));
+      join<4>(acc, lane);
+      part[k0 / 8] = acc[0];
+    }
+    const int32_t blk = block;
+    const float scale = sc;
+    if (j0 + stride < N) {
+      look_up(j0 + stride + l * kSub + sub);
+      fetch(0);
+    }
+#pragma unroll
+    for (int o = kLanes / 2; o >= 8; o >>= 1) {
+#pragma unroll
+      for (int k = 0; k < o / 8; ++k) {
+        const int send = l & o ? part[k] : part[k + o / 8], keep = l & o ? part[k + o / 8] : part[k];
+        part[k] = keep + __shfl_xor_sync(0xffffffffu, send, o);
+      }
+    }
+    const int j = j0 + l * kSub + sub;
     if (j < N) {
-      block = table[j];
-      if (block < 0 || block >= a.n_blocks) {
-        flag_error(a.status, MAPS_E_RANGE);
-        block = -1;
-      } else {
-        sc = a.scale[static_cast<int64_t>(block) * a.H + h];
-      }
-    }
-    int acc[kLanes];
-#pragma unroll
-    for (int k0 = 0; k0 < kLanes; k0 += kBatch) {
-      int4 c[kBatch];
-#pragma unroll
-      for (int k = 0; k < kBatch; ++k) {
-        const int32_t blk = __shfl_sync(0xffffffffu, block, sub * kLanes + k0 + k);
-        c[k] = make_int4(0, 0, 0, 0);
-        if (blk >= 0) c[k] = *reinterpret_cast<const int4 *>(a.codes + (static_cast<int64_t>(blk) * a.H + h) * (2 * D) + 16 * l);
-      }
-#pragma unroll
-      for (int k = 0; k < kBatch; ++k) acc[k0 + k] = __dp4a(c[k].x, w.x, __dp4a(c[k].y, w.y, __dp4a(c[k].z, w.z, __dp4a(c[k].w, w.w, 0))));
-    }
-#pragma unroll
-    for (int o = kLanes / 2; o > 0; o >>= 1) {
-      const bool up = l & o;
-#pragma unroll
-      for (int k = 0; k < o; ++k) {
-        const int send = up ? acc[k] : acc[k + o], keep = up ? acc[k + o] : acc[k];
-        acc[k] = keep + __shfl_xor_sync(0xffffffffu, send, o);
-      }
-    }
-    if (j < N) {
-      const uint32_t key = no_number || block < 0 ? 0xfffffffeu : key_of(__fmul_rn(static_cast<float>(acc[0]), sc));
+      const uint32_t key = no_number || blk < 0 ? 0xfffffffeu : key_of(__fmul_rn(static_cast<float>(part[0]), scale));
       keys[j] = key;
-      least = min(least, key);
-      greatest = max(greatest, key);
+      lo = min(lo, key);
+      hi = max(hi, key);
     }
   }
-  least = __reduce_min_sync(0xffffffffu, least);
-  greatest = __reduce_max_sync(0xffffffffu, greatest);
-  if (lane == 0) s_warp[warp][0] = least, s_warp[warp][1] = greatest;
+  if (sharers > 1) {
+    cluster_arrive();
+    if (rank > 0) return;
+    cluster_wait();
+    keys = fits ? s_keys : keys;
+    lo = 0xffffffffu, hi = 0;
+    for (int j = tid; j < N; j += kThreads) {
+      const uint32_t key = fits ? keys[j] : __ldcg(keys + j);
+      lo = min(lo, key);
+      hi = max(hi, key);
+    }
+  }
+  lo = __reduce_min_sync(0xffffffffu, lo);
+  hi = __reduce_max_sync(0xffffffffu, hi);
+  if (lane == 0) s_warp[warp][0] = lo, s_warp[warp][1] = hi;
+  for (int x = tid; x < kBins; x += kThreads) s_hist[x] = 0;
   __syncthreads();
-  uint32_t lo = 0xffffffffu, hi = 0;
 #pragma unroll
   for (int x = 0; x < kWarps; ++x) lo = min(lo, s_warp[x][0]), hi = max(hi, s_warp[x][1]);
+  __syncthreads();
 
   // ---- the least key that is taken: the keys in question are those of [lo, hi], of which `need` are wanted, the greatest first
   while (lo < hi) {
     const int shift = max(0, 32 - __clz(hi - lo) - kBinBits);
-    for (int x = tid; x < kBins; x += kThreads) s_hist[x] = 0;
-    __syncthreads();
     for (int j = tid; j < N; j += kThreads) {
       const uint32_t key = keys[j];
       if (key >= lo && key <= hi) atomicAdd(&s_hist[(key - lo) >> shift], 1u);
     }
     __syncthreads();
     constexpr int kOwn = kBins / kThreads;  // bins of a thread, from the top down
-    uint32_t own[kOwn], mine = 0;
+    uint32_t own[kOwn], own_sum = 0;
 #pragma unroll
-    for (int x = 0; x < kOwn; ++x) own[x] = s_hist[kBins - 1 - (tid * kOwn + x)], mine += own[x];
-    uint32_t sum = mine;
+    for (int x = 0; x < kOwn; ++x) {
+      uint32_t &bin = s_hist[kBins - 1 - (tid * kOwn + x)];
+      own[x] = bin;
+      own_sum += own[x];
+      bin = 0;  // for the next turn
+    }
+    uint32_t sum = own_sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const uint32_t y = __shfl_up_sync(0xffffffffu, sum, o);
@@ -208,7 +292,7 @@ __global__ void __launch_bounds__(kThreads) kv4_select_kernel(const SelectArgs a
     }
     if (lane == 31) s_warp[warp][0] = sum;
     __syncthreads();
-    uint32_t above = sum - mine;
+    uint32_t above = sum - own_sum;
     for (int x = 0; x < warp; ++x) above += s_warp[x][0];
 #pragma unroll
     for (int x = 0; x < kOwn; ++x) {
@@ -218,10 +302,10 @@ __global__ void __launch_bounds__(kThreads) kv4_select_kernel(const SelectArgs a
     __syncthreads();
     lo += s_found[0] << shift;
     need -= s_found[1];
-    const bool all = s_found[2] == need;
+    const bool whole = s_found[2] == need;
     hi = lo + min(hi - lo, (1u << shift) - 1u);
     __syncthreads();
-    if (all) {
+    if (whole) {
       need = 0;
       break;
     }
@@ -254,21 +338,62 @@ __global__ void __launch_bounds__(kThreads) kv4_select_kernel(const SelectArgs a
   }
 }
 
-size_t key_bytes(int64_t T, int32_t H, int64_t max_blocks) {
-  return max_blocks > kSmemKeys ? static_cast<size_t>(T) * static_cast<size_t>(H) * static_cast<size_t>(max_blocks) * 4 : 0;
+// How a call is split: blocks that share a row and head, a power of two, and rows of a launch where their keys lie in the workspace.
+struct Split {
+  int32_t cluster = 1;
+  int64_t rows, stride;
+  bool in_ws;
+  Split(int64_t T, int32_t H, int64_t max_blocks) {
+    const int64_t steps = (max_blocks + kThreads - 1) / kThreads, most = static_cast<int64_t>(sm_count()) * kBlocksOfSm;
+    while (cluster < kMaxCluster && cluster < steps && 2 * cluster * T * H <= most) cluster *= 2;
+    in_ws = max_blocks > kSmemKeys;
+    stride = max_blocks;
+    rows = T;
+    const size_t row = static_cast<size_t>(stride) * static_cast<size_t>(H);
+    if (in_ws && row * T > kMostKeys) rows = static_cast<int64_t>(kMostKeys / row);
+    if (rows < 1) rows = 1;
+  }
+};
+
+void carve_keys(Carve &c, SelectArgs &a, const Split &p, int32_t H) {
+  if (p.in_ws) a.keys = c.take<uint32_t>(static_cast<size_t>(p.rows) * H * p.stride);
 }
 
 template <class T, int D>
-int launch(const SelectArgs &a, cudaStream_t s) {
-  const size_t smem = a.keys ? 0 : static_cast<size_t>(a.max_blocks) * 4;
+int launch(SelectArgs a, const Split &p, cudaStream_t s) {
   constexpr auto kernel = kv4_select_kernel<T, D>;
-  MAPS_TRY(cuda_ok(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemKeys * 4)));
-  launch_pdl(kernel, static_cast<unsigned>(a.T * a.H), kThreads, smem, s, a);
+  static std::atomic<uint64_t> done;  // devices that have been asked for clusters of 16
+  int dev = 0;
+  MAPS_TRY(cuda_ok(cudaGetDevice(&dev)));
+  const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
+  if (p.cluster > 8 && !(done.load(std::memory_order_relaxed) & bit)) {
+    MAPS_TRY(cuda_ok(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1)));
+    done.fetch_or(bit, std::memory_order_relaxed);
+  }
+  a.smem_keys = static_cast<int32_t>(a.max_blocks < kSmemKeys ? a.max_blocks : kSmemKeys);
+  a.cluster = p.cluster;
+  cudaLaunchConfig_t cfg = {};
+  cfg.blockDim = kThreads;
+  cfg.dynamicSmemBytes = static_cast<size_t>(a.smem_keys) * 4;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = p.cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = p.cluster > 1 ? 2 : 1;
+  for (a.row0 = 0; a.row0 < a.T; a.row0 += p.rows) {
+    const int64_t rows = a.T - a.row0 < p.rows ? a.T - a.row0 : p.rows;
+    cfg.gridDim = dim3(static_cast<unsigned>(rows * a.H * p.cluster));
+    MAPS_TRY(cuda_ok(cudaLaunchKernelEx(&cfg, kernel, static_cast<const SelectArgs &>(a))));
+  }
   return launch_ok();
 }
 template <class T>
-int launch_dim(int D, const SelectArgs &a, cudaStream_t s) {
-  return D == 64 ? launch<T, 64>(a, s) : D == 128 ? launch<T, 128>(a, s) : launch<T, 256>(a, s);
+int launch_dim(int D, const SelectArgs &a, const Split &p, cudaStream_t s) {
+  return D == 64 ? launch<T, 64>(a, p, s) : D == 128 ? launch<T, 128>(a, p, s) : launch<T, 256>(a, p, s);
 }
 
 }  // namespace
@@ -278,7 +403,10 @@ extern "C" {
 
 size_t maps_kv4_select_blocks_workspace_size(int64_t T, int32_t H, int64_t max_blocks) {
   using namespace maps;
-  return kCtrlBytes + (T > 0 && H > 0 && max_blocks > 0 ? (key_bytes(T, H, max_blocks) + kAlign - 1) / kAlign * kAlign : 0);
+  Carve c(nullptr);
+  SelectArgs a = {};
+  if (T > 0 && H > 0 && max_blocks > 0) carve_keys(c, a, Split(T, H, max_blocks), H);
+  return c.bytes();
 }
 
 int maps_kv4_select_blocks(int32_t dtype, int32_t B, int64_t T, int32_t Hq, int32_t H, int32_t D, int32_t S, const void *q, int64_t q_row,
@@ -296,11 +424,13 @@ int maps_kv4_select_blocks(int32_t dtype, int32_t B, int64_t T, int32_t Hq, int3
       (n_blocks > 0 && (codes == nullptr || scale == nullptr)) || !aligned(q, 2) || !aligned(codes, 16) || !aligned(scale, 4) ||
       !aligned(qo_off, 8) || !aligned(kv_len, 4) || !aligned(table, 4) || !aligned(blocks, 4) || !aligned(tokens, 4))
     return MAPS_E_INVALID;
-  SelectArgs a = {B, Hq, H, S, T, max_blocks, n_blocks, q, q_row, q_head, qo_off, kv_len, table, codes, scale, first, last, n_list,
-                  blocks, tokens, nullptr, status_word(ws)};
-  if (key_bytes(T, H, max_blocks)) a.keys = reinterpret_cast<uint32_t *>(static_cast<char *>(ws) + kCtrlBytes);
+  SelectArgs a = {B, Hq, H, S, T, max_blocks, n_blocks, q, q_row, q_head, qo_off, kv_len, table, codes, scale, first, last, n_list, blocks, tokens};
+  a.status = status_word(ws);
+  const Split p(T, H, max_blocks < 1 ? 1 : max_blocks);
+  Carve c(ws);
+  carve_keys(c, a, p, H);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  return dtype == MAPS_BF16 ? launch_dim<__nv_bfloat16>(D, a, s) : launch_dim<__half>(D, a, s);
+  return dtype == MAPS_BF16 ? launch_dim<__nv_bfloat16>(D, a, p, s) : launch_dim<__half>(D, a, p, s);
 }
 
 }  // extern "C"
