@@ -7,8 +7,8 @@
 //
 // A block takes a row and KV head, or a cluster of them where there are few: 256 cache blocks each in turn.  Scores become keys, whole
 // numbers in the scores' order, in the shared memory of the cluster's first block, which goes on alone (in the workspace where they
-// are too many).  The least key that is taken is found by histograms of the keys that are still in question, ten bits at a
-// time; then the list is written in order.
+// are too many).  The least key that is taken is found by bisection, up to 16 keys a thread in registers, or for longer rows by
+// histograms of the keys that are still in question, ten bits at a time; then the list is written in order.
 #include <atomic>
 
 #include "kv4.cuh"
@@ -16,12 +16,15 @@
 namespace maps {
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kBinBits = 10, kBins = 1 << kBinBits;
 constexpr int kSmemKeys = 8192;   // of shared memory; longer rows of keys stay in the workspace
-constexpr int kBlocksOfSm = 8;    // blocks of a multiprocessor up to which a row and head is shared out
+constexpr int kThreadsOfSm = 2048;  // of a multiprocessor up to which a row and head is shared out
+constexpr int kWideRow = 2048;      // blocks of a row from which on 512 threads take it, where rows are few
 constexpr int kMaxCluster = 16;
 constexpr size_t kMostKeys = size_t(1) << 26;  // in the workspace: more rows take their turns
+
+template <int kValue>
+struct Int { static constexpr int value = kValue; };
 
 struct SelectArgs {
   int32_t B, Hq, H, S;
@@ -64,6 +67,7 @@ __device__ __forceinline__ uint32_t *of_first_block(uint32_t *p) {  // the same 
 }
 
 // The greatest b with off[b] <= i of b in [0, B], -1 where there is none.  All threads call it.
+template <int kThreads>
 __device__ __forceinline__ int request_of(const int64_t *off, int B, int64_t i) {
   int64_t lo = 0, n = static_cast<int64_t>(B) + 1;
   for (;;) {
@@ -90,8 +94,9 @@ __device__ __forceinline__ void join(int (&acc)[8], int lane) {
   }
 }
 
-template <class T, int D>
-__global__ void __launch_bounds__(kThreads, 3) kv4_select_kernel(const SelectArgs a) {
+template <class T, int D, int kThreads>
+__global__ void __launch_bounds__(kThreads, 768 / kThreads) kv4_select_kernel(const SelectArgs a) {
+  constexpr int kWarps = kThreads / 32;
   constexpr int kLanes = D / 8, kSub = 32 / kLanes;  // lanes of a block's 2 D codes, and blocks of a warp's load
   constexpr int kBatch = 8;                          // loads under way at once; D/8 of them make a step of 32 blocks
   extern __shared__ __align__(16) uint32_t s_keys[];
@@ -99,10 +104,20 @@ __global__ void __launch_bounds__(kThreads, 3) kv4_select_kernel(const SelectArg
   __shared__ uint32_t s_hist[kBins];
   __shared__ uint32_t s_warp[kWarps][2];
   __shared__ uint32_t s_found[3];
+  __shared__ uint32_t s_count[2][kWarps];
+  __shared__ struct { int32_t b, n; int64_t q1; } s_request;
   pdl_prologue();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = static_cast<int>(blockIdx.x) & (a.cluster - 1);
   const int64_t here = blockIdx.x / a.cluster, item = a.row0 * a.H + here, i = a.row0 + here / a.H;
   const int h = static_cast<int>(here % a.H);
+  // the first queries are under way before anything is known of the request
+  constexpr int kHeads = 4;
+  const int group = a.Hq / a.H;
+  const T *q = static_cast<const T *>(a.q) + i * a.q_row + static_cast<int64_t>(h) * group * a.q_head + tid;
+  T y[kHeads];
+#pragma unroll
+  for (int x = 0; x < kHeads; ++x)
+    if (tid < D && x < group) y[x] = q[x * a.q_head];
   // the row's request: the one of its number, where each has one row, else searched for
   int64_t b = i, q1 = 0;
   int32_t n = 0;
@@ -113,9 +128,19 @@ __global__ void __launch_bounds__(kThreads, 3) kv4_select_kernel(const SelectArg
     n = a.len[i];
     found = q0 >= 0 && q0 <= i && i < q1;
   }
-  if (!found) {
-    b = request_of(a.off, a.B, i);
-    if (b < 0 || b == a.B) return;  // no request's
+  if (!found && a.B <= kThreads) {  // every thread looks at one, so that its length comes with it
+    bool mine = false;
+    if (tid < a.B) {
+      const int64_t next = a.off[tid + 1];
+      const int32_t length = a.len[tid];
+      mine = a.off[tid] <= i && i < next;
+      if (mine) s_request.b = tid, s_request.n = length, s_request.q1 = next;
+    }
+    if (!__syncthreads_or(mine)) return;  // no request's
+    b = s_request.b, n = s_request.n, q1 = s_request.q1;
+  } else if (!found) {
+    b = request_of<kThreads>(a.off, a.B, i);
+    if (b < 0 || b == a.B) return;
     q1 = a.off[b + 1];
     n = a.len[b];
   }
@@ -125,27 +150,32 @@ __global__ void __launch_bounds__(kThreads, 3) kv4_select_kernel(const SelectArg
     n = 0;
   }
   const int64_t seen = n - (q1 - i) + 1;  // keys
-  const int32_t nb = n == 0 || seen <= 0 ? 0 : static_cast<int32_t>((seen + a.S - 1) / a.S), count = min(nb, a.n_list);
+  const int32_t nb = n == 0 || seen <= 0 ? 0 : static_cast<int32_t>(static_cast<uint32_t>(seen + a.S - 1) / static_cast<uint32_t>(a.S)), count = min(nb, a.n_list);
   const int32_t N = nb - a.first - a.last;           // blocks in question
   uint32_t need = a.n_list - a.first - a.last;       // of which so many are taken
   const bool all = nb <= a.n_list;
   const int sharers = all || need == 0 ? 1 : min(a.cluster, (N + kThreads - 1) / kThreads);
   if (rank >= sharers) return;  // the cluster's barriers count those that are left
   const int32_t *table = a.table + b * a.max_blocks;
-  if (rank == 0) {
+  // what needs no scores: the ends of the list, and its tokens
+  auto write_ends = [&]() {
     if (tid == 0) a.tokens[item] = nb == 0 ? 0 : static_cast<int32_t>((count - 1) * static_cast<int64_t>(a.S) + seen - (nb - 1) * static_cast<int64_t>(a.S));
-    for (int x = count + tid; x < a.n_list; x += kThreads) out[x] = -1;
-    if (all) {
-      for (int x = tid; x < nb; x += kThreads) out[x] = table[x];
-    } else {
-      for (int x = tid; x < a.first; x += kThreads) out[x] = table[x];
-      for (int x = tid; x < a.last; x += kThreads) out[count - a.last + x] = table[nb - a.last + x];
+    for (int x = tid; x < a.first + a.last; x += kThreads) {
+      const bool front = x < a.first;
+      out[front ? x : x - a.first + count - a.last] = table[front ? x : x - a.first + nb - a.last];
     }
+  };
+  if (all || need == 0) {
+    if (!all) {
+      write_ends();
+      return;
+    }
+    if (tid == 0) a.tokens[item] = static_cast<int32_t>(nb == 0 ? 0 : seen);
+    for (int x = tid; x < a.n_list; x += kThreads) out[x] = x < nb ? table[x] : -1;
+    return;
   }
-  if (all || need == 0) return;
   if (sharers > 1) cluster_arrive();  // this block runs, so its shared memory may be written
-  table += a.first;
-  out += a.first;
+  const int32_t *inner = table + a.first;  // the blocks in question
 
   // ---- the first blocks' codes are under way while the queries' weights are made
   const int l = lane % kLanes, sub = lane / kLanes;
@@ -156,7 +186,7 @@ __global__ void __launch_bounds__(kThreads, 3) kv4_select_kernel(const SelectArg
     block = -1;
     sc = 0.0f;
     if (j >= N) return;
-    block = table[j];
+    block = inner[j];
     if (block < 0 || block >= a.n_blocks) {
       flag_error(a.status, MAPS_E_RANGE);
       block = -1;
@@ -176,16 +206,17 @@ __global__ void __launch_bounds__(kThreads, 3) kv4_select_kernel(const SelectArg
     }
   };
   look_up(first + l * kSub + sub);
-  const int group = a.Hq / a.H;
   float P = 0.0f, Pe = 0.0f, M = 0.0f, Me = 0.0f;
+  auto add = [&](float x) {
+    add_twice(P, Pe, x > 0.0f || x != x ? x : 0.0f);
+    add_twice(M, Me, x < 0.0f || x != x ? x : 0.0f);
+  };
   if (tid < D) {
-    const T *src = static_cast<const T *>(a.q) + i * a.q_row + static_cast<int64_t>(h) * group * a.q_head + tid;
+#pragma unroll
+    for (int x = 0; x < kHeads; ++x)
+      if (x < group) add(Cvt<T>::to(y[x]));
 #pragma unroll 4
-    for (int x = 0; x < group; ++x) {
-      const float y = Cvt<T>::to(src[x * a.q_head]);
-      add_twice(P, Pe, y > 0.0f || y != y ? y : 0.0f);
-      add_twice(M, Me, y < 0.0f || y != y ? y : 0.0f);
-    }
+    for (int x = kHeads; x < group; ++x) add(Cvt<T>::to(q[x * a.q_head]));
     P = __fadd_rn(P, Pe);
     M = __fadd_rn(M, Me);
   }
@@ -242,8 +273,6 @@ __global__ void __launch_bounds__(kThreads, 3) kv4_select_kernel(const SelectArg
     if (j < N) {
       const uint32_t key = no_number || blk < 0 ? 0xfffffffeu : key_of(__fmul_rn(static_cast<float>(part[0]), scale));
       keys[j] = key;
-      lo = min(lo, key);
-      hi = max(hi, key);
     }
   }
   if (sharers > 1) {
@@ -251,12 +280,99 @@ __global__ void __launch_bounds__(kThreads, 3) kv4_select_kernel(const SelectArg
     if (rank > 0) return;
     cluster_wait();
     keys = fits ? s_keys : keys;
-    lo = 0xffffffffu, hi = 0;
-    for (int j = tid; j < N; j += kThreads) {
-      const uint32_t key = fits ? keys[j] : __ldcg(keys + j);
-      lo = min(lo, key);
-      hi = max(hi, key);
+  } else {
+    __syncthreads();
+  }
+  const uint32_t wanted = need;
+  int32_t *inner_out = out + a.first;
+
+  // ---- the least key that is taken, where a thread's keys fit its registers: by bisection, until the right number are above
+  const unsigned below = (1u << lane) - 1u;
+  auto in_registers = [&](auto per) {
+    constexpr int kPer = decltype(per)::value;
+    const int j0 = warp * 32 * kPer + lane;
+    uint32_t key[kPer];
+    int32_t name[kPer];
+#pragma unroll
+    for (int x = 0; x < kPer; ++x) {
+      const int j = j0 + 32 * x;
+      key[x] = j < N ? keys[j] : 0u;  // less than any score's
+      name[x] = j < N ? inner[j] : -1;
     }
+    uint32_t lo = 0xffffffffu, hi = 0;
+#pragma unroll
+    for (int x = 0; x < kPer; ++x) lo = key[x] ? min(lo, key[x]) : lo, hi = max(hi, key[x]);
+    lo = __reduce_min_sync(0xffffffffu, lo);
+    hi = __reduce_max_sync(0xffffffffu, hi);
+    if (lane == 0) s_warp[warp][0] = lo, s_warp[warp][1] = hi;
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < kWarps; ++x) lo = min(lo, s_warp[x][0]), hi = max(hi, s_warp[x][1]);
+    // keys >= lo: `wanted` or more; keys >= hi: `above`, fewer
+    ++hi;
+    uint32_t above = 0, ties = 0;
+    int turn = 0;
+    for (;; turn ^= 1) {
+      if (hi - lo == 1) {
+        ties = wanted - above;
+        lo = hi;
+        break;
+      }
+      const uint32_t mid = lo + (hi - lo) / 2;
+      uint32_t c = 0;
+      if (kPer == 1) {
+        c = __syncthreads_count(key[0] >= mid);
+      } else {
+#pragma unroll
+        for (int x = 0; x < kPer; ++x) c += key[x] >= mid;
+        c = __reduce_add_sync(0xffffffffu, c);
+        if (lane == 0) s_count[turn][warp] = c;
+        __syncthreads();
+        c = 0;
+#pragma unroll
+        for (int x = 0; x < kWarps; ++x) c += s_count[turn][x];
+      }
+      if (c >= wanted) lo = mid;
+      if (c < wanted) hi = mid, above = c;
+      if (c == wanted) break;
+    }
+    // taken: the keys from lo on, and of those one below the first `ties`
+    uint32_t over = 0, same = 0;
+    unsigned overs[kPer], sames[kPer];
+#pragma unroll
+    for (int x = 0; x < kPer; ++x) {
+      overs[x] = __ballot_sync(0xffffffffu, key[x] >= lo);
+      sames[x] = __ballot_sync(0xffffffffu, ties > 0 && key[x] == lo - 1);
+      over += __popc(overs[x]);
+      same += __popc(sames[x]);
+    }
+    __syncthreads();  // everybody has read the last turn's
+    if (lane == 0) s_warp[warp][0] = over, s_warp[warp][1] = same;
+    __syncthreads();
+    over = same = 0;
+#pragma unroll
+    for (int x = 0; x < kWarps; ++x)
+      if (x < warp) over += s_warp[x][0], same += s_warp[x][1];
+#pragma unroll
+    for (int x = 0; x < kPer; ++x) {
+      const uint32_t rank_same = same + __popc(sames[x] & below);
+      const bool tie = sames[x] >> lane & 1u && rank_same < ties;
+      if (overs[x] >> lane & 1u || tie) inner_out[over + __popc(overs[x] & below) + min(rank_same, ties)] = name[x];
+      over += __popc(overs[x]);
+      same += __popc(sames[x]);
+    }
+    write_ends();
+  };
+  if (fits && N <= kThreads) return in_registers(Int<1>{});
+  if (fits && N <= 4 * kThreads) return in_registers(Int<4>{});
+  if (fits && N <= 16 * kThreads) return in_registers(Int<16>{});
+
+  // ---- more keys: by histograms
+  lo = 0xffffffffu, hi = 0;
+  for (int j = tid; j < N; j += kThreads) {
+    const uint32_t key = fits ? keys[j] : __ldcg(keys + j);
+    lo = min(lo, key);
+    hi = max(hi, key);
   }
   lo = __reduce_min_sync(0xffffffffu, lo);
   hi = __reduce_max_sync(0xffffffffu, hi);
@@ -266,8 +382,7 @@ __global__ void __launch_bounds__(kThreads, 3) kv4_select_kernel(const SelectArg
 #pragma unroll
   for (int x = 0; x < kWarps; ++x) lo = min(lo, s_warp[x][0]), hi = max(hi, s_warp[x][1]);
   __syncthreads();
-
-  // ---- the least key that is taken: the keys in question are those of [lo, hi], of which `need` are wanted, the greatest first
+  // the keys in question are those of [lo, hi], of which `need` are wanted, the greatest first
   while (lo < hi) {
     const int shift = max(0, 32 - __clz(hi - lo) - kBinBits);
     for (int j = tid; j < N; j += kThreads) {
@@ -313,7 +428,9 @@ __global__ void __launch_bounds__(kThreads, 3) kv4_select_kernel(const SelectArg
   // taken: keys above hi, with need == 0 those from lo on, else the first `need` of those that are lo
   const uint32_t from = need == 0 ? lo : lo + 1;
 
-  // ---- the list, in the order of the blocks
+  // ---- the list, in the order of the blocks: first their numbers, in shared memory where there is room
+  uint32_t *pick = s_hist;
+  const bool room = wanted <= kBins;
   const int span = (N + kThreads - 1) / kThreads * 32;  // of a warp
   const int j0 = min(warp * span, N), j1 = min(j0 + span, N);
   uint32_t over = 0, same = 0;
@@ -323,18 +440,28 @@ __global__ void __launch_bounds__(kThreads, 3) kv4_select_kernel(const SelectArg
     same += __popc(__ballot_sync(0xffffffffu, j < j1 && key == lo));
   }
   if (lane == 0) s_warp[warp][0] = over, s_warp[warp][1] = same;
+  write_ends();
   __syncthreads();
   over = same = 0;
   for (int x = 0; x < warp; ++x) over += s_warp[x][0], same += s_warp[x][1];
-  const unsigned below = (1u << lane) - 1u;
   for (int j = j0 + lane; j - lane < j1; j += 32) {
     const uint32_t key = j < j1 ? keys[j] : 0;
     const bool is_over = j < j1 && key >= from, is_same = j < j1 && key == lo && need > 0;
     const unsigned overs = __ballot_sync(0xffffffffu, is_over), sames = __ballot_sync(0xffffffffu, is_same);
-    const uint32_t rank = same + __popc(sames & below);
-    if (is_over || (is_same && rank < need)) out[over + __popc(overs & below) + min(rank, need)] = table[j];
+    const uint32_t rank_same = same + __popc(sames & below);
+    if (is_over || (is_same && rank_same < need)) {
+      const uint32_t at = over + __popc(overs & below) + min(rank_same, need);
+      if (room)
+        pick[at] = j;
+      else
+        inner_out[at] = inner[j];
+    }
     over += __popc(overs);
     same += __popc(sames);
+  }
+  if (room) {
+    __syncthreads();
+    for (uint32_t x = tid; x < wanted; x += kThreads) inner_out[x] = inner[pick[x]];
   }
 }
 
@@ -342,9 +469,10 @@ __global__ void __launch_bounds__(kThreads, 3) kv4_select_kernel(const SelectArg
 struct Split {
   int32_t cluster = 1;
   int64_t rows, stride;
-  bool in_ws;
+  bool in_ws, wide;
   Split(int64_t T, int32_t H, int64_t max_blocks) {
-    const int64_t steps = (max_blocks + kThreads - 1) / kThreads, most = static_cast<int64_t>(sm_count()) * kBlocksOfSm;
+    wide = max_blocks > kWideRow && T * H <= sm_count();
+    const int64_t steps = (max_blocks + threads() - 1) / threads(), most = static_cast<int64_t>(sm_count()) * kThreadsOfSm / threads();
     while (cluster < kMaxCluster && cluster < steps && 2 * cluster * T * H <= most) cluster *= 2;
     in_ws = max_blocks > kSmemKeys;
     stride = max_blocks;
@@ -353,15 +481,16 @@ struct Split {
     if (in_ws && row * T > kMostKeys) rows = static_cast<int64_t>(kMostKeys / row);
     if (rows < 1) rows = 1;
   }
+  int threads() const { return wide ? 512 : 256; }
 };
 
 void carve_keys(Carve &c, SelectArgs &a, const Split &p, int32_t H) {
   if (p.in_ws) a.keys = c.take<uint32_t>(static_cast<size_t>(p.rows) * H * p.stride);
 }
 
-template <class T, int D>
+template <class T, int D, int kThreads>
 int launch(SelectArgs a, const Split &p, cudaStream_t s) {
-  constexpr auto kernel = kv4_select_kernel<T, D>;
+  constexpr auto kernel = kv4_select_kernel<T, D, kThreads>;
   static std::atomic<uint64_t> done;  // devices that have been asked for clusters of 16
   int dev = 0;
   MAPS_TRY(cuda_ok(cudaGetDevice(&dev)));
@@ -391,9 +520,9 @@ int launch(SelectArgs a, const Split &p, cudaStream_t s) {
   }
   return launch_ok();
 }
-template <class T>
+template <class T, int kThreads>
 int launch_dim(int D, const SelectArgs &a, const Split &p, cudaStream_t s) {
-  return D == 64 ? launch<T, 64>(a, p, s) : D == 128 ? launch<T, 128>(a, p, s) : launch<T, 256>(a, p, s);
+  return D == 64 ? launch<T, 64, kThreads>(a, p, s) : D == 128 ? launch<T, 128, kThreads>(a, p, s) : launch<T, 256, kThreads>(a, p, s);
 }
 
 }  // namespace
@@ -430,7 +559,8 @@ int maps_kv4_select_blocks(int32_t dtype, int32_t B, int64_t T, int32_t Hq, int3
   Carve c(ws);
   carve_keys(c, a, p, H);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  return dtype == MAPS_BF16 ? launch_dim<__nv_bfloat16>(D, a, p, s) : launch_dim<__half>(D, a, p, s);
+  if (dtype == MAPS_BF16) return p.wide ? launch_dim<__nv_bfloat16, 512>(D, a, p, s) : launch_dim<__nv_bfloat16, 256>(D, a, p, s);
+  return p.wide ? launch_dim<__half, 512>(D, a, p, s) : launch_dim<__half, 256>(D, a, p, s);
 }
 
 }  // extern "C"
