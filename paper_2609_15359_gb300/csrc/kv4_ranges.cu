@@ -148,15 +148,14 @@ __global__ void __launch_bounds__(32 * kWarps, 4) kv4_ranges_kernel(const RangeA
     if (sc > 0.0f) {
 #pragma unroll
       for (int c = 0; c < kOwn; ++c) {
-        // rounded down and up to whole numbers in one step, right or one off, which a remainder of one rounding tells
+        // rounded down and up to whole numbers in one step, right or one off, which exact products tell
         constexpr float kWhole = 12582912.0f;  // 1.5 * 2^23
-        const float fx = __fmaf_rd(lo[c], inv, kWhole), fy = __fmaf_ru(hi[c], inv, kWhole);
-        const float rx = __fmaf_rn(kWhole - fx, sc, lo[c]), ry = __fmaf_rn(kWhole - fy, sc, hi[c]);
+        const float fx = __fmaf_rd(lo[c], inv, kWhole), fy = __fmaf_ru(hi[c], inv, kWhole), wx = fx - kWhole, wy = fy - kWhole;
         int x = __float_as_int(fx), y = __float_as_int(fy);
-        if (rx < 0.0f) --x;
-        if (rx >= sc) ++x;
-        if (ry > 0.0f) ++y;
-        if (ry <= -sc) --y;
+        if (__fmul_rn(wx, sc) > lo[c]) --x;
+        if (__fmul_rn(wx + 1.0f, sc) <= lo[c]) ++x;
+        if (__fmul_rn(wy, sc) < hi[c]) ++y;
+        if (__fmul_rn(wy - 1.0f, sc) >= hi[c]) --y;
         out[0][c / 4] |= (static_cast<uint32_t>(x) & 255u) << (c % 4 * 8);
         out[1][c / 4] |= (static_cast<uint32_t>(y) & 255u) << (c % 4 * 8);
       }
