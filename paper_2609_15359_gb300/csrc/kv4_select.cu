@@ -18,7 +18,7 @@ namespace {
 
 constexpr int kBinBits = 10, kBins = 1 << kBinBits;
 constexpr int kSmemKeys = 8192;   // of shared memory; longer rows of keys stay in the workspace
-constexpr int kThreadsOfSm = 2048;  // of a multiprocessor up to which a row and head is shared out
+constexpr int kThreadsOfSm = 512;  // of a multiprocessor up to which a row and head is shared out
 constexpr int kWideRow = 2048;      // blocks of a row from which on 512 threads take it, where rows are few
 constexpr int kMaxCluster = 16;
 constexpr size_t kMostKeys = size_t(1) << 26;  // in the workspace: more rows take their turns
@@ -95,10 +95,10 @@ __device__ __forceinline__ void join(int (&acc)[8], int lane) {
 }
 
 template <class T, int D, int kThreads>
-__global__ void __launch_bounds__(kThreads, 768 / kThreads) kv4_select_kernel(const SelectArgs a) {
+__global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : 1) kv4_select_kernel(const SelectArgs a) {
   constexpr int kWarps = kThreads / 32;
   constexpr int kLanes = D / 8, kSub = 32 / kLanes;  // lanes of a block's 2 D codes, and blocks of a warp's load
-  constexpr int kBatch = 8;                          // loads under way at once; D/8 of them make a step of 32 blocks
+  constexpr int kBatch = 4;                          // loads under way at once; D/8 of them make a step of 32 blocks
   extern __shared__ __align__(16) uint32_t s_keys[];
   __shared__ __align__(16) int8_t s_w[2 * D];
   __shared__ uint32_t s_hist[kBins];
@@ -118,7 +118,10 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) kv4_select_kernel(co
 #pragma unroll
   for (int x = 0; x < kHeads; ++x)
     if (tid < D && x < group) y[x] = q[x * a.q_head];
-  // the row's request: the one of its number, where each has one row, else searched for
+  // the row's request: the one of its number, where each has one row, else searched for; so the first blocks are looked up at once
+  const int l = lane % kLanes, sub = lane / kLanes, mine = l * kSub + sub;  // of a step's 32 blocks, that whose score this lane ends up with
+  const int start = (rank * kWarps + warp) * 32;
+  int32_t raw = i < a.B && a.first + start + mine < a.max_blocks ? a.table[i * a.max_blocks + a.first + start + mine] : -1;
   int64_t b = i, q1 = 0;
   int32_t n = 0;
   bool found = false;
@@ -129,14 +132,14 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) kv4_select_kernel(co
     found = q0 >= 0 && q0 <= i && i < q1;
   }
   if (!found && a.B <= kThreads) {  // every thread looks at one, so that its length comes with it
-    bool mine = false;
+    bool this_one = false;
     if (tid < a.B) {
       const int64_t next = a.off[tid + 1];
       const int32_t length = a.len[tid];
-      mine = a.off[tid] <= i && i < next;
-      if (mine) s_request.b = tid, s_request.n = length, s_request.q1 = next;
+      this_one = a.off[tid] <= i && i < next;
+      if (this_one) s_request.b = tid, s_request.n = length, s_request.q1 = next;
     }
-    if (!__syncthreads_or(mine)) return;  // no request's
+    if (!__syncthreads_or(this_one)) return;  // no request's
     b = s_request.b, n = s_request.n, q1 = s_request.q1;
   } else if (!found) {
     b = request_of<kThreads>(a.off, a.B, i);
@@ -145,7 +148,7 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) kv4_select_kernel(co
     n = a.len[b];
   }
   int32_t *out = a.blocks + item * a.n_list;
-  if (q1 > a.T || i >= q1 || n < 0 || n > 0x7fffffff - 1023 || n > a.max_blocks * a.S) {
+  if (q1 > a.T || i >= q1 || n < 0 || n > 0x7fffffff - 1023 || n > a.max_blocks * a.S || (n > 0 && a.n_blocks == 0)) {
     if (tid == 0) flag_error(a.status, MAPS_E_RANGE);
     n = 0;
   }
@@ -178,34 +181,30 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) kv4_select_kernel(co
   const int32_t *inner = table + a.first;  // the blocks in question
 
   // ---- the first blocks' codes are under way while the queries' weights are made
-  const int l = lane % kLanes, sub = lane / kLanes;
-  const int first = (rank * kWarps + warp) * 32, stride = sharers * kThreads;
-  int32_t block = -1;
+  const int stride = sharers * kThreads;
+  int32_t block = 0;
   float sc = 0.0f;
-  auto look_up = [&](int j) {  // the block whose score this lane ends up with
-    block = -1;
-    sc = 0.0f;
-    if (j >= N) return;
-    block = inner[j];
-    if (block < 0 || block >= a.n_blocks) {
-      flag_error(a.status, MAPS_E_RANGE);
-      block = -1;
-    } else {
-      sc = a.scale[static_cast<int64_t>(block) * a.H + h];
-    }
+  auto ask = [&](int j) { raw = j < N ? inner[j] : -1; };
+  auto settle = [&](int j) {  // places past the end stand for block 0, whose score nobody wants
+    const bool good = raw >= 0 && raw < a.n_blocks;
+    block = good ? raw : 0;
+    sc = NAN;
+    if (j < N && !good) flag_error(a.status, MAPS_E_RANGE);
+    if (good) sc = a.scale[static_cast<int64_t>(block) * a.H + h];
   };
   int4 c[kBatch];
-  const int8_t *mine = a.codes + static_cast<int64_t>(h) * (2 * D) + 16 * l;
-  const int64_t block_bytes = static_cast<int64_t>(a.H) * (2 * D);
+  const int8_t *codes = a.codes + static_cast<int64_t>(h) * (2 * D) + 16 * l;
+  const uint32_t block_bytes = static_cast<uint32_t>(a.H) * (2 * D);
   auto fetch = [&](int k0) {
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k) {
-      const int32_t blk = __shfl_sync(0xffffffffu, block, sub * kLanes + k0 + k);
-      c[k] = make_int4(0, 0, 0, 0);
-      if (blk >= 0) c[k] = *reinterpret_cast<const int4 *>(mine + blk * block_bytes);
-    }
+    for (int k = 0; k < kBatch; ++k)
+      c[k] = *reinterpret_cast<const int4 *>(codes + static_cast<uint64_t>(block_bytes) * static_cast<uint32_t>(__shfl_sync(0xffffffffu, block, sub * kLanes + k0 + k)));
   };
-  look_up(first + l * kSub + sub);
+  if (!found) ask(start + mine);
+  if (start + mine >= N) raw = -1;
+  settle(start + mine);
+  fetch(0);
+  ask(start + stride + mine);
   float P = 0.0f, Pe = 0.0f, M = 0.0f, Me = 0.0f;
   auto add = [&](float x) {
     add_twice(P, Pe, x > 0.0f || x != x ? x : 0.0f);
@@ -220,7 +219,6 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) kv4_select_kernel(co
     P = __fadd_rn(P, Pe);
     M = __fadd_rn(M, Me);
   }
-  fetch(0);
   // NaN's bits are above infinity's
   const uint32_t most = __reduce_max_sync(0xffffffffu, max(__float_as_uint(P) & 0x7fffffffu, __float_as_uint(M) & 0x7fffffffu));
   if (lane == 0) s_warp[warp][0] = most;
@@ -243,23 +241,27 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) kv4_select_kernel(co
   uint32_t lo = 0xffffffffu, hi = 0;
   const int4 w = *reinterpret_cast<const int4 *>(s_w + 16 * l);
   if (sharers > 1) cluster_wait();
-  for (int j0 = first; j0 < N; j0 += stride) {
-    // a step's D/8 loads eight at a time: their sums over 8 lanes, lane x keeping that of load x; then over the rest of a block's lanes
+  for (int j0 = start; j0 < N; j0 += stride) {
+    // a step's D/8 loads, their sums eight at a time joined over 8 lanes, lane x keeping that of load x; then over the rest of a block's lanes
     int part[kLanes / 8];
 #pragma unroll
     for (int k0 = 0; k0 < kLanes; k0 += 8) {
-      if (k0 > 0) fetch(k0);
       int acc[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) acc[k] = __dp4a(c[k].x, w.x, __dp4a(c[k].y, w.y, __dp4a(c[k].z, w.z, __dp4a(c[k].w, w.w, 0))));
+      for (int k1 = 0; k1 < 8; k1 += kBatch) {
+        if (k0 + k1 > 0) fetch(k0 + k1);
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) acc[k1 + k] = __dp4a(c[k].x, w.x, __dp4a(c[k].y, w.y, __dp4a(c[k].z, w.z, __dp4a(c[k].w, w.w, 0))));
+      }
       join<4>(acc, lane);
       part[k0 / 8] = acc[0];
     }
-    const int32_t blk = block;
     const float scale = sc;
+    const int j = j0 + mine;
     if (j0 + stride < N) {
-      look_up(j0 + stride + l * kSub + sub);
+      settle(j + stride);
       fetch(0);
+      ask(j + 2 * stride);
     }
 #pragma unroll
     for (int o = kLanes / 2; o >= 8; o >>= 1) {
@@ -269,11 +271,7 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) kv4_select_kernel(co
         part[k] = keep + __shfl_xor_sync(0xffffffffu, send, o);
       }
     }
-    const int j = j0 + l * kSub + sub;
-    if (j < N) {
-      const uint32_t key = no_number || blk < 0 ? 0xfffffffeu : key_of(__fmul_rn(static_cast<float>(part[0]), scale));
-      keys[j] = key;
-    }
+    if (j < N) keys[j] = no_number ? 0xfffffffeu : key_of(__fmul_rn(static_cast<float>(part[0]), scale));
   }
   if (sharers > 1) {
     cluster_arrive();
@@ -308,7 +306,8 @@ __global__ void __launch_bounds__(kThreads, 768 / kThreads) kv4_select_kernel(co
     __syncthreads();
 #pragma unroll
     for (int x = 0; x < kWarps; ++x) lo = min(lo, s_warp[x][0]), hi = max(hi, s_warp[x][1]);
-    // keys >= lo: `wanted` or more; keys >= hi: `above`, fewer
+    // Keys >= lo: `wanted` or more; keys >= hi: `above`, fewer.  (A place between them guessed from the counts took more turns, and
+    // longer ones: 128 requests 27 us for 23.)
     ++hi;
     uint32_t above = 0, ties = 0;
     int turn = 0;
