@@ -704,6 +704,7 @@ int maps_kv4_append_rotated(int32_t dtype, int64_t T, int32_t Hq, int32_t H, int
  *                       may be in a list twice, and counts twice.  tokens in [0, n_list *
  *                       S], 0 giving zeros; with a negative number a row's heads are
  *                       neither read nor written, as for rows that no request has.
+ *   ws                  maps_kv4_workspace_size() bytes.
  *   all others          as for maps_kv4_attention.
  * ---------------------------------------------------------------------- */
 int maps_kv4_block_ranges(int32_t B, int32_t H, int32_t D, int32_t S, const int32_t *held,
@@ -718,7 +719,6 @@ int maps_kv4_select_blocks(int32_t dtype, int32_t B, int64_t T, int32_t Hq, int3
                            int64_t n_blocks, int32_t first, int32_t last, int32_t n_list,
                            int32_t *blocks, int32_t *tokens, void *ws, size_t ws_bytes,
                            void *stream);
-size_t maps_kv4_attention_blocks_workspace_size(int64_t T, int32_t Hq, int32_t H, int32_t D);
 int maps_kv4_attention_blocks(int32_t dtype, int64_t T, int32_t Hq, int32_t H, int32_t D, int32_t S,
                               const void *q, int64_t q_row, int64_t q_head, const int32_t *blocks,
                               const int32_t *tokens, int64_t n_list, const void *cache,

@@ -115,7 +115,6 @@ def _load():
         "maps_kv4_select_blocks_workspace_size": ([i64, i32, i64], sz),
         "maps_kv4_select_blocks": ([i32, i32, i64, i32, i32, i32, i32, vp, i64, i64, vp, vp, vp, i64, vp, vp,
                                     i64, i32, i32, i32, vp, vp, vp, sz, vp], ctypes.c_int),
-        "maps_kv4_attention_blocks_workspace_size": ([i64, i32, i32, i32], sz),
         "maps_kv4_attention_blocks": ([i32, i64, i32, i32, i32, i32, vp, i64, i64, vp, vp, i64, vp, i64, f32,
                                        vp, i64, i64, vp, vp, sz, vp], ctypes.c_int),
         "maps_kv4_attention_workspace_size": ([i32, i64, i32, i32, i32], sz),
@@ -144,7 +143,7 @@ EXPORTS = ("maps_version", "maps_last_cuda_error", "maps_check", "maps_set_dispa
            "maps_kv4_workspace_size", "maps_kv4_append", "maps_kv4_read",
            "maps_kv4_attention_workspace_size", "maps_kv4_attention", "maps_kv4_append_rotated",
            "maps_kv4_block_ranges", "maps_kv4_select_blocks_workspace_size", "maps_kv4_select_blocks",
-           "maps_kv4_attention_blocks_workspace_size", "maps_kv4_attention_blocks")
+           "maps_kv4_attention_blocks")
 
 
 # The handle of the current stream without a stream object, which costs 3.2 us, a third of a call.  PyTorch promises
@@ -555,7 +554,7 @@ def maps_kv4_attention_blocks(q, blocks, tokens, cache, S: int, sm_scale: float,
         raise ValueError("q and out are [T, Hq, D], blocks [T, H, n_list], tokens [T, H]")
     if lse_out is not None and tuple(lse_out.shape) != (T, Hq):
         raise ValueError("lse_out is [T, Hq]")
-    ws, on = _scratch(ws, _need(torch.cuda.current_device(), "maps_kv4_attention_blocks_workspace_size", T, Hq, H, D), stream)
+    ws, on = _scratch(ws, _need(None, "maps_kv4_workspace_size"), stream)
     return lib.maps_kv4_attention_blocks(_dtype(q), T, Hq, H, D, S, *_rows(q), _ptr(blocks, torch.int32),
                                          _ptr(tokens, torch.int32), blocks.shape[2], _kv4(cache, S, D, H),
                                          cache.shape[0], float(sm_scale), *_rows(out, q.dtype),
