@@ -702,8 +702,8 @@ int maps_kv4_append_rotated(int32_t dtype, int64_t T, int32_t Hq, int32_t H, int
  *   T                   rows (<= 2^30, T * Hq <= 2^31 - 1,024).
  *   blocks, tokens, n_list   as maps_kv4_select_blocks leaves them, or any others; a block
  *                       may be in a list twice, and counts twice.  tokens in [0, n_list *
- *                       S], 0 giving zeros; with a negative number a row's heads are
- *                       neither read nor written, as for rows that no request has.
+ *                       S], 0 giving zeros; with a negative number a row and KV
+ *                       head is left as it is, as rows that no request has are.
  *   ws                  maps_kv4_workspace_size() bytes.
  *   all others          as for maps_kv4_attention.
  * ---------------------------------------------------------------------- */

@@ -4,22 +4,24 @@
 // steps, the running maximum and sum of the softmax, weights relative to the largest weight times scale.
 //
 // Split.  Lists have much the same length, so no run crosses from one to the next: four warps have an item, which is a row, KV head
-// and tile of 8 or 16 of the head's query heads, and share its tokens in groups of 16; two or three items pass on a multiprocessor side by
-// side.  Where items are few, a cluster of up to 16 such blocks shares one.  Parts meet in shared memory, the block's and
-// then the cluster's, in the order of the list: no workspace, and results that depend on sizes and lengths alone.
+// and tile of 8 or 16 of the head's query heads, and take its units of 32 to 64 tokens in turn; two to four items pass on a multiprocessor
+// side by side.  Where items are few, and for the last ones that do not fill the device, a cluster of such blocks shares one.  Parts meet
+// in shared memory, the block's and then the cluster's, in the order of the warps: no workspace, and results that depend on sizes and
+// lengths alone.
 #include "kv4_attention_products.cuh"
 
 namespace maps {
 namespace {
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
-constexpr int kMaxCluster = 16;
+constexpr int kMaxCluster = 8;
 
 struct ListArgs {
   int32_t Hq, H, group, tiles;  // query heads to a KV head, and tiles of them
   int32_t block_groups, block_shift;  // groups of a block, and their logarithm where they are a power of two, else -1
   int64_t n_list, n_blocks, block_bytes;
-  int32_t S, wide, cluster;
+  int32_t S, wide;
+  uint32_t single, cluster;  // items of one block each, the first; of a cluster's blocks, the rest
   const void *q;
   int64_t q_row, q_head, o_row, o_head;
   const int32_t *blocks, *tokens;
@@ -34,12 +36,12 @@ template <int D, int NT>
 struct ListShape {
   static constexpr int kRows = 8 * NT;  // query rows of a tile
   // Groups of 16 tokens in a unit, which shares the row maxima, as in the form for few queries.
-  static constexpr int kGroups = D == 256 ? 2 : D == 64 && NT == 1 ? 6 : 3;
+  static constexpr int kGroups = D == 256 ? 2 : NT == 1 ? 4 : 3;
   static constexpr int kTok = kGroups * kGroup;
   static constexpr int kBytes = kGroups * kv4_group_bytes(D);  // of a stage
   static constexpr int kStages = D == 64 && NT == 2 ? 4 : 2;
   static constexpr int kPart = kRows * D + 2 * kRows;  // floats of a part: sums, maxima, totals
-  static constexpr int kBlocks = NT == 2 || D == 256 ? 2 : 3;  // of a multiprocessor
+  static constexpr int kBlocks = NT == 2 || D == 256 ? 2 : D == 64 ? 4 : 3;  // of a multiprocessor
   static constexpr size_t kSmem = static_cast<size_t>(kWarps) * kStages * kBytes + kPart * 4 + kWarps * kStages * 8;
   static_assert(kPart * 4 <= kStages * kBytes, "a warp's part lies in its ring");
 };
@@ -67,16 +69,45 @@ __global__ void __launch_bounds__(kThreads, ListShape<D, NT>::kBlocks) attn_list
   __syncwarp();
   pdl_prologue();
 
-  const uint32_t item = blockIdx.x / a.cluster, rank = blockIdx.x % a.cluster, list = item / a.tiles;
+  const bool shared = blockIdx.x >= a.single;
+  const uint32_t past = blockIdx.x - a.single, cluster = shared ? a.cluster : 1, rank = shared ? past % a.cluster : 0;
+  const uint32_t item = shared ? a.single + past / a.cluster : blockIdx.x, list = item / a.tiles;
   const int tile = static_cast<int>(item - list * a.tiles), h = static_cast<int>(list % a.H);
   const int64_t i = list / a.H;
+  const int head0 = h * a.group + tile * Sh::kRows, rows = min(Sh::kRows, a.group - tile * Sh::kRows);  // the tile's query heads
+  // Worker w has the units w, w + workers, ...: so its first blocks are looked up, and the queries are under way, before the list's length is known.
+  const int32_t workers = static_cast<int32_t>(cluster) * kWarps, me = static_cast<int32_t>(rank) * kWarps + warp;
+  const int32_t *blocks = a.blocks + static_cast<int64_t>(list) * a.n_list;
+  int32_t ahead = me * Sh::kGroups + lane;  // the group that this lane moves next
+  int32_t block = -1, place = 0;
+  auto fetch = [&]() {
+    const int32_t page = a.block_shift >= 0 ? ahead >> a.block_shift : ahead / a.block_groups;
+    place = ahead - page * a.block_groups;
+    if (lane < Sh::kGroups && page < a.n_list) block = blocks[page];
+  };
+  fetch();
+  uint4 raw[NT][kWords];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int R = nt * 8 + g;
+    const T *src = static_cast<const T *>(a.q) + i * a.q_row + (head0 + min(R, rows - 1)) * a.q_head + t * (D / 4);
+#pragma unroll
+    for (int x = 0; x < kWords; ++x) {
+      if (a.wide) {
+        raw[nt][x] = *reinterpret_cast<const uint4 *>(src + 8 * x);
+      } else {
+        T *z = reinterpret_cast<T *>(&raw[nt][x]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[e] = src[8 * x + e];
+      }
+    }
+  }
   int32_t n = a.tokens[list];
   if (n < 0) return;  // nobody's row
   if (n > a.n_list * a.S) {
     if (tid == 0) flag_error(a.status, MAPS_E_RANGE);
     n = 0;
   }
-  const int head0 = h * a.group + tile * Sh::kRows, rows = min(Sh::kRows, a.group - tile * Sh::kRows);  // the tile's query heads
   T *out = static_cast<T *>(a.out) + i * a.o_row + head0 * a.o_head;
   float *lse = a.lse ? a.lse + i * a.Hq + head0 : nullptr;
   auto put = [&](T *dst, const auto &y) {
@@ -100,21 +131,11 @@ __global__ void __launch_bounds__(kThreads, ListShape<D, NT>::kBlocks) attn_list
     if (lse && tid < rows) lse[tid] = -INFINITY;
     return;
   }
-  // ---- this warp's groups of 16 tokens
-  const int32_t all = (n + kGroup - 1) / kGroup, workers = a.cluster * kWarps, me = static_cast<int32_t>(rank) * kWarps + warp;
-  const int32_t per = all / workers, more = all % workers;
-  const int32_t begin = me * per + min(me, more), end = begin + per + (me < more ? 1 : 0);
-  const int32_t *blocks = a.blocks + static_cast<int64_t>(list) * a.n_list;
+  // ---- this warp's units
+  const int32_t groups = (n + kGroup - 1) / kGroup, all = (groups + Sh::kGroups - 1) / Sh::kGroups, units = all > me ? (all - me + workers - 1) / workers : 0;
   const uint8_t *cache = a.cache + static_cast<int64_t>(h) * a.block_groups * kv4_group_bytes(D);
-  int32_t ahead = begin + lane;  // the group that this lane moves next
-  int32_t block = -1, place = 0;
-  auto fetch = [&]() {
-    const int32_t page = a.block_shift >= 0 ? ahead >> a.block_shift : ahead / a.block_groups;
-    place = ahead - page * a.block_groups;
-    if (lane < Sh::kGroups && ahead < end) block = blocks[page];
-  };
   auto issue = [&](int stage) {
-    const bool mine = lane < Sh::kGroups && ahead < end, good = mine && block >= 0 && block < a.n_blocks;
+    const bool mine = lane < Sh::kGroups && ahead < groups, good = mine && block >= 0 && block < a.n_blocks;
     if (mine && !good) flag_error(a.status, MAPS_E_RANGE);
     const uint32_t count = __popc(__ballot_sync(0xffffffffu, good));
     if (lane == 0) bar_expect(bar32 + 8 * stage, count * kv4_group_bytes(D));
@@ -122,30 +143,12 @@ __global__ void __launch_bounds__(kThreads, ListShape<D, NT>::kBlocks) attn_list
     if (good)
       bulk_load(ring32 + stage * Sh::kBytes + lane * kv4_group_bytes(D), cache + (block * a.block_bytes + place * static_cast<int64_t>(kv4_group_bytes(D))),
                 kv4_group_bytes(D), bar32 + 8 * stage);
-    ahead += Sh::kGroups;
-    fetch();
+    ahead += workers * Sh::kGroups;
+    if (ahead < groups) fetch();
   };
-  fetch();
 
   // ---- the queries, as the columns of the first product
   const float sl2 = a.scale * 1.4426950408889634f, k_sign = a.scale < 0.0f ? -1.0f : 1.0f, k_unit = k_sign * kEven;
-  uint4 raw[NT][kWords];
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const int R = nt * 8 + g;
-    const T *src = static_cast<const T *>(a.q) + i * a.q_row + (head0 + min(R, rows - 1)) * a.q_head + t * (D / 4);
-#pragma unroll
-    for (int x = 0; x < kWords; ++x) {
-      if (a.wide) {
-        raw[nt][x] = *reinterpret_cast<const uint4 *>(src + 8 * x);
-      } else {
-        T *z = reinterpret_cast<T *>(&raw[nt][x]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) z[e] = src[8 * x + e];
-      }
-    }
-  }
-  const int32_t units = (end - begin + Sh::kGroups - 1) / Sh::kGroups;
 #pragma unroll
   for (int s = 0; s < Sh::kStages; ++s)
     if (s < units) issue(s);
@@ -202,7 +205,6 @@ __global__ void __launch_bounds__(kThreads, ListShape<D, NT>::kBlocks) attn_list
 
   int stage = 0;
   uint32_t parity = 0;
-  const int32_t limit = min(n, end * kGroup);  // of this warp's tokens
   for (int32_t u = 0; u < units; ++u) {
     if (!warp_wait(bar32 + 8 * stage, parity)) {
       if (lane == 0) flag_error(a.status, MAPS_E_TIMEOUT);
@@ -210,9 +212,9 @@ __global__ void __launch_bounds__(kThreads, ListShape<D, NT>::kBlocks) attn_list
       break;
     }
     const uint8_t *buf = ring + stage * Sh::kBytes;
-    const int32_t tok0 = (begin + u * Sh::kGroups) * kGroup;
+    const int32_t tok0 = (me + u * workers) * Sh::kTok;
     auto unit_sums = [&](auto every) {
-      constexpr bool kEvery = decltype(every)::value;  // every place holds a token of this warp's
+      constexpr bool kEvery = decltype(every)::value;  // every place holds a token
       // ---- scores, up to a row's factor: 16 tokens x 8 rows, depth D
       float s[Sh::kGroups][NT][4];
       float vs[Sh::kGroups][2];
@@ -253,7 +255,7 @@ __global__ void __launch_bounds__(kThreads, ListShape<D, NT>::kBlocks) attn_list
           const float2 v = kv4_param(par[16 + g + 8 * half]);
           vs[gr][half] = v.x;
           const float ks = p.x * k_unit, kz = p.y * k_sign, ls = fmaxf(lg2(fmaxf(v.x, fabsf(v.y) * kLeastScale)), kMinLog);
-          const bool out_of = !kEvery && tok0 + gr * kGroup + g + 8 * half >= limit;
+          const bool out_of = !kEvery && tok0 + gr * kGroup + g + 8 * half >= n;
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -307,7 +309,7 @@ __global__ void __launch_bounds__(kThreads, ListShape<D, NT>::kBlocks) attn_list
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           const float vz = fmaf(Value<T>::kCentre, vs[gr][half], kv4_param(par[g + 8 * half]).y);
-          const bool out_of = !kEvery && tok0 + gr * kGroup + g + 8 * half >= limit;  // its weight is 0, and its scale, whatever it is, stays out
+          const bool out_of = !kEvery && tok0 + gr * kGroup + g + 8 * half >= n;  // its weight is 0, and its scale, whatever it is, stays out
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
             float ps[2];
@@ -344,7 +346,7 @@ __global__ void __launch_bounds__(kThreads, ListShape<D, NT>::kBlocks) attn_list
         }
       }
     };
-    if (tok0 + Sh::kTok <= limit)
+    if (tok0 + Sh::kTok <= n)
       unit_sums(Yes{});
     else
       unit_sums(No{});
@@ -413,18 +415,18 @@ __global__ void __launch_bounds__(kThreads, ListShape<D, NT>::kBlocks) attn_list
   for (int x = 4 * tid; x < Sh::kRows * D; x += 4 * kThreads) {
     const int R = x / D, d = x % D;
     const Sum<4> s = join(R, d, kWarps, [&](int k) { return reinterpret_cast<const float *>(smem + k * Sh::kStages * Sh::kBytes); });
-    if (a.cluster == 1) {
+    if (cluster == 1) {
       write(R, d, s);
     } else {
       *reinterpret_cast<float4 *>(joined + in_part<D>(R, d)) = *reinterpret_cast<const float4 *>(s.num);
       if (d == 0) joined[Sh::kRows * D + R] = s.top, joined[Sh::kRows * D + Sh::kRows + R] = s.den;
     }
   }
-  if (a.cluster == 1) return;
+  if (cluster == 1) return;
   cluster_arrive();
   cluster_wait();
-  for (int x = 4 * (tid * a.cluster + static_cast<int>(rank)); x < Sh::kRows * D; x += 4 * kThreads * a.cluster)
-    write(x / D, x % D, join(x / D, x % D, a.cluster, [&](int k) { return of_block(joined, k); }));
+  for (int x = 4 * static_cast<int>(tid * cluster + rank); x < Sh::kRows * D; x += 4 * kThreads * static_cast<int>(cluster))
+    write(x / D, x % D, join(x / D, x % D, static_cast<int>(cluster), [&](int k) { return of_block(joined, k); }));
   cluster_arrive();  // nobody leaves before the others have read
   cluster_wait();
 }
@@ -436,19 +438,15 @@ int launch(ListArgs a, int64_t T_, cudaStream_t s) {
   MAPS_TRY(allow_smem<kernel>(Sh::kSmem));
   a.tiles = (a.group + Sh::kRows - 1) / Sh::kRows;
   const int64_t items = T_ * a.H * a.tiles, room = static_cast<int64_t>(sm_count()) * Sh::kBlocks, groups = a.n_list * a.block_groups;
-  int32_t cluster = 1;
-  while (cluster < kMaxCluster && 2 * cluster * items <= room && 2 * cluster * kWarps <= groups) cluster *= 2;
-  static std::atomic<uint64_t> done;  // devices that have been asked for clusters of 16
-  int dev = 0;
-  MAPS_TRY(cuda_ok(cudaGetDevice(&dev)));
-  const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
-  if (cluster > 8 && !(done.load(std::memory_order_relaxed) & bit)) {
-    MAPS_TRY(cuda_ok(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1)));
-    done.fetch_or(bit, std::memory_order_relaxed);
-  }
+  // what does not fill the device once more is shared out
+  int64_t single = items / room * room;
+  uint32_t cluster = 1;
+  while (cluster < kMaxCluster && 2 * cluster * (items - single) <= room && 2 * cluster * kWarps <= groups) cluster *= 2;
+  single = cluster == 1 ? items : single / cluster * cluster;
   a.cluster = cluster;
+  a.single = static_cast<uint32_t>(single);
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(items * cluster));
+  cfg.gridDim = dim3(static_cast<unsigned>(single + (items - single) * cluster));
   cfg.blockDim = kThreads;
   cfg.dynamicSmemBytes = Sh::kSmem;
   cfg.stream = s;
