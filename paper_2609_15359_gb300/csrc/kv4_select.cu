@@ -19,6 +19,7 @@ namespace {
 constexpr int kBinBits = 10, kBins = 1 << kBinBits;
 constexpr int kSmemKeys = 8192;   // of shared memory; longer rows of keys stay in the workspace
 constexpr int kThreadsOfSm = 512;  // of a multiprocessor up to which a row and head is shared out
+constexpr int kNarrowRows = 4;      // rows and heads for each multiprocessor from which on 128 threads take one, so that more are under way
 constexpr int kWideRow = 2048;      // blocks of a row from which on 512 threads take it, where rows are few
 constexpr int kMaxCluster = 16;
 constexpr size_t kMostKeys = size_t(1) << 26;  // in the workspace: more rows take their turns
@@ -95,7 +96,7 @@ __device__ __forceinline__ void join(int (&acc)[8], int lane) {
 }
 
 template <class T, int D, int kThreads>
-__global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : 1) kv4_select_kernel(const SelectArgs a) {
+__global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : kThreads == 256 ? 4 : 6) kv4_select_kernel(const SelectArgs a) {
   constexpr int kWarps = kThreads / 32;
   constexpr int kLanes = D / 8, kSub = 32 / kLanes;  // lanes of a block's 2 D codes, and blocks of a warp's load
   constexpr int kBatch = 4;                          // loads under way at once; D/8 of them make a step of 32 blocks
@@ -111,13 +112,15 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : 1) kv4_select_
   const int64_t here = blockIdx.x / a.cluster, item = a.row0 * a.H + here, i = a.row0 + here / a.H;
   const int h = static_cast<int>(here % a.H);
   // the first queries are under way before anything is known of the request
-  constexpr int kHeads = 4;
+  constexpr int kHeads = 4, kOwnCh = (D + kThreads - 1) / kThreads;  // channels of a thread
   const int group = a.Hq / a.H;
-  const T *q = static_cast<const T *>(a.q) + i * a.q_row + static_cast<int64_t>(h) * group * a.q_head + tid;
-  T y[kHeads];
+  const T *q = static_cast<const T *>(a.q) + i * a.q_row + static_cast<int64_t>(h) * group * a.q_head;
+  T y[kOwnCh][kHeads];
 #pragma unroll
-  for (int x = 0; x < kHeads; ++x)
-    if (tid < D && x < group) y[x] = q[x * a.q_head];
+  for (int c = 0; c < kOwnCh; ++c)
+#pragma unroll
+    for (int x = 0; x < kHeads; ++x)
+      if (tid + c * kThreads < D && x < group) y[c][x] = q[x * a.q_head + tid + c * kThreads];
   // the row's request: the one of its number, where each has one row, else searched for; so the first blocks are looked up at once
   const int l = lane % kLanes, sub = lane / kLanes, mine = l * kSub + sub;  // of a step's 32 blocks, that whose score this lane ends up with
   const int start = (rank * kWarps + warp) * 32;
@@ -205,22 +208,28 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : 1) kv4_select_
   settle(start + mine);
   fetch(0);
   ask(start + stride + mine);
-  float P = 0.0f, Pe = 0.0f, M = 0.0f, Me = 0.0f;
-  auto add = [&](float x) {
-    add_twice(P, Pe, x > 0.0f || x != x ? x : 0.0f);
-    add_twice(M, Me, x < 0.0f || x != x ? x : 0.0f);
-  };
-  if (tid < D) {
+  float P[kOwnCh], M[kOwnCh];
+  uint32_t most = 0;  // NaN's bits are above infinity's
 #pragma unroll
-    for (int x = 0; x < kHeads; ++x)
-      if (x < group) add(Cvt<T>::to(y[x]));
+  for (int c = 0; c < kOwnCh; ++c) {
+    float Pe = 0.0f, Me = 0.0f;
+    P[c] = M[c] = 0.0f;
+    auto add = [&](float x) {
+      add_twice(P[c], Pe, x > 0.0f || x != x ? x : 0.0f);
+      add_twice(M[c], Me, x < 0.0f || x != x ? x : 0.0f);
+    };
+    if (tid + c * kThreads < D) {
+#pragma unroll
+      for (int x = 0; x < kHeads; ++x)
+        if (x < group) add(Cvt<T>::to(y[c][x]));
 #pragma unroll 4
-    for (int x = kHeads; x < group; ++x) add(Cvt<T>::to(q[x * a.q_head]));
-    P = __fadd_rn(P, Pe);
-    M = __fadd_rn(M, Me);
+      for (int x = kHeads; x < group; ++x) add(Cvt<T>::to(q[x * a.q_head + tid + c * kThreads]));
+      P[c] = __fadd_rn(P[c], Pe);
+      M[c] = __fadd_rn(M[c], Me);
+    }
+    most = max(most, max(__float_as_uint(P[c]) & 0x7fffffffu, __float_as_uint(M[c]) & 0x7fffffffu));
   }
-  // NaN's bits are above infinity's
-  const uint32_t most = __reduce_max_sync(0xffffffffu, max(__float_as_uint(P) & 0x7fffffffu, __float_as_uint(M) & 0x7fffffffu));
+  most = __reduce_max_sync(0xffffffffu, most);
   if (lane == 0) s_warp[warp][0] = most;
   __syncthreads();
   uint32_t top = 0;
@@ -229,9 +238,13 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : 1) kv4_select_
   const float step = __fmul_rn(__uint_as_float(top), 1.0f / 127.0f);
   const bool no_number = !(step < INFINITY);
   const float inv = step >= 1.17549435e-38f ? __fdiv_rn(1.0f, step) : 0.0f;
-  if (tid < D && !no_number) {
-    s_w[tid] = static_cast<int8_t>(fminf(fmaxf(rintf(__fmul_rn(M, inv)), -127.0f), 127.0f));
-    s_w[D + tid] = static_cast<int8_t>(fminf(fmaxf(rintf(__fmul_rn(P, inv)), -127.0f), 127.0f));
+#pragma unroll
+  for (int c = 0; c < kOwnCh; ++c) {
+    const int d = tid + c * kThreads;
+    if (d < D && !no_number) {
+      s_w[d] = static_cast<int8_t>(fminf(fmaxf(rintf(__fmul_rn(M[c], inv)), -127.0f), 127.0f));
+      s_w[D + d] = static_cast<int8_t>(fminf(fmaxf(rintf(__fmul_rn(P[c], inv)), -127.0f), 127.0f));
+    }
   }
   __syncthreads();
 
@@ -363,6 +376,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : 1) kv4_select_
     write_ends();
   };
   if (fits && N <= kThreads) return in_registers(Int<1>{});
+  if (fits && N <= 2 * kThreads) return in_registers(Int<2>{});
   if (fits && N <= 4 * kThreads) return in_registers(Int<4>{});
   if (fits && N <= 16 * kThreads) return in_registers(Int<16>{});
 
@@ -468,10 +482,11 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 4 : 1) kv4_select_
 struct Split {
   int32_t cluster = 1;
   int64_t rows, stride;
-  bool in_ws, wide;
+  bool in_ws;
+  int32_t threads;
   Split(int64_t T, int32_t H, int64_t max_blocks) {
-    wide = max_blocks > kWideRow && T * H <= sm_count();
-    const int64_t steps = (max_blocks + threads() - 1) / threads(), most = static_cast<int64_t>(sm_count()) * kThreadsOfSm / threads();
+    threads = max_blocks > kWideRow && T * H <= sm_count() ? 512 : T * H >= static_cast<int64_t>(kNarrowRows) * sm_count() ? 128 : 256;
+    const int64_t steps = (max_blocks + threads - 1) / threads, most = static_cast<int64_t>(sm_count()) * kThreadsOfSm / threads;
     while (cluster < kMaxCluster && cluster < steps && 2 * cluster * T * H <= most) cluster *= 2;
     in_ws = max_blocks > kSmemKeys;
     stride = max_blocks;
@@ -480,7 +495,6 @@ struct Split {
     if (in_ws && row * T > kMostKeys) rows = static_cast<int64_t>(kMostKeys / row);
     if (rows < 1) rows = 1;
   }
-  int threads() const { return wide ? 512 : 256; }
 };
 
 void carve_keys(Carve &c, SelectArgs &a, const Split &p, int32_t H) {
@@ -524,6 +538,11 @@ int launch_dim(int D, const SelectArgs &a, const Split &p, cudaStream_t s) {
   return D == 64 ? launch<T, 64, kThreads>(a, p, s) : D == 128 ? launch<T, 128, kThreads>(a, p, s) : launch<T, 256, kThreads>(a, p, s);
 }
 
+template <class T>
+int launch_threads(int D, const SelectArgs &a, const Split &p, cudaStream_t s) {
+  return p.threads == 512 ? launch_dim<T, 512>(D, a, p, s) : p.threads == 256 ? launch_dim<T, 256>(D, a, p, s) : launch_dim<T, 128>(D, a, p, s);
+}
+
 }  // namespace
 }  // namespace maps
 
@@ -558,8 +577,7 @@ int maps_kv4_select_blocks(int32_t dtype, int32_t B, int64_t T, int32_t Hq, int3
   Carve c(ws);
   carve_keys(c, a, p, H);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (dtype == MAPS_BF16) return p.wide ? launch_dim<__nv_bfloat16, 512>(D, a, p, s) : launch_dim<__nv_bfloat16, 256>(D, a, p, s);
-  return p.wide ? launch_dim<__half, 512>(D, a, p, s) : launch_dim<__half, 256>(D, a, p, s);
+  return dtype == MAPS_BF16 ? launch_threads<__nv_bfloat16>(D, a, p, s) : launch_threads<__half>(D, a, p, s);
 }
 
 }  // extern "C"
