@@ -43,7 +43,8 @@ ROTATE = [  # T, Hq, H, D, S, type, axes, rot, interleaved, layout, share of tok
     (50, 7, 1, 128, 4096, "bf16", 3, 96, False, "gaps", 0), (64, 2, 2, 64, 16, "fp16", 1, 0, False, "plain", 0.1),
     (700, 8, 4, 128, 16, "bf16", 3, 128, False, "fused", 0.02), (3001, 10, 5, 64, 32, "fp16", 3, 64, True, "plain", 0.1),
     (5003, 4, 4, 128, 16, "bf16", 1, 128, False, "odd", 0), (6000, 3, 3, 256, 16, "bf16", 2, 16, True, "fused", 0),
-    (9000, 6, 6, 64, 64, "bf16", 1, 32, False, "plain", 0)]
+    (9000, 6, 6, 64, 64, "bf16", 1, 32, False, "plain", 0), (7001, 3, 3, 256, 16, "bf16", 4, 256, False, "fused", 0.01),
+    (6600, 6, 3, 256, 32, "fp16", 2, 240, True, "odd", 0.1)]
 
 
 def lay(x, layout, dtype):
@@ -348,6 +349,24 @@ def test_select_blocks(M, case):
     rng = np.random.default_rng(100 + case)
     check_select(M, SELECT[case], *select_data(SELECT[case], rng))
     check_select(M, SELECT[case], *select_data(SELECT[case], rng), lay_q="odd")
+
+
+@pytest.mark.parametrize("Hq,H,D,kind", [(2, 2, 64, "bf16"), (12, 2, 128, "fp16"), (14, 2, 256, "bf16")])
+def test_select_blocks_of_many_rows(M, Hq, H, D, kind):
+    """So many that few threads take each: rows of every length that these handle in a way of its own."""
+    rng = np.random.default_rng(D)
+    lens = np.concatenate([rng.integers(0, 3000, 300), [16 * 21, 16 * 149, 16 * 150, 16 * 278, 16 * 279, 16 * 534, 16 * 535, 16 * 2070, 16 * 2071, 16 * 4000]])
+    case = (Hq, H, D, 16, kind, list(rng.permutation(lens)), [1] * len(lens), 2, 1, 22)
+    check_select(M, case, *select_data(case, rng))
+    check_select(M, case, *select_data(case, rng, 40))
+
+
+@pytest.mark.parametrize("D,kind", [(128, "bf16"), (256, "fp16")])
+def test_select_blocks_of_long_rows(M, D, kind):
+    """A cluster's blocks share a row, whose last blocks are few or none for some of them."""
+    for n in (2049, 4100, 8193, 9001):
+        case = (6, 1, D, 16, kind, [16 * n - 3, 16 * 40], [1, 2], 1, 2, 127)
+        check_select(M, case, *select_data(case, np.random.default_rng(n)))
 
 
 @pytest.mark.parametrize("levels", [1, 2, 3, 50])
