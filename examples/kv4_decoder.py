@@ -11,7 +11,13 @@ token for one that decodes.  A request that has all its tokens gives its blocks
 back at the next step.  Keys, values and queries stand in for a model's: they
 are drawn at random.
 
+With --sparse N keys and queries are turned by their positions on the way
+(maps_kv4_append_rotated), the ranges of the blocks that new tokens went to are kept
+(maps_kv4_block_ranges), and every query attends over the N blocks alone that score highest
+for it (maps_kv4_select_blocks, maps_kv4_attention_blocks).
+
     python examples/kv4_decoder.py --requests 256 --blocks 8192
+    python examples/kv4_decoder.py --requests 256 --blocks 8192 --sparse 32
 """
 from __future__ import annotations
 
@@ -35,7 +41,7 @@ class Decoder:
     """State of one decoder: requests, block tables, free blocks and the cache of one layer."""
 
     def __init__(self, prompt, output, bound, blocks: int, heads=(32, 8), D: int = 128, S: int = 16, chunk: int = 512,
-                 max_wait: int = 1000, dtype=torch.bfloat16, seed: int = 0):
+                 max_wait: int = 1000, dtype=torch.bfloat16, seed: int = 0, sparse: int = 0):
         self.R, self.S, self.D, self.chunk, self.max_wait, self.dtype = prompt.numel(), S, D, chunk, max_wait, dtype
         self.Hq, self.H = heads
         self.device = prompt.device
@@ -54,6 +60,12 @@ class Decoder:
         self.wait, self.zero = torch.zeros(self.R, **i32), torch.zeros(self.R, **i32)
         self.order, self.seg = torch.zeros(self.R, **i32), torch.zeros(2, dtype=torch.int64, device=self.device)
         self.ws = M.Workspace(device=self.device)
+        self.sparse = sparse
+        if sparse:
+            self.codes = torch.zeros(M.kv4_range_shape(blocks, self.H, D), dtype=torch.int8, device=self.device)
+            self.scale = torch.zeros(blocks, self.H, device=self.device)
+            angle = torch.arange(most * S, dtype=torch.float64)[:, None] * 10000.0 ** (-torch.arange(D // 2, dtype=torch.float64) / (D // 2))
+            self.cos_sin = torch.cat([angle.cos(), angle.sin()], 1).float().to(self.device)
 
     def done(self) -> bool:
         return bool((self.held >= self.total).all())
@@ -78,21 +90,30 @@ class Decoder:
         off = torch.empty(self.R + 1, dtype=torch.int64, device=self.device)
         slots = torch.empty(T, dtype=torch.int64, device=self.device)
         got, n_free = torch.empty_like(self.held), torch.empty_like(self.n_free)
+        pos = torch.empty(T, dtype=torch.int32, device=self.device)
         ok(M.maps_block_tables(S, tokens_held, want, self.table, self.free, self.n_free, n_free, got, off, slots,
-                               order=self.order, ws=self.ws))
+                               pos_out=pos, order=self.order, ws=self.ws))
         rows = lambda h: torch.randn(T, h, self.D, device=self.device, generator=self.gen).to(self.dtype)  # noqa: E731
         q, k, v = rows(self.Hq), rows(self.H), rows(self.H)
-        ok(M.maps_kv4_append(k, v, slots, self.cache, S, ws=self.ws))
         granted = live & (got == want)  # all that are live: admission leaves blocks for them
         n = torch.where(granted, got, 0)
         out = torch.empty_like(q)
-        ok(M.maps_kv4_attention(q, off, n, self.table, self.cache, S, self.D ** -0.5, out, ws=self.ws))
+        if self.sparse:
+            ok(M.maps_kv4_append_rotated(q, k, v, pos, self.cos_sin, slots, self.cache, S, q, ws=self.ws))
+            ok(M.maps_kv4_block_ranges(tokens_held, n, self.table, self.cache, S, self.codes, self.scale, ws=self.ws))
+            lists = torch.empty(T, self.H, self.sparse, dtype=torch.int32, device=self.device)
+            tokens = torch.empty(T, self.H, dtype=torch.int32, device=self.device)
+            ok(M.maps_kv4_select_blocks(q, off, n, self.table, self.codes, self.scale, S, 1, 2, lists, tokens, ws=self.ws))
+            ok(M.maps_kv4_attention_blocks(q, lists, tokens, self.cache, S, self.D ** -0.5, out, ws=self.ws))
+        else:
+            ok(M.maps_kv4_append(k, v, slots, self.cache, S, ws=self.ws))
+            ok(M.maps_kv4_attention(q, off, n, self.table, self.cache, S, self.D ** -0.5, out, ws=self.ws))
         self.wait += 1
         self.wait[granted] = 0
         self.returned |= finished
         self.held = torch.where(finished, self.held, got)
         self.n_free = n_free
-        return dict(q=q, k=k, v=v, slots=slots, off=off, n=n, out=out, granted=granted)
+        return dict(q=q, k=k, v=v, slots=slots, pos=pos, off=off, n=n, out=out, granted=granted)
 
 
 def main() -> None:
@@ -100,12 +121,13 @@ def main() -> None:
     ap.add_argument("--requests", type=int, default=256)
     ap.add_argument("--blocks", type=int, default=8192)
     ap.add_argument("--steps", type=int, default=5000, help="at most so many")
+    ap.add_argument("--sparse", type=int, default=0, help="cache blocks that a query attends over (3 at least); 0: all")
     a = ap.parse_args()
     g = torch.Generator().manual_seed(1)
     prompt = torch.randint(32, 2049, (a.requests,), generator=g, dtype=torch.int32)
     output = torch.empty(a.requests).log_normal_(5.5, 1.0, generator=g).clamp(1, 1024).int()
     bound = (output.float() * 1.5).int()
-    d = Decoder(prompt.cuda(), output.cuda(), bound.cuda(), a.blocks)
+    d = Decoder(prompt.cuda(), output.cuda(), bound.cuda(), a.blocks, sparse=a.sparse)
     t0, steps, tokens = time.perf_counter(), 0, 0
     while not d.done() and steps < a.steps:
         r = d.step()

@@ -7,14 +7,19 @@
 // and tile of 8 or 16 of the head's query heads, and take its units of 32 to 64 tokens in turn; two to four items pass on a multiprocessor
 // side by side.  Where items are few, and for the last ones that do not fill the device, a cluster of such blocks shares one.  Parts meet
 // in shared memory, the block's and then the cluster's, in the order of the warps: no workspace, and results that depend on sizes and
-// lengths alone.
+// lengths alone.  (Equal runs of units over all lists, as behind block tables, cost a plan, parts in memory and joins across blocks: 66 us
+// for 53 in the case below, 11.8 for 6.1 with one row.)
+//
+// Bound: 128 rows of 2,048 tokens, 8 KV heads of 128 channels, 285 MB, take 52.6 us (5.4 TB/s, 0.80 of the measured copy rate), the rest
+// what a list costs before its first unit and after its last.  One row: 6.1 us, launch, three rounds of loads, a unit, two joins.  Lists of
+// 64 channels and five query heads: issue slots, 210 instructions for 16 tokens.
 #include "kv4_attention_products.cuh"
 
 namespace maps {
 namespace {
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
-constexpr int kMaxCluster = 8;
+constexpr int kMaxCluster = 8;  // one row of 8 heads: 6.2 us, with 16 blocks 7.5, with four 7.2, with two 9.3
 
 struct ListArgs {
   int32_t Hq, H, group, tiles;  // query heads to a KV head, and tiles of them
@@ -35,13 +40,14 @@ struct ListArgs {
 template <int D, int NT>
 struct ListShape {
   static constexpr int kRows = 8 * NT;  // query rows of a tile
-  // Groups of 16 tokens in a unit, which shares the row maxima, as in the form for few queries.
+  // Groups of 16 tokens in a unit, which shares the row maxima: 128 rows of 128 channels with four 52.6 us, three 55.6, two 60; of 256
+  // channels with two 19.7, one 33, three 21.
   static constexpr int kGroups = D == 256 ? 2 : NT == 1 ? 4 : 3;
   static constexpr int kTok = kGroups * kGroup;
   static constexpr int kBytes = kGroups * kv4_group_bytes(D);  // of a stage
   static constexpr int kStages = D == 64 && NT == 2 ? 4 : 2;
   static constexpr int kPart = kRows * D + 2 * kRows;  // floats of a part: sums, maxima, totals
-  static constexpr int kBlocks = NT == 2 || D == 256 ? 2 : D == 64 ? 4 : 3;  // of a multiprocessor
+  static constexpr int kBlocks = NT == 2 || D == 256 ? 2 : D == 64 ? 4 : 3;  // of a multiprocessor, as registers allow (64 channels: four 40.5 us, three 42.2)
   static constexpr size_t kSmem = static_cast<size_t>(kWarps) * kStages * kBytes + kPart * 4 + kWarps * kStages * 8;
   static_assert(kPart * 4 <= kStages * kBytes, "a warp's part lies in its ring");
 };

@@ -4,6 +4,10 @@
 // lengths.  A key is fl(scale * code + zero); least and greatest are taken of these 32-bit values, and the codes of the ends are
 // exact: a code times the scale has 15 bits, so a comparison in 32 bits settles where a product's rounding may have crossed a
 // whole number.
+//
+// Bound: the pipe that takes codes out of words and compares (two operations a code), not the bytes.  48 prompts of 1,500 to 8,192
+// tokens, 8 heads of 128 channels, 156 MB: 88 us (1.8 TB/s).  One token each of 512 requests: 6.2 us, launch, counting, two rounds
+// of loads.  Four blocks a multiprocessor instead of two: 87 and 7.4 us.
 #include "kv4_rows.cuh"
 
 namespace maps {

@@ -9,6 +9,10 @@
 // numbers in the scores' order, in the shared memory of the cluster's first block, which goes on alone (in the workspace where they
 // are too many).  The least key that is taken is found by bisection, up to 16 keys a thread in registers, or for longer rows by
 // histograms of the keys that are still in question, ten bits at a time; then the list is written in order.
+//
+// Bound: chains of dependent steps.  Where rows are many, enough of them side by side hide these: 128 requests of 64 to 8,192 tokens, 8
+// heads of 128 channels, 68 MB of ranges, 19.2 us (floor 10.6).  One request of 100,000 to 131,072 tokens: 17.6 us, of which look-ups
+// and first codes 3, its 8,192 blocks' codes 1.5, the cluster's barrier 1.5, bisection 5, the list 2.
 #include <atomic>
 
 #include "kv4.cuh"
@@ -18,9 +22,14 @@ namespace {
 
 constexpr int kBinBits = 10, kBins = 1 << kBinBits;
 constexpr int kSmemKeys = 8192;   // of shared memory; longer rows of keys stay in the workspace
-constexpr int kThreadsOfSm = 512;  // of a multiprocessor up to which a row and head is shared out
-constexpr int kNarrowRows = 4;      // rows and heads for each multiprocessor from which on 128 threads take one, so that more are under way
-constexpr int kWideRow = 2048;      // blocks of a row from which on 512 threads take it, where rows are few
+// Threads of a multiprocessor up to which a row and head is shared out.  35 rows of 4 heads and up to 1,024 blocks: 512 8.4 us, 2,048 9.6.
+constexpr int kThreadsOfSm = 512;
+// Rows and heads for each multiprocessor from which on 128 threads take one, six a multiprocessor: 1,024 of them 19.2 us, by 256
+// threads 23.2.  Below, 256 threads end a row sooner.
+constexpr int kNarrowRows = 4;
+// Blocks of a row from which on 512 threads take it, where rows are few: 8 rows of 8,192 blocks 17.7 us, by 256 threads 20.7.  Clusters of 16
+// 17.7, of 8 26, of 4 39.
+constexpr int kWideRow = 2048;
 constexpr int kMaxCluster = 16;
 constexpr size_t kMostKeys = size_t(1) << 26;  // in the workspace: more rows take their turns
 
