@@ -2,15 +2,21 @@
 
 Each ``csrc/*.cu`` is compiled in parallel with nvcc, then linked into one
 shared library next to this file.  A source or header newer than the
-library triggers a rebuild.
+library triggers a rebuild.  ``csrc/marshal.cpp``, the binding's native
+argument marshalling, becomes ``_marshal.so`` beside it; where PyTorch's or
+Python's headers do not compile, the binding does that work in Python.
 """
 from __future__ import annotations
 
 import concurrent.futures as cf
 import glob
+import importlib.util
 import os
+import re
 import shutil
 import subprocess
+import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -18,6 +24,7 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libmaps.so")
+MARSHAL = os.path.join(PKG, "_marshal.so")
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ARCH + ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC",
@@ -36,7 +43,7 @@ def sources() -> list[str]:
 
 
 def _inputs() -> list[str]:
-    return (sources() + glob.glob(os.path.join(CSRC, "*.cuh")) +
+    return (sources() + glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(CSRC, "*.cpp")) +
             glob.glob(os.path.join(INCLUDE, "*.h")) + [os.path.abspath(__file__)])
 
 
@@ -45,6 +52,30 @@ def up_to_date() -> bool:
         return False
     t = os.path.getmtime(LIB)
     return all(os.path.getmtime(f) <= t for f in _inputs())
+
+
+def torch_version(root: str) -> str:
+    with open(os.path.join(root, "version.py")) as f:
+        return re.search(r"__version__ = ['\"]([^'\"]+)", f.read()).group(1)
+
+
+def build_marshal() -> None:
+    tmp = MARSHAL + f".{os.getpid()}.tmp"
+    try:
+        torch = os.path.dirname(importlib.util.find_spec("torch").origin)
+        cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f'-DMAPS_TORCH_VERSION="{torch_version(torch)}"', "-I", INCLUDE,
+               "-isystem", sysconfig.get_paths()["include"], "-isystem", os.path.join(torch, "include"),
+               os.path.join(CSRC, "marshal.cpp"), "-o", tmp, "-L", os.path.join(torch, "lib"), "-ltorch_python", "-lc10"]
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        if r.returncode == 0:
+            os.replace(tmp, MARSHAL)
+            return
+        why = r.stderr[:2000]
+    except (OSError, AttributeError) as e:
+        why = str(e)
+    if os.path.exists(MARSHAL):  # of other sources
+        os.remove(MARSHAL)
+    print(f"arguments are marshalled in Python: {why}", file=sys.stderr)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
@@ -64,8 +95,10 @@ def build(force: bool = False, verbose: bool = False) -> str:
         return obj
 
     srcs = sources()
-    with cf.ThreadPoolExecutor(max_workers=min(len(srcs), os.cpu_count() or 4)) as ex:
+    with cf.ThreadPoolExecutor(max_workers=min(len(srcs) + 1, os.cpu_count() or 4)) as ex:
+        marshal = ex.submit(build_marshal)
         objs = list(ex.map(compile_one, srcs))
+        marshal.result()
     tmp = LIB + f".{os.getpid()}.tmp"
     cmd = [nvcc, *ARCH, "-shared", "-o", tmp, *objs]
     r = subprocess.run(cmd, capture_output=True, text=True)

@@ -1,6 +1,7 @@
 """Thin Python binding of the MAPS C ABI (``include/maps.h``).
 
-Argument marshalling only: every function passes torch tensors' device
+Argument marshalling only (that of a decode step's calls in native code, ``csrc/marshal.cpp``,
+where it was built): every function passes torch tensors' device
 pointers and the current CUDA stream to the function of the same name in
 ``libmaps.so`` and returns its status.  Every step of the computation runs in
 the library's CUDA kernels; there is no CPU path.  Importing this module
@@ -207,7 +208,8 @@ class Workspace:
 
     @buf.setter
     def buf(self, buf) -> None:
-        self._buf, self.ptr, self.nbytes = buf, ctypes.c_void_p(buf.data_ptr()), buf.numel()
+        self._buf, self.address, self.nbytes = buf, buf.data_ptr(), buf.numel()
+        self.ptr = ctypes.c_void_p(self.address)
 
     def _meet(self, stream) -> None:
         s = torch.cuda.current_stream(self.device) if stream is None else stream
@@ -241,6 +243,31 @@ def _scratch(ws: Workspace | None, nbytes: int, stream):
 def _need(device: int | None, query: str, *sizes: int) -> int:
     """A size query: it depends on the sizes alone, or on the multiprocessors of `device` too."""
     return getattr(lib, query)(*sizes)
+
+
+def _load_marshal():
+    """The native marshalling of the calls that a decode step makes, where it was built (for this PyTorch)."""
+    try:
+        from . import _marshal
+    except ImportError:
+        return None
+    if _marshal.torch_version != torch.__version__:
+        return None
+    _marshal.bind(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in (
+        "maps_kv4_record_bytes", "maps_kv4_append", "maps_kv4_read", "maps_kv4_append_rotated", "maps_kv4_block_ranges",
+        "maps_kv4_select_blocks_workspace_size", "maps_kv4_select_blocks", "maps_kv4_attention_blocks")))
+    return _marshal
+
+
+_fast = _load_marshal()
+_KV4_WS = lib.maps_kv4_workspace_size()
+
+
+def _quick(call, ws, stream, *args):
+    """The status of a call whose arguments are as its native marshalling expects, else None: the caller then goes
+    through them one by one, and says what is wrong."""
+    ws, on = _scratch(ws, _KV4_WS, stream)
+    return call(*args, ws.address, ws.nbytes, on)
 
 
 def maps_check(ws: Workspace, stream=None) -> int:
@@ -433,6 +460,10 @@ def _kv4(cache, S: int, D: int, H: int):
 
 def maps_kv4_append(k, v, slots, cache, S: int, ws: Workspace | None = None, stream=None) -> int:
     """Writes k, v [T, H, D] (bf16 or fp16) to the slots [T] int64 of the cache."""
+    if _fast is not None and ws is not None:
+        st = _quick(_fast.append, ws, stream, k, v, slots, cache, S)
+        if st is not None:
+            return st
     T, H, D = k.shape
     if v.shape != k.shape or slots.numel() != T:
         raise ValueError("k, v and slots differ in size")
@@ -445,6 +476,10 @@ def maps_kv4_append(k, v, slots, cache, S: int, ws: Workspace | None = None, str
 def maps_kv4_read(slots, cache, S: int, k_out, v_out, ws: Workspace | None = None,
                   stream=None) -> int:
     """Reads the slots [T] of the cache back into k_out, v_out [T, H, D]."""
+    if _fast is not None and ws is not None:
+        st = _quick(_fast.read, ws, stream, slots, cache, S, k_out, v_out)
+        if st is not None:
+            return st
     T, H, D = k_out.shape
     if v_out.shape != k_out.shape or slots.numel() != T:
         raise ValueError("k_out, v_out and slots differ in size")
@@ -481,6 +516,10 @@ def maps_kv4_append_rotated(q, k, v, pos, cos_sin, slots, cache, S: int, q_out, 
     """Turns q [T, Hq, D] into q_out and k [T, H, D] on its way into the cache by the
     tokens' positions: pos [axes, T] (or [T]) int32, cos_sin [n_pos, rot] float32 (cosines,
     then sines), axis [rot / 2] int32 or None; q and q_out None: keys and values alone."""
+    if _fast is not None and ws is not None:
+        st = _quick(_fast.append_rotated, ws, stream, q, k, v, pos, cos_sin, slots, cache, S, q_out, axis, interleaved)
+        if st is not None:
+            return st
     T, H, D = k.shape
     if v.shape != k.shape or slots.numel() != T:
         raise ValueError("k, v and slots differ in size")
@@ -517,6 +556,10 @@ def maps_kv4_block_ranges(held, kv_len, table, cache, S: int, codes, scale,
                           ws: Workspace | None = None, stream=None) -> int:
     """Ranges of the keys of the blocks that tokens went to since there were held [B]
     int32 (None: all blocks): codes [blocks, H, 2, D] int8 and scale [blocks, H] float32."""
+    if _fast is not None and ws is not None:
+        st = _quick(_fast.block_ranges, ws, stream, held, kv_len, table, cache, S, codes, scale)
+        if st is not None:
+            return st
     B, n_blocks, H, D = kv_len.numel(), cache.shape[0], cache.shape[1], codes.shape[-1]
     if held is not None and held.numel() != B or table.dim() != 2 or table.shape[0] != B:
         raise ValueError("held, kv_len and table differ in size")
@@ -530,6 +573,10 @@ def maps_kv4_select_blocks(q, qo_off, kv_len, table, codes, scale, S: int, first
                            blocks_out, tokens_out, ws: Workspace | None = None, stream=None) -> int:
     """For each row of q [T, Hq, D] and KV head the cache blocks of the highest scores, the
     first and last ones always: blocks_out [T, H, n_list] and tokens_out [T, H] int32."""
+    if _fast is not None and ws is not None:
+        st = _quick(_fast.select_blocks, ws, stream, q, qo_off, kv_len, table, codes, scale, S, first, last, blocks_out, tokens_out)
+        if st is not None:
+            return st
     T, Hq, D = q.shape
     B, (n_blocks, H) = kv_len.numel(), codes.shape[:2]
     if codes.shape[-1] != D or qo_off.numel() != B + 1 or table.dim() != 2 or table.shape[0] != B:
@@ -548,6 +595,10 @@ def maps_kv4_attention_blocks(q, blocks, tokens, cache, S: int, sm_scale: float,
                               ws: Workspace | None = None, stream=None) -> int:
     """Attention of q [T, Hq, D] over the first tokens [T, H] tokens of the cache blocks
     blocks [T, H, n_list] (both int32); out like q, lse_out [T][Hq] float32 or None."""
+    if _fast is not None and ws is not None:
+        st = _quick(_fast.attention_blocks, ws, stream, q, blocks, tokens, cache, S, sm_scale, out, lse_out)
+        if st is not None:
+            return st
     T, Hq, D = q.shape
     H = cache.shape[1]
     if out.shape != q.shape or blocks.dim() != 3 or tuple(blocks.shape[:2]) != (T, H) or tuple(tokens.shape) != (T, H):
