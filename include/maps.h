@@ -2,7 +2,7 @@
  * maps.h -- C ABI of the MAPS memory-aware predictive scheduler hot path,
  * implemented as integer-only CUDA kernels for GB300 (sm_103a), and of the KV
  * memory that its decoders run on: block tables (integers too), a cache held in
- * 4 bits, and attention over that cache.
+ * 4 bits, attention over that cache, and sparse decoding on it.
  *
  * The four scheduling calls follow the scheduler's problem statement (Sec.
  * 3.3): decoders d_k with KV-token capacity C_k and waiting-queue length Q_k;
@@ -689,8 +689,9 @@ int maps_kv4_append_rotated(int32_t dtype, int64_t T, int32_t Hq, int32_t H, int
  *   blocks              [T][H][n_list] int32 out: the blocks of the cache, then -1.
  *   tokens              [T][H] int32 out: the tokens of the list, of which only the
  *                       last block may have less than S; 0: the row sees no key.
- *   ws                  maps_kv4_select_blocks_workspace_size bytes; more than the
- *                       256 of the control block only where max_blocks passes 32,768.
+ *   ws                  maps_kv4_select_blocks_workspace_size bytes: 256, and where
+ *                       max_blocks passes 8,192 room for keys of 4 bytes, at most
+ *                       256 MB or what one row of q takes (4 H max_blocks).
  * Rows that no request has are left as they are.  A length, an offset or a used table
  * entry out of its domain is MAPS_E_RANGE (via maps_check); such a request's rows get
  * empty lists, such a block has score NaN, and nothing outside the arrays is read.
@@ -698,6 +699,8 @@ int maps_kv4_append_rotated(int32_t dtype, int64_t T, int32_t Hq, int32_t H, int
  * maps_kv4_attention_blocks: attention as maps_kv4_attention has it, of query head x
  * of row i over the first tokens[i][h] tokens of the blocks blocks[i][h][..], h = x /
  * (Hq / H), all of which it sees.  Its results keep to the same limits.
+ * Each row reads its own lists, so chunks of prompts are attended to sooner by
+ * maps_kv4_attention.
  *
  *   T                   rows (<= 2^30, T * Hq <= 2^31 - 1,024).
  *   blocks, tokens, n_list   as maps_kv4_select_blocks leaves them, or any others; a block

@@ -7,8 +7,8 @@
 // (16 bytes) each; extremes are joined by shuffles.
 //
 // Bound: the bytes of the 16-bit rows and the records.  65,536 tokens of 8 heads and 128 channels, 340 MB a call,
-// take 84 us to append (4.1 TB/s, 0.60 of the measured copy rate; a row's minimum, maximum and
-// codes cost about as many issue slots) and 52 us to read (6.5 TB/s).  A decode step's rows take 2-5 us,
+// take 79 us to append (4.3 TB/s, 0.64 of the measured copy rate; a row's minimum, maximum and
+// codes cost about as many issue slots) and 54 us to read (6.3 TB/s).  A decode step's rows take 2-5 us,
 // which is launch and latency.
 #include "kv4_rows.cuh"
 

@@ -17,6 +17,9 @@ namespace {
 // Warps of a multiprocessor up to which a token's heads are shared out among several.  512 tokens of 40 heads: 8 or 16 warps 6.1 us, 32 6.8,
 // 64 6.7.
 constexpr int kUnitWarps = 16;
+// Warps of a multiprocessor from which on values pass in groups of 16 tokens: 3,001 tokens of 5 heads of 64 channels (6 warps) 8.6 us, row by
+// row 9.1; 512 tokens of 8 heads (2 warps) 5.4 either way.
+constexpr int kGroupWarps = 4;
 
 struct RotArgs {
   KVArgs kv;
@@ -213,7 +216,7 @@ void launch_rows(const RotArgs &a, cudaStream_t s) {
   const int32_t per = static_cast<int32_t>((passes + (cut < passes ? cut : passes) - 1) / (cut < passes ? cut : passes)) * kRows;
   const int32_t units = (a.Hq + a.kv.H + per - 1) / per;
   const int64_t warps = T_ * units, groups = (T_ + kGroup - 1) / kGroup * a.kv.H;
-  const bool many = groups >= static_cast<int64_t>(kManyWarps) * sm_count();
+  const bool many = groups >= static_cast<int64_t>(kGroupWarps) * sm_count();
   const int64_t values = many ? (groups + 7) / 8 : (T_ * a.kv.H + 8 * kRows - 1) / (8 * kRows);
   const unsigned grid = static_cast<unsigned>(values + (warps + 7) / 8);
   if (many)
