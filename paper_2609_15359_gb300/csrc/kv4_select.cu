@@ -513,16 +513,7 @@ void carve_keys(Carve &c, SelectArgs &a, const Split &p, int32_t H) {
 template <class T, int D, int kThreads>
 int launch(SelectArgs a, const Split &p, cudaStream_t s) {
   constexpr auto kernel = kv4_select_kernel<T, D, kThreads>;
-  static std::atomic<uint64_t> done;  // devices that have been asked for clusters of 16
-  int dev = 0;
-  MAPS_TRY(cuda_ok(cudaGetDevice(&dev)));
-  const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
-  if (p.cluster > 8 && !(done.load(std::memory_order_relaxed) & bit)) {
-    MAPS_TRY(cuda_ok(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1)));
-    done.fetch_or(bit, std::memory_order_relaxed);
-  }
   a.smem_keys = static_cast<int32_t>(a.max_blocks < kSmemKeys ? a.max_blocks : kSmemKeys);
-  a.cluster = p.cluster;
   cudaLaunchConfig_t cfg = {};
   cfg.blockDim = kThreads;
   cfg.dynamicSmemBytes = static_cast<size_t>(a.smem_keys) * 4;
@@ -535,9 +526,28 @@ int launch(SelectArgs a, const Split &p, cudaStream_t s) {
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = p.cluster > 1 ? 2 : 1;
+  a.cluster = p.cluster;
+  if (a.cluster > 8) {  // more than every device takes: asked for once, and 8 where it is not to be had
+    static std::atomic<uint64_t> asked, had;
+    int dev = 0;
+    MAPS_TRY(cuda_ok(cudaGetDevice(&dev)));
+    const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
+    if (!(asked.load(std::memory_order_acquire) & bit)) {
+      int clusters = 0;
+      cfg.gridDim = dim3(static_cast<unsigned>(a.cluster));
+      if (cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+          cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg) == cudaSuccess && clusters > 0)
+        had.fetch_or(bit, std::memory_order_relaxed);
+      else
+        (void)cudaGetLastError();
+      asked.fetch_or(bit, std::memory_order_release);
+    }
+    if (!(had.load(std::memory_order_relaxed) & bit)) a.cluster = 8;
+    attr[1].val.clusterDim.x = a.cluster;
+  }
   for (a.row0 = 0; a.row0 < a.T; a.row0 += p.rows) {
     const int64_t rows = a.T - a.row0 < p.rows ? a.T - a.row0 : p.rows;
-    cfg.gridDim = dim3(static_cast<unsigned>(rows * a.H * p.cluster));
+    cfg.gridDim = dim3(static_cast<unsigned>(rows * a.H * a.cluster));
     MAPS_TRY(cuda_ok(cudaLaunchKernelEx(&cfg, kernel, static_cast<const SelectArgs &>(a))));
   }
   return launch_ok();
