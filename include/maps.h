@@ -624,7 +624,8 @@ int maps_kv4_attention(int32_t dtype, int32_t B, int64_t T, int32_t Hq, int32_t 
  *                       axis 0.
  *   rot, interleaved    channels that are turned: a multiple of 16 up to D, 0
  *                       for none; 0 or 1.
- *   cos_sin, n_pos      [n_pos][rot] float: a position's cosines, then its sines.
+ *   cos_sin, n_pos      [n_pos][rot] float: a position's cosines, then its sines;
+ *                       16-byte aligned.
  *   all others          as for maps_kv4_append.
  * A position outside [0, n_pos) or an axis outside [0, axes) is MAPS_E_RANGE (via
  * maps_check), and pairs on it are not turned.
