@@ -24,6 +24,14 @@ decltype(&maps_kv4_select_blocks_workspace_size) select_workspace;
 decltype(&maps_kv4_select_blocks) select_blocks;
 decltype(&maps_kv4_attention_blocks) attention_blocks;
 
+// A dense tensor, asked for everything at once: what has no memory throws when it is asked for it, which has to be while the
+// interpreter is held.  None where that may be: p is NULL, and so it is for an empty tensor.
+struct Dense {
+  void *p = nullptr;
+  bool given = false;
+  int64_t n = 0, dims = 0, size[4] = {};
+};
+
 // Arguments one after the other; `ok` falls at the first that is not as expected.
 struct Args {
   PyObject *const *at;
@@ -68,17 +76,22 @@ struct Args {
     want(t.is_cuda());
     return ok ? &t : nullptr;
   }
-  // The same, dense.
-  const at::Tensor *dense(at::ScalarType type, int64_t dims, bool may_be_none = false) {
+  // The same, dense; of any number of dimensions where that is -1.
+  Dense dense(at::ScalarType type, int64_t dims, bool may_be_none = false) {
+    Dense d;
     const at::Tensor *t = tensor(may_be_none);
-    if (t != nullptr) want(t->scalar_type() == type && (dims < 0 || t->dim() == dims) && t->is_contiguous());
-    return ok ? t : nullptr;
+    if (t == nullptr) return d;
+    want(t->scalar_type() == type && (dims < 0 || t->dim() == dims) && t->is_contiguous());
+    if (!ok) return d;
+    d.p = t->data_ptr(), d.given = true, d.n = t->numel(), d.dims = t->dim();
+    for (int64_t i = 0; i < d.dims && i < 4; ++i) d.size[i] = t->size(i);
+    return d;
   }
 };
 
 template <class T>
-T *data(const at::Tensor *t) {
-  return t == nullptr ? nullptr : static_cast<T *>(t->data_ptr());
+T *data(const Dense &d) {
+  return static_cast<T *>(d.p);
 }
 
 // Rows of heads whose channels lie side by side: [rows, heads, channels].
@@ -106,8 +119,8 @@ struct Cache {
   void *p = nullptr;
   int64_t n = 0, H = 0, bytes = 0;
   explicit Cache(Args &a) {
-    const at::Tensor *t = a.dense(at::kByte, 3);
-    if (t != nullptr) p = t->data_ptr(), n = t->size(0), H = t->size(1), bytes = t->size(2);
+    const Dense t = a.dense(at::kByte, 3);
+    p = t.p, n = t.size[0], H = t.size[1], bytes = t.size[2];
   }
   bool holds(int64_t heads, int32_t S, int64_t D) const {
     return H == heads && bytes > 0 && D <= INT32_MAX && bytes == static_cast<int64_t>(record_bytes(S, static_cast<int32_t>(D)));
@@ -121,6 +134,7 @@ struct Last {  // workspace and stream, which end every call's arguments
   explicit Last(Args &a) : ws(a.address()), bytes(static_cast<size_t>(a.integer())), stream(a.address()) { a.want(a.left == 0); }
 };
 
+// `call` works on plain values alone: it runs without the interpreter, and may not throw.
 template <class Call>
 PyObject *status(const Args &a, Call call) {
   if (!a.ok) Py_RETURN_NONE;
@@ -134,11 +148,11 @@ PyObject *status(const Args &a, Call call) {
 PyObject *py_append(PyObject *, PyObject *const *args, Py_ssize_t n) {
   Args a{args, n};
   const Rows k(a), v(a);
-  const at::Tensor *slots = a.dense(at::kLong, -1);
+  const Dense slots = a.dense(at::kLong, -1);
   const Cache cache(a);
   const int32_t S = a.integer32();
   const Last l(a);
-  if (a.ok) a.want(v.like(k) && slots->numel() == k.n && cache.holds(k.heads, S, k.D));
+  if (a.ok) a.want(v.like(k) && slots.n == k.n && cache.holds(k.heads, S, k.D));
   return status(a, [&] {
     return append(k.dtype(), k.n, static_cast<int32_t>(k.heads), static_cast<int32_t>(k.D), S, k.p, k.row, k.head, v.p, v.row, v.head, data<int64_t>(slots), cache.p,
                   cache.n, l.ws, l.bytes, l.stream);
@@ -147,12 +161,12 @@ PyObject *py_append(PyObject *, PyObject *const *args, Py_ssize_t n) {
 
 PyObject *py_read(PyObject *, PyObject *const *args, Py_ssize_t n) {
   Args a{args, n};
-  const at::Tensor *slots = a.dense(at::kLong, -1);
+  const Dense slots = a.dense(at::kLong, -1);
   const Cache cache(a);
   const int32_t S = a.integer32();
   const Rows k(a), v(a);
   const Last l(a);
-  if (a.ok) a.want(v.like(k) && slots->numel() == k.n && cache.holds(k.heads, S, k.D));
+  if (a.ok) a.want(v.like(k) && slots.n == k.n && cache.holds(k.heads, S, k.D));
   return status(a, [&] {
     return read(k.dtype(), k.n, static_cast<int32_t>(k.heads), static_cast<int32_t>(k.D), S, data<int64_t>(slots), cache.p, cache.n, k.p, k.row, k.head, v.p, v.row,
                 v.head, l.ws, l.bytes, l.stream);
@@ -162,93 +176,93 @@ PyObject *py_read(PyObject *, PyObject *const *args, Py_ssize_t n) {
 PyObject *py_append_rotated(PyObject *, PyObject *const *args, Py_ssize_t n) {
   Args a{args, n};
   const Rows q(a, true), k(a), v(a);
-  const at::Tensor *pos = a.dense(at::kInt, -1), *cos_sin = a.dense(at::kFloat, 2), *slots = a.dense(at::kLong, -1);
+  const Dense pos = a.dense(at::kInt, -1), cos_sin = a.dense(at::kFloat, 2), slots = a.dense(at::kLong, -1);
   const Cache cache(a);
   const int32_t S = a.integer32();
   const Rows out(a, true);
-  const at::Tensor *axis = a.dense(at::kInt, -1, true);
+  const Dense axis = a.dense(at::kInt, -1, true);
   const int32_t interleaved = a.integer() != 0;
   const Last l(a);
   int64_t axes = 1, rot = 0;
   if (a.ok) {
-    axes = pos->dim() == 2 ? pos->size(0) : 1;
-    rot = cos_sin->size(1);
-    a.want(v.like(k) && slots->numel() == k.n && cache.holds(k.heads, S, k.D) && (q.p == nullptr) == (out.p == nullptr) && axes <= INT32_MAX &&
-           pos->numel() == axes * k.n && rot <= INT32_MAX && (axis == nullptr || axis->numel() == rot / 2));
+    axes = pos.dims == 2 ? pos.size[0] : 1;
+    rot = cos_sin.size[1];
+    a.want(v.like(k) && slots.n == k.n && cache.holds(k.heads, S, k.D) && (q.p == nullptr) == (out.p == nullptr) && axes <= INT32_MAX &&
+           pos.n == axes * k.n && rot <= INT32_MAX && (!axis.given || axis.n == rot / 2));
     if (q.p != nullptr) a.want(out.like(q) && q.n == k.n && q.D == k.D && q.type == k.type);
   }
   return status(a, [&] {
     return append_rotated(k.dtype(), k.n, static_cast<int32_t>(q.heads), static_cast<int32_t>(k.heads), static_cast<int32_t>(k.D), S, q.p, q.row, q.head, k.p, k.row,
                           k.head, v.p, v.row, v.head, static_cast<int32_t>(axes), data<int32_t>(pos), data<int32_t>(axis), static_cast<int32_t>(rot), interleaved,
-                          data<float>(cos_sin), cos_sin->size(0), data<int64_t>(slots), cache.p, cache.n, out.p, out.row, out.head, l.ws, l.bytes, l.stream);
+                          data<float>(cos_sin), cos_sin.size[0], data<int64_t>(slots), cache.p, cache.n, out.p, out.row, out.head, l.ws, l.bytes, l.stream);
   });
 }
 
 // Ranges of blocks of the cache: codes [blocks, H, 2, D], scale [blocks, H].
 struct Ranges {
-  const at::Tensor *codes, *scale;
+  Dense codes, scale;
   int64_t n = 0, H = 0, D = 0;
   explicit Ranges(Args &a) : codes(a.dense(at::kChar, 4)), scale(a.dense(at::kFloat, 2)) {
     if (!a.ok) return;
-    n = codes->size(0), H = codes->size(1), D = codes->size(3);
-    a.want(codes->size(2) == 2 && scale->size(0) == n && scale->size(1) == H && H <= INT32_MAX && D <= INT32_MAX);
+    n = codes.size[0], H = codes.size[1], D = codes.size[3];
+    a.want(codes.size[2] == 2 && scale.size[0] == n && scale.size[1] == H && H <= INT32_MAX && D <= INT32_MAX);
   }
 };
 
 PyObject *py_block_ranges(PyObject *, PyObject *const *args, Py_ssize_t n) {
   Args a{args, n};
-  const at::Tensor *held = a.dense(at::kInt, -1, true), *len = a.dense(at::kInt, -1), *table = a.dense(at::kInt, 2);
+  const Dense held = a.dense(at::kInt, -1, true), len = a.dense(at::kInt, -1), table = a.dense(at::kInt, 2);
   const Cache cache(a);
   const int32_t S = a.integer32();
   const Ranges r(a);
   const Last l(a);
   if (a.ok) {
-    const int64_t B = len->numel();
-    a.want(B <= INT32_MAX && (held == nullptr || held->numel() == B) && table->size(0) == B && cache.n == r.n && cache.holds(r.H, S, r.D));
+    const int64_t B = len.n;
+    a.want(B <= INT32_MAX && (!held.given || held.n == B) && table.size[0] == B && cache.n == r.n && cache.holds(r.H, S, r.D));
   }
   return status(a, [&] {
-    return block_ranges(static_cast<int32_t>(len->numel()), static_cast<int32_t>(r.H), static_cast<int32_t>(r.D), S, data<int32_t>(held), data<int32_t>(len),
-                        data<int32_t>(table), table->size(1), cache.p, cache.n, data<int8_t>(r.codes), data<float>(r.scale), l.ws, l.bytes, l.stream);
+    return block_ranges(static_cast<int32_t>(len.n), static_cast<int32_t>(r.H), static_cast<int32_t>(r.D), S, data<int32_t>(held), data<int32_t>(len),
+                        data<int32_t>(table), table.size[1], cache.p, cache.n, data<int8_t>(r.codes), data<float>(r.scale), l.ws, l.bytes, l.stream);
   });
 }
 
 PyObject *py_select_blocks(PyObject *, PyObject *const *args, Py_ssize_t n) {
   Args a{args, n};
   const Rows q(a);
-  const at::Tensor *off = a.dense(at::kLong, -1), *len = a.dense(at::kInt, -1), *table = a.dense(at::kInt, 2);
+  const Dense off = a.dense(at::kLong, -1), len = a.dense(at::kInt, -1), table = a.dense(at::kInt, 2);
   const Ranges r(a);
   const int32_t S = a.integer32(), first = a.integer32(), last = a.integer32();
-  const at::Tensor *blocks = a.dense(at::kInt, 3), *tokens = a.dense(at::kInt, 2);
+  const Dense blocks = a.dense(at::kInt, 3), tokens = a.dense(at::kInt, 2);
   const Last l(a);
   if (a.ok) {
-    const int64_t B = len->numel();
-    a.want(B <= INT32_MAX && q.D == r.D && off->numel() == B + 1 && table->size(0) == B && blocks->size(0) == q.n && blocks->size(1) == r.H &&
-           blocks->size(2) <= INT32_MAX && tokens->size(0) == q.n && tokens->size(1) == r.H &&
-           l.bytes >= select_workspace(q.n, static_cast<int32_t>(r.H), table->size(1)));
+    const int64_t B = len.n;
+    a.want(B <= INT32_MAX && q.D == r.D && off.n == B + 1 && table.size[0] == B && blocks.size[0] == q.n && blocks.size[1] == r.H &&
+           blocks.size[2] <= INT32_MAX && tokens.size[0] == q.n && tokens.size[1] == r.H &&
+           l.bytes >= select_workspace(q.n, static_cast<int32_t>(r.H), table.size[1]));
   }
   return status(a, [&] {
-    return select_blocks(q.dtype(), static_cast<int32_t>(len->numel()), q.n, static_cast<int32_t>(q.heads), static_cast<int32_t>(r.H), static_cast<int32_t>(q.D), S, q.p,
-                         q.row, q.head, data<int64_t>(off), data<int32_t>(len), data<int32_t>(table), table->size(1), data<int8_t>(r.codes), data<float>(r.scale), r.n,
-                         first, last, static_cast<int32_t>(blocks->size(2)), data<int32_t>(blocks), data<int32_t>(tokens), l.ws, l.bytes, l.stream);
+    return select_blocks(q.dtype(), static_cast<int32_t>(len.n), q.n, static_cast<int32_t>(q.heads), static_cast<int32_t>(r.H), static_cast<int32_t>(q.D), S, q.p,
+                         q.row, q.head, data<int64_t>(off), data<int32_t>(len), data<int32_t>(table), table.size[1], data<int8_t>(r.codes), data<float>(r.scale), r.n,
+                         first, last, static_cast<int32_t>(blocks.size[2]), data<int32_t>(blocks), data<int32_t>(tokens), l.ws, l.bytes, l.stream);
   });
 }
 
 PyObject *py_attention_blocks(PyObject *, PyObject *const *args, Py_ssize_t n) {
   Args a{args, n};
   const Rows q(a);
-  const at::Tensor *blocks = a.dense(at::kInt, 3), *tokens = a.dense(at::kInt, 2);
+  const Dense blocks = a.dense(at::kInt, 3), tokens = a.dense(at::kInt, 2);
   const Cache cache(a);
   const int32_t S = a.integer32();
   const float scale = a.number();
   const Rows out(a);
-  const at::Tensor *lse = a.dense(at::kFloat, 2, true);
+  const Dense lse = a.dense(at::kFloat, 2, true);
   const Last l(a);
   if (a.ok)
-    a.want(out.like(q) && cache.holds(cache.H, S, q.D) && cache.H <= INT32_MAX && blocks->size(0) == q.n && blocks->size(1) == cache.H &&
-           tokens->size(0) == q.n && tokens->size(1) == cache.H && (lse == nullptr || (lse->size(0) == q.n && lse->size(1) == q.heads)));
+    a.want(out.like(q) && cache.holds(cache.H, S, q.D) && cache.H <= INT32_MAX && blocks.size[0] == q.n && blocks.size[1] == cache.H &&
+           tokens.size[0] == q.n && tokens.size[1] == cache.H && (!lse.given || (lse.size[0] == q.n && lse.size[1] == q.heads)));
   return status(a, [&] {
     return attention_blocks(q.dtype(), q.n, static_cast<int32_t>(q.heads), static_cast<int32_t>(cache.H), static_cast<int32_t>(q.D), S, q.p, q.row, q.head,
-                            data<int32_t>(blocks), data<int32_t>(tokens), blocks->size(2), cache.p, cache.n, scale, out.p, out.row, out.head, data<float>(lse), l.ws,
+                            data<int32_t>(blocks), data<int32_t>(tokens), blocks.size[2], cache.p, cache.n, scale, out.p, out.row, out.head, data<float>(lse), l.ws,
                             l.bytes, l.stream);
   });
 }
@@ -271,6 +285,7 @@ PyObject *guarded(PyObject *self, PyObject *const *args, Py_ssize_t n) {
   try {
     return kCall(self, args, n);
   } catch (...) {
+    PyErr_Clear();
     Py_RETURN_NONE;
   }
 }
