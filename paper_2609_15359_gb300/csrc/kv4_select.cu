@@ -172,12 +172,16 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : kThreads == 25
   const int sharers = all || need == 0 ? 1 : min(a.cluster, (N + kThreads - 1) / kThreads);
   if (rank >= sharers) return;  // the cluster's barriers count those that are left
   const int32_t *table = a.table + b * a.max_blocks;
+  auto checked = [&](int32_t block) {  // an entry that goes into the list without a score
+    if (block < 0 || block >= a.n_blocks) flag_error(a.status, MAPS_E_RANGE);
+    return block;
+  };
   // what needs no scores: the ends of the list, and its tokens
   auto write_ends = [&]() {
     if (tid == 0) a.tokens[item] = nb == 0 ? 0 : static_cast<int32_t>((count - 1) * static_cast<int64_t>(a.S) + seen - (nb - 1) * static_cast<int64_t>(a.S));
     for (int x = tid; x < a.first + a.last; x += kThreads) {
       const bool front = x < a.first;
-      out[front ? x : x - a.first + count - a.last] = table[front ? x : x - a.first + nb - a.last];
+      out[front ? x : x - a.first + count - a.last] = checked(table[front ? x : x - a.first + nb - a.last]);
     }
   };
   if (all || need == 0) {
@@ -186,7 +190,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : kThreads == 25
       return;
     }
     if (tid == 0) a.tokens[item] = static_cast<int32_t>(nb == 0 ? 0 : seen);
-    for (int x = tid; x < a.n_list; x += kThreads) out[x] = x < nb ? table[x] : -1;
+    for (int x = tid; x < a.n_list; x += kThreads) out[x] = x < nb ? checked(table[x]) : -1;
     return;
   }
   if (sharers > 1) cluster_arrive();  // this block runs, so its shared memory may be written
