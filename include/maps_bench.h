@@ -57,12 +57,14 @@ int maps_test_absent_block(int32_t block);
 int maps_test_calibrate_absent_block(int32_t block, uint32_t spin_limit);
 
 /* Exercises the bounded waits inside maps_kv4_attention's form for many
- * queries: on the current device, block `block` of later calls never learns
- * that a step's keys are there, so the waits of all its warps run out, each
- * after `spin_limit` tries of up to 20 microseconds (0: the library default).
- * The call records MAPS_E_TIMEOUT (read with maps_check), what it has not
- * written of its outputs stays as it was, and the device stays usable; its
- * workspace is to be zero-filled anew.  block = -1, spin_limit = 0 restores
+ * queries and maps_kv4_attention_blocks: on the current device, block `block`
+ * of later calls never learns that a step's keys are there, so the waits of
+ * all its warps run out, each after `spin_limit` tries of up to 20
+ * microseconds (0: the library default).  The call records MAPS_E_TIMEOUT
+ * (read with maps_check) and the device stays usable.  What
+ * maps_kv4_attention has not written of its outputs stays as it was, and its
+ * workspace is to be zero-filled anew; maps_kv4_attention_blocks writes wrong
+ * outputs for the rows and heads that the block has a part of.  block = -1, spin_limit = 0 restores
  * the normal behaviour.  Calls in flight must have finished before the
  * settings change.  Returns MAPS_OK or MAPS_E_CUDA. */
 int maps_test_attention_withhold(int32_t block, uint32_t spin_limit);

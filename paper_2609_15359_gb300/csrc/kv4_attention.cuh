@@ -12,12 +12,13 @@ namespace maps {
 // 300 tokens: 18 us themselves, 25 with the kernel; 512: 52, 58; 2,048: 173, 178).
 constexpr int kMaxLocalB = 2048;
 
-// Lets a kernel have `bytes` of dynamic shared memory, once for each device.
+// Lets a kernel have `bytes` of dynamic shared memory, once for each device.  `current` receives the device.
 template <auto kKernel>
-int allow_smem(size_t bytes) {
+int allow_smem(size_t bytes, int *current = nullptr) {
   static std::atomic<uint64_t> done;
   int dev = 0;
   MAPS_TRY(cuda_ok(cudaGetDevice(&dev)));
+  if (current != nullptr) *current = dev;
   const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
   if (done.load(std::memory_order_relaxed) & bit) return MAPS_OK;
   MAPS_TRY(cuda_ok(cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes))));
@@ -83,9 +84,11 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
   return ok != 0;
 }
 constexpr uint32_t kTries = 1u << 18;
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, uint32_t tries = kTries) {  // bounded
-  for (uint32_t i = 0; i < tries; ++i)
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, uint32_t tries = kTries) {  // bounded; tries >= 1
+  uint32_t i = 0;
+  do
     if (bar_try(bar, parity)) return true;
+  while (++i < tries);
   return false;
 }
 // The same for a warp, whose lanes go on, or give up, together.
@@ -161,5 +164,8 @@ __device__ __forceinline__ int32_t many_over(const AttnArgs &a) {
 bool attn_many_dim(int D);
 void attn_many_carve(Carve &c, AttnArgs &a, int32_t B, int D);
 int attn_many(int32_t dtype, int D, const AttnArgs &a, cudaStream_t s);
+
+// maps_test_attention_withhold for attention over lists (kv4_attention_blocks.cu).
+int attn_lists_withhold(int32_t block, uint32_t tries);
 
 }  // namespace maps

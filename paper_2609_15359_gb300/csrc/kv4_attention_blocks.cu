@@ -21,11 +21,22 @@ namespace {
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kMaxCluster = 8;  // one row of 8 heads: 6.2 us, with 16 blocks 7.5, with four 7.2, with two 9.3
 
+// Test aid (maps_test_attention_withhold), for a device: the block that never learns that its copies have landed, plus 1, and the
+// tries after which a wait gives up (0: as by default).  They come with the call's arguments: in constant memory of their own the first
+// look at them cost 0.2 us a block.
+struct Withheld {
+  std::atomic<int32_t> block{0};
+  std::atomic<uint32_t> tries{0};
+};
+Withheld g_withheld[64];
+
 struct ListArgs {
   int32_t Hq, H, group, tiles;  // query heads to a KV head, and tiles of them
   int32_t block_groups, block_shift;  // groups of a block, and their logarithm where they are a power of two, else -1
   int64_t n_list, n_blocks, block_bytes;
   int32_t S, wide;
+  int32_t withheld;
+  uint32_t tries;
   uint32_t single, cluster;  // items of one block each, the first; of a cluster's blocks, the rest
   const void *q;
   int64_t q_row, q_head, o_row, o_head;
@@ -70,7 +81,7 @@ __global__ void __launch_bounds__(kThreads, ListShape<D, NT>::kBlocks) attn_list
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
   uint8_t *ring = smem + warp * Sh::kStages * Sh::kBytes;
   const uint32_t ring32 = smem_u32(ring), bar32 = smem_u32(bars + warp * Sh::kStages);
-  if (lane < Sh::kStages) bar_init(bar32 + 8 * lane, 1);
+  if (lane < Sh::kStages) bar_init(bar32 + 8 * lane, static_cast<int>(blockIdx.x) == a.withheld ? 2 : 1);  // of two arrivals one never comes
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   __syncwarp();
   pdl_prologue();
@@ -211,10 +222,15 @@ __global__ void __launch_bounds__(kThreads, ListShape<D, NT>::kBlocks) attn_list
 
   int stage = 0;
   uint32_t parity = 0;
+  bool landed = true;  // nothing of this warp's is under way
   for (int32_t u = 0; u < units; ++u) {
-    if (!warp_wait(bar32 + 8 * stage, parity)) {
+    if (!warp_wait(bar32 + 8 * stage, parity, a.tries)) {
       if (lane == 0) flag_error(a.status, MAPS_E_TIMEOUT);
-      for (int s = 0; s < Sh::kStages; ++s) (void)bar_wait(bar32 + 8 * s, s < stage ? parity ^ 1 : parity);  // what is under way lands before the block ends
+      // the copies of this unit and of the next ones that the ring holds land before the block ends; the others' stages wait for nothing
+      for (int k = 0; k < Sh::kStages && u + k < units; ++k) {
+        const bool wrapped = stage + k >= Sh::kStages;
+        landed &= warp_wait(bar32 + 8 * (stage + k - (wrapped ? Sh::kStages : 0)), parity ^ (wrapped ? 1u : 0u), a.tries);
+      }
       break;
     }
     const uint8_t *buf = ring + stage * Sh::kBytes;
@@ -361,7 +377,7 @@ __global__ void __launch_bounds__(kThreads, ListShape<D, NT>::kBlocks) attn_list
     if (++stage == Sh::kStages) stage = 0, parity ^= 1;
   }
 
-  // ---- this warp's part, into its ring, which has been read to the end
+  // ---- this warp's part, into its ring, which has been read to the end (and not where copies may still come: the row is lost anyway)
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -379,6 +395,7 @@ __global__ void __launch_bounds__(kThreads, ListShape<D, NT>::kBlocks) attn_list
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       const int R = nt * 8 + 2 * t + e;
+      if (!landed) continue;
 #pragma unroll
       for (int j = 0; j < kSteps; j += 2)
         *reinterpret_cast<float4 *>(part + in_part<D>(R, g * kCh + 2 * j)) =
@@ -441,7 +458,11 @@ template <class T, int D, int NT>
 int launch(ListArgs a, int64_t T_, cudaStream_t s) {
   using Sh = ListShape<D, NT>;
   constexpr auto kernel = attn_lists_kernel<T, D, NT>;
-  MAPS_TRY(allow_smem<kernel>(Sh::kSmem));
+  int dev = 0;
+  MAPS_TRY(allow_smem<kernel>(Sh::kSmem, &dev));
+  a.withheld = dev < 64 ? g_withheld[dev].block.load(std::memory_order_relaxed) - 1 : -1;
+  const uint32_t tries = dev < 64 ? g_withheld[dev].tries.load(std::memory_order_relaxed) : 0;
+  a.tries = tries ? tries : kTries;
   a.tiles = (a.group + Sh::kRows - 1) / Sh::kRows;
   const int64_t items = T_ * a.H * a.tiles, room = static_cast<int64_t>(sm_count()) * Sh::kBlocks, groups = a.n_list * a.block_groups;
   // what does not fill the device once more is shared out
@@ -476,6 +497,16 @@ int launch_dim(int D, const ListArgs &a, int64_t rows, cudaStream_t s) {
 }
 
 }  // namespace
+
+int attn_lists_withhold(int32_t block, uint32_t tries) {
+  int dev = 0;
+  MAPS_TRY(cuda_ok(cudaGetDevice(&dev)));
+  if (dev >= 64) return MAPS_E_INVALID;
+  g_withheld[dev].block = block + 1;
+  g_withheld[dev].tries = tries;
+  return MAPS_OK;
+}
+
 }  // namespace maps
 
 extern "C" {

@@ -1112,5 +1112,5 @@ extern "C" int maps_test_attention_withhold(int32_t block, uint32_t spin_limit) 
   const uint32_t tries = spin_limit == 0 ? kTries : spin_limit;
   MAPS_TRY(cuda_ok(cudaMemcpyToSymbol(c_withheld, &block, sizeof(block))));
   MAPS_TRY(cuda_ok(cudaMemcpyToSymbol(c_tries, &tries, sizeof(tries))));
-  return MAPS_OK;
+  return attn_lists_withhold(block, tries);
 }
