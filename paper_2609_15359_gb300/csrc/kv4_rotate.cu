@@ -39,17 +39,21 @@ struct RotArgs {
 template <bool kInter>
 struct Turn {
   float c[8], s[8];
-  uint32_t on;  // all bits, or none: channels that do not turn, which are x 1 + 0 (-0), x itself whatever it is
+  // Of two channels each: 16 bits set, or none for a channel that does not turn, which is x 1 + 0 (-0), x itself whatever it and its
+  // partner are.  (One mask for all eight, and channels without a position apart by a branch: 65,536 tokens 263.5 us for 260.7.)
+  uint32_t on[4];
   int partner;  // lanes from here
   __device__ __forceinline__ void load(const RotArgs &a, int64_t tok, int l) {
     constexpr int kN = kInter ? 4 : 8;  // pairs
     const int F = a.rot / 2;
-    on = 8 * l < a.rot ? 0xffffffffu : 0u;
+    const bool turns = 8 * l < a.rot;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) on[i] = turns ? 0xffffffffu : 0u;
     const bool second = !kInter && 8 * l >= F;
-    partner = !on ? 0 : second ? -(F / 8) : F / 8;
+    partner = !turns ? 0 : second ? -(F / 8) : F / 8;
 #pragma unroll
     for (int i = 0; i < 8; ++i) c[i] = 1.0f, s[i] = -0.0f;
-    if (!on) return;
+    if (!turns) return;
     const int f0 = kInter ? 4 * l : second ? 8 * l - F : 8 * l;
     int32_t ax[kN] = {};
     if (a.axis) {
@@ -73,6 +77,7 @@ struct Turn {
       return static_cast<int64_t>(p) * a.rot;
     };
     int64_t at = row_of(ax[0]);
+    uint32_t lost = 0;  // pairs
     bool same = true;
 #pragma unroll
     for (int i = 1; i < kN; ++i) same &= ax[i] == ax[0];
@@ -84,12 +89,17 @@ struct Turn {
           *reinterpret_cast<float4 *>(c + i) = *reinterpret_cast<const float4 *>(src + i);
           *reinterpret_cast<float4 *>(s + i) = *reinterpret_cast<const float4 *>(src + F + i);
         }
+      } else {
+        lost = (1u << kN) - 1u;
       }
     } else {
 #pragma unroll
       for (int i = 0; i < kN; ++i) {
         if (i > 0 && ax[i] != ax[i - 1]) at = row_of(ax[i]);
-        if (at >= 0) c[i] = a.cos_sin[at + f0 + i], s[i] = a.cos_sin[at + F + f0 + i];
+        if (at >= 0)
+          c[i] = a.cos_sin[at + f0 + i], s[i] = a.cos_sin[at + F + f0 + i];
+        else
+          lost |= 1u << i;
       }
     }
     if (kInter) {
@@ -98,6 +108,12 @@ struct Turn {
     } else if (!second) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) s[i] = -s[i];
+    }
+    if (lost) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (lost >> (kInter ? i / 2 : i) & 1u) s[i] = -0.0f, on[i / 2] &= i % 2 ? 0x0000ffffu : 0xffff0000u;
+      }
     }
   }
   // A row's 8 channels, turned.  All lanes of the warp call it.  A product of two is a fused one with minus_zero, which
@@ -114,7 +130,7 @@ struct Turn {
       other.z = __shfl_sync(0xffffffffu, raw.z, from);
       other.w = __shfl_sync(0xffffffffu, raw.w, from);
     }
-    other.x &= on, other.y &= on, other.z &= on, other.w &= on;
+    other.x &= on[0], other.y &= on[1], other.z &= on[2], other.w &= on[3];
     const T *x = reinterpret_cast<const T *>(&raw), *z = reinterpret_cast<const T *>(&other);
     const Two none(minus_zero, minus_zero);
 #pragma unroll
