@@ -511,6 +511,7 @@ struct Split {
 };
 
 void carve_keys(Carve &c, SelectArgs &a, const Split &p, int32_t H) {
+  a.stride = p.stride;
   if (p.in_ws) a.keys = c.take<uint32_t>(static_cast<size_t>(p.rows) * H * p.stride);
 }
 
