@@ -25,8 +25,11 @@ constexpr int kSmemKeys = 8192;   // of shared memory; longer rows of keys stay 
 // Threads of a multiprocessor up to which a row and head is shared out.  35 rows of 4 heads and up to 1,024 blocks: 512 8.4 us, 2,048 9.6.
 constexpr int kThreadsOfSm = 512;
 // Rows and heads for each multiprocessor from which on 128 threads take one, six a multiprocessor: 1,024 of them 19.2 us, by 256
-// threads 23.2.  Below, 256 threads end a row sooner.
+// threads 23.2.  Below, 256 threads end a row sooner.  So they do where rows have more blocks than kNarrowBlocks, which 128 threads sift
+// slowly: 128 requests x 8 heads of 131,072 tokens (8,192 blocks) by 128 threads 656 us, by 256 361, of 64 to 131,072 tokens 368 and 230;
+// up to 65,536 tokens 121 and 124, of 65,536 each 253 and 194.
 constexpr int kNarrowRows = 4;
+constexpr int kNarrowBlocks = 4096;
 // Blocks of a row from which on 512 threads take it, where rows are few: 8 rows of 8,192 blocks 17.7 us, by 256 threads 20.7.  Clusters of 16
 // 17.7, of 8 26, of 4 39.
 constexpr int kWideRow = 2048;
@@ -498,7 +501,7 @@ struct Split {
   bool in_ws;
   int32_t threads;
   Split(int64_t T, int32_t H, int64_t max_blocks) {
-    threads = max_blocks > kWideRow && T * H <= sm_count() ? 512 : T * H >= static_cast<int64_t>(kNarrowRows) * sm_count() ? 128 : 256;
+    threads = max_blocks > kWideRow && T * H <= sm_count() ? 512 : T * H >= static_cast<int64_t>(kNarrowRows) * sm_count() && max_blocks <= kNarrowBlocks ? 128 : 256;
     const int64_t steps = (max_blocks + threads - 1) / threads, most = static_cast<int64_t>(sm_count()) * kThreadsOfSm / threads;
     while (cluster < kMaxCluster && cluster < steps && 2 * cluster * T * H <= most) cluster *= 2;
     in_ws = max_blocks > kSmemKeys;
