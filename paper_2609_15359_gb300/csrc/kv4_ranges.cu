@@ -159,73 +159,103 @@ __global__ void __launch_bounds__(kThreads, kBlocksOfSm) kv4_ranges_kernel(const
   __shared__ int32_t s_first[kRequests], s_len[kRequests];
   __shared__ int64_t s_warp[kWarps];
   __shared__ int2 s_block[kThreads];  // a block of the cache, and its places that hold a token
-  for (int32_t b0 = 0; b0 < a.B; b0 += kRequests) {
-    // ---- the requests' blocks, counted; this block of threads has an equal share of them, whatever the lengths
-    constexpr int kOwn = kRequests / kThreads;
-    int32_t first[kOwn], count[kOwn], len[kOwn];
-    int64_t sum = 0;
-#pragma unroll
-    for (int k = 0; k < kOwn; ++k) {
-      const int32_t b = b0 + tid * kOwn + k;
-      len[k] = b < a.B ? a.len[b] : 0;
-      first[k] = b < a.B && a.held ? a.held[b] : 0;
+  // The blocks of a request: its first, and the one behind its last.
+  auto length = [&](int64_t b) { return b < a.B ? a.len[b] : 0; };
+  auto before = [&](int64_t b) { return b < a.B && a.held ? a.held[b] : 0; };
+  auto blocks_of = [&](int32_t &len, int32_t &first) -> int32_t {
+    if (len < 0 || len > 0x7fffffff - 1023 || len > a.max_blocks * a.S || first < 0) {
+      flag_error(a.status, MAPS_E_RANGE);
+      len = first = 0;
     }
+    first = min(first, len) / a.S;
+    return static_cast<int32_t>(static_cast<uint32_t>(len + a.S - 1) / static_cast<uint32_t>(a.S));
+  };
+  // A request has blocks behind its first; one that is to be reported counts as such.
+  auto has_more = [&](int32_t len, int32_t held) { return len < 0 || held < 0 || (len > held && static_cast<uint32_t>(len - 1) / a.S > static_cast<uint32_t>(held) / a.S); };
+  constexpr int kOwn = kRequests / kThreads;
+  int32_t some_len[kOwn], some_held[kOwn];  // all loads under way at once
 #pragma unroll
-    for (int k = 0; k < kOwn; ++k) {
-      if (len[k] < 0 || len[k] > 0x7fffffff - 1023 || len[k] > a.max_blocks * a.S || first[k] < 0) {
-        flag_error(a.status, MAPS_E_RANGE);
-        len[k] = first[k] = 0;
+  for (int k = 0; k < kOwn; ++k) some_len[k] = length(tid + k * kThreads), some_held[k] = before(tid + k * kThreads);
+  const int64_t mine = blockIdx.x + static_cast<int64_t>(tid) * gridDim.x;
+  int32_t my_len = length(mine), my_first = before(mine);
+  const bool mine_there = blocks_of(my_len, my_first) > my_first;
+  const int32_t my_block = mine_there ? a.table[mine * a.max_blocks + my_first] : -1;
+  bool more = false;
+#pragma unroll
+  for (int k = 0; k < kOwn; ++k) more |= has_more(some_len[k], some_held[k]);
+  for (int64_t b = tid + kRequests; b < a.B; b += kThreads) more |= has_more(length(b), before(b));
+  const int step_x = kWarps / a.H, step_h = kWarps % a.H;
+  // First every request's first block, dealt out in turn: a decode step has no others.  Then the others, in turns of kRequests.
+  for (int32_t b0 = -kRequests; b0 < a.B; b0 += kRequests) {
+    const bool others = b0 >= 0;
+    int64_t from = 0, to = (a.B - static_cast<int64_t>(blockIdx.x) + gridDim.x - 1) / gridDim.x;
+    if (others) {
+      // ---- counted; this block of threads has an equal share of them, whatever the lengths
+      int32_t count[kOwn];
+      int64_t sum = 0;
+#pragma unroll
+      for (int k = 0; k < kOwn; ++k) {
+        int32_t len = length(b0 + tid * kOwn + k), first = before(b0 + tid * kOwn + k);
+        count[k] = max(blocks_of(len, first) - first - 1, 0);
+        s_first[tid * kOwn + k] = first + 1;
+        s_len[tid * kOwn + k] = len;
+        sum += count[k];
       }
-      first[k] = min(first[k], len[k]) / a.S;
-      count[k] = static_cast<int32_t>(static_cast<uint32_t>(len[k] + a.S - 1) / static_cast<uint32_t>(a.S)) - first[k];
-      s_first[tid * kOwn + k] = first[k];
-      s_len[tid * kOwn + k] = len[k];
-      sum += count[k];
-    }
-    int64_t ahead = sum;
+      int64_t ahead = sum;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int64_t x = __shfl_up_sync(0xffffffffu, ahead, o);
-      if (lane >= o) ahead += x;
-    }
-    if (lane == 31) s_warp[warp] = ahead;
-    __syncthreads();
-    ahead -= sum;
-    int64_t total = 0;
+      for (int o = 1; o < 32; o <<= 1) {
+        const int64_t x = __shfl_up_sync(0xffffffffu, ahead, o);
+        if (lane >= o) ahead += x;
+      }
+      if (lane == 31) s_warp[warp] = ahead;
+      __syncthreads();
+      ahead -= sum;
+      int64_t total = 0;
 #pragma unroll
-    for (int k = 0; k < kWarps; ++k) {
-      if (k < warp) ahead += s_warp[k];
-      total += s_warp[k];
-    }
+      for (int k = 0; k < kWarps; ++k) {
+        if (k < warp) ahead += s_warp[k];
+        total += s_warp[k];
+      }
 #pragma unroll
-    for (int k = 0; k < kOwn; ++k) s_before[tid * kOwn + k] = ahead, ahead += count[k];
-    if (tid == 0) s_before[kRequests] = total;
-    __syncthreads();
-    const int64_t from = total * blockIdx.x / gridDim.x, to = total * (blockIdx.x + 1) / gridDim.x;
+      for (int k = 0; k < kOwn; ++k) s_before[tid * kOwn + k] = ahead, ahead += count[k];
+      if (tid == 0) s_before[kRequests] = total;
+      __syncthreads();
+      from = total * blockIdx.x / gridDim.x, to = total * (blockIdx.x + 1) / gridDim.x;
+    }
     for (int64_t x0 = from; x0 < to; x0 += kThreads) {
       // ---- up to kThreads of them, looked up side by side
       const int here = static_cast<int>(min(to - x0, static_cast<int64_t>(kThreads)));
       if (tid < here) {
-        int lo = 0;  // the last request with s_before <= x0 + tid
+        int32_t j = my_first, len = my_len, block = my_block;
+        bool there = mine_there;
+        if (others) {
+          int lo = 0;  // the last request with s_before <= x0 + tid
 #pragma unroll
-        for (int o = kRequests / 2; o > 0; o >>= 1)
-          if (s_before[lo + o] <= x0 + tid) lo += o;
-        const int32_t j = s_first[lo] + static_cast<int32_t>(x0 + tid - s_before[lo]);
-        int32_t block = a.table[(b0 + lo) * a.max_blocks + j];
-        if (block < 0 || block >= a.n_blocks) {
+          for (int o = kRequests / 2; o > 0; o >>= 1)
+            if (s_before[lo + o] <= x0 + tid) lo += o;
+          j = s_first[lo] + static_cast<int32_t>(x0 + tid - s_before[lo]), len = s_len[lo], there = true;
+          block = a.table[(b0 + lo) * a.max_blocks + j];
+        } else if (x0 > 0) {
+          const int64_t b = mine + x0 * gridDim.x;
+          len = length(b), j = before(b);
+          there = blocks_of(len, j) > j;
+          block = there ? a.table[b * a.max_blocks + j] : -1;
+        }
+        if (there && (block < 0 || block >= a.n_blocks)) {
           flag_error(a.status, MAPS_E_RANGE);
           block = -1;
         }
-        s_block[tid] = make_int2(block, min(a.S, s_len[lo] - j * a.S));
+        s_block[tid] = make_int2(block, min(a.S, len - j * a.S));
       }
       __syncthreads();
-      for (int64_t u = warp; u < static_cast<int64_t>(here) * a.H; u += kWarps) {
-        const int x = static_cast<int>(u / a.H);
-        unit<D>(a, s_block[x].x, static_cast<int>(u - static_cast<int64_t>(x) * a.H), s_block[x].y);
+      for (int x = warp / a.H, h = warp % a.H; x < here; x += step_x) {
+        unit<D>(a, s_block[x].x, h, s_block[x].y);
+        h += step_h;
+        if (h >= a.H) h -= a.H, ++x;
       }
       __syncthreads();
     }
-    __syncthreads();
+    if (!__syncthreads_or(more)) return;
   }
 }
 
