@@ -13,8 +13,9 @@ are drawn at random.
 
 With --sparse N keys and queries are turned by their positions on the way
 (maps_kv4_append_rotated), the ranges of the blocks that new tokens went to are kept
-(maps_kv4_block_ranges), and every query attends over the N blocks alone that score highest
-for it (maps_kv4_select_blocks, maps_kv4_attention_blocks).
+(maps_kv4_block_ranges), and the query of a request that decodes attends over the N blocks
+alone that score highest for it (maps_kv4_select_blocks, maps_kv4_attention_blocks).  Prompts
+attend over all their keys (maps_kv4_attention), as chunks of many queries do sooner.
 
     python examples/kv4_decoder.py --requests 256 --blocks 8192
     python examples/kv4_decoder.py --requests 256 --blocks 8192 --sparse 32
@@ -103,7 +104,12 @@ class Decoder:
             ok(M.maps_kv4_block_ranges(tokens_held, n, self.table, self.cache, S, self.codes, self.scale, ws=self.ws))
             lists = torch.empty(T, self.H, self.sparse, dtype=torch.int32, device=self.device)
             tokens = torch.empty(T, self.H, dtype=torch.int32, device=self.device)
-            ok(M.maps_kv4_select_blocks(q, off, n, self.table, self.codes, self.scale, S, 1, 2, lists, tokens, ws=self.ws))
+            prompts = self.held < self.prompt
+            alone = torch.where(prompts, 0, n)
+            ok(M.maps_kv4_select_blocks(q, off, alone, self.table, self.codes, self.scale, S, 1, 2, lists, tokens, ws=self.ws))
+            if bool((live & prompts).any()):  # their rows first, zeros for the others; then lists for those, -1 leaving the prompts' rows
+                ok(M.maps_kv4_attention(q, off, n - alone, self.table, self.cache, S, self.D ** -0.5, out, ws=self.ws))
+                tokens[prompts.repeat_interleave(off.diff(), output_size=T)] = -1
             ok(M.maps_kv4_attention_blocks(q, lists, tokens, self.cache, S, self.D ** -0.5, out, ws=self.ws))
         else:
             ok(M.maps_kv4_append(k, v, slots, self.cache, S, ws=self.ws))
@@ -121,7 +127,7 @@ def main() -> None:
     ap.add_argument("--requests", type=int, default=256)
     ap.add_argument("--blocks", type=int, default=8192)
     ap.add_argument("--steps", type=int, default=5000, help="at most so many")
-    ap.add_argument("--sparse", type=int, default=0, help="cache blocks that a query attends over (3 at least); 0: all")
+    ap.add_argument("--sparse", type=int, default=0, help="cache blocks that a decoding request's query attends over (3 at least); 0: all")
     a = ap.parse_args()
     g = torch.Generator().manual_seed(1)
     prompt = torch.randint(32, 2049, (a.requests,), generator=g, dtype=torch.int32)
