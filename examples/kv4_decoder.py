@@ -71,6 +71,14 @@ class Decoder:
     def done(self) -> bool:
         return bool((self.held >= self.total).all())
 
+    def attend_lists(self, q, off, n):
+        """Attention of each query over the blocks of its own list."""
+        lists = torch.empty(len(q), self.H, self.sparse, dtype=torch.int32, device=self.device)
+        tokens, out = torch.empty(len(q), self.H, dtype=torch.int32, device=self.device), torch.empty_like(q)
+        ok(M.maps_kv4_select_blocks(q, off, n, self.table, self.codes, self.scale, self.S, 1, 2, lists, tokens, ws=self.ws))
+        ok(M.maps_kv4_attention_blocks(q, lists, tokens, self.cache, self.S, self.D ** -0.5, out, ws=self.ws))
+        return out
+
     def step(self) -> dict:
         """One step; returns the tokens' queries, keys, values, slots and outputs."""
         S = self.S
@@ -94,23 +102,24 @@ class Decoder:
         pos = torch.empty(T, dtype=torch.int32, device=self.device)
         ok(M.maps_block_tables(S, tokens_held, want, self.table, self.free, self.n_free, n_free, got, off, slots,
                                pos_out=pos, order=self.order, ws=self.ws))
-        rows = lambda h: torch.randn(T, h, self.D, device=self.device, generator=self.gen).to(self.dtype)  # noqa: E731
-        q, k, v = rows(self.Hq), rows(self.H), rows(self.H)
+        draw = lambda h: torch.randn(T, h, self.D, device=self.device, generator=self.gen).to(self.dtype)  # noqa: E731
+        q, k, v = draw(self.Hq), draw(self.H), draw(self.H)
         granted = live & (got == want)  # all that are live: admission leaves blocks for them
         n = torch.where(granted, got, 0)
         out = torch.empty_like(q)
         if self.sparse:
             ok(M.maps_kv4_append_rotated(q, k, v, pos, self.cos_sin, slots, self.cache, S, q, ws=self.ws))
             ok(M.maps_kv4_block_ranges(tokens_held, n, self.table, self.cache, S, self.codes, self.scale, ws=self.ws))
-            lists = torch.empty(T, self.H, self.sparse, dtype=torch.int32, device=self.device)
-            tokens = torch.empty(T, self.H, dtype=torch.int32, device=self.device)
             prompts = self.held < self.prompt
-            alone = torch.where(prompts, 0, n)
-            ok(M.maps_kv4_select_blocks(q, off, alone, self.table, self.codes, self.scale, S, 1, 2, lists, tokens, ws=self.ws))
-            if bool((live & prompts).any()):  # their rows first, zeros for the others; then lists for those, -1 leaving the prompts' rows
+            alone = torch.where(prompts, 0, n)  # requests that decode
+            if bool((live & prompts).any()):
                 ok(M.maps_kv4_attention(q, off, n - alone, self.table, self.cache, S, self.D ** -0.5, out, ws=self.ws))
-                tokens[prompts.repeat_interleave(off.diff(), output_size=T)] = -1
-            ok(M.maps_kv4_attention_blocks(q, lists, tokens, self.cache, S, self.D ** -0.5, out, ws=self.ws))
+                new = off.diff()
+                rows = (~prompts).repeat_interleave(new, output_size=T).nonzero()[:, 0]
+                ends = torch.where(prompts, 0, new).cumsum(0)
+                out[rows] = self.attend_lists(q[rows], torch.cat([ends.new_zeros(1), ends]), alone)
+            else:
+                out = self.attend_lists(q, off, alone)
         else:
             ok(M.maps_kv4_append(k, v, slots, self.cache, S, ws=self.ws))
             ok(M.maps_kv4_attention(q, off, n, self.table, self.cache, S, self.D ** -0.5, out, ws=self.ws))
