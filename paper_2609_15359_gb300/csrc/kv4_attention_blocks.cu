@@ -10,7 +10,7 @@
 // lengths alone.  (Equal runs of units over all lists, as behind block tables, cost a plan, parts in memory and joins across blocks: 66 us
 // for 53 in the case below, 11.8 for 6.1 with one row.)
 //
-// Bound: 128 rows of 2,048 tokens, 8 KV heads of 128 channels, 285 MB, take 52.6 us (5.4 TB/s, 0.80 of the measured copy rate), the rest
+// Bound: 128 rows of 2,048 tokens, 8 KV heads of 128 channels, 285 MB, take 53.0 us (5.4 TB/s, 0.80 of the measured copy rate), the rest
 // what a list costs before its first unit and after its last.  One row: 6.1 us, launch, three rounds of loads, a unit, two joins.  Lists of
 // 64 channels and five query heads: issue slots, 210 instructions for 16 tokens.
 #include "kv4_attention_products.cuh"

@@ -1,13 +1,15 @@
 // kv4_ranges.cu -- the range of each channel over the keys of a cache block, 8 bits an end: what a block's score is made from.
 //
-// A warp takes a block and KV head; the blocks that are asked for are counted and dealt out evenly, whatever the requests'
-// lengths.  A key is fl(scale * code + zero); least and greatest are taken of these 32-bit values, and the codes of the ends are
+// A warp takes a block and KV head.  The first block that each request's tokens went to is dealt out in turn, as a decode step has no
+// others; where there are more, those are counted and dealt out evenly, whatever the requests' lengths.  A key is fl(scale * code + zero); least and greatest are taken of these 32-bit values, and the codes of the ends are
 // exact: a code times the scale has 15 bits, so a comparison in 32 bits settles where a product's rounding may have crossed a
 // whole number.
 //
-// Bound: the pipe that takes codes out of words and compares (two operations a code), not the bytes.  48 prompts of 1,500 to 8,192
-// tokens, 8 heads of 128 channels, 156 MB: 88 us (1.8 TB/s).  One token each of 512 requests: 6.2 us, launch, counting, two rounds
-// of loads.  Four blocks a multiprocessor instead of two: 87 and 7.4 us.
+// Bound: neither the bytes nor one pipe.  A block and head of 16 x 128 keys takes 518 instructions, of which 230 take codes out of
+// words, make keys and compare; 16 warps a multiprocessor, as many as 128 registers allow, issue 0.6 of what they could and wait for
+// loads the rest.  48 prompts of 1,500 to 8,192 tokens, 8 heads of 128 channels, 162 MB: 86 us (1.9 TB/s, 0.28 of the measured copy
+// rate).  One token each of 512 requests: 5.5 us, launch and three rounds of loads.  Four blocks a multiprocessor instead of two: 84 and
+// 6.8 us.  (256 channels: 48 bytes a thread are spilled.)
 #include "kv4_rows.cuh"
 
 namespace maps {

@@ -7,7 +7,7 @@
 // D/8 lanes share a row, 8 channels (16 bytes) each; a channel's partner is rot/16 lanes away, or beside it.
 //
 // Bound: long batches by the bytes, of which queries are most, with issue slots close behind.  65,536 tokens of 32 query heads and 8 KV
-// heads of 128 channels on three axes, 1.42 GB, take 262 us (5.4 TB/s, 0.80 of the measured copy rate).  Short ones by launch and
+// heads of 128 channels on three axes, 1.42 GB, take 261 us (5.4 TB/s, 0.81 of the measured copy rate).  Short ones by launch and
 // three rounds of loads (position, angles, rows): 512 tokens 5.4 us.
 #include "kv4_rows.cuh"
 
@@ -153,7 +153,9 @@ __device__ __forceinline__ uint4 rounded(const float (&y)[8]) {
 // A unit is a token and `per` of its query and key heads (queries first); a warp takes one and keeps the angles in registers for
 // all its rows, of which 32 / (D/8) pass side by side and kAhead more are under way.  Values, which do not turn, are
 // other blocks' of the same launch: row by row, or (kGroups) 16 tokens of a head to a warp, as in maps_kv4_append.
-// Four: 65,536 tokens take 262 us, with two 275, with eight (registers) 374.  Four blocks a multiprocessor: 262, three 280.
+// Four: 65,536 tokens take 261 us, with two 275 (512 tokens 5.2 for 5.4), with eight (registers) 313.  Four blocks a multiprocessor: 261,
+// three 277.  Four leave 64 registers a thread, of which all these kernels spill some: 48 bytes in that case, 44 to 240 in the others,
+// most where channels do not lie on 16 bytes.
 constexpr int kAhead = 4;
 
 template <class T, int D, bool kWide, bool kInter, bool kGroups>

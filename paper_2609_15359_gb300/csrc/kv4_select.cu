@@ -11,8 +11,9 @@
 // histograms of the keys that are still in question, ten bits at a time; then the list is written in order.
 //
 // Bound: chains of dependent steps.  Where rows are many, enough of them side by side hide these: 128 requests of 64 to 8,192 tokens, 8
-// heads of 128 channels, 68 MB of ranges, 19.2 us (floor 10.6).  One request of 100,000 to 131,072 tokens: 17.6 us, of which look-ups
-// and first codes 3, its 8,192 blocks' codes 1.5, the cluster's barrier 1.5, bisection 5, the list 2.
+// heads of 128 channels, 68 MB of ranges, 19.3 us (floor 10.6).  One request of 100,000 to 131,072 tokens: 15 us where its ranges lie in
+// L2, 19 from memory; of 17.6 between look-ups and first codes took 3, its 8,192 blocks' codes 1.5, the cluster's barrier 1.5, bisection
+// 5, the list 2.  Many long rows: 64 requests of 131,072 tokens, 1.1 GB, 186 us (5.9 TB/s), 128 of 65,536 255 (4.3 TB/s).
 #include <atomic>
 
 #include "kv4.cuh"
@@ -107,6 +108,8 @@ __device__ __forceinline__ void join(int (&acc)[8], int lane) {
   }
 }
 
+// 256 threads four times a multiprocessor leave 64 registers a thread, of which the branch of 16 keys a thread spills 208 to 296 bytes;
+// 128 threads spill 20 to 32.
 template <class T, int D, int kThreads>
 __global__ void __launch_bounds__(kThreads, kThreads == 512 ? 1 : kThreads == 256 ? 4 : 6) kv4_select_kernel(const SelectArgs a) {
   constexpr int kWarps = kThreads / 32;
