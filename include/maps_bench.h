@@ -64,9 +64,10 @@ int maps_test_calibrate_absent_block(int32_t block, uint32_t spin_limit);
  * (read with maps_check) and the device stays usable.  What
  * maps_kv4_attention has not written of its outputs stays as it was, and its
  * workspace is to be zero-filled anew; maps_kv4_attention_blocks writes wrong
- * outputs for the rows and heads that the block has a part of.  block = -1, spin_limit = 0 restores
- * the normal behaviour.  Calls in flight must have finished before the
- * settings change.  Returns MAPS_OK or MAPS_E_CUDA. */
+ * outputs for the rows and heads that the block has a part of.  block = -1,
+ * spin_limit = 0 restores the normal behaviour.  Calls in flight must have
+ * finished before the settings change.  Returns MAPS_OK, MAPS_E_CUDA, or
+ * MAPS_E_INVALID on a device past the 64th. */
 int maps_test_attention_withhold(int32_t block, uint32_t spin_limit);
 
 #ifdef __cplusplus
