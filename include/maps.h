@@ -710,6 +710,7 @@ int maps_kv4_append_rotated(int32_t dtype, int64_t T, int32_t Hq, int32_t H, int
  *                       head is left as it is, as rows that no request has are.
  *   ws                  maps_kv4_workspace_size() bytes.
  *   all others          as for maps_kv4_attention.
+ * After MAPS_E_TIMEOUT (via maps_check) the outputs are not to be used.
  * ---------------------------------------------------------------------- */
 int maps_kv4_block_ranges(int32_t B, int32_t H, int32_t D, int32_t S, const int32_t *held,
                           const int32_t *kv_len, const int32_t *table, int64_t max_blocks,
